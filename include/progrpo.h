@@ -342,6 +342,127 @@ pg_status pg_attention_network(const uint16_t *q, const uint16_t *k, const uint1
                                int32_t B, int32_t Lq, int32_t Lk, int32_t Lk_pad, int32_t heads, int32_t hd,
                                int32_t kernel, void *stream);
 
+/* ---- rollouts of a token policy: a paged key/value cache, attention of new tokens over it, logits and draws ----
+ *
+ * The same funnel for a policy that emits tokens one by one: a group's members start from one prompt whose pages they
+ * share, pg_ovf_select picks the survivors, and pg_cache_select with its sel_idx drops the others' pages.
+ * All of these calls are context-free and asynchronous; arrays are [device] unless tagged otherwise. */
+
+enum { PG_CACHE_BF16 = 0, PG_CACHE_E4M3 = 1 };
+
+/*
+ * Paged cache of keys and values ([host] struct, read during the call; the device memory is the caller's).
+ * Sequence r holds tokens 0 .. lens[r]-1; token t lies at slot t % page of page table[r * width + t / page].
+ *   k: [layers, n_pages, heads, page, head_dim]      v: [layers, n_pages, heads, head_dim, page] (values transposed)
+ * both 16-byte aligned, bf16 or 8-bit e4m3 codes (value = code * scale[layer, head]).  page 16, 32, 64 or 128;
+ * head_dim 32, 64 or 128; width * page < 2^31.  Every table passed with a cache has `width` entries a row; entries
+ * past the last page of a row are not read (calls that write tables write -1 there).
+ * refs[p]: rows that hold page p, 0 if it is free (any order of calls on one stream keeps it so).  A page that is
+ * part filled belongs to one row.  Taking pages is deterministic: the free page of the lowest number first, in row order.
+ * status[0] (sticky; pg_cache_check reports it): |= 4 a row got no page (pool or table width exhausted), |= 8 an
+ * index, length or count out of range.  Kernels keep every access in bounds in both cases.
+ */
+typedef struct pg_cache {
+  int32_t layers, n_pages, heads, page, head_dim, dtype, width;
+  void *k, *v;
+  const float *k_scale, *v_scale; /* [layers, heads] each, > 0; NULL: 1 (and NULL with bf16) */
+  int32_t *refs;                  /* [n_pages] */
+  int32_t *status;                /* [4] */
+} pg_cache;
+
+/* Rows of one pg_cache_reserve, and of either side of one pg_cache_select. */
+#define PG_CACHE_MAX_ROWS 16384
+
+/* All pages free, status 0 (the pools' contents stay as they are). */
+pg_status pg_cache_clear(const pg_cache *cache, void *stream);
+
+/* Pages for add[r] >= 0 more tokens in each row; lens_out[r] = lens[r] + add[r] (lens_out may be lens).  A row whose
+ * pages are not all there, counted in row order, gets none and keeps its length (status 4), as do rows after it that need any. */
+pg_status pg_cache_reserve(const pg_cache *cache, int32_t *table, const int32_t *lens, const int32_t *add,
+                           int32_t *lens_out, int32_t n_rows, void *stream);
+
+/* Writes the keys and values of the LAST tokens of each row (lens counts them already): tokens cu[r] .. cu[r+1]-1 of
+ * k_new / v_new are the last cu[r+1] - cu[r] of row r (cu: n_rows + 1 ascending offsets, cu[n_rows] == n_tokens; NULL: one token
+ * a row).  k_new, v_new: bf16 [n_tokens, heads, head_dim], a token every token_stride elements (multiple of 8, so that slices
+ * of a fused projection are taken as they are), 16-byte aligned.  e4m3 codes: round-to-nearest-even of x / scale, limited to +-448. */
+pg_status pg_cache_append(const pg_cache *cache, int32_t layer, const uint16_t *k_new, const uint16_t *v_new,
+                          int64_t token_stride, const int32_t *table, const int32_t *lens, const int32_t *cu,
+                          int32_t n_rows, int32_t n_tokens, void *stream);
+
+/* int32 scratch of pg_cache_select (at most n_rows rows on either side) and pg_cache_compact. */
+int64_t pg_cache_scratch_ints(const pg_cache *cache, int32_t n_rows);
+
+/* Fork, reorder and free: row r of (table_out, lens_out) is the sequence src[r] of (table_in, lens_in); src[r] == -1: an empty
+ * row.  Whole pages are shared (refs += users - 1; a sequence without users gives its pages back), a part-filled last page stays
+ * with the first of its users and is copied, in all layers, for the others, on pages that were free before the call.  A row whose
+ * copy finds no page ends at its last whole page (status 4).  The new table replaces the old one, which must not be used
+ * afterwards; the two must not overlap, nor the two arrays of lengths. */
+pg_status pg_cache_select(const pg_cache *cache, const int32_t *table_in, const int32_t *lens_in, int32_t n_in,
+                          const int32_t *src, int32_t *table_out, int32_t *lens_out, int32_t n_out, int32_t *scratch,
+                          void *stream);
+
+/* Moves the live pages to page numbers 0 .. live - 1 (the i-th live page past them into the i-th hole) in all layers and
+ * rewrites `table` and refs.  `table` has to be the only one that holds pages of this cache. */
+pg_status pg_cache_compact(const pg_cache *cache, int32_t *table, const int32_t *lens, int32_t n_rows, int32_t *scratch,
+                           void *stream);
+
+/* Synchronises the stream and reports status: PG_EWORKSPACE (4), PG_EINVAL (8). */
+pg_status pg_cache_check(const pg_cache *cache, void *stream);
+
+/* Attention of one new token of each of n_q queries over the cache: query i sees tokens 0 .. lens[i]-1 of table row row_of[i]
+ * (NULL: i; rows may repeat, so a prompt can go through as queries of growing lengths on one row; n_rows: rows of the table).
+ * q, out: bf16 [n_q, heads_q, head_dim], a query every q_stride / out_stride elements (multiples of 8, 16-byte aligned);
+ * heads_q a multiple of cache->heads, query head j reads key/value head j / (heads_q / heads).  logits scaled by `scale`
+ * (0: 1/sqrt(head_dim)).  lse (nullable) fp32 [n_q, heads_q]: natural logarithm of the softmax's denominator.  A query of no
+ * tokens gives zeros and -inf.  max_len >= every length: sizes the split (longer rows are right too, but slower).  All sums in fp32.
+ * workspace: pg_paged_attention_workspace() bytes, 16-byte aligned (may be NULL where that is 0). */
+size_t pg_paged_attention_workspace(const pg_cache *cache, int32_t n_q, int32_t heads_q, int32_t max_len);
+pg_status pg_paged_attention(const pg_cache *cache, int32_t layer, const uint16_t *q, int64_t q_stride,
+                             const int32_t *table, int32_t n_rows, const int32_t *row_of, const int32_t *lens,
+                             int32_t n_q, int32_t heads_q, double scale, int32_t max_len, uint16_t *out,
+                             int64_t out_stride, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+enum { PG_LOGITS_F32 = 0, PG_LOGITS_BF16 = 1 };
+
+/*
+ * Logits and what is to be done to them ([host] struct, read during the call).  For row r and token v, x = logits[r, v]:
+ *   z = x
+ *   if v is among tokens[r, 0 .. n_tokens[r]-1]:      z = z > 0 ? z / repetition[r] : z * repetition[r]
+ *   z -= frequency[r] * c;  if c > 0: z -= presence[r]    with c = how often v is among tokens[r, n_prompt[r] .. n_tokens[r]-1]
+ *   z += bias of v in the row's list;  not allowed: z = -inf
+ * each operation rounded to fp32.  Everything but the logits may be NULL (left out).  Ids outside 0 .. vocab-1 are passed over.
+ */
+typedef struct pg_logits {
+  const void *logits;             /* [rows, vocab], a row every `stride` elements */
+  int64_t stride;
+  int32_t dtype, rows, vocab;
+  int32_t tokens_stride;          /* >= every n_tokens[r]: longer counts are cut there */
+  const int32_t *tokens;          /* [rows, tokens_stride]: prompt, then output */
+  const int32_t *n_prompt;        /* [rows]; NULL: 0 */
+  const int32_t *n_tokens;        /* [rows]; not NULL with tokens */
+  const float *repetition, *frequency, *presence; /* [rows] each */
+  const int32_t *bias_offsets;    /* [rows + 1]: row r's list is entries bias_offsets[r] .. bias_offsets[r+1]-1 */
+  const int32_t *bias_ids;        /* ascending within a row's list (of equal ids the first counts) */
+  const float *bias_values;
+  int32_t n_bias;                 /* entries of bias_ids and bias_values */
+  int32_t n_masks;                /* rows of allow */
+  const uint32_t *allow;          /* [n_masks, ceil(vocab / 32)]: bit v % 32 of word v / 32 set = v is allowed */
+  const int32_t *allow_row;       /* [rows] mask of each row, -1: everything is allowed; NULL: mask r */
+} pg_logits;
+
+/* out[r, v] = z, fp32, a row every out_stride elements; out may be the logits themselves (fp32, equal strides). */
+pg_status pg_logits_adjust(const pg_logits *desc, float *out, int64_t out_stride, void *stream);
+
+/* Draws token[r] from softmax(y), y = z * (1 / temperature[r]), and logp[r] = y[token] - ln sum exp(y), in one pass over the logits:
+ * token = argmax_v y_v - ln E_v, E_v = -log1p(-min((n + 1/2) 2^-32, 1 - 2^-24)) exponential variates from word n = (v mod 4) of the
+ * Philox-4x32-10 block with counter (v div 4, step, ids[r], 2) and key (seed low, seed high); ids NULL: r.  The draw of a
+ * trajectory depends on its id alone, not on where pruning has packed it.  temperature[r] == 0: argmax z, logp at temperature 1; NULL: 1.
+ * Equal scores: the lowest token.  A row with nothing left: token -1, logp -inf.  A row with an allowed z that is NaN or +inf, or with
+ * a temperature that is negative, infinite or NaN: token -1, logp NaN.  scratch: pg_sample_scratch_floats(rows, vocab) floats. */
+int64_t pg_sample_scratch_floats(int32_t rows, int32_t vocab);
+pg_status pg_sample_tokens(const pg_logits *desc, const float *temperature, uint64_t seed, uint32_t step,
+                           const int32_t *ids, int32_t *token, float *logp, float *scratch, void *stream);
+
 /* ---- measurement hooks (process-wide, not thread-safe) ----
  * Between pg_profile_begin and pg_profile_end every launch of the heavy kernels is bracketed by a
  * pair of HIP events on the stream it is launched on (at most max_records launches are recorded).

@@ -55,6 +55,20 @@ class pg_buffers(C.Structure):
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("x_hist", C.c_void_p)]
 
 
+class pg_cache(C.Structure):
+    _fields_ = [("layers", C.c_int32), ("n_pages", C.c_int32), ("heads", C.c_int32), ("page", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("width", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("refs", C.c_void_p), ("status", C.c_void_p)]
+
+
+class pg_logits(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("stride", C.c_int64), ("dtype", C.c_int32), ("rows", C.c_int32),
+                ("vocab", C.c_int32), ("tokens_stride", C.c_int32), ("tokens", C.c_void_p), ("n_prompt", C.c_void_p),
+                ("n_tokens", C.c_void_p), ("repetition", C.c_void_p), ("frequency", C.c_void_p), ("presence", C.c_void_p),
+                ("bias_offsets", C.c_void_p), ("bias_ids", C.c_void_p), ("bias_values", C.c_void_p),
+                ("n_bias", C.c_int32), ("n_masks", C.c_int32), ("allow", C.c_void_p), ("allow_row", C.c_void_p)]
+
+
 class PgError(RuntimeError):
     def __init__(self, status, message):
         super().__init__(f"{STATUS_NAMES[status] if 0 <= status < 7 else status}: {message}")
@@ -62,6 +76,7 @@ class PgError(RuntimeError):
 
 
 _vp, _i32, _i64, _u64, _u32, _f64 = C.c_void_p, C.c_int32, C.c_int64, C.c_uint64, C.c_uint32, C.c_double
+_cp, _lp = C.POINTER(pg_cache), C.POINTER(pg_logits)
 _SIGNATURES = {
     "pg_last_error": (C.c_char_p, []),
     "pg_create": (_i32, [C.POINTER(pg_config), C.POINTER(_vp)]),
@@ -105,6 +120,19 @@ _SIGNATURES = {
     "pg_attention_kernel": (_i32, [_i32] * 5),
     "pg_attention_network": (_i32, [_vp, _vp, _vp, _vp] + [_i32] * 7 + [_vp]),
     "pg_mfma_probe": (_i32, [_i32, _i32, C.c_float, _vp, _dp, _vp]),
+    "pg_cache_clear": (_i32, [_cp, _vp]),
+    "pg_cache_reserve": (_i32, [_cp, _vp, _vp, _vp, _vp, _i32, _vp]),
+    "pg_cache_append": (_i32, [_cp, _i32, _vp, _vp, _i64, _vp, _vp, _vp, _i32, _i32, _vp]),
+    "pg_cache_scratch_ints": (_i64, [_cp, _i32]),
+    "pg_cache_select": (_i32, [_cp, _vp, _vp, _i32, _vp, _vp, _vp, _i32, _vp, _vp]),
+    "pg_cache_compact": (_i32, [_cp, _vp, _vp, _i32, _vp, _vp]),
+    "pg_cache_check": (_i32, [_cp, _vp]),
+    "pg_paged_attention_workspace": (C.c_size_t, [_cp, _i32, _i32, _i32]),
+    "pg_paged_attention": (_i32, [_cp, _i32, _vp, _i64, _vp, _i32, _vp, _vp, _i32, _i32, _f64, _i32, _vp, _i64, _vp, _vp,
+                                  C.c_size_t, _vp]),
+    "pg_logits_adjust": (_i32, [_lp, _vp, _i64, _vp]),
+    "pg_sample_scratch_floats": (_i64, [_i32, _i32]),
+    "pg_sample_tokens": (_i32, [_lp, _vp, _u64, _u32, _vp, _vp, _vp, _vp, _vp]),
     "pg_profile_begin": (_i32, [_i32]),
     "pg_profile_read": (_i32, [_i32, _dp, _dp, C.POINTER(_i64)]),
     "pg_profile_end": (_i32, []),
@@ -446,6 +474,158 @@ def pg_attention_kernel(B, Lq, Lk, heads, hd):
 
 def pg_attention_network(q, k, vt, out, B, Lq, Lk, Lk_pad, heads, hd, kernel=0, stream=None):
     _check(_lib.pg_attention_network(_ptr(q), _ptr(k), _ptr(vt), _ptr(out), B, Lq, Lk, Lk_pad, heads, hd, kernel, _stream(stream)))
+
+
+# ---------------------------------------------------------------- rollouts of a token policy
+
+PG_CACHE_BF16, PG_CACHE_E4M3 = 0, 1
+PG_CACHE_MAX_ROWS = 16384
+PG_LOGITS_F32, PG_LOGITS_BF16 = 0, 1
+
+
+def _i32s(t, *shape):
+    """A contiguous int32 tensor of this shape (None: any extent), or None."""
+    if t is not None:
+        assert str(t.dtype) == "torch.int32" and len(t.shape) == len(shape) and all(n is None or n == m for n, m in zip(shape, t.shape)), \
+            f"int32 {shape} wanted: {t.dtype} {tuple(t.shape)}"
+    return _ptr(t)
+
+
+def _f32s(t, *shape):
+    if t is not None:
+        assert str(t.dtype) == "torch.float32" and tuple(t.shape) == shape, f"float32 {shape} wanted: {t.dtype} {tuple(t.shape)}"
+    return _ptr(t)
+
+
+def _rows(t, heads, head_dim):
+    """Address and row stride (in elements) of [rows, heads, head_dim] in bf16 whose rows may be slices of longer ones."""
+    assert t.element_size() == 2 and tuple(t.shape[1:]) == (heads, head_dim), f"[rows, {heads}, {head_dim}] bf16 wanted: {t.dtype} {tuple(t.shape)}"
+    assert t.stride(2) == 1 and (heads == 1 or t.stride(1) == head_dim), "heads and channels of a row must be contiguous"
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), heads * head_dim)
+
+
+class Cache:
+    """Device tensors of a paged cache (the caller's) + the filled pg_cache.
+
+    k: [layers, pages, heads, page, head_dim], v: [layers, pages, heads, head_dim, page], both bf16 (or 16-bit patterns) or uint8
+    codes; refs: int32 [pages]; width: entries of a table's row."""
+
+    def __init__(self, k, v, refs, width, k_scale=None, v_scale=None, status=None):
+        import torch
+        layers, n_pages, heads, page, head_dim = k.shape
+        assert tuple(v.shape) == (layers, n_pages, heads, head_dim, page) and k.element_size() == v.element_size() <= 2
+        self.k, self.v, self.refs, self.k_scale, self.v_scale = k, v, refs, k_scale, v_scale
+        self.status = torch.zeros(4, dtype=torch.int32, device=k.device) if status is None else status
+        c = pg_cache()
+        c.layers, c.n_pages, c.heads, c.page, c.head_dim, c.width = layers, n_pages, heads, page, head_dim, width
+        c.dtype = PG_CACHE_BF16 if k.element_size() == 2 else PG_CACHE_E4M3
+        c.k, c.v = _ptr(k), _ptr(v)
+        c.k_scale, c.v_scale = _f32s(k_scale, layers, heads), _f32s(v_scale, layers, heads)
+        c.refs, c.status = _i32s(refs, n_pages), _i32s(self.status, 4)
+        self.c = c
+
+    @classmethod
+    def create(cls, layers, n_pages, heads, page, head_dim, width, dtype=PG_CACHE_BF16, device="cuda:0"):
+        """A cache with all pages free; e4m3 codes with scales of 1 to be overwritten."""
+        import torch
+        kind = torch.bfloat16 if dtype == PG_CACHE_BF16 else torch.uint8
+        z = lambda *shape, dtype=kind: torch.zeros(*shape, dtype=dtype, device=device)
+        scales = (None, None) if dtype == PG_CACHE_BF16 else (z(layers, heads, dtype=torch.float32) + 1, z(layers, heads, dtype=torch.float32) + 1)
+        return cls(z(layers, n_pages, heads, page, head_dim), z(layers, n_pages, heads, head_dim, page), z(n_pages, dtype=torch.int32), width, *scales)
+
+
+def pg_cache_clear(cache, stream=None):
+    _check(_lib.pg_cache_clear(C.byref(cache.c), _stream(stream)))
+
+
+def pg_cache_reserve(cache, table, lens, add, lens_out, stream=None):
+    n = lens.shape[0]
+    _check(_lib.pg_cache_reserve(C.byref(cache.c), _i32s(table, n, cache.c.width), _i32s(lens, n), _i32s(add, n), _i32s(lens_out, n), n,
+                                 _stream(stream)))
+
+
+def pg_cache_append(cache, layer, k_new, v_new, table, lens, cu=None, stream=None):
+    c, n = cache.c, lens.shape[0]
+    k, ks = _rows(k_new, c.heads, c.head_dim)
+    v, vs = _rows(v_new, c.heads, c.head_dim)
+    assert k_new.shape[0] == v_new.shape[0] and (ks == vs or k_new.shape[0] < 2), "keys and values of the same number and stride"
+    _check(_lib.pg_cache_append(C.byref(c), layer, k, v, ks, _i32s(table, n, c.width), _i32s(lens, n), _i32s(cu, n + 1), n, k_new.shape[0],
+                                _stream(stream)))
+
+
+def pg_cache_scratch_ints(cache, n_rows):
+    return int(_lib.pg_cache_scratch_ints(C.byref(cache.c), n_rows))
+
+
+def pg_cache_select(cache, table_in, lens_in, src, table_out, lens_out, scratch, stream=None):
+    n, m, w = lens_in.shape[0], src.shape[0], cache.c.width
+    assert scratch.numel() >= pg_cache_scratch_ints(cache, max(n, m))
+    _check(_lib.pg_cache_select(C.byref(cache.c), _i32s(table_in, n, w), _i32s(lens_in, n), n, _i32s(src, m), _i32s(table_out, m, w),
+                                _i32s(lens_out, m), m, _i32s(scratch, None), _stream(stream)))
+
+
+def pg_cache_compact(cache, table, lens, scratch, stream=None):
+    n = lens.shape[0]
+    assert scratch.numel() >= pg_cache_scratch_ints(cache, 0)
+    _check(_lib.pg_cache_compact(C.byref(cache.c), _i32s(table, n, cache.c.width), _i32s(lens, n), n, _i32s(scratch, None), _stream(stream)))
+
+
+def pg_cache_check(cache, stream=None):
+    _check(_lib.pg_cache_check(C.byref(cache.c), _stream(stream)))
+
+
+def pg_paged_attention_workspace(cache, n_q, heads_q, max_len):
+    return int(_lib.pg_paged_attention_workspace(C.byref(cache.c), n_q, heads_q, max_len))
+
+
+def pg_paged_attention(cache, layer, q, table, lens, out, max_len, workspace=None, lse=None, row_of=None, scale=0.0, stream=None):
+    c, (n, heads, hd) = cache.c, q.shape
+    qp, qs = _rows(q, heads, c.head_dim)
+    op, os_ = _rows(out, heads, c.head_dim)
+    assert out.shape == q.shape
+    _check(_lib.pg_paged_attention(C.byref(c), layer, qp, qs, _i32s(table, None, c.width), table.shape[0], _i32s(row_of, n), _i32s(lens, n), n,
+                                   heads, scale, max_len, op, os_, _f32s(lse, n, heads), _ptr(workspace),
+                                   0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+class Logits:
+    """Logits [rows, vocab] (fp32 or bf16; rows may be slices of longer ones), what is to be done to them, and the filled pg_logits."""
+
+    def __init__(self, logits, tokens=None, n_prompt=None, n_tokens=None, repetition=None, frequency=None, presence=None,
+                 bias_offsets=None, bias_ids=None, bias_values=None, allow=None, allow_row=None):
+        rows, vocab = logits.shape
+        assert str(logits.dtype) in ("torch.float32", "torch.bfloat16") and (vocab == 1 or logits.stride(1) == 1)
+        self.keep = (logits, tokens, n_prompt, n_tokens, repetition, frequency, presence, bias_offsets, bias_ids, bias_values, allow, allow_row)
+        d = pg_logits()
+        d.logits, d.stride = logits.data_ptr(), logits.stride(0) if rows > 1 else max(logits.stride(0), vocab)
+        d.dtype = PG_LOGITS_F32 if logits.element_size() == 4 else PG_LOGITS_BF16
+        d.rows, d.vocab = rows, vocab
+        d.tokens, d.tokens_stride = _i32s(tokens, rows, None), 0 if tokens is None else tokens.shape[1]
+        d.n_prompt, d.n_tokens = _i32s(n_prompt, rows), _i32s(n_tokens, rows)
+        d.repetition, d.frequency, d.presence = (_f32s(t, rows) for t in (repetition, frequency, presence))
+        d.bias_offsets = _i32s(bias_offsets, rows + 1)
+        d.n_bias = 0 if bias_ids is None else bias_ids.shape[0]
+        d.bias_ids, d.bias_values = _i32s(bias_ids, d.n_bias), _f32s(bias_values, d.n_bias)
+        d.allow, d.n_masks = _i32s(allow, None, (vocab + 31) // 32), 0 if allow is None else allow.shape[0]
+        d.allow_row = _i32s(allow_row, rows)
+        self.c = d
+
+
+def pg_logits_adjust(desc, out, stream=None):
+    d = desc.c
+    assert tuple(out.shape) == (d.rows, d.vocab) and str(out.dtype) == "torch.float32" and (d.vocab == 1 or out.stride(1) == 1)
+    _check(_lib.pg_logits_adjust(C.byref(d), out.data_ptr(), out.stride(0) if d.rows > 1 else max(out.stride(0), d.vocab), _stream(stream)))
+
+
+def pg_sample_scratch_floats(rows, vocab):
+    return int(_lib.pg_sample_scratch_floats(rows, vocab))
+
+
+def pg_sample_tokens(desc, temperature, seed, step, ids, token, logp, scratch, stream=None):
+    d = desc.c
+    assert scratch.numel() >= pg_sample_scratch_floats(d.rows, d.vocab)
+    _check(_lib.pg_sample_tokens(C.byref(d), _f32s(temperature, d.rows), seed, step, _i32s(ids, d.rows), _i32s(token, d.rows),
+                                 _f32s(logp, d.rows), _ptr(scratch), _stream(stream)))
 
 
 def pg_mfma_probe(blocks, iters, operand_scale, out, stream=None):
