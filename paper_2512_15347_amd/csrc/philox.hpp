@@ -19,15 +19,17 @@ constexpr uint32_t STREAM_STEP = 1u;
 struct u32x4 { uint32_t x, y, z, w; };
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
+// XOR3: the round's two exclusive ors in one instruction each (the compiler takes two), for the draws, which the vector ALU bounds
+template <bool XOR3 = false>
 __device__ __forceinline__ u32x4 philox4x32_10(u32x4 c, uint32_t k0, uint32_t k1) {
 #pragma unroll
   for (int r = 0; r < 10; ++r) {
     const uint64_t p0 = (uint64_t)PHILOX_M0 * c.x;
     const uint64_t p1 = (uint64_t)PHILOX_M1 * c.z;
     u32x4 n;
-    n.x = (uint32_t)(p1 >> 32) ^ c.y ^ k0;
+    n.x = XOR3 ? __builtin_amdgcn_bitop3_b32((uint32_t)(p1 >> 32), c.y, k0, 0x96) : (uint32_t)(p1 >> 32) ^ c.y ^ k0;
     n.y = (uint32_t)p1;
-    n.z = (uint32_t)(p0 >> 32) ^ c.w ^ k1;
+    n.z = XOR3 ? __builtin_amdgcn_bitop3_b32((uint32_t)(p0 >> 32), c.w, k1, 0x96) : (uint32_t)(p0 >> 32) ^ c.w ^ k1;
     n.w = (uint32_t)p0;
     c = n;
     k0 += PHILOX_W0;

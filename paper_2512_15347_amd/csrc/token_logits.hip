@@ -1,9 +1,9 @@
 // Logits of a token policy: penalties, biases and grammar masks, and the draw of a token with its log-prob.
 //
-// A workgroup takes chunks of one row's vocabulary.  How often each of a chunk's tokens occurs is counted in LDS from the row's
-// history (32 bits a token: integer sums, so their order does not matter), so no counts are kept between calls and nothing but the
-// history has to follow a member through a prune.  The logits are read once, asked for before the counting starts; groups of eight tokens
-// without a count or a bias skip the rules.
+// A workgroup takes a range of one row's vocabulary and goes through it in groups of eight tokens a lane.  Few tokens have a penalty or a
+// bias: for every 4096 tokens the row's history is counted in LDS (32 bits a token: integer sums, so their order does not matter), the
+// tokens that occur are worked out once each and left in LDS, and the groups pick them up by a bit.  So no counts are kept
+// between calls, and nothing but the history has to follow a member through a prune.  The logits are read once.
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
@@ -19,13 +19,13 @@ constexpr int LANE_TOKENS = 8;                       // a group: 16 or 32 bytes,
 constexpr int PASS_TOKENS = LOGIT_THREADS * LANE_TOKENS;
 constexpr uint32_t STREAM_TOKEN = 2u;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-// LDS word of a token: how often it is in the output, and whether it is in the prompt or has a bias
+// LDS word of a token: how often it is in the output, and whether it is in the prompt or has a bias; then its z
 constexpr uint32_t IN_PROMPT = 1u << 31, HAS_BIAS = 1u << 30, COUNT = HAS_BIAS - 1;
 
 struct LogitArgs {
   pg_logits d;
   int words;                                         // of a mask
-  int per;                                           // chunks of a workgroup
+  int range;                                         // tokens of a workgroup, a multiple of the counted stretch
   bool count;                                        // there is a history or a bias list
 };
 
@@ -59,129 +59,218 @@ __device__ __forceinline__ RowRules row_rules(const LogitArgs& a, int r) {
   return q;
 }
 
-// A lane's groups of one chunk: logits from any address that is a multiple of their size (the hardware takes unaligned 16-byte
-// loads) and mask bytes.  Group g of the workgroup starts at token g * PASS_TOKENS of the chunk.
-template <bool BF16, int G>
-struct Groups {
-  uint32_t raw[G][BF16 ? 4 : 8];
-  uint32_t allowed[G];
+// A lane's group: eight logits from any address that is a multiple of their size (the hardware takes unaligned 16-byte loads) and
+// their bits of the mask; tokens past the end of the row are not allowed.
+template <bool BF16>
+struct Group {
+  uint32_t raw[BF16 ? 4 : 8];
+  uint32_t allowed;
 
-  __device__ __forceinline__ void load(const LogitArgs& a, const RowRules& q, int64_t row, int v0, int n) {
+  __device__ __forceinline__ void load(const LogitArgs& a, const RowRules& q, int64_t row, int64_t v) {
+    const int64_t left = a.d.vocab - v;
+    allowed = 0;
+    if (left <= 0) return;
+    const char* p = (const char*)a.d.logits + (row + v) * (BF16 ? 2 : 4);
+    if (left >= LANE_TOKENS) {
+      __builtin_memcpy(raw, p, BF16 ? 16 : 32);
+    } else {
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-      const int i = g * PASS_TOKENS + (int)threadIdx.x * LANE_TOKENS, left = n - i;
-      allowed[g] = 0;
-      if (left <= 0) continue;
-      const char* p = (const char*)a.d.logits + (row + v0 + i) * (BF16 ? 2 : 4);
-      if (left >= LANE_TOKENS) {
-        __builtin_memcpy(raw[g], p, BF16 ? 16 : 32);
-      } else {
-#pragma unroll
-        for (int e = 0; e < LANE_TOKENS; ++e) {
-          const uint32_t x = e >= left ? 0u : BF16 ? ((const uint16_t*)p)[e] : ((const uint32_t*)p)[e];
-          if (!BF16) raw[g][e] = x;
-          else raw[g][e >> 1] = e & 1 ? raw[g][e >> 1] | x << 16 : x;
-        }
+      for (int e = 0; e < LANE_TOKENS; ++e) {
+        const uint32_t x = e >= left ? 0u : BF16 ? ((const uint16_t*)p)[e] : ((const uint32_t*)p)[e];
+        if (!BF16) raw[e] = x;
+        else raw[e >> 1] = e & 1 ? raw[e >> 1] | x << 16 : x;
       }
-      allowed[g] = (q.allow ? q.allow[(v0 + i) >> 3] : 0xFFu) & (left >= LANE_TOKENS ? 0xFFu : (1u << left) - 1);
     }
+    allowed = (q.allow ? q.allow[v >> 3] : 0xFFu) & (left >= LANE_TOKENS ? 0xFFu : (1u << left) - 1);
   }
-  __device__ __forceinline__ float logit(int g, int e) const {
-    return __builtin_bit_cast(float, !BF16 ? raw[g][e] : e & 1 ? raw[g][e >> 1] & 0xFFFF0000u : raw[g][e >> 1] << 16);
+  __device__ __forceinline__ float logit(int e) const {
+    return __builtin_bit_cast(float, !BF16 ? raw[e] : e & 1 ? raw[e >> 1] & 0xFFFF0000u : raw[e >> 1] << 16);
   }
 };
 
-// The chunk's LDS words from the history and the bias list.
+// LDS of a counted stretch of G * PASS_TOKENS tokens: all zero between stretches (a group clears what it picks up).
 template <int G>
-__device__ __forceinline__ void count_tokens(const LogitArgs& a, const RowRules& q, int r, int v0, int n, uint32_t* lds) {
-  const pg_logits& d = a.d;
-  __syncthreads();                                   // the words of the chunk before have been read
+struct Stretch {
+  static constexpr int TOKENS = G * PASS_TOKENS;
+  uint32_t word[TOKENS];
+  uint32_t ready[TOKENS / 32];                       // bit: word holds z
+  uint16_t seen[TOKENS];                             // tokens that occur past the part of the history in registers, in no particular order
+  int n_seen;
+};
+
+// A lane's part of the row's history and bias list: the first entries stay in registers from stretch to stretch.
+struct RowLists {
+  static constexpr int KEPT = 4;                     // 1024 tokens of the workgroup's
+  int32_t token[KEPT];
+  int32_t bias_id, bias_before;
+  float bias;
+};
+constexpr int32_t NO_TOKEN = -1;                     // is in no stretch
+
+__device__ __forceinline__ RowLists row_lists(const LogitArgs& a, const RowRules& q, int r) {
+  RowLists l;
+  const int32_t* t = a.d.tokens + (int64_t)r * a.d.tokens_stride;
 #pragma unroll
-  for (int g = 0; g < 2 * G; ++g) ((uint4*)lds)[g * LOGIT_THREADS + threadIdx.x] = uint4{0, 0, 0, 0};
-  __syncthreads();
-  const int32_t* t = d.tokens + (int64_t)r * d.tokens_stride;
-#pragma unroll 4
-  for (int i = threadIdx.x; i < q.made; i += LOGIT_THREADS) {
-    const uint32_t at = (uint32_t)t[i] - (uint32_t)v0;
-    if (at < (uint32_t)n) {
-      if (i < q.prompt) atomicOr(&lds[at], IN_PROMPT);
-      else atomicAdd(&lds[at], 1u);
-    }
+  for (int k = 0; k < RowLists::KEPT; ++k) {
+    const int i = threadIdx.x + k * LOGIT_THREADS;
+    l.token[k] = a.d.tokens && i < a.d.tokens_stride ? t[i] : NO_TOKEN;      // asked for beside the count itself
   }
-  for (int i = q.bias_lo + threadIdx.x; i < q.bias_hi; i += LOGIT_THREADS) {
-    const uint32_t at = (uint32_t)d.bias_ids[i] - (uint32_t)v0;
-    if (at < (uint32_t)n) atomicOr(&lds[at], HAS_BIAS);
-  }
-  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < RowLists::KEPT; ++k)
+    if ((int)threadIdx.x + k * LOGIT_THREADS >= q.made) l.token[k] = NO_TOKEN;
+  const int i = q.bias_lo + threadIdx.x;
+  const bool there = i < q.bias_hi;
+  l.bias_id = there ? a.d.bias_ids[i] : NO_TOKEN;
+  l.bias_before = there && i > q.bias_lo ? a.d.bias_ids[i - 1] : NO_TOKEN;
+  l.bias = there ? a.d.bias_values[i] : 0.0f;
+  return l;
 }
 
-// z of one token that has a count or a bias; the order and the rounding of the operations are the interface's.
-__device__ __forceinline__ float adjusted(const LogitArgs& a, const RowRules& q, float x, uint32_t word, int v) {
+// z from the history alone; the order and the rounding of the operations are the interface's.
+__device__ __forceinline__ float penalised(const RowRules& q, float x, uint32_t word) {
   if (word & (IN_PROMPT | COUNT)) {
     x = x > 0.0f ? x / q.rep : x * q.rep;
     x = x - q.freq * (float)(word & COUNT);
     if (word & COUNT) x = x - q.pres;
   }
-  if (word & HAS_BIAS) {
-    int lo = q.bias_lo, hi = q.bias_hi - 1;          // the first entry that is not below v
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (a.d.bias_ids[mid] < v) lo = mid + 1; else hi = mid;
-    }
-    if (a.d.bias_ids[lo] == v) x = x + a.d.bias_values[lo];
-  }
   return x;
 }
 
-// z of group g; tokens that are not allowed, or past the row, get -inf
+// z of the tokens of v0 .. v0 + n - 1 that have a count or a bias.  Each word has one owner, who turns it into z: the first of its
+// bias entries, or else the history entry that found it zero.
 template <bool BF16, int G>
-__device__ __forceinline__ void group_logits(const LogitArgs& a, const RowRules& q, const Groups<BF16, G>& x, int g, int v0, const uint32_t* lds,
-                                             float* z) {
+__device__ __forceinline__ void prepare_stretch(const LogitArgs& a, const RowRules& q, const RowLists& l, int r, int v0, int n, Stretch<G>& s) {
+  const pg_logits& d = a.d;
+  const int64_t row = (int64_t)r * d.stride + v0;
+  auto logit = [&](uint32_t at) { return BF16 ? bf16_to_f32(((const uint16_t*)d.logits)[row + at]) : ((const float*)d.logits)[row + at]; };
+  auto count = [&](uint32_t at, int i) { return i < q.prompt ? atomicOr(&s.word[at], IN_PROMPT) : atomicAdd(&s.word[at], 1u); };
+  auto finish = [&](uint32_t at, float z) {
+    s.word[at] = __builtin_bit_cast(uint32_t, z);
+    atomicOr(&s.ready[at >> 5], 1u << (at & 31));
+  };
+  __syncthreads();                                   // the stretch before has been read
+  if (threadIdx.x == 0) s.n_seen = 0;
+  float x[RowLists::KEPT], bias_x = 0.0f;
+  uint32_t owner = 0;
+  const uint32_t bias_at = (uint32_t)l.bias_id - (uint32_t)v0;
+  if (bias_at < (uint32_t)n) {
+    bias_x = logit(bias_at);
+    atomicOr(&s.word[bias_at], HAS_BIAS);
+  }
+  const bool more = q.made > RowLists::KEPT * LOGIT_THREADS;
+  if (more) __syncthreads();                         // n_seen
 #pragma unroll
-  for (int e = 0; e < LANE_TOKENS; ++e) z[e] = x.logit(g, e);
-  if (a.count) {
-    const int i = g * PASS_TOKENS + (int)threadIdx.x * LANE_TOKENS;
-    const uint4 w0 = *(const uint4*)(lds + i), w1 = *(const uint4*)(lds + i + 4);
-    const uint32_t w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
-    if ((w[0] | w[1] | w[2] | w[3]) | (w[4] | w[5] | w[6] | w[7])) {
+  for (int k = 0; k < RowLists::KEPT; ++k) {
+    const uint32_t at = (uint32_t)l.token[k] - (uint32_t)v0;
+    if (at < (uint32_t)n && (count(at, threadIdx.x + k * LOGIT_THREADS) & ~HAS_BIAS) == 0) {
+      x[k] = logit(at);
+      owner |= 1u << k;
+    }
+  }
+  if (more) {
+    const int32_t* t = d.tokens + (int64_t)r * d.tokens_stride;
+#pragma unroll 4
+    for (int i = RowLists::KEPT * LOGIT_THREADS + threadIdx.x; i < q.made; i += LOGIT_THREADS) {
+      const uint32_t at = (uint32_t)t[i] - (uint32_t)v0;
+      if (at < (uint32_t)n && (count(at, i) & ~HAS_BIAS) == 0) s.seen[atomicAdd(&s.n_seen, 1)] = (uint16_t)at;
+    }
+  }
+  for (int i = q.bias_lo + LOGIT_THREADS + threadIdx.x; i < q.bias_hi; i += LOGIT_THREADS) {
+    const uint32_t at = (uint32_t)d.bias_ids[i] - (uint32_t)v0;
+    if (at < (uint32_t)n) atomicOr(&s.word[at], HAS_BIAS);
+  }
+  __syncthreads();
 #pragma unroll
-      for (int e = 0; e < LANE_TOKENS; ++e)
-        if (w[e]) z[e] = adjusted(a, q, z[e], w[e], v0 + i + e);
+  for (int k = 0; k < RowLists::KEPT; ++k)
+    if (owner >> k & 1) {
+      const uint32_t at = (uint32_t)l.token[k] - (uint32_t)v0, word = s.word[at];
+      if (!(word & HAS_BIAS)) finish(at, penalised(q, x[k], word));
+    }
+  if (more)
+    for (int k = threadIdx.x; k < s.n_seen; k += LOGIT_THREADS) {
+      const uint32_t at = s.seen[k], word = s.word[at];
+      if (!(word & HAS_BIAS)) finish(at, penalised(q, logit(at), word));
+    }
+  if (q.bias_lo < q.bias_hi) __syncthreads();        // the history's owners have looked for HAS_BIAS in words that become z here
+  if (bias_at < (uint32_t)n && l.bias_before != l.bias_id) finish(bias_at, penalised(q, bias_x, s.word[bias_at]) + l.bias);
+  for (int i = q.bias_lo + LOGIT_THREADS + threadIdx.x; i < q.bias_hi; i += LOGIT_THREADS) {
+    const uint32_t at = (uint32_t)d.bias_ids[i] - (uint32_t)v0;
+    if (at < (uint32_t)n && d.bias_ids[i - 1] != d.bias_ids[i]) finish(at, penalised(q, logit(at), s.word[at]) + d.bias_values[i]);
+  }
+  __syncthreads();
+}
+
+// z of a group whose first token is number `at` of its stretch; tokens that are not allowed get -inf
+template <bool BF16, int G>
+__device__ __forceinline__ void group_logits(bool count, const Group<BF16>& x, int at, Stretch<G>& s, float* z) {
+#pragma unroll
+  for (int e = 0; e < LANE_TOKENS; ++e) z[e] = x.logit(e);
+  if (count) {
+    const uint32_t ready = ((const uint8_t*)s.ready)[at >> 3];
+    if (ready) {
+      const float4 w0 = *(const float4*)(s.word + at), w1 = *(const float4*)(s.word + at + 4);
+      *(uint4*)(s.word + at) = *(uint4*)(s.word + at + 4) = uint4{0, 0, 0, 0};
+      ((uint8_t*)s.ready)[at >> 3] = 0;
+      const float w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+#pragma unroll
+      for (int e = 0; e < LANE_TOKENS; ++e) z[e] = ready >> e & 1 ? w[e] : z[e];
     }
   }
 #pragma unroll
-  for (int e = 0; e < LANE_TOKENS; ++e) z[e] = x.allowed[g] >> e & 1 ? z[e] : -INFINITY;
+  for (int e = 0; e < LANE_TOKENS; ++e) z[e] = x.allowed >> e & 1 ? z[e] : -INFINITY;
+}
+
+// Goes through the workgroup's range, one group a lane and call of each(group, first token, place in the stretch); the next group is
+// asked for before a group is worked on.
+template <bool BF16, int G, class Each>
+__device__ __forceinline__ void through_range(const LogitArgs& a, const RowRules& q, int r, Stretch<G>& s, Each each) {
+  const int64_t row = (int64_t)r * a.d.stride, first = (int64_t)blockIdx.x * a.range;
+  const int64_t end = min(first + a.range, (int64_t)a.d.vocab);
+  RowLists lists;
+  if (a.count) {
+    lists = row_lists(a, q, r);
+#pragma unroll
+    for (int g = 0; g < 2 * G; ++g) ((uint4*)s.word)[g * LOGIT_THREADS + threadIdx.x] = uint4{0, 0, 0, 0};
+    if (threadIdx.x < Stretch<G>::TOKENS / 32) s.ready[threadIdx.x] = 0;
+  }
+  Group<BF16> x;
+  x.load(a, q, row, first + threadIdx.x * LANE_TOKENS);
+#pragma unroll 1
+  for (int64_t base = first; base < end; base += PASS_TOKENS) {
+    const int at = (int)((base - first) % Stretch<G>::TOKENS);
+    if (a.count && at == 0) prepare_stretch<BF16, G>(a, q, lists, r, (int)base, (int)min((int64_t)Stretch<G>::TOKENS, end - base), s);
+    const int64_t v = base + threadIdx.x * LANE_TOKENS;
+    Group<BF16> next;
+    next.load(a, q, row, base + PASS_TOKENS < end ? v + PASS_TOKENS : (int64_t)a.d.vocab);
+    each(x, v, at + (int)threadIdx.x * LANE_TOKENS);
+    x = next;
+  }
 }
 
 template <bool BF16, int G>
 __global__ __launch_bounds__(LOGIT_THREADS) void logits_adjust_kernel(LogitArgs a, float* out, int64_t out_stride) {
-  extern __shared__ uint32_t lds[];
-  constexpr int CHUNK = G * PASS_TOKENS;
-  const int r = blockIdx.y, v0 = blockIdx.x * CHUNK;
-  const int n = min(CHUNK, a.d.vocab - v0);
+  extern __shared__ __align__(16) char lds[];
+  Stretch<G>& s = *(Stretch<G>*)lds;
+  const int r = blockIdx.y;
   const RowRules q = row_rules(a, r);
-  Groups<BF16, G> x;
-  x.load(a, q, (int64_t)r * a.d.stride, v0, n);
-  if (a.count) count_tokens<G>(a, q, r, v0, n, lds);
-  float* to = out + (int64_t)r * out_stride + v0;
-#pragma unroll
-  for (int g = 0; g < G; ++g) {
-    const int i = g * PASS_TOKENS + (int)threadIdx.x * LANE_TOKENS, left = n - i;
-    if (left <= 0) continue;
+  float* to = out + (int64_t)r * out_stride;
+  through_range<BF16, G>(a, q, r, s, [&](const Group<BF16>& x, int64_t v, int at) {
+    const int64_t left = a.d.vocab - v;
+    if (left <= 0) return;
     float z[8];
-    group_logits<BF16, G>(a, q, x, g, v0, lds, z);
+    group_logits<BF16, G>(a.count, x, at, s, z);
     if (left >= LANE_TOKENS) {
-      __builtin_memcpy(to + i, z, 32);
+      __builtin_memcpy(to + v, z, 32);
     } else {
 #pragma unroll
       for (int e = 0; e < LANE_TOKENS; ++e)
-        if (e < left) to[i + e] = z[e];
+        if (e < left) to[v + e] = z[e];
     }
-  }
+  });
 }
 
 // ---------------------------------------------------------------- the draw
-// What a chunk, a wave or a lane knows of a row: the largest y and the sum of exp(y - top) (NaN once a y was NaN or +inf), the best
+// What a workgroup, a wave or a lane knows of a row: the largest y and the sum of exp(y - top) (NaN once a y was NaN or +inf), the best
 // score with its token and that token's y.
 struct Draw {
   float top, sum, score, y;
@@ -229,12 +318,12 @@ __device__ __forceinline__ Draw wave_join(Draw a) {
 // Philox word, one exponential and one multiply-add; b is the best lower bound y - ln w - w (ln E <= ln w + w for w <= 1/2) of
 // a token that the workgroup has seen, and only tokens that reach it get their score, from the C library's logarithms.
 template <bool BF16, int G>
-__global__ __launch_bounds__(LOGIT_THREADS) void sample_chunk_kernel(LogitArgs a, const float* temperature, uint32_t k0, uint32_t k1,
+__global__ __launch_bounds__(LOGIT_THREADS) void sample_range_kernel(LogitArgs a, const float* temperature, uint32_t k0, uint32_t k1,
                                                                      uint32_t step, const int32_t* ids, Draw* parts) {
-  extern __shared__ uint32_t lds[];
+  extern __shared__ __align__(16) char lds[];
+  Stretch<G>& s = *(Stretch<G>*)lds;
   __shared__ Draw waves[LOGIT_WAVES];
   __shared__ int shared_bound;                       // the bits of a float, ordered as integers
-  constexpr int CHUNK = G * PASS_TOKENS;
   const int r = blockIdx.y;
   const RowRules q = row_rules(a, r);
   const float t = temperature ? temperature[r] : 1.0f;
@@ -243,81 +332,81 @@ __global__ __launch_bounds__(LOGIT_THREADS) void sample_chunk_kernel(LogitArgs a
   const uint32_t id = ids ? (uint32_t)ids[r] : (uint32_t)r;
   auto ordered = [](int b) { return b ^ (b >> 31 & 0x7FFFFFFF); };       // its own inverse
   if (threadIdx.x == 0) shared_bound = ordered(__builtin_bit_cast(int, -INFINITY));
-  if (!a.count) __syncthreads();
+  __syncthreads();
   Draw mine = no_draw();
-  for (int c = 0; c < a.per; ++c) {
-    const int64_t first = ((int64_t)blockIdx.x * a.per + c) * CHUNK;
-    if (first >= a.d.vocab) break;
-    const int v0 = (int)first, n = min(CHUNK, a.d.vocab - v0);
-    Groups<BF16, G> x;
-    x.load(a, q, (int64_t)r * a.d.stride, v0, n);
-    if (a.count) count_tokens<G>(a, q, r, v0, n, lds);
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-      const int i = g * PASS_TOKENS + (int)threadIdx.x * LANE_TOKENS, v = v0 + i;
-      if (n - (g * PASS_TOKENS + (int)(threadIdx.x & ~63u) * LANE_TOKENS) <= 0) continue;      // nothing of the wave's
-      float y[8];
-      group_logits<BF16, G>(a, q, x, g, v0, lds, y);
-      if (greedy) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (y[e] > mine.score) {                   // tokens ascend within a lane
-            mine.score = mine.y = y[e];
-            mine.token = v + e;
-          }
-      }
-      float top = mine.top;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        y[e] *= inv;
-        top = fmaxf(top, y[e]);
-      }
-      float sum = mine.sum * exp_of(mine.top - top);
-      mine.top = top;
-      float p[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[e] = exp_of(y[e] - top);
-        sum += p[e];
-      }
-      mine.sum = sum;
-      if (greedy) continue;
-      const u32x4 b0 = philox4x32_10(u32x4{(uint32_t)v >> 2, step, id, STREAM_TOKEN}, k0, k1);
-      const u32x4 b1 = philox4x32_10(u32x4{((uint32_t)v >> 2) + 1, step, id, STREAM_TOKEN}, k0, k1);
-      const float w[8] = {(float)b0.x, (float)b0.y, (float)b0.z, (float)b0.w, (float)b1.x, (float)b1.y, (float)b1.z, (float)b1.w};
-      float bound = __builtin_bit_cast(float, ordered(*(volatile int*)&shared_bound));
-      // 2^32, and 1e-3 for the rounding of the exponentials
-      const float reach = exp_of(top - bound) * 4.2992672e9f;
-      float far = -1.0f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) far = fmaxf(far, __builtin_fmaf(p[e], reach, -w[e]));
-      if (!__ballot(far >= 0.0f)) continue;
-      float up[8], low = -INFINITY;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float u = (w[e] + 0.5f) * 2.3283064365386963e-10f;
-        up[e] = y[e] - LN2 * __builtin_amdgcn_logf(u);
-        if (u < 0.5f) low = fmaxf(low, up[e] - u);
-      }
-      low = wave_max(low);
-      low -= 1e-4f + 1e-6f * fabsf(low);             // what the logarithms above may be off
-      if (low > bound) {
-        bound = low;
-        atomicMax(&shared_bound, ordered(__builtin_bit_cast(int, bound)));
-      }
+  through_range<BF16, G>(a, q, r, s, [&](const Group<BF16>& x, int64_t v, int at) {
+    if (a.d.vocab - (v - (int)(threadIdx.x & 63) * LANE_TOKENS) <= 0) return;      // nothing of the wave's
+    float y[8];
+    group_logits<BF16, G>(a.count, x, at, s, y);
+    if (greedy) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (up[e] >= bound && y[e] > -INFINITY) {
-          const float u = fminf((w[e] + 0.5f) * 2.3283064365386963e-10f, 0.99999994f);
-          const float score = y[e] - logf(-log1pf(-u));
-          if (score > mine.score) {
-            mine.score = score;
-            mine.token = v + e;
-            mine.y = y[e];
-          }
+        if (y[e] > mine.score) {                     // tokens ascend within a lane
+          mine.score = mine.y = y[e];
+          mine.token = (int)v + e;
         }
     }
-  }
+    float top = mine.top;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      y[e] *= inv;
+      top = fmaxf(top, y[e]);
+    }
+    float sum = mine.sum * exp_of(mine.top - top);
+    mine.top = top;
+    float p[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      p[e] = exp_of(y[e] - top);
+      sum += p[e];
+    }
+    mine.sum = sum;
+    if (greedy) return;
+    const uint32_t block = (uint32_t)v >> 2;
+    const u32x4 b0 = philox4x32_10<true>(u32x4{block, step, id, STREAM_TOKEN}, k0, k1);
+    const u32x4 b1 = philox4x32_10<true>(u32x4{block + 1, step, id, STREAM_TOKEN}, k0, k1);
+    const float w[8] = {(float)b0.x, (float)b0.y, (float)b0.z, (float)b0.w, (float)b1.x, (float)b1.y, (float)b1.z, (float)b1.w};
+    float bound = __builtin_bit_cast(float, ordered(__hip_atomic_load(&shared_bound, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP)));
+    // 2^32, and 1e-3 for the rounding of the exponentials
+    const float reach = exp_of(top - bound) * 4.2992672e9f;
+    float far = -1.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) far = fmaxf(far, __builtin_fmaf(p[e], reach, -w[e]));
+    if (!__ballot(far >= 0.0f)) return;
+    float up[8], low = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float u = (w[e] + 0.5f) * 2.3283064365386963e-10f;
+      up[e] = y[e] - LN2 * __builtin_amdgcn_logf(u);
+      if (u < 0.5f) low = fmaxf(low, up[e] - u);
+    }
+    low = wave_max(low);
+    low -= 1e-4f + 1e-6f * fabsf(low);               // what the logarithms above may be off
+    if (low > bound) {
+      bound = low;
+      atomicMax(&shared_bound, ordered(__builtin_bit_cast(int, bound)));
+    }
+    uint32_t reached = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) reached |= (uint32_t)(up[e] >= bound && y[e] > -INFINITY) << e;
+    while (reached) {                                // a token or two of the wave's
+      const int e = __builtin_ctz(reached);
+      reached &= reached - 1;
+      float ye = y[0], we = w[0];
+#pragma unroll
+      for (int k = 1; k < 8; ++k) {
+        ye = e == k ? y[k] : ye;
+        we = e == k ? w[k] : we;
+      }
+      const float u = fminf((we + 0.5f) * 2.3283064365386963e-10f, 0.99999994f);
+      const float score = ye - logf(-log1pf(-u));
+      if (score > mine.score) {
+        mine.score = score;
+        mine.token = (int)v + e;
+        mine.y = ye;
+      }
+    }
+  });
   if (!(t >= 0.0f && t < INFINITY)) mine.sum = __builtin_nanf("");
   mine = wave_join(mine);
   if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = mine;
@@ -328,10 +417,10 @@ __global__ __launch_bounds__(LOGIT_THREADS) void sample_chunk_kernel(LogitArgs a
   }
 }
 
-__global__ __launch_bounds__(WAVE) void sample_finish_kernel(const Draw* parts, int chunks, int32_t* token, float* logp) {
+__global__ __launch_bounds__(WAVE) void sample_finish_kernel(const Draw* parts, int ranges, int32_t* token, float* logp) {
   const int r = blockIdx.x;
   Draw mine = no_draw();
-  for (int i = threadIdx.x; i < chunks; i += WAVE) join(mine, parts[(int64_t)r * chunks + i]);
+  for (int i = threadIdx.x; i < ranges; i += WAVE) join(mine, parts[(int64_t)r * ranges + i]);
   mine = wave_join(mine);
   if (threadIdx.x == 0) {
     const bool bad = mine.sum != mine.sum, none = mine.token == INT32_MAX;
@@ -342,22 +431,17 @@ __global__ __launch_bounds__(WAVE) void sample_finish_kernel(const Draw* parts, 
 
 // ---------------------------------------------------------------- host side
 
-// Groups of a lane in a chunk (1, 2 or 4).  The history is read once a chunk and LDS holds 4 bytes a token, so chunks are long (8192
-// tokens: 32 KB, five workgroups a compute unit) unless there are too few rows to fill the device with such.
-static int groups_of(int64_t rows, int64_t vocab) {
-  int g = 4;
-  while (g > 1 && rows * ((vocab + g * PASS_TOKENS - 1) / (g * PASS_TOKENS)) < 1024) g /= 2;
-  return g;
+// How a call is laid out: tokens of a counted stretch (2048 or 4096: a shorter one where there are few rows, so that more workgroups
+// share them) and of a workgroup, and workgroups a row.  `few`: workgroups that are enough; a draw's workgroup finds the bound that the tokens
+// have to reach anew, so it takes several stretches where that leaves so many.
+struct LogitGrid { int groups, range, workgroups; };
+static LogitGrid logit_grid(int64_t rows, int64_t vocab, int64_t few) {
+  const int g = rows * ((vocab + 2 * PASS_TOKENS - 1) / (2 * PASS_TOKENS)) < 1024 ? 1 : 2;
+  const int64_t stretches = (vocab + g * PASS_TOKENS - 1) / (g * PASS_TOKENS);
+  const int64_t per = std::min<int64_t>(stretches, std::max<int64_t>(1, rows * stretches / few));
+  return LogitGrid{g, (int)(per * g * PASS_TOKENS), (int)((stretches + per - 1) / per)};
 }
-// Chunks of a workgroup in a draw: the bound that the tokens have to reach is found anew by each workgroup, so it takes several chunks
-// where that leaves enough workgroups.
-struct DrawGrid { int groups, per, workgroups; };
-static DrawGrid draw_grid(int64_t rows, int64_t vocab) {
-  const int g = groups_of(rows, vocab);
-  const int64_t chunks = (vocab + g * PASS_TOKENS - 1) / (g * PASS_TOKENS);
-  const int64_t per = std::min<int64_t>(chunks, std::max<int64_t>(1, rows * chunks / 2048));
-  return DrawGrid{g, (int)per, (int)((chunks + per - 1) / per)};
-}
+constexpr int64_t FEW_ADJUST = 8192, FEW_DRAW = 4096;
 
 static pg_status logit_args(const pg_logits* d, const char* who, LogitArgs& a) {
   if (!d) return fail(PG_EINVAL, "%s: desc is NULL", who);
@@ -383,15 +467,12 @@ static pg_status logit_args(const pg_logits* d, const char* who, LogitArgs& a) {
 }
 
 // launches F<bf16, groups>
-#define PG_LOGIT_KERNEL(F, groups, ...)                                                   \
-  do {                                                                                    \
-    const bool b = a.d.dtype == PG_LOGITS_BF16;                                           \
-    const size_t lds = a.count ? (size_t)(groups) * PASS_TOKENS * 4 : 0;                  \
-    switch (groups) {                                                                     \
-      case 1: b ? F<true, 1><<<grid, block, lds, s>>>(__VA_ARGS__) : F<false, 1><<<grid, block, lds, s>>>(__VA_ARGS__); break; \
-      case 2: b ? F<true, 2><<<grid, block, lds, s>>>(__VA_ARGS__) : F<false, 2><<<grid, block, lds, s>>>(__VA_ARGS__); break; \
-      default: b ? F<true, 4><<<grid, block, lds, s>>>(__VA_ARGS__) : F<false, 4><<<grid, block, lds, s>>>(__VA_ARGS__);      \
-    }                                                                                     \
+#define PG_LOGIT_KERNEL(F, groups, ...)                                                                                          \
+  do {                                                                                                                           \
+    const bool b = a.d.dtype == PG_LOGITS_BF16;                                                                                  \
+    const size_t lds = !a.count ? 0 : (groups) == 1 ? sizeof(Stretch<1>) : sizeof(Stretch<2>);                                   \
+    if ((groups) == 1) b ? F<true, 1><<<grid, block, lds, s>>>(__VA_ARGS__) : F<false, 1><<<grid, block, lds, s>>>(__VA_ARGS__); \
+    else b ? F<true, 2><<<grid, block, lds, s>>>(__VA_ARGS__) : F<false, 2><<<grid, block, lds, s>>>(__VA_ARGS__);               \
   } while (0)
 
 }  // namespace pg
@@ -406,17 +487,18 @@ extern "C" pg_status pg_logits_adjust(const pg_logits* desc, float* out, int64_t
   if ((uintptr_t)out & 3 || out_stride < a.d.vocab) return fail(PG_ESHAPE, "pg_logits_adjust: out rows %lld floats apart", (long long)out_stride);
   if ((const void*)out == a.d.logits && (a.d.dtype != PG_LOGITS_F32 || out_stride != a.d.stride))
     return fail(PG_EINVAL, "pg_logits_adjust: in place needs fp32 logits of the same stride");
-  const int groups = groups_of(a.d.rows, a.d.vocab);
-  const dim3 grid((unsigned)((a.d.vocab + groups * PASS_TOKENS - 1) / (groups * PASS_TOKENS)), (unsigned)a.d.rows), block(LOGIT_THREADS);
+  const LogitGrid g = logit_grid(a.d.rows, a.d.vocab, FEW_ADJUST);
+  a.range = g.range;
+  const dim3 grid((unsigned)g.workgroups, (unsigned)a.d.rows), block(LOGIT_THREADS);
   hipStream_t s = (hipStream_t)stream;
-  PG_LOGIT_KERNEL(logits_adjust_kernel, groups, a, out, out_stride);
+  PG_LOGIT_KERNEL(logits_adjust_kernel, g.groups, a, out, out_stride);
   PG_LAUNCH_CHECK("logits_adjust_kernel");
   return PG_OK;
 }
 
 extern "C" int64_t pg_sample_scratch_floats(int32_t rows, int32_t vocab) {
   if (rows < 1 || vocab < 1) return 0;
-  return (int64_t)rows * draw_grid(rows, vocab).workgroups * (int64_t)(sizeof(Draw) / sizeof(float));
+  return (int64_t)rows * logit_grid(rows, vocab, FEW_DRAW).workgroups * (int64_t)(sizeof(Draw) / sizeof(float));
 }
 
 extern "C" pg_status pg_sample_tokens(const pg_logits* desc, const float* temperature, uint64_t seed, uint32_t step, const int32_t* ids,
@@ -426,11 +508,11 @@ extern "C" pg_status pg_sample_tokens(const pg_logits* desc, const float* temper
   if (a.d.rows == 0) return PG_OK;
   if (!token || !logp || !scratch) return fail(PG_EINVAL, "pg_sample_tokens: null pointer");
   hipStream_t s = (hipStream_t)stream;
-  const DrawGrid g = draw_grid(a.d.rows, a.d.vocab);
-  a.per = g.per;
+  const LogitGrid g = logit_grid(a.d.rows, a.d.vocab, FEW_DRAW);
+  a.range = g.range;
   const dim3 grid((unsigned)g.workgroups, (unsigned)a.d.rows), block(LOGIT_THREADS);
-  PG_LOGIT_KERNEL(sample_chunk_kernel, g.groups, a, temperature, (uint32_t)seed, (uint32_t)(seed >> 32), step, ids, (Draw*)scratch);
-  PG_LAUNCH_CHECK("sample_chunk_kernel");
+  PG_LOGIT_KERNEL(sample_range_kernel, g.groups, a, temperature, (uint32_t)seed, (uint32_t)(seed >> 32), step, ids, (Draw*)scratch);
+  PG_LAUNCH_CHECK("sample_range_kernel");
   sample_finish_kernel<<<dim3((unsigned)a.d.rows), dim3(WAVE), 0, s>>>((const Draw*)scratch, (int)grid.x, token, logp);
   PG_LAUNCH_CHECK("sample_finish_kernel");
   return PG_OK;

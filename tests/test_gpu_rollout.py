@@ -454,7 +454,8 @@ def adjusted_rows(rows):
     return [ref.adjusted(*(rows[n][r] for n in ("x", "prompt", "output", "rep", "freq", "pres", "bias", "allowed"))) for r in range(len(rows["x"]))]
 
 
-CASES = [(1, 1, 0, 0, 0), (3, 7, 5, 1, 3), (5, 1000, 40, 3, 20), (2, 2047, 0, 2, 0), (2, 2049, 300, 0, 0), (4, 32001, 1178, 2, 64), (40, 65537, 64, 4, 300)]
+CASES = [(1, 1, 0, 0, 0), (3, 7, 5, 1, 3), (5, 1000, 40, 3, 20), (2, 2047, 0, 2, 0), (2, 2049, 300, 0, 0), (4, 32001, 1178, 2, 64), (40, 65537, 64, 4, 300),
+         (12, 4099, 2500, 2, 4000), (3, 9000, 20000, 0, 500)]      # nearly every token has both; a history longer than what stays in registers
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
