@@ -36,26 +36,25 @@ struct RowRules {
   int bias_lo, bias_hi, made, prompt;
 };
 
+// What is left out is read from here: then all loads of a row's rules are under way at once instead of behind a branch each.
+static __device__ const uint32_t NOTHING[2] = {0, 0};
+
 __device__ __forceinline__ RowRules row_rules(const LogitArgs& a, int r) {
   const pg_logits& d = a.d;
+  auto entry = [&](const auto* p, int i) { return p ? p + i : (decltype(p))NOTHING; };
+  const float rep = *entry(d.repetition, r), freq = *entry(d.frequency, r), pres = *entry(d.presence, r);
+  const int m = *entry(d.allow_row, r), lo = *entry(d.bias_offsets, r), hi = *entry(d.bias_offsets, r + 1);
+  const int made = *entry(d.n_tokens, r), prompt = *entry(d.n_prompt, r);
   RowRules q;
-  q.rep = d.repetition ? d.repetition[r] : 1.0f;
-  q.freq = d.frequency ? d.frequency[r] : 0.0f;
-  q.pres = d.presence ? d.presence[r] : 0.0f;
-  q.allow = nullptr;
-  if (d.allow) {
-    const int m = d.allow_row ? d.allow_row[r] : r;
-    if (m >= 0 && m < d.n_masks) q.allow = (const uint8_t*)(d.allow + (int64_t)m * a.words);
-  }
-  q.bias_lo = q.bias_hi = q.made = q.prompt = 0;
-  if (d.bias_offsets) {
-    q.bias_lo = max(0, d.bias_offsets[r]);
-    q.bias_hi = min(d.n_bias, d.bias_offsets[r + 1]);
-  }
-  if (d.tokens) {
-    q.made = min(max(d.n_tokens[r], 0), d.tokens_stride);
-    q.prompt = d.n_prompt ? min(max(d.n_prompt[r], 0), q.made) : 0;
-  }
+  q.rep = d.repetition ? rep : 1.0f;
+  q.freq = freq;
+  q.pres = pres;
+  const int mask = d.allow_row ? m : r;
+  q.allow = d.allow && mask >= 0 && mask < d.n_masks ? (const uint8_t*)(d.allow + (int64_t)mask * a.words) : nullptr;
+  q.bias_lo = max(0, lo);
+  q.bias_hi = d.bias_offsets ? min(d.n_bias, hi) : 0;
+  q.made = d.tokens ? min(max(made, 0), d.tokens_stride) : 0;
+  q.prompt = min(max(prompt, 0), q.made);
   return q;
 }
 
@@ -94,7 +93,7 @@ struct Stretch {
   static constexpr int TOKENS = G * PASS_TOKENS;
   uint32_t word[TOKENS];
   uint32_t ready[TOKENS / 32];                       // bit: word holds z
-  uint16_t seen[TOKENS];                             // tokens that occur past the part of the history in registers, in no particular order
+  uint16_t seen[TOKENS];                             // tokens that occur in the history, in no particular order
   int n_seen;
 };
 
@@ -137,60 +136,47 @@ __device__ __forceinline__ float penalised(const RowRules& q, float x, uint32_t 
 }
 
 // z of the tokens of v0 .. v0 + n - 1 that have a count or a bias.  Each word has one owner, who turns it into z: the first of its
-// bias entries, or else the history entry that found it zero.
+// bias entries, or else the place of the token among the seen.
 template <bool BF16, int G>
 __device__ __forceinline__ void prepare_stretch(const LogitArgs& a, const RowRules& q, const RowLists& l, int r, int v0, int n, Stretch<G>& s) {
   const pg_logits& d = a.d;
   const int64_t row = (int64_t)r * d.stride + v0;
   auto logit = [&](uint32_t at) { return BF16 ? bf16_to_f32(((const uint16_t*)d.logits)[row + at]) : ((const float*)d.logits)[row + at]; };
-  auto count = [&](uint32_t at, int i) { return i < q.prompt ? atomicOr(&s.word[at], IN_PROMPT) : atomicAdd(&s.word[at], 1u); };
+  auto count = [&](uint32_t at, int i) {
+    const uint32_t old = i < q.prompt ? atomicOr(&s.word[at], IN_PROMPT) : atomicAdd(&s.word[at], 1u);
+    if ((old & ~HAS_BIAS) == 0) s.seen[atomicAdd(&s.n_seen, 1)] = (uint16_t)at;
+  };
   auto finish = [&](uint32_t at, float z) {
     s.word[at] = __builtin_bit_cast(uint32_t, z);
     atomicOr(&s.ready[at >> 5], 1u << (at & 31));
   };
-  __syncthreads();                                   // the stretch before has been read
-  if (threadIdx.x == 0) s.n_seen = 0;
-  float x[RowLists::KEPT], bias_x = 0.0f;
-  uint32_t owner = 0;
+  __syncthreads();                                   // the stretch before has been read, and its n_seen
+  float bias_x = 0.0f;
   const uint32_t bias_at = (uint32_t)l.bias_id - (uint32_t)v0;
   if (bias_at < (uint32_t)n) {
     bias_x = logit(bias_at);
     atomicOr(&s.word[bias_at], HAS_BIAS);
   }
-  const bool more = q.made > RowLists::KEPT * LOGIT_THREADS;
-  if (more) __syncthreads();                         // n_seen
 #pragma unroll
   for (int k = 0; k < RowLists::KEPT; ++k) {
     const uint32_t at = (uint32_t)l.token[k] - (uint32_t)v0;
-    if (at < (uint32_t)n && (count(at, threadIdx.x + k * LOGIT_THREADS) & ~HAS_BIAS) == 0) {
-      x[k] = logit(at);
-      owner |= 1u << k;
-    }
+    if (at < (uint32_t)n) count(at, threadIdx.x + k * LOGIT_THREADS);
   }
-  if (more) {
-    const int32_t* t = d.tokens + (int64_t)r * d.tokens_stride;
+  const int32_t* t = d.tokens + (int64_t)r * d.tokens_stride;
 #pragma unroll 4
-    for (int i = RowLists::KEPT * LOGIT_THREADS + threadIdx.x; i < q.made; i += LOGIT_THREADS) {
-      const uint32_t at = (uint32_t)t[i] - (uint32_t)v0;
-      if (at < (uint32_t)n && (count(at, i) & ~HAS_BIAS) == 0) s.seen[atomicAdd(&s.n_seen, 1)] = (uint16_t)at;
-    }
+  for (int i = RowLists::KEPT * LOGIT_THREADS + threadIdx.x; i < q.made; i += LOGIT_THREADS) {
+    const uint32_t at = (uint32_t)t[i] - (uint32_t)v0;
+    if (at < (uint32_t)n) count(at, i);
   }
   for (int i = q.bias_lo + LOGIT_THREADS + threadIdx.x; i < q.bias_hi; i += LOGIT_THREADS) {
     const uint32_t at = (uint32_t)d.bias_ids[i] - (uint32_t)v0;
     if (at < (uint32_t)n) atomicOr(&s.word[at], HAS_BIAS);
   }
   __syncthreads();
-#pragma unroll
-  for (int k = 0; k < RowLists::KEPT; ++k)
-    if (owner >> k & 1) {
-      const uint32_t at = (uint32_t)l.token[k] - (uint32_t)v0, word = s.word[at];
-      if (!(word & HAS_BIAS)) finish(at, penalised(q, x[k], word));
-    }
-  if (more)
-    for (int k = threadIdx.x; k < s.n_seen; k += LOGIT_THREADS) {
-      const uint32_t at = s.seen[k], word = s.word[at];
-      if (!(word & HAS_BIAS)) finish(at, penalised(q, logit(at), word));
-    }
+  for (int k = threadIdx.x; k < s.n_seen; k += LOGIT_THREADS) {
+    const uint32_t at = s.seen[k], word = s.word[at];
+    if (!(word & HAS_BIAS)) finish(at, penalised(q, logit(at), word));
+  }
   if (q.bias_lo < q.bias_hi) __syncthreads();        // the history's owners have looked for HAS_BIAS in words that become z here
   if (bias_at < (uint32_t)n && l.bias_before != l.bias_id) finish(bias_at, penalised(q, bias_x, s.word[bias_at]) + l.bias);
   for (int i = q.bias_lo + LOGIT_THREADS + threadIdx.x; i < q.bias_hi; i += LOGIT_THREADS) {
@@ -198,6 +184,7 @@ __device__ __forceinline__ void prepare_stretch(const LogitArgs& a, const RowRul
     if (at < (uint32_t)n && d.bias_ids[i - 1] != d.bias_ids[i]) finish(at, penalised(q, logit(at), s.word[at]) + d.bias_values[i]);
   }
   __syncthreads();
+  if (threadIdx.x == 0) s.n_seen = 0;
 }
 
 // z of a group whose first token is number `at` of its stretch; tokens that are not allowed get -inf
@@ -232,6 +219,7 @@ __device__ __forceinline__ void through_range(const LogitArgs& a, const RowRules
 #pragma unroll
     for (int g = 0; g < 2 * G; ++g) ((uint4*)s.word)[g * LOGIT_THREADS + threadIdx.x] = uint4{0, 0, 0, 0};
     if (threadIdx.x < Stretch<G>::TOKENS / 32) s.ready[threadIdx.x] = 0;
+    if (threadIdx.x == 0) s.n_seen = 0;
   }
   Group<BF16> x;
   x.load(a, q, row, first + threadIdx.x * LANE_TOKENS);
@@ -316,9 +304,9 @@ __device__ __forceinline__ Draw wave_join(Draw a) {
 // Few tokens can win: with E >= w (w the uniform variate of E = -log1p(-w)) a token's score y - ln E reaches a bound b only if
 // w <= exp(y - b) = p exp(top - b), where p = exp(y - top) is what the softmax's sum needs anyway.  So a token costs its
 // Philox word, one exponential and one multiply-add; b is the best lower bound y - ln w - w (ln E <= ln w + w for w <= 1/2) of
-// a token that the workgroup has seen, and only tokens that reach it get their score, from the C library's logarithms.
+// a token that the workgroup has seen, and only tokens that reach it get their score.
 template <bool BF16, int G>
-__global__ __launch_bounds__(LOGIT_THREADS) void sample_range_kernel(LogitArgs a, const float* temperature, uint32_t k0, uint32_t k1,
+__global__ __launch_bounds__(LOGIT_THREADS, 6) void sample_range_kernel(LogitArgs a, const float* temperature, uint32_t k0, uint32_t k1,
                                                                      uint32_t step, const int32_t* ids, Draw* parts) {
   extern __shared__ __align__(16) char lds[];
   Stretch<G>& s = *(Stretch<G>*)lds;
@@ -399,7 +387,11 @@ __global__ __launch_bounds__(LOGIT_THREADS) void sample_range_kernel(LogitArgs a
         we = e == k ? w[k] : we;
       }
       const float u = fminf((we + 0.5f) * 2.3283064365386963e-10f, 0.99999994f);
-      const float score = ye - logf(-log1pf(-u));
+      // -log1p(-u): below 1/8 the series up to u^8 (the next term is 7e-9 of it), above the logarithm of 1 - u, whose rounding is 2e-7 of it
+      float series = 1.0f / 8;
+#pragma unroll
+      for (int k = 7; k; --k) series = series * u + 1.0f / k;
+      const float score = ye - LN2 * __builtin_amdgcn_logf(u < 0.125f ? series * u : -LN2 * __builtin_amdgcn_logf(1.0f - u));
       if (score > mine.score) {
         mine.score = score;
         mine.token = (int)v + e;
