@@ -483,25 +483,46 @@ PG_CACHE_MAX_ROWS = 16384
 PG_LOGITS_F32, PG_LOGITS_BF16 = 0, 1
 
 
+class _Types:
+    """torch's type objects, looked up once: comparing them costs a tenth of comparing their names."""
+
+    def __getattr__(self, name):
+        import torch
+        self.int32, self.float32, self.bfloat16 = torch.int32, torch.float32, torch.bfloat16
+        return self.__dict__[name]
+
+
+_types = _Types()
+
+
+def _wanted(t, kind, shape):
+    raise AssertionError(f"a contiguous {kind} tensor of shape {shape} is wanted: {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
+
+
 def _i32s(t, *shape):
-    """A contiguous int32 tensor of this shape (None: any extent), or None."""
-    if t is not None:
-        assert str(t.dtype) == "torch.int32" and len(t.shape) == len(shape) and all(n is None or n == m for n, m in zip(shape, t.shape)), \
-            f"int32 {shape} wanted: {t.dtype} {tuple(t.shape)}"
-    return _ptr(t)
+    """Address of a contiguous int32 tensor of this shape, or None."""
+    if t is None:
+        return None
+    if t.dtype is not _types.int32 or t.shape != shape or not t.is_contiguous():
+        _wanted(t, "int32", shape)
+    return t.data_ptr()
 
 
 def _f32s(t, *shape):
-    if t is not None:
-        assert str(t.dtype) == "torch.float32" and tuple(t.shape) == shape, f"float32 {shape} wanted: {t.dtype} {tuple(t.shape)}"
-    return _ptr(t)
+    if t is None:
+        return None
+    if t.dtype is not _types.float32 or t.shape != shape or not t.is_contiguous():
+        _wanted(t, "float32", shape)
+    return t.data_ptr()
 
 
 def _rows(t, heads, head_dim):
     """Address and row stride (in elements) of [rows, heads, head_dim] in bf16 whose rows may be slices of longer ones."""
-    assert t.element_size() == 2 and tuple(t.shape[1:]) == (heads, head_dim), f"[rows, {heads}, {head_dim}] bf16 wanted: {t.dtype} {tuple(t.shape)}"
-    assert t.stride(2) == 1 and (heads == 1 or t.stride(1) == head_dim), "heads and channels of a row must be contiguous"
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), heads * head_dim)
+    rows, n, d = t.shape
+    s0, s1, s2 = t.stride()
+    assert n == heads and d == head_dim and t.element_size() == 2 and s2 == 1 and (s1 == d or n == 1), \
+        f"[rows, {heads}, {head_dim}] in 16 bits with contiguous heads wanted: {t.dtype} {tuple(t.shape)}, strides {t.stride()}"
+    return t.data_ptr(), s0 if rows > 1 else max(s0, n * d)
 
 
 class Cache:
@@ -522,7 +543,8 @@ class Cache:
         c.k, c.v = _ptr(k), _ptr(v)
         c.k_scale, c.v_scale = _f32s(k_scale, layers, heads), _f32s(v_scale, layers, heads)
         c.refs, c.status = _i32s(refs, n_pages), _i32s(self.status, 4)
-        self.c = c
+        self.c, self.ref = c, C.byref(c)
+        self.heads, self.head_dim, self.width = heads, head_dim, width
 
     @classmethod
     def create(cls, layers, n_pages, heads, page, head_dim, width, dtype=PG_CACHE_BF16, device="cuda:0"):
@@ -535,61 +557,62 @@ class Cache:
 
 
 def pg_cache_clear(cache, stream=None):
-    _check(_lib.pg_cache_clear(C.byref(cache.c), _stream(stream)))
+    _check(_lib.pg_cache_clear(cache.ref, _stream(stream)))
 
 
 def pg_cache_reserve(cache, table, lens, add, lens_out, stream=None):
     n = lens.shape[0]
-    _check(_lib.pg_cache_reserve(C.byref(cache.c), _i32s(table, n, cache.c.width), _i32s(lens, n), _i32s(add, n), _i32s(lens_out, n), n,
-                                 _stream(stream)))
+    _check(_lib.pg_cache_reserve(cache.ref, _i32s(table, n, cache.width), _i32s(lens, n), _i32s(add, n), _i32s(lens_out, n), n, _stream(stream)))
 
 
 def pg_cache_append(cache, layer, k_new, v_new, table, lens, cu=None, stream=None):
-    c, n = cache.c, lens.shape[0]
-    k, ks = _rows(k_new, c.heads, c.head_dim)
-    v, vs = _rows(v_new, c.heads, c.head_dim)
-    assert k_new.shape[0] == v_new.shape[0] and (ks == vs or k_new.shape[0] < 2), "keys and values of the same number and stride"
-    _check(_lib.pg_cache_append(C.byref(c), layer, k, v, ks, _i32s(table, n, c.width), _i32s(lens, n), _i32s(cu, n + 1), n, k_new.shape[0],
+    n, tokens = lens.shape[0], k_new.shape[0]
+    k, ks = _rows(k_new, cache.heads, cache.head_dim)
+    v, vs = _rows(v_new, cache.heads, cache.head_dim)
+    assert v_new.shape[0] == tokens and (ks == vs or tokens < 2), "keys and values of the same number and stride"
+    _check(_lib.pg_cache_append(cache.ref, layer, k, v, ks, _i32s(table, n, cache.width), _i32s(lens, n), _i32s(cu, n + 1), n, tokens,
                                 _stream(stream)))
 
 
 def pg_cache_scratch_ints(cache, n_rows):
-    return int(_lib.pg_cache_scratch_ints(C.byref(cache.c), n_rows))
+    return int(_lib.pg_cache_scratch_ints(cache.ref, n_rows))
 
 
 def pg_cache_select(cache, table_in, lens_in, src, table_out, lens_out, scratch, stream=None):
-    n, m, w = lens_in.shape[0], src.shape[0], cache.c.width
+    n, m, w = lens_in.shape[0], src.shape[0], cache.width
     assert scratch.numel() >= pg_cache_scratch_ints(cache, max(n, m))
-    _check(_lib.pg_cache_select(C.byref(cache.c), _i32s(table_in, n, w), _i32s(lens_in, n), n, _i32s(src, m), _i32s(table_out, m, w),
-                                _i32s(lens_out, m), m, _i32s(scratch, None), _stream(stream)))
+    _check(_lib.pg_cache_select(cache.ref, _i32s(table_in, n, w), _i32s(lens_in, n), n, _i32s(src, m), _i32s(table_out, m, w),
+                                _i32s(lens_out, m), m, _i32s(scratch, scratch.shape[0]), _stream(stream)))
 
 
 def pg_cache_compact(cache, table, lens, scratch, stream=None):
     n = lens.shape[0]
     assert scratch.numel() >= pg_cache_scratch_ints(cache, 0)
-    _check(_lib.pg_cache_compact(C.byref(cache.c), _i32s(table, n, cache.c.width), _i32s(lens, n), n, _i32s(scratch, None), _stream(stream)))
+    _check(_lib.pg_cache_compact(cache.ref, _i32s(table, n, cache.width), _i32s(lens, n), n, _i32s(scratch, scratch.shape[0]), _stream(stream)))
 
 
 def pg_cache_check(cache, stream=None):
-    _check(_lib.pg_cache_check(C.byref(cache.c), _stream(stream)))
+    _check(_lib.pg_cache_check(cache.ref, _stream(stream)))
 
 
 def pg_paged_attention_workspace(cache, n_q, heads_q, max_len):
-    return int(_lib.pg_paged_attention_workspace(C.byref(cache.c), n_q, heads_q, max_len))
+    return int(_lib.pg_paged_attention_workspace(cache.ref, n_q, heads_q, max_len))
 
 
 def pg_paged_attention(cache, layer, q, table, lens, out, max_len, workspace=None, lse=None, row_of=None, scale=0.0, stream=None):
-    c, (n, heads, hd) = cache.c, q.shape
-    qp, qs = _rows(q, heads, c.head_dim)
-    op, os_ = _rows(out, heads, c.head_dim)
-    assert out.shape == q.shape
-    _check(_lib.pg_paged_attention(C.byref(c), layer, qp, qs, _i32s(table, None, c.width), table.shape[0], _i32s(row_of, n), _i32s(lens, n), n,
-                                   heads, scale, max_len, op, os_, _f32s(lse, n, heads), _ptr(workspace),
-                                   0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)))
+    n, heads, hd = q.shape
+    rows = table.shape[0]
+    qp, qs = _rows(q, heads, cache.head_dim)
+    op, os_ = _rows(out, heads, cache.head_dim)
+    assert out.shape[0] == n
+    wp, size = (None, 0) if workspace is None else (_ptr(workspace), workspace.numel() * workspace.element_size())
+    _check(_lib.pg_paged_attention(cache.ref, layer, qp, qs, _i32s(table, rows, cache.width), rows, _i32s(row_of, n), _i32s(lens, n), n,
+                                   heads, scale, max_len, op, os_, _f32s(lse, n, heads), wp, size, _stream(stream)))
 
 
 class Logits:
-    """Logits [rows, vocab] (fp32 or bf16; rows may be slices of longer ones), what is to be done to them, and the filled pg_logits."""
+    """Logits [rows, vocab] (fp32 or bf16; rows may be slices of longer ones), what is to be done to them, and the filled pg_logits.
+    It is a handle: the tensors' contents may change between calls."""
 
     def __init__(self, logits, tokens=None, n_prompt=None, n_tokens=None, repetition=None, frequency=None, presence=None,
                  bias_offsets=None, bias_ids=None, bias_values=None, allow=None, allow_row=None):
@@ -600,21 +623,26 @@ class Logits:
         d.logits, d.stride = logits.data_ptr(), logits.stride(0) if rows > 1 else max(logits.stride(0), vocab)
         d.dtype = PG_LOGITS_F32 if logits.element_size() == 4 else PG_LOGITS_BF16
         d.rows, d.vocab = rows, vocab
-        d.tokens, d.tokens_stride = _i32s(tokens, rows, None), 0 if tokens is None else tokens.shape[1]
+        d.tokens_stride = 0 if tokens is None else tokens.shape[1]
+        d.tokens = _i32s(tokens, rows, d.tokens_stride)
         d.n_prompt, d.n_tokens = _i32s(n_prompt, rows), _i32s(n_tokens, rows)
         d.repetition, d.frequency, d.presence = (_f32s(t, rows) for t in (repetition, frequency, presence))
         d.bias_offsets = _i32s(bias_offsets, rows + 1)
         d.n_bias = 0 if bias_ids is None else bias_ids.shape[0]
         d.bias_ids, d.bias_values = _i32s(bias_ids, d.n_bias), _f32s(bias_values, d.n_bias)
-        d.allow, d.n_masks = _i32s(allow, None, (vocab + 31) // 32), 0 if allow is None else allow.shape[0]
+        d.n_masks = 0 if allow is None else allow.shape[0]
+        d.allow = _i32s(allow, d.n_masks, (vocab + 31) // 32)
         d.allow_row = _i32s(allow_row, rows)
-        self.c = d
+        self.c, self.ref, self.rows, self.vocab = d, C.byref(d), rows, vocab
+        self.scratch = pg_sample_scratch_floats(rows, vocab)
 
 
 def pg_logits_adjust(desc, out, stream=None):
-    d = desc.c
-    assert tuple(out.shape) == (d.rows, d.vocab) and str(out.dtype) == "torch.float32" and (d.vocab == 1 or out.stride(1) == 1)
-    _check(_lib.pg_logits_adjust(C.byref(d), out.data_ptr(), out.stride(0) if d.rows > 1 else max(out.stride(0), d.vocab), _stream(stream)))
+    rows, vocab = desc.rows, desc.vocab
+    s0, s1 = out.stride()
+    if out.shape != (rows, vocab) or out.dtype is not _types.float32 or (vocab > 1 and s1 != 1):
+        _wanted(out, "float32", (rows, vocab))
+    _check(_lib.pg_logits_adjust(desc.ref, out.data_ptr(), s0 if rows > 1 else max(s0, vocab), _stream(stream)))
 
 
 def pg_sample_scratch_floats(rows, vocab):
@@ -622,10 +650,10 @@ def pg_sample_scratch_floats(rows, vocab):
 
 
 def pg_sample_tokens(desc, temperature, seed, step, ids, token, logp, scratch, stream=None):
-    d = desc.c
-    assert scratch.numel() >= pg_sample_scratch_floats(d.rows, d.vocab)
-    _check(_lib.pg_sample_tokens(C.byref(d), _f32s(temperature, d.rows), seed, step, _i32s(ids, d.rows), _i32s(token, d.rows),
-                                 _f32s(logp, d.rows), _ptr(scratch), _stream(stream)))
+    n = desc.rows
+    assert scratch.numel() >= desc.scratch
+    _check(_lib.pg_sample_tokens(desc.ref, _f32s(temperature, n), seed, step, _i32s(ids, n), _i32s(token, n), _f32s(logp, n), _ptr(scratch),
+                                 _stream(stream)))
 
 
 def pg_mfma_probe(blocks, iters, operand_scale, out, stream=None):

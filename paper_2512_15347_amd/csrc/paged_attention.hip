@@ -8,8 +8,14 @@
 // the kernel is bound by HBM as long as enough loads are in flight.  Both products run on the matrix pipe, S^T = K Q^T and
 // O^T = V^T P^T with the keys / channels as rows and 16 query heads as columns (empty ones are zero): then a lane's keys
 // of S^T are just the keys it multiplies in O^T, and keys and transposed values are loaded straight into operand registers, 16 bytes
-// a lane, without LDS.  A step is 32 keys of bf16 or 64 keys of codes.  Codes are converted to bf16, which holds them exactly; the
-// scales go into the logits and the output.
+// a lane, without LDS.  A step is 32 keys of bf16 or 64 keys of codes; the next step's keys are asked for when this step's have been
+// multiplied, its values likewise.  Codes are converted to bf16, which holds them exactly; the scales go into the logits and the output.
+//
+// Work is split in one of two ways.  Short rows, and very many rows, are one workgroup each per key/value head (WHOLE): no second launch.
+// Otherwise (EVEN) the units of 4 steps of all rows and heads, one after another, are cut into as many equal ranges as the device
+// holds workgroups, wherever a row begins or ends: rows of any lengths end together, and a workgroup streams through its range with one
+// start only.  A range has at most two rows that it does not cover whole, its first and its last; their pieces go to the
+// workspace and a second launch joins them.
 #include <algorithm>
 #include <cmath>
 #include "paged_cache.hpp"
@@ -23,6 +29,9 @@ typedef float f32x4v __attribute__((ext_vector_type(4)));
 constexpr int PA_THREADS = 256, PA_WAVES = 4;
 constexpr int PA_HEADS = 16;                         // query heads of a tile: the columns of a 16 x 16 MFMA
 
+constexpr int PA_PAGES = 512;                        // page numbers in LDS at a time
+constexpr int PA_EVEN_QUERIES = 2048;                // whose prefix sums are held in LDS
+
 struct PagedArgs {
   CacheView c;
   const uint8_t *k, *v;                              // of the layer
@@ -30,11 +39,27 @@ struct PagedArgs {
   const uint16_t* q;
   int64_t q_stride, out_stride;
   const int32_t *table, *row_of, *lens;
-  int n_rows, heads_q, group, q_tiles, splits;
+  int n_q, n_rows, heads_q, group, q_tiles;
   float scale_log2;
   uint16_t* out;
-  float *lse, *parts;                                // parts: [query, query head, split][HD + 2]
+  float* lse;
+  int ranges;                                        // EVEN: workgroups, a multiple of 8
+  int64_t* starts;                                   // EVEN: first unit of each range and the end of the last, for the second launch
+  int4* opened;                                      // EVEN: query, head tile, unit and units of the row that each range begins in
+  float* parts;                                      // EVEN: [range][first, last][query head of the tile][HD + 4]: m, l, -, -, o'
 };
+
+// tokens of a query, and whether its row and length are what the table holds
+__device__ __forceinline__ int query_length(const PagedArgs& a, int query, int& row) {
+  row = a.row_of ? a.row_of[query] : query;
+  const int len = a.lens[query];
+  if ((unsigned)row < (unsigned)a.n_rows && len >= 0 && (int64_t)len <= (int64_t)a.c.width << a.c.page_shift) return len;
+  atomicOr(a.c.status, CACHE_RANGE);
+  row = 0;
+  return 0;
+}
+// first unit of a range
+__device__ __forceinline__ int64_t range_start(int64_t total, int ranges, int r) { return total * r / ranges; }
 
 __device__ __forceinline__ bf16x8 as_bf16(uint4 w) { return __builtin_bit_cast(bf16x8, w); }
 // eight codes -> eight bf16 (exact: e4m3 has three bits of fraction)
@@ -64,26 +89,100 @@ __device__ __forceinline__ int channel_of(int j, int c) {
 
 struct Piece { float m, l; };
 
-template <int HD, bool F8>
-__global__ __launch_bounds__(PA_THREADS) void paged_attention_kernel(PagedArgs a) {
+template <int HD, bool F8, bool EVEN>
+__global__ __launch_bounds__(PA_THREADS, 2) void paged_attention_kernel(PagedArgs a) {
   using S = Step<HD, F8>;
-  constexpr int DT = HD / 16;                        // tiles of channels
+  constexpr int DT = HD / 16, U = S::U;              // tiles of channels, groups of 32 keys
+  constexpr int UNIT = PA_WAVES * S::KEYS;           // tokens: a step of each wave
   __shared__ __align__(16) float lds_o[PA_WAVES][PA_HEADS][HD + 4];
   __shared__ Piece lds_ml[PA_WAVES][PA_HEADS];
+  __shared__ int lds_page[PA_PAGES + 4];
+  __shared__ int lds_cum[EVEN ? PA_EVEN_QUERIES : 1];
   const int lane = threadIdx.x & 63, n = lane & 15, c = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int split = blockIdx.x, h = blockIdx.y / a.q_tiles, tile = blockIdx.y % a.q_tiles, query = blockIdx.z;
-  const int heads = min(PA_HEADS, a.group - tile * PA_HEADS);           // of this tile
-  const int row = a.row_of ? a.row_of[query] : query;
-  int len = a.lens[query];
-  if ((unsigned)row >= (unsigned)a.n_rows || len < 0 || (int64_t)len > (int64_t)a.c.width << a.c.page_shift) {
-    if (threadIdx.x == 0) atomicOr(a.c.status, CACHE_RANGE);
-    len = 0;
+  const int shift = a.c.page_shift, page_tokens = 1 << shift;
+  const uint32_t head_bytes = (uint32_t)(HD * S::ELT) << shift, page_bytes = head_bytes * (uint32_t)a.c.heads;
+
+  // EVEN: consecutive ranges on one XCD, so that rows of one head that share pages find them in its L2
+  const int range = EVEN ? (int)(blockIdx.x % 8) * (a.ranges / 8) + (int)(blockIdx.x / 8) : 0;
+  int units = 0;                                     // of all queries, one head and tile
+  int64_t at = 0, stop = 1;                          // EVEN: units, of all heads and tiles
+  if constexpr (EVEN) {
+    int mine[PA_EVEN_QUERIES / PA_THREADS];
+    const int per = (a.n_q + PA_THREADS - 1) / PA_THREADS, first = threadIdx.x * per;
+#pragma unroll
+    for (int i = 0; i < PA_EVEN_QUERIES / PA_THREADS; ++i) {
+      int row;
+      mine[i] = i < per && first + i < a.n_q ? (query_length(a, first + i, row) + UNIT - 1) / UNIT : 0;
+    }
+    int sum = 0;
+#pragma unroll
+    for (int i = 0; i < PA_EVEN_QUERIES / PA_THREADS; ++i) sum += mine[i];
+    int incl = sum;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int y = __shfl_up(incl, d);
+      if (lane >= d) incl += y;
+    }
+    if (lane == 63) lds_page[wave] = incl;
+    __syncthreads();
+    int before = incl - sum;
+#pragma unroll
+    for (int w = 0; w < PA_WAVES; ++w) {
+      before += w < wave ? lds_page[w] : 0;
+      units += lds_page[w];
+    }
+#pragma unroll
+    for (int i = 0; i < PA_EVEN_QUERIES / PA_THREADS; ++i)
+      if (i < per && first + i < a.n_q) {
+        lds_cum[first + i] = before += mine[i];
+        if (mine[i] == 0 && (first + i) % a.ranges == range)     // no tokens: nobody else comes by
+          for (int e = 0; e < a.heads_q; ++e) {
+            for (int ch = 0; ch < HD; ch += 8) *(uint4*)(a.out + (first + i) * a.out_stride + (int64_t)e * HD + ch) = uint4{0, 0, 0, 0};
+            if (a.lse) a.lse[(int64_t)(first + i) * a.heads_q + e] = -INFINITY;
+          }
+      }
+    __syncthreads();
+    const int64_t total = (int64_t)units * a.c.heads * a.q_tiles;
+    at = range_start(total, a.ranges, range);
+    stop = range_start(total, a.ranges, range + 1);
+    if (threadIdx.x == 0) {
+      a.starts[range] = at;
+      if (range == a.ranges - 1) a.starts[a.ranges] = stop;
+      if (at >= stop) a.opened[range] = int4{0, 0, 0, 0};
+    }
   }
-  const int32_t* table = a.table + (int64_t)(len ? row : 0) * a.c.width;
-  const int steps = (len + S::KEYS - 1) / S::KEYS;
-  const int per = (steps + a.splits - 1) / a.splits;
-  const int begin = min(steps, split * per), end = min(steps, begin + per);
+  int query = EVEN ? -1 : (int)blockIdx.z, ht = EVEN ? 0 : (int)blockIdx.y;
+  for (bool opening = true; at < stop; opening = false) {
+  int begin = 0, row, len, whole_units = 0, first_unit = 0, last_unit = 0;
+  if constexpr (EVEN) {
+    ht = (int)(at / units);
+    const int rest = (int)(at % units);
+    if (query < 0) {                                 // first query with cum > rest
+      int lo = 0, hi = a.n_q - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (lds_cum[mid] > rest) hi = mid; else lo = mid + 1;
+      }
+      query = lo;
+    } else {
+      do query = query + 1 < a.n_q ? query + 1 : 0;
+      while (lds_cum[query] <= rest);
+    }
+    query = __builtin_amdgcn_readfirstlane(query);
+    const int base = query ? lds_cum[query - 1] : 0;
+    whole_units = lds_cum[query] - base;
+    first_unit = rest - base;
+    last_unit = (int)min((int64_t)whole_units, first_unit + (stop - at));
+    at += last_unit - first_unit;
+    begin = first_unit * UNIT;
+    if (opening && threadIdx.x == 0) a.opened[range] = int4{query, ht, first_unit, whole_units};
+  }
+  len = query_length(a, query, row);
+  const int finish = EVEN ? min(len, last_unit * UNIT) : len;
+  if constexpr (!EVEN) at = stop;
+  const int h = ht / a.q_tiles, tile = ht % a.q_tiles;
+  const int heads = min(PA_HEADS, a.group - tile * PA_HEADS);           // of this tile
   const int head0 = h * a.group + tile * PA_HEADS;
 
   bf16x8 q[S::OCTETS];
@@ -99,97 +198,139 @@ __global__ __launch_bounds__(PA_THREADS) void paged_attention_kernel(PagedArgs a
 #pragma unroll
   for (int d = 0; d < DT; ++d) o[d] = f32x4v{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.0f;
-  const int page_tokens = 1 << a.c.page_shift, last_page = (len - 1) >> a.c.page_shift;
-  const int64_t page_bytes = ((int64_t)a.c.heads << a.c.page_shift) * HD * S::ELT;
-  const int64_t head_bytes = ((int64_t)h << a.c.page_shift) * HD * S::ELT;
+  const uint8_t* k_head = a.k + (int64_t)h * head_bytes;
+  const uint8_t* v_head = a.v + (int64_t)h * head_bytes;
+  // lane (r = n, c): key row r of tile t is key 8 U (r / 4) + 4 t + r % 4 of the step; it multiplies keys 8 U c ... 8 U c + 8 U - 1
+  const int key_lane = 8 * U * (n >> 2) + (n & 3), key_values = 8 * U * c;
 
-  for (int step = begin + wave; step < end; step += PA_WAVES) {
-    const int key0 = step * S::KEYS;
-    // lane (r = n, c): key row r of tile t is key 8 U (r / 4) + 4 t + r % 4, of the step; it multiplies keys 8 U c ... 8 U c + 8 U - 1
-    const int key_lane = 8 * S::U * (n >> 2) + (n & 3), key_values = 8 * S::U * c;
-    auto page_base = [&](int key) -> int64_t {
-      const int p = table[min((key0 + key) >> a.c.page_shift, last_page)];
+  for (; begin < finish; begin += PA_PAGES << shift) {
+    const int end = (int)min((int64_t)finish, begin + ((int64_t)PA_PAGES << shift));
+    const int pages = (end - begin + (begin & (page_tokens - 1)) + page_tokens - 1) >> shift;
+    const int32_t* table = a.table + (int64_t)row * a.c.width + (begin >> shift);
+    __syncthreads();                                 // what was there has been read
+    // page numbers; steps that reach past the last page find it again
+    for (int i = threadIdx.x; i < pages + 4; i += PA_THREADS) {
+      int p = table[min(i, pages - 1)];
       if ((unsigned)p >= (unsigned)a.c.n_pages) {
         atomicOr(a.c.status, CACHE_RANGE);
-        return head_bytes;
+        p = 0;
       }
-      return p * page_bytes + head_bytes;
+      lds_page[i] = p;
+    }
+    __syncthreads();
+    uint4 kr[2 * U][S::PIECES], vr[DT];
+    auto load_keys = [&](int key0) {                 // key0: of the step, from the chunk's begin
+#pragma unroll
+      for (int t = 0; t < 2 * U; ++t) {
+        const int key = key0 + key_lane + 4 * t;
+        const uint8_t* p = k_head + (uint64_t)(uint32_t)lds_page[key >> shift] * page_bytes +
+                           (uint32_t)((key & (page_tokens - 1)) * (HD * S::ELT) + c * S::PIECE);
+#pragma unroll
+        for (int j = 0; j < S::PIECES; ++j) {
+          if constexpr (S::PIECE == 16) kr[t][j] = *(const uint4*)(p + j * 64);
+          else *(uint2*)&kr[t][j] = *(const uint2*)p;
+        }
+      }
     };
-    f32x4v s[2 * S::U];
+    auto load_values = [&](int key0) {
+      const int key = key0 + key_values;
+      const uint8_t* p = v_head + (uint64_t)(uint32_t)lds_page[key >> shift] * page_bytes +
+                         (uint32_t)(((n << shift) + (key & (page_tokens - 1))) * S::ELT);
 #pragma unroll
-    for (int t = 0; t < 2 * S::U; ++t) {
-      const int key = key_lane + 4 * t;
-      const uint8_t* kp = a.k + page_base(key) + (int64_t)((key0 + key) & (page_tokens - 1)) * (HD * S::ELT) + c * S::PIECE;
-      s[t] = f32x4v{0.f, 0.f, 0.f, 0.f};
+      for (int d = 0; d < DT; ++d) vr[d] = *(const uint4*)(p + (((uint32_t)d * 16 * S::ELT) << shift));
+    };
+    const int tokens = end - begin;
+    int key0 = wave * S::KEYS;
+    if (key0 < tokens) {
+      load_keys(key0);
+      load_values(key0);
+    }
+    for (; key0 < tokens; key0 += PA_WAVES * S::KEYS) {
+      const int next = key0 + PA_WAVES * S::KEYS;
+      f32x4v s[2 * U];
 #pragma unroll
-      for (int j = 0; j < S::PIECES; ++j) {
-        if constexpr (!F8) {
-          s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(*(const uint4*)(kp + j * 64)), q[j], s[t], 0, 0, 0);
-        } else if constexpr (S::PIECE == 8) {
-          const uint2 w = *(const uint2*)kp;
-          s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_bf16(w.x, w.y), q[j], s[t], 0, 0, 0);
-        } else {
-          const uint4 w = *(const uint4*)(kp + j * 64);
-          s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_bf16(w.x, w.y), q[2 * j], s[t], 0, 0, 0);
-          s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_bf16(w.z, w.w), q[2 * j + 1], s[t], 0, 0, 0);
+      for (int t = 0; t < 2 * U; ++t) {
+        s[t] = f32x4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < S::PIECES; ++j) {
+          const uint4 w = kr[t][j];
+          if constexpr (!F8) {
+            s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(w), q[j], s[t], 0, 0, 0);
+          } else if constexpr (S::PIECE == 8) {
+            s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_bf16(w.x, w.y), q[j], s[t], 0, 0, 0);
+          } else {
+            s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_bf16(w.x, w.y), q[2 * j], s[t], 0, 0, 0);
+            s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_bf16(w.z, w.w), q[2 * j + 1], s[t], 0, 0, 0);
+          }
         }
       }
-    }
-    const int there = len - key0;                    // keys of the step that exist, if fewer than KEYS
-    float top = -INFINITY;
+      if (next < tokens) load_keys(next);
+      const int there = tokens - key0;               // keys of the step that exist, if fewer than KEYS
+      float top = -INFINITY;
 #pragma unroll
-    for (int t = 0; t < 2 * S::U; ++t)
+      for (int t = 0; t < 2 * U; ++t) {
+        s[t] *= scale;
+        if (there < S::KEYS) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s[t][i] = key_values + 4 * t + i < there ? s[t][i] * scale : -INFINITY;
-        top = fmaxf(top, s[t][i]);
+          for (int i = 0; i < 4; ++i) s[t][i] = key_values + 4 * t + i < there ? s[t][i] : -INFINITY;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
       }
-    top = across_rows(top, [](float x, float y) { return fmaxf(x, y); });
-    const float m_new = fmaxf(m, top);
-    const float shrink = exp2f(m - m_new);
-    m = m_new;
-    l *= shrink;
+      top = across_rows(top, [](float x, float y) { return fmaxf(x, y); });
+      if (__ballot(top > m)) {                       // seldom after a row's first steps
+        const float m_new = fmaxf(m, top);
+        const float shrink = __builtin_amdgcn_exp2f(m - m_new);
+        m = m_new;
+        l *= shrink;
 #pragma unroll
-    for (int d = 0; d < DT; ++d) o[d] *= shrink;
-    // a probability is kept as the sum of two bf16: the matrix pipe has time for both, and 8 bits alone would double the output's error
-    bf16x8 hi[S::U], lo[S::U];
-#pragma unroll
-    for (int u = 0; u < S::U; ++u) {
-      float p[8], rest[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[e] = exp2f(s[2 * u + (e >> 2)][e & 3] - m);
-        l += p[e];
+        for (int d = 0; d < DT; ++d) o[d] *= shrink;
       }
-      const uint4 w = {pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])};
-      hi[u] = as_bf16(w);
+      // a probability is kept as the sum of two bf16: the matrix pipe has time for both, and 8 bits alone would make the output's error
+      // 1.4 times as large
+      bf16x8 hi[U], lo[U];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) rest[e] = p[e] - (float)hi[u][e];
-      lo[u] = as_bf16(uint4{pack_bf16x2(rest[0], rest[1]), pack_bf16x2(rest[2], rest[3]), pack_bf16x2(rest[4], rest[5]), pack_bf16x2(rest[6], rest[7])});
-    }
-    const uint8_t* vp = a.v + page_base(key_values) + ((int64_t)n * page_tokens + ((key0 + key_values) & (page_tokens - 1))) * S::ELT;
+      for (int u = 0; u < U; ++u) {
+        float p[8], rest[8];
 #pragma unroll
-    for (int d = 0; d < DT; ++d) {
-      uint4 w = *(const uint4*)(vp + (int64_t)d * 16 * page_tokens * S::ELT);
+        for (int e = 0; e < 8; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(s[2 * u + (e >> 2)][e & 3] - m);
+          l += p[e];
+        }
+        const uint4 w = {pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])};
+        hi[u] = as_bf16(w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) rest[e] = p[e] - (float)hi[u][e];
+        lo[u] = as_bf16(uint4{pack_bf16x2(rest[0], rest[1]), pack_bf16x2(rest[2], rest[3]), pack_bf16x2(rest[4], rest[5]), pack_bf16x2(rest[6], rest[7])});
+      }
       if (there < S::KEYS) {                         // what lies behind the last token may be anything, NaN too
-        uint32_t* x = (uint32_t*)&w;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          constexpr int PER = 4 / S::ELT;            // keys of a word
-          const int left = there - key_values - e * PER;
-          x[e] = left >= PER ? x[e] : left <= 0 ? 0u : x[e] & ((1u << (8 * S::ELT * left)) - 1);
+        for (int d = 0; d < DT; ++d) {
+          uint32_t w[4] = {vr[d].x, vr[d].y, vr[d].z, vr[d].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            constexpr int PER = 4 / S::ELT;          // keys of a word
+            const int left = there - key_values - e * PER;
+            w[e] = left >= PER ? w[e] : left <= 0 ? 0u : w[e] & ((1u << (8 * S::ELT * left)) - 1);
+          }
+          vr[d] = uint4{w[0], w[1], w[2], w[3]};
         }
       }
-      if constexpr (!F8) {
-        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(w), hi[0], o[d], 0, 0, 0);
-        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(w), lo[0], o[d], 0, 0, 0);
-      } else {
-        const bf16x8 v0 = codes_to_bf16(w.x, w.y), v1 = codes_to_bf16(w.z, w.w);
-        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, hi[0], o[d], 0, 0, 0);
-        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, lo[0], o[d], 0, 0, 0);
-        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, hi[1], o[d], 0, 0, 0);
-        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, lo[1], o[d], 0, 0, 0);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const uint4 w = vr[d];
+        if constexpr (!F8) {
+          o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(w), hi[0], o[d], 0, 0, 0);
+          o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(w), lo[0], o[d], 0, 0, 0);
+        } else {
+          const bf16x8 v0 = codes_to_bf16(w.x, w.y), v1 = codes_to_bf16(w.z, w.w);
+          o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, hi[0], o[d], 0, 0, 0);
+          o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, lo[0], o[d], 0, 0, 0);
+          o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, hi[1], o[d], 0, 0, 0);
+          o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, lo[1], o[d], 0, 0, 0);
+        }
       }
+      if (next < tokens) load_values(next);
     }
   }
   l = across_rows(l, [](float x, float y) { return x + y; });
@@ -210,57 +351,81 @@ __global__ __launch_bounds__(PA_THREADS) void paged_attention_kernel(PagedArgs a
     for (int w = 0; w < PA_WAVES; ++w) {
       const Piece p = lds_ml[w][head];
       if (p.m > -INFINITY) {
-        const float f = exp2f(p.m - top);
+        const float f = __builtin_amdgcn_exp2f(p.m - top);
         sum += p.l * f;
         acc += *(const f32x4v*)&lds_o[w][head][ch] * f;
       }
     }
+    acc *= v_scale;
     const int64_t item = (int64_t)query * a.heads_q + head0 + head;
-    if (a.splits == 1) {
-      const float f = sum > 0.0f ? v_scale / sum : 0.0f;
-      acc *= f;
+    if (!EVEN || last_unit - first_unit == whole_units) {
+      acc *= sum > 0.0f ? 1.0f / sum : 0.0f;
       *(uint2*)(a.out + query * a.out_stride + (int64_t)(head0 + head) * HD + ch) = pack_bf16x4(float4{acc[0], acc[1], acc[2], acc[3]});
       if (a.lse && ch == 0) a.lse[item] = sum > 0.0f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
     } else {
-      float* part = a.parts + (item * a.splits + split) * (HD + 4);
-      *(f32x4v*)(part + 4 + ch) = acc * v_scale;
-      if (ch == 0) {
-        part[0] = top;
-        part[1] = sum;
-      }
+      float* part = a.parts + (((int64_t)range * 2 + !opening) * PA_HEADS + head) * (HD + 4);
+      *(f32x4v*)(part + 4 + ch) = acc;
+      if (ch == 0) *(float2*)part = float2{top, sum};
     }
   }
-}
-
-// joins the splits of one query head: one wave
-template <int HD>
-__global__ __launch_bounds__(WAVE) void paged_join_kernel(PagedArgs a) {
-  const int64_t item = (int64_t)blockIdx.y * a.heads_q + blockIdx.x;
-  const float* part = a.parts + item * a.splits * (HD + 4);
-  float top = -INFINITY, sum = 0.0f, acc[(HD + 63) / 64] = {};
-  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, part[s * (HD + 4)]);
-  for (int s = 0; s < a.splits; ++s) {
-    const float* p = part + s * (HD + 4);
-    if (!(p[0] > -INFINITY)) continue;
-    const float f = exp2f(p[0] - top);
-    sum += p[1] * f;
-#pragma unroll
-    for (int i = 0; i < (HD + 63) / 64; ++i)
-      if (threadIdx.x + 64 * i < HD) acc[i] += p[4 + threadIdx.x + 64 * i] * f;
   }
-  const float f = sum > 0.0f ? 1.0f / sum : 0.0f;
-#pragma unroll
-  for (int i = 0; i < (HD + 63) / 64; ++i)
-    if (threadIdx.x + 64 * i < HD)
-      a.out[blockIdx.y * a.out_stride + (int64_t)blockIdx.x * HD + threadIdx.x + 64 * i] = (uint16_t)(pack_bf16x2(acc[i] * f, 0.0f) & 0xFFFF);
-  if (a.lse && threadIdx.x == 0) a.lse[item] = sum > 0.0f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
 }
 
-// Enough workgroups to fill the device, none with fewer than 256 keys.
-static int splits_of(const pg_cache* c, int64_t n_q, int heads_q, int max_len) {
-  const int64_t tiles = (heads_q / c->heads + PA_HEADS - 1) / PA_HEADS, items = n_q * c->heads * tiles;
-  const int64_t want = std::max<int64_t>(1, 1024 / std::max<int64_t>(1, items));
-  return (int)std::min<int64_t>(want, std::max(1, max_len / 256));
+// Joins the pieces of the row that range r begins in, if r is the first to begin inside of it: one query head, every HD / 4 threads go
+// through a part of the pieces, four channels each.
+template <int HD>
+__global__ __launch_bounds__(PA_THREADS) void paged_join_kernel(PagedArgs a) {
+  constexpr int LANES = HD / 4, PARTS = PA_THREADS / LANES;
+  __shared__ __align__(16) float lds_o[PARTS][HD];
+  __shared__ Piece lds_ml[PARTS];
+  const int r0 = blockIdx.x, column = blockIdx.y, part = threadIdx.x / LANES, ch = threadIdx.x % LANES * 4;
+  const int4 row = a.opened[r0];
+  if (row.z == 0) return;
+  const int64_t start0 = a.starts[r0], begin = start0 - row.z, end = begin + row.w;
+  const int tile = row.y % a.q_tiles, head = row.y / a.q_tiles * a.group + tile * PA_HEADS + column;
+  int before = r0 - 1;                               // the range that ends here; there are empty ones where units are few
+  while (a.starts[before] == start0) --before;
+  if (a.starts[before] > begin || column >= a.group - tile * PA_HEADS) return;
+  Piece x = {-INFINITY, 0.0f};
+  f32x4v acc = {0.f, 0.f, 0.f, 0.f};
+  auto add = [&](Piece y, f32x4v o) {
+    if (!(y.m > -INFINITY)) return;
+    const float m = fmaxf(x.m, y.m), f = __builtin_amdgcn_exp2f(x.m - m), g = __builtin_amdgcn_exp2f(y.m - m);
+    x = Piece{m, x.l * f + y.l * g};
+    acc = acc * f + o * g;
+  };
+  // pieces: the last of that range (its first, if it begins with the row), the first of all others
+#pragma unroll 4
+  for (int r = before + part; r < a.ranges; r += PARTS) {
+    const int64_t start = a.starts[r];
+    if (start >= end) break;
+    if (start == a.starts[r + 1]) continue;
+    const int last = start < begin;
+    const float* p = a.parts + (((int64_t)r * 2 + last) * PA_HEADS + column) * (HD + 4);
+    const float2 ml = *(const float2*)p;
+    add(Piece{ml.x, ml.y}, *(const f32x4v*)(p + 4 + ch));
+  }
+  *(f32x4v*)&lds_o[part][ch] = acc;
+  if (ch == 0) lds_ml[part] = x;
+  __syncthreads();
+  if (part) return;
+#pragma unroll
+  for (int i = 1; i < PARTS; ++i) add(lds_ml[i], *(const f32x4v*)&lds_o[i][ch]);
+  acc *= x.l > 0.0f ? 1.0f / x.l : 0.0f;
+  *(uint2*)(a.out + row.x * a.out_stride + (int64_t)head * HD + ch) = pack_bf16x4(float4{acc[0], acc[1], acc[2], acc[3]});
+  if (a.lse && ch == 0) a.lse[(int64_t)row.x * a.heads_q + head] = x.l > 0.0f ? (x.m + log2f(x.l)) * 0.6931471805599453f : -INFINITY;
+}
+
+// Ranges of an EVEN call, 0 for WHOLE: two workgroups a compute unit are what the registers of the widest heads leave room for.  A row
+// alone takes about as many microseconds as it has units, and the prefix sums and the second launch of EVEN cost about eight; the rows
+// are taken to be half as long as the longest on average.
+constexpr int PA_RANGES = 512;
+static int ranges_of(const pg_cache* c, int64_t n_q, int heads_q, int max_len) {
+  const int64_t items = n_q * c->heads * ((heads_q / c->heads + PA_HEADS - 1) / PA_HEADS), unit = c->dtype == PG_CACHE_E4M3 ? 256 : 128;
+  const int64_t units = (max_len + unit - 1) / unit;
+  if (n_q > PA_EVEN_QUERIES || units <= 8 + items * units / (2 * PA_RANGES)) return 0;
+  if (n_q * ((int64_t)c->width * c->page / unit + 1) > 1 << 30) return 0;      // units are counted in 32 bits
+  return PA_RANGES;
 }
 
 static pg_status paged_sizes(const pg_cache* c, int32_t n_q, int32_t heads_q, int32_t max_len, const char* who) {
@@ -278,8 +443,8 @@ using namespace pg;
 
 extern "C" size_t pg_paged_attention_workspace(const pg_cache* c, int32_t n_q, int32_t heads_q, int32_t max_len) {
   if (paged_sizes(c, n_q, heads_q, max_len, "pg_paged_attention_workspace") != PG_OK) return 0;
-  const int splits = splits_of(c, n_q, heads_q, max_len);
-  return splits > 1 ? (size_t)n_q * heads_q * splits * (c->head_dim + 4) * sizeof(float) : 0;
+  const int ranges = ranges_of(c, n_q, heads_q, max_len);
+  return ranges ? 16 + (size_t)ranges * (sizeof(int64_t) + sizeof(int4) + 2 * PA_HEADS * (c->head_dim + 4) * sizeof(float)) : 0;
 }
 
 extern "C" pg_status pg_paged_attention(const pg_cache* c, int32_t layer, const uint16_t* q, int64_t q_stride, const int32_t* table,
@@ -311,22 +476,30 @@ extern "C" pg_status pg_paged_attention(const pg_cache* c, int32_t layer, const 
   a.q = q; a.q_stride = q_stride; a.out = out; a.out_stride = out_stride;
   a.table = table; a.row_of = row_of; a.lens = lens; a.n_rows = n_rows;
   a.heads_q = heads_q; a.group = heads_q / c->heads; a.q_tiles = (a.group + PA_HEADS - 1) / PA_HEADS;
-  a.splits = splits_of(c, n_q, heads_q, max_len);
+  a.n_q = n_q;
+  a.ranges = ranges_of(c, n_q, heads_q, max_len);
   a.scale_log2 = (float)((scale == 0.0 ? 1.0 / std::sqrt((double)c->head_dim) : scale) * 1.4426950408889634);
-  a.lse = lse; a.parts = (float*)workspace;
-  const dim3 grid((unsigned)a.splits, (unsigned)(c->heads * a.q_tiles), (unsigned)n_q), block(PA_THREADS), join((unsigned)heads_q, (unsigned)n_q);
+  a.lse = lse;
+  a.opened = (int4*)workspace; a.parts = (float*)(a.opened + a.ranges);
+  a.starts = (int64_t*)(a.parts + (size_t)a.ranges * 2 * PA_HEADS * (c->head_dim + 4));
+  const dim3 block(PA_THREADS), join((unsigned)a.ranges, (unsigned)std::min(a.group, PA_HEADS));
+  const dim3 grid = a.ranges ? dim3((unsigned)a.ranges) : dim3(1, (unsigned)(c->heads * a.q_tiles), (unsigned)n_q);
   hipStream_t s = (hipStream_t)stream;
   const bool f8 = c->dtype == PG_CACHE_E4M3;
-#define PG_PAGED(HD)                                                                                       \
-  (f8 ? paged_attention_kernel<HD, true><<<grid, block, 0, s>>>(a) : paged_attention_kernel<HD, false><<<grid, block, 0, s>>>(a))
-  c->head_dim == 32 ? PG_PAGED(32) : c->head_dim == 64 ? PG_PAGED(64) : PG_PAGED(128);
+#define PG_PAGED(HD)                                                                                                       \
+  do {                                                                                                                     \
+    if (!a.ranges) {                                                                                                       \
+      f8 ? paged_attention_kernel<HD, true, false><<<grid, block, 0, s>>>(a) : paged_attention_kernel<HD, false, false><<<grid, block, 0, s>>>(a); \
+    } else {                                                                                                               \
+      f8 ? paged_attention_kernel<HD, true, true><<<grid, block, 0, s>>>(a) : paged_attention_kernel<HD, false, true><<<grid, block, 0, s>>>(a);   \
+      PG_LAUNCH_CHECK("paged_attention_kernel");                                                                           \
+      paged_join_kernel<HD><<<join, block, 0, s>>>(a);                                                                     \
+    }                                                                                                                      \
+  } while (0)
+  if (c->head_dim == 32) PG_PAGED(32);
+  else if (c->head_dim == 64) PG_PAGED(64);
+  else PG_PAGED(128);
 #undef PG_PAGED
-  PG_LAUNCH_CHECK("paged_attention_kernel");
-  if (a.splits > 1) {
-    if (c->head_dim == 32) paged_join_kernel<32><<<join, dim3(WAVE), 0, s>>>(a);
-    else if (c->head_dim == 64) paged_join_kernel<64><<<join, dim3(WAVE), 0, s>>>(a);
-    else paged_join_kernel<128><<<join, dim3(WAVE), 0, s>>>(a);
-    PG_LAUNCH_CHECK("paged_join_kernel");
-  }
+  PG_LAUNCH_CHECK(a.ranges ? "paged_join_kernel" : "paged_attention_kernel");
   return PG_OK;
 }
