@@ -433,7 +433,8 @@ static pg_status paged_sizes(const pg_cache* c, int32_t n_q, int32_t heads_q, in
   if (n_q < 0 || heads_q < 1 || max_len < 0) return fail(PG_EINVAL, "%s: %d queries of %d heads, lengths up to %d", who, n_q, heads_q, max_len);
   if (heads_q % c->heads) return fail(PG_ESHAPE, "%s: %d query heads for %d key/value heads", who, heads_q, c->heads);
   const int64_t tiles = (heads_q / c->heads + PA_HEADS - 1) / PA_HEADS;
-  if (n_q > 65535 || c->heads * tiles > 65535) return fail(PG_ESHAPE, "%s: grid limit", who);
+  if (n_q > 65535 || c->heads * tiles > 65535 || n_q * c->heads * tiles >= 1 << 24)
+    return fail(PG_ESHAPE, "%s: %d queries of %d heads pass a launch's 65535 rows or 2^24 workgroups", who, n_q, heads_q);
   return PG_OK;
 }
 

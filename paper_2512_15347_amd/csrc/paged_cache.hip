@@ -4,6 +4,8 @@
 // does follows from its arguments whatever order workgroups run in.  The calls that take pages are one workgroup that scans
 // the counts (4 bytes a page) and stops at the last page it needs; the pages' data, tables and counts are then gone through by
 // the whole device in a second launch.
+#include <cmath>
+#include <type_traits>
 #include "paged_cache.hpp"
 #include "operands.hpp"
 
@@ -12,7 +14,7 @@ namespace pg {
 constexpr int PLAN_THREADS = 1024;
 constexpr int PLAN_WAVES = PLAN_THREADS / WAVE;
 constexpr int APPLY_THREADS = 256;
-constexpr int MAX_COPY_BLOCKS = 2048;              // eight workgroups a compute unit
+constexpr int MAX_COPY_BLOCKS = 8192;              // four times what the device holds (512: 71 us, 2048: 64, 8192: 62 for 248 MB)
 
 // Exclusive prefix sum of v over the workgroup; total: the sum.  `sums` holds PLAN_WAVES + 1 values.
 template <class T>
@@ -134,17 +136,20 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_reserve_kernel(CacheView c
 }
 
 // ---------------------------------------------------------------- select
-// scratch: [0] copies, [4 ..] users of each source row, then per output row the page of its copy (-1: none found, -2: none needed),
-// then the rows with copies in order
+// scratch: [0] copies, [4 ..] of each copy in row order the page it is of and the page it goes to, then users of each source row, then
+// per output row the page of its copy (-1: none)
 struct SelectPlan {
-  int32_t *count, *users, *fresh, *copies;
+  int32_t* count;
+  int2* copies;
+  int32_t *users, *fresh;
 };
-__host__ __device__ inline SelectPlan select_plan(int32_t* scratch, int n_in, int n_out) {
-  return SelectPlan{scratch, scratch + 4, scratch + 4 + n_in, scratch + 4 + n_in + n_out};
+inline SelectPlan select_plan(int32_t* scratch, int n_in, int n_out) {
+  return SelectPlan{scratch, (int2*)(scratch + 4), scratch + 4 + 2 * (int64_t)n_out, scratch + 4 + 2 * (int64_t)n_out + n_in};
 }
 
-__global__ __launch_bounds__(PLAN_THREADS) void cache_select_plan_kernel(CacheView c, int32_t* refs, const int32_t* lens_in, int n_in,
-                                                                         const int32_t* src, int32_t* lens_out, int n_out, SelectPlan plan) {
+__global__ __launch_bounds__(PLAN_THREADS) void cache_select_plan_kernel(CacheView c, int32_t* refs, const int32_t* table_in,
+                                                                         const int32_t* lens_in, int n_in, const int32_t* src,
+                                                                         int32_t* lens_out, int n_out, SelectPlan plan) {
   extern __shared__ int lds[];
   int *users = lds, *first = lds + n_in;
   __shared__ int sums[PLAN_WAVES];
@@ -182,21 +187,29 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_select_plan_kernel(CacheVi
         copied = (n & part) && first[s] != r;
       }
       lens_out[r] = n;
-      plan.fresh[r] = copied ? -1 : -2;
+      plan.fresh[r] = -1;
     }
     int total;
     const int rank = wanted + block_scan<int>(copied, sums, total);
-    if (copied) plan.copies[rank] = r;
+    if (copied) {
+      int from = table_in[(int64_t)src[r] * c.width + (n >> c.page_shift)];
+      if ((unsigned)from >= (unsigned)c.n_pages) {
+        atomicOr(&bits, CACHE_RANGE);
+        from = 0;
+      }
+      plan.copies[rank] = int2{from, r};
+    }
     wanted += total;
   }
   for (int s = threadIdx.x; s < n_in; s += PLAN_THREADS) plan.users[s] = users[s];
   __syncthreads();
   const int found = free_pages(refs, c.n_pages, wanted, sums, [&](int rank, int page) {
-    plan.fresh[plan.copies[rank]] = page;
+    plan.fresh[plan.copies[rank].y] = page;
+    plan.copies[rank].y = page;
     refs[page] = 1;
   });
   for (int k = found + threadIdx.x; k < wanted; k += PLAN_THREADS) {
-    const int r = plan.copies[k];
+    const int r = plan.copies[k].y;
     lens_out[r] = lens_out[r] & ~part;
     atomicOr(&bits, CACHE_FULL);
   }
@@ -207,7 +220,9 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_select_plan_kernel(CacheVi
   }
 }
 
-// page copies over all layers: item i is 16 KB (or a page's rest) of one pool's copy of one page
+// page copies over all layers: item i is 16 KB (or a page's rest) of one pool's copy of one page; nothing of it is read again soon, so it
+// is kept out of the way in the caches (248 MB of copies: 63 us, 75 without the hints)
+typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
 struct PageCopy {
   uint8_t *k, *v;
   int64_t layer_bytes;                               // of one pool
@@ -223,22 +238,22 @@ __device__ __forceinline__ void copy_pages(const PageCopy& a, int copies, int bl
     const int64_t j = i / pieces;
     const int pool = (int)(j & 1), layer = (int)((j >> 1) % a.layers);
     int from, to;
-    if (!pages((int)((j >> 1) / a.layers), from, to)) continue;
+    pages((int)((j >> 1) / a.layers), from, to);
     uint8_t* base = (pool ? a.v : a.k) + layer * a.layer_bytes;
     const int lo = piece * COPY_PIECE, n = min(COPY_PIECE, a.page_bytes - lo);
-    const uint4* in = (const uint4*)(base + (int64_t)from * a.page_bytes + lo);
-    uint4* out = (uint4*)(base + (int64_t)to * a.page_bytes + lo);
+    const u32x4v* in = (const u32x4v*)(base + (int64_t)from * a.page_bytes + lo);
+    u32x4v* out = (u32x4v*)(base + (int64_t)to * a.page_bytes + lo);
     constexpr int PER = COPY_PIECE / 16 / APPLY_THREADS;
-    uint4 x[PER];
+    u32x4v x[PER];
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
       const int at = threadIdx.x + e * APPLY_THREADS;
-      if (at < n / 16) x[e] = in[at];
+      if (at < n / 16) x[e] = __builtin_nontemporal_load(in + at);
     }
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
       const int at = threadIdx.x + e * APPLY_THREADS;
-      if (at < n / 16) out[at] = x[e];
+      if (at < n / 16) __builtin_nontemporal_store(x[e], out + at);
     }
   }
 }
@@ -274,10 +289,9 @@ __global__ __launch_bounds__(APPLY_THREADS) void cache_select_apply_kernel(Cache
   }
   block -= n_in;
   copy_pages(data, plan.count[0], block, gridDim.x - n_out - n_in, [&](int i, int& from, int& to) {
-    const int r = plan.copies[i];
-    to = plan.fresh[r];
-    from = table_in[(int64_t)src[r] * c.width + pages_of(lens_out[r], c.page_shift) - 1];
-    return valid(from);
+    const int2 pair = plan.copies[i];
+    from = pair.x;
+    to = pair.y;
   });
 }
 
@@ -345,7 +359,6 @@ __global__ __launch_bounds__(APPLY_THREADS) void cache_compact_apply_kernel(Cach
   copy_pages(data, plan.count[0], block - n_rows, gridDim.x - n_rows, [&](int i, int& from, int& to) {
     from = plan.movers[i];
     to = plan.holes[i];
-    return true;
   });
 }
 
@@ -369,10 +382,23 @@ __device__ __forceinline__ uint32_t to_e4m3x4(float a, float b, float c, float d
   w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, w, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
 }
-__device__ __forceinline__ float limited(uint32_t bits16, float scale) {
-  const float x = bf16_to_f32((uint16_t)bits16) / scale;
-  return x == x ? fminf(fmaxf(x, -448.0f), 448.0f) : x;
-}
+// x / scale correctly rounded, limited to +-448 (NaN stays NaN).  With r = 1 / scale correctly rounded, q = x r and one step
+// q - (q scale - x) r give the quotient's rounding (Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor",
+// 1990; in this form of the step -0 stays -0).  x is limited before, to 448 scale, whose quotient rounds to 448.  The compiler's own
+// division, which is longer than everything else here together, is for scales for which one of the two is not finite.
+struct Quotient {
+  float scale, r, most;
+  __device__ explicit Quotient(float s) : scale(s), r(1.0f / s), most(448.0f * s) {}
+  static __device__ __forceinline__ float within(float x, float most) {
+    return __builtin_elementwise_minimum(__builtin_elementwise_maximum(x, -most), most);
+  }
+  __device__ __forceinline__ float operator()(uint32_t bits32) const {
+    const float x = __builtin_bit_cast(float, bits32);
+    if (!(r < INFINITY && most < INFINITY)) return within(x / scale, 448.0f);
+    const float y = within(x, most), q = y * r;
+    return __builtin_fmaf(-__builtin_fmaf(q, scale, -y), r, q);
+  }
+};
 
 struct AppendArgs {
   CacheView c;
@@ -381,29 +407,32 @@ struct AppendArgs {
   const uint16_t *k_new, *v_new;
   int64_t token_stride;
   const int32_t *table, *lens, *cu;
-  int n_rows, n_tokens;
+  int n_rows, n_tokens, units;
 };
 
 // One wave: 16 positions of a row (those of them that are new) of one head.  Keys are copied, values go through LDS to be
-// written along the tokens: a whole block of 16 positions is 32 (bf16) or 16 contiguous bytes of each channel's row.
+// written along the tokens: a whole block of 16 positions is 32 (bf16) or 16 contiguous bytes of each channel's row.  The four waves
+// of a workgroup take consecutive blocks, so that a line of values is written from one XCD.
 template <int HD, bool F8>
 __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a) {
-  constexpr int PAD = 18;                            // tokens of a channel's row in LDS, two of them padding
-  __shared__ __align__(16) uint16_t tile[4][HD * PAD];
+  using Value = typename std::conditional<F8, uint8_t, uint16_t>::type;
+  constexpr int PAD = F8 ? 20 : 18;                  // tokens of a channel's row in LDS, one word of them padding
+  __shared__ __align__(16) Value tile[4][HD * PAD];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int head = blockIdx.y * 4 + wave;
   const CacheView& c = a.c;
-  int row = blockIdx.x, t0 = row, fresh = 1, part = 0;
+  const int head = blockIdx.x % (unsigned)c.heads, unit = (int)(blockIdx.x / (unsigned)c.heads) * 4 + wave;       // a token's heads lie together
+  if (unit >= a.units) return;
+  int row = unit, t0 = row, fresh = 1, part = 0;
   if (a.cu) {
     // row r owns the numbers cu[r]/16 + 2 r ..., at least as many as it has blocks of 16 positions
-    row = last_not_above(a.n_rows, blockIdx.x, [&](int r) { return (int64_t)(a.cu[r] >> 4) + 2ll * r; });
+    row = last_not_above(a.n_rows, unit, [&](int r) { return (int64_t)(a.cu[r] >> 4) + 2ll * r; });
     t0 = a.cu[row];
     fresh = a.cu[row + 1] - t0;
-    part = blockIdx.x - ((t0 >> 4) + 2 * row);
+    part = unit - ((t0 >> 4) + 2 * row);
   }
   const int len = a.lens[row];
   if (part < 0 || t0 < 0 || fresh < 0 || t0 + (int64_t)fresh > a.n_tokens || fresh > len || !length_fits(len, c)) {
-    if (threadIdx.x == 0 && blockIdx.y == 0) atomicOr(c.status, CACHE_RANGE);
+    if (lane == 0 && head == 0) atomicOr(c.status, CACHE_RANGE);
     return;
   }
   const int begin = len - fresh;
@@ -411,67 +440,67 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a) {
   if (at >= len) return;
   const int page = a.table[(int64_t)row * c.width + (at >> c.page_shift)];
   if ((unsigned)page >= (unsigned)c.n_pages) {
-    if (threadIdx.x == 0 && blockIdx.y == 0) atomicOr(c.status, CACHE_RANGE);
+    if (lane == 0 && head == 0) atomicOr(c.status, CACHE_RANGE);
     return;
   }
-  if (head >= c.heads) return;
   const int slot = (int)at & ((1 << c.page_shift) - 1);
-  const int i = lane & 15;                           // position in the block
-  const bool mine = at + i >= begin && at + i < len;
-  const int64_t from = (t0 + (at + i - begin)) * a.token_stride + (int64_t)head * HD;
   const int64_t to = (((int64_t)page * c.heads + head) << c.page_shift) * HD;
-  const float ks = F8 && a.k_scale ? a.k_scale[head] : 1.0f, vs = F8 && a.v_scale ? a.v_scale[head] : 1.0f;
-  uint16_t* t = tile[wave];
-  for (int ch = (lane >> 4) * 8; ch < HD; ch += 32) {
-    if (mine) {
-      const uint4 kx = *(const uint4*)(a.k_new + from + ch);
-      const uint4 vx = *(const uint4*)(a.v_new + from + ch);
+  const Quotient ks(F8 && a.k_scale ? a.k_scale[head] : 1.0f), vs(F8 && a.v_scale ? a.v_scale[head] : 1.0f);
+  Value* t = tile[wave];
+  // COLS lanes read 16 bytes each of a token's channels side by side, a whole line of 128 bytes where the head has one; all loads first
+  constexpr int COLS = HD / 8 < 8 ? HD / 8 : 8, TOKENS = 64 / COLS, PASSES = 16 / TOKENS, ITERS = HD / 8 / COLS;
+  const int i0 = lane / COLS, col = lane % COLS * 8;
+  auto there = [&](int i) { return at + i >= begin && at + i < len; };      // position i of the block is new
+  uint4 kx[PASSES][ITERS], vx[PASSES][ITERS];
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p)
+#pragma unroll
+    for (int it = 0; it < ITERS; ++it)
+      if (there(i0 + p * TOKENS)) {
+        const int64_t from = (t0 + (at + i0 + p * TOKENS - begin)) * a.token_stride + (int64_t)head * HD + col + it * COLS * 8;
+        kx[p][it] = *(const uint4*)(a.k_new + from);
+        vx[p][it] = *(const uint4*)(a.v_new + from);
+      }
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p)
+#pragma unroll
+    for (int it = 0; it < ITERS; ++it) {
+      const int i = i0 + p * TOKENS, ch = col + it * COLS * 8;
+      if (!there(i)) continue;
       const int64_t kt = to + (int64_t)(slot + i) * HD + ch;
-      const uint32_t vw[4] = {vx.x, vx.y, vx.z, vx.w};
-      if (F8) {
-        const uint32_t w[4] = {kx.x, kx.y, kx.z, kx.w};
-        float f[8];
+      if constexpr (F8) {
+        auto codes = [](uint4 x, const Quotient& over) {
+          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+          float f[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = limited(w[e >> 1] >> (16 * (e & 1)) & 0xFFFF, ks);
-        *(uint2*)((uint8_t*)a.k + kt) = uint2{to_e4m3x4(f[0], f[1], f[2], f[3]), to_e4m3x4(f[4], f[5], f[6], f[7])};
+          for (int e = 0; e < 8; ++e) f[e] = over(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
+          return uint2{to_e4m3x4(f[0], f[1], f[2], f[3]), to_e4m3x4(f[4], f[5], f[6], f[7])};
+        };
+        *(uint2*)((uint8_t*)a.k + kt) = codes(kx[p][it], ks);
+        const uint2 w = codes(vx[p][it], vs);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = limited(vw[e >> 1] >> (16 * (e & 1)) & 0xFFFF, vs);
-        const uint32_t codes[2] = {to_e4m3x4(f[0], f[1], f[2], f[3]), to_e4m3x4(f[4], f[5], f[6], f[7])};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) t[(ch + e) * PAD + i] = (uint16_t)(codes[e >> 2] >> (8 * (e & 3)) & 0xFF);
+        for (int e = 0; e < 8; ++e) t[(ch + e) * PAD + i] = (uint8_t)((e < 4 ? w.x : w.y) >> (8 * (e & 3)));
       } else {
-        *(uint4*)((uint16_t*)a.k + kt) = kx;
+        *(uint4*)((uint16_t*)a.k + kt) = kx[p][it];
+        const uint32_t w[4] = {vx[p][it].x, vx[p][it].y, vx[p][it].z, vx[p][it].w};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) t[(ch + e) * PAD + i] = (uint16_t)(vw[e >> 1] >> (16 * (e & 1)));
+        for (int e = 0; e < 8; ++e) t[(ch + e) * PAD + i] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
       }
     }
-  }
   wave_lds_sync();
   const int64_t vrow = to + slot;                    // channel 0 of the block
   const int width = 1 << c.page_shift;
   if (at >= begin && at + 16 <= len) {
     for (int ch = lane; ch < HD; ch += 64) {
       const uint32_t* s = (const uint32_t*)(t + ch * PAD);
-      uint32_t w[8];
+      uint4* o = (uint4*)((Value*)a.v + vrow + (int64_t)ch * width);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = s[e];
-      if (F8) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = (w[2 * e] & 0xFF) | (w[2 * e] >> 8 & 0xFF00) | (w[2 * e + 1] & 0xFF) << 16 | (w[2 * e + 1] >> 16 & 0xFF) << 24;
-        *(uint4*)((uint8_t*)a.v + vrow + (int64_t)ch * width) = uint4{w[0], w[1], w[2], w[3]};
-      } else {
-        uint4* o = (uint4*)((uint16_t*)a.v + vrow + (int64_t)ch * width);
-        o[0] = uint4{w[0], w[1], w[2], w[3]};
-        o[1] = uint4{w[4], w[5], w[6], w[7]};
-      }
+      for (int e = 0; e < (F8 ? 1 : 2); ++e) o[e] = uint4{s[4 * e], s[4 * e + 1], s[4 * e + 2], s[4 * e + 3]};
     }
   } else {
+    const int i = lane & 15;
     for (int ch = lane >> 4; ch < HD; ch += 4)
-      if (mine) {
-        const uint16_t x = t[ch * PAD + i];
-        if (F8) ((uint8_t*)a.v)[vrow + (int64_t)ch * width + i] = (uint8_t)x;
-        else ((uint16_t*)a.v)[vrow + (int64_t)ch * width + i] = x;
-      }
+      if (there(i)) ((Value*)a.v)[vrow + (int64_t)ch * width + i] = t[ch * PAD + i];
   }
 }
 
@@ -556,8 +585,8 @@ extern "C" pg_status pg_cache_append(const pg_cache* c, int32_t layer, const uin
   if (token_stride < (int64_t)c->heads * c->head_dim || token_stride % 8 || (((uintptr_t)k_new | (uintptr_t)v_new) & 15))
     return fail(PG_ESHAPE, "pg_cache_append: tokens must be 16-byte aligned, %lld elements apart", (long long)token_stride);
   const int64_t units = cu ? n_tokens / 16 + 2ll * n_rows : n_rows;
-  const int64_t tiles = (c->heads + 3ll) / 4;
-  if (units > 1 << 23 || tiles > 65535) return fail(PG_ESHAPE, "pg_cache_append: grid limit");
+  const int64_t blocks = (units + 3) / 4 * c->heads;
+  if (blocks >= 1 << 24) return fail(PG_ESHAPE, "pg_cache_append: %lld workgroups (a launch has room for 2^24 of 256 lanes)", (long long)blocks);
   AppendArgs a{};
   a.c = view_of(c);
   const size_t layer_bytes = page_bytes(c) * c->n_pages;
@@ -566,8 +595,8 @@ extern "C" pg_status pg_cache_append(const pg_cache* c, int32_t layer, const uin
   a.k_scale = c->k_scale ? c->k_scale + (int64_t)layer * c->heads : nullptr;
   a.v_scale = c->v_scale ? c->v_scale + (int64_t)layer * c->heads : nullptr;
   a.k_new = k_new; a.v_new = v_new; a.token_stride = token_stride;
-  a.table = table; a.lens = lens; a.cu = cu; a.n_rows = n_rows; a.n_tokens = n_tokens;
-  const dim3 grid((unsigned)units, (unsigned)tiles), block(256);
+  a.table = table; a.lens = lens; a.cu = cu; a.n_rows = n_rows; a.n_tokens = n_tokens; a.units = (int)units;
+  const dim3 grid((unsigned)blocks), block(256);
   hipStream_t s = (hipStream_t)stream;
   const bool f8 = c->dtype == PG_CACHE_E4M3;
   switch (c->head_dim) {
@@ -581,7 +610,7 @@ extern "C" pg_status pg_cache_append(const pg_cache* c, int32_t layer, const uin
 
 extern "C" int64_t pg_cache_scratch_ints(const pg_cache* c, int32_t n_rows) {
   if (!c || n_rows < 0 || c->n_pages < 0) return 0;
-  const int64_t select = 4 + 3ll * n_rows, compact = 4 + 2 * ((int64_t)c->n_pages / 2 + 1) + c->n_pages;
+  const int64_t select = 4 + 4ll * n_rows, compact = 4 + 2 * ((int64_t)c->n_pages / 2 + 1) + c->n_pages;
   return select > compact ? select : compact;
 }
 
@@ -601,8 +630,8 @@ extern "C" pg_status pg_cache_select(const pg_cache* c, const int32_t* table_in,
   hipStream_t s = (hipStream_t)stream;
   const SelectPlan plan = select_plan(scratch, n_in, n_out);
   PG_TRY(allow_lds((const void*)cache_select_plan_kernel, (size_t)n_in * 2 * sizeof(int)));
-  cache_select_plan_kernel<<<dim3(1), dim3(PLAN_THREADS), (size_t)n_in * 2 * sizeof(int), s>>>(view_of(c), c->refs, lens_in, n_in, src, lens_out,
-                                                                                              n_out, plan);
+  cache_select_plan_kernel<<<dim3(1), dim3(PLAN_THREADS), (size_t)n_in * 2 * sizeof(int), s>>>(view_of(c), c->refs, table_in, lens_in, n_in, src,
+                                                                                              lens_out, n_out, plan);
   PG_LAUNCH_CHECK("cache_select_plan_kernel");
   cache_select_apply_kernel<<<dim3((unsigned)(n_out + n_in + copy_blocks(c, n_out))), dim3(APPLY_THREADS), 0, s>>>(
       view_of(c), copy_of(c), c->refs, table_in, lens_in, n_in, src, table_out, lens_out, n_out, plan);

@@ -440,7 +440,8 @@ static pg_status logit_args(const pg_logits* d, const char* who, LogitArgs& a) {
   if (d->rows < 0 || d->vocab < 1 || (d->dtype != PG_LOGITS_F32 && d->dtype != PG_LOGITS_BF16))
     return fail(PG_EINVAL, "%s: %d rows of %d tokens, dtype %d", who, d->rows, d->vocab, d->dtype);
   if (d->rows > 65535) return fail(PG_ESHAPE, "%s: %d rows (at most 65535)", who, d->rows);
-  if (d->vocab > 1 << 30) return fail(PG_ESHAPE, "%s: %d tokens", who, d->vocab);
+  if (d->vocab > 1 << 30 || d->rows * ((d->vocab + PASS_TOKENS - 1ll) / PASS_TOKENS) >= 1 << 24)
+    return fail(PG_ESHAPE, "%s: %d rows of %d tokens pass 2^24 workgroups", who, d->rows, d->vocab);
   if (d->rows && !d->logits) return fail(PG_EINVAL, "%s: logits is NULL", who);
   if (d->stride < d->vocab) return fail(PG_EINVAL, "%s: rows %lld elements apart hold no %d tokens", who, (long long)d->stride, d->vocab);
   if ((uintptr_t)d->logits & (d->dtype == PG_LOGITS_BF16 ? 1 : 3)) return fail(PG_ESHAPE, "%s: logits are not aligned to their size", who);

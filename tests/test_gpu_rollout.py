@@ -289,6 +289,28 @@ def test_every_code_round_trips_and_ties_go_to_even(lib):
     np.testing.assert_array_equal(want, xb.float().clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8).numpy()[:, 0])
 
 
+def test_codes_are_those_of_the_rounded_quotient_for_every_bf16_and_any_scale(lib):
+    say("e4m3 codes of all 65536 patterns")
+    scales = np.array([1.0, 3.0, 1 / 3, 0.0173, 0.7, 1.9999999, 1.0000001, 448.0, 1e-3, 7e4, 1e30, 3e38, 1e-30, 1.2e-38, 1e-38, 2e-39, 1e-40, 1e-45,
+                       0.0625, 5.5, 11.0, 0.3, 123.456, 0.99999994], dtype=np.float32).reshape(3, 8)
+    bits = torch.arange(65536, dtype=torch.int32).to(torch.int16)
+    x = bits.view(torch.bfloat16).reshape(1024, 1, 64).expand(-1, 8, -1).contiguous()
+    cache = lib.Cache.create(3, 64, 8, 16, 64, 64, dtype=lib.PG_CACHE_E4M3)
+    cache.k_scale.copy_(torch.from_numpy(scales))
+    cache.v_scale.copy_(torch.from_numpy(scales))
+    table = torch.arange(64, dtype=torch.int32, device=DEV)[None]
+    for layer in range(3):
+        lib.pg_cache_append(cache, layer, x.to(DEV), x.to(DEV), table, dev([1024]), cu=dev([0, 1024]))
+        k = cache.k[layer].permute(1, 0, 2, 3).reshape(8, 65536).cpu().numpy()
+        v = cache.v[layer].permute(1, 0, 3, 2).reshape(8, 65536).cpu().numpy()
+        for h in range(8):
+            with np.errstate(all="ignore"):
+                want = ref.to_e4m3(x[:, h].reshape(-1).float().numpy() / scales[layer, h])
+            nan = want & 0x7F == 0x7F
+            for got in (k[h], v[h]):
+                assert ((got & 0x7F == 0x7F) == nan).all() and (got[~nan] == want[~nan]).all(), (scales[layer, h], np.flatnonzero((got != want) & ~nan)[:5])
+
+
 # ------------------------------------------------------------------ pages
 
 class Both:

@@ -209,3 +209,15 @@ def test_checkers_logits_by_hand():
     s, y = ref.scores(np.array([0.3, 0.2]), 0.0, 1, 2, 3)
     assert s.tolist() == y.tolist() == [0.3, 0.2]
     assert abs(ref.log_softmax_at(np.array([1.0, 1.0, -math.inf]), 1) + math.log(2)) < 1e-15
+
+
+def test_more_workgroups_than_a_launch_has_room_for_are_refused():
+    """2^24 workgroups of 256 lanes: what lies beyond 2^32 lanes would not run, without an error."""
+    f = pg._lib
+    wide = cache(heads=64, width=1 << 20)
+    assert f.pg_cache_append(wide, 0, P, P, 64 * 64, P, P, P, 1 << 20, 1, None) == pg.PG_ESHAPE
+    assert f.pg_paged_attention(cache(heads=512), 0, P, 512 * 64, P, 40000, None, P, 40000, 512, 0.0, 16, P, 512 * 64, None, None, 0, None) == pg.PG_ESHAPE
+    assert f.pg_paged_attention(cache(), 0, P, 256, P, 70000, None, P, 70000, 4, 0.0, 16, P, 256, None, None, 0, None) == pg.PG_ESHAPE
+    big = logits(rows=65535, vocab=1 << 20, stride=1 << 20)
+    assert f.pg_logits_adjust(big, P, 1 << 20, None) == pg.PG_ESHAPE and f.pg_sample_tokens(big, None, 0, 0, None, P, P, P, None) == pg.PG_ESHAPE
+    assert f.pg_logits_adjust(logits(rows=65536), P, 100, None) == pg.PG_ESHAPE
