@@ -40,19 +40,20 @@ __device__ __forceinline__ T block_scan(T v, T* sums, T& total) {
   return before + x - v;
 }
 
+// Counts of pages p .. p + 3; those past the pool's end are no free ones.
+__device__ __forceinline__ int4 counts_of(const int32_t* refs, int n_pages, int p) {
+  if (p + 4 <= n_pages) return *(const int4*)(refs + p);
+  return int4{p < n_pages ? refs[p] : 1, p + 1 < n_pages ? refs[p + 1] : 1, p + 2 < n_pages ? refs[p + 2] : 1, 1};
+}
 // The free pages in ascending order, handed out until `wanted` are found: take(rank, page).  Returns how many there were.
+// `head`: the lane's counts of the first tile, which the caller has asked for before the work that precedes this.
 template <class Take>
-__device__ __forceinline__ int free_pages(const int32_t* refs, int n_pages, int wanted, int* sums, Take take) {
+__device__ __forceinline__ int free_pages(const int32_t* refs, int n_pages, int4 head, int wanted, int* sums, Take take) {
   int found = 0;
   for (int base = 0; base < n_pages && found < wanted; base += PLAN_THREADS * 4) {
     const int p = base + (int)threadIdx.x * 4;
-    unsigned free = 0;
-    if (p + 4 <= n_pages) {
-      const int4 r = *(const int4*)(refs + p);
-      free = (r.x == 0) | (r.y == 0) << 1 | (r.z == 0) << 2 | (r.w == 0) << 3;
-    } else {
-      for (int i = 0; p + i < n_pages; ++i) free |= (unsigned)(refs[p + i] == 0) << i;
-    }
+    const int4 r = base ? counts_of(refs, n_pages, p) : head;
+    const unsigned free = (r.x == 0) | (r.y == 0) << 1 | (r.z == 0) << 2 | (r.w == 0) << 3;
     int total;
     int rank = found + block_scan<int>(__popc(free), sums, total);
 #pragma unroll
@@ -82,54 +83,60 @@ __global__ __launch_bounds__(256) void cache_clear_kernel(int32_t* refs, int n_p
 __global__ __launch_bounds__(PLAN_THREADS) void cache_reserve_kernel(CacheView c, int32_t* refs, int32_t* table, const int32_t* lens,
                                                                      const int32_t* add, int32_t* lens_out, int n_rows) {
   extern __shared__ int cum[];
+  const int4 head = counts_of(refs, c.n_pages, (int)threadIdx.x * 4);
+  int* first = cum + n_rows;                         // where page number `rank` of a row goes: first[r] + rank
   __shared__ int64_t sums64[PLAN_WAVES];
   __shared__ int sums[PLAN_WAVES];
   __shared__ int bits;
   if (threadIdx.x == 0) bits = 0;
   __syncthreads();
   const int64_t room = (int64_t)c.width << c.page_shift;
-  auto wants = [&](int r, int& flag) {               // pages that row r asks for, and what is wrong with it
-    const int64_t n = lens[r], m = add[r];
+  auto wants = [&](int64_t n, int64_t m, int& flag) {            // pages that a row asks for, and what is wrong with it
     flag = n < 0 || n > room || m < 0 ? CACHE_RANGE : n + m > room ? CACHE_FULL : 0;
     return flag ? 0 : pages_of(n + m, c.page_shift) - pages_of(n, c.page_shift);
   };
   int64_t carry = 0;
+  int n = 0, m = 0;                                  // of the lane's row, where it has only one
   for (int base = 0; base < n_rows; base += PLAN_THREADS) {
     const int r = base + threadIdx.x;
-    int flag = 0;
-    const int need = r < n_rows ? wants(r, flag) : 0;
+    int flag = 0, need = 0;
+    if (r < n_rows) need = wants(n = lens[r], m = add[r], flag);
     if (flag) atomicOr(&bits, flag);
     int64_t total;
     const int64_t before = carry + block_scan<int64_t>(need, sums64, total);
-    if (r < n_rows) cum[r] = (int)min(before + need, (int64_t)c.n_pages + 1);
+    if (r < n_rows) {
+      cum[r] = (int)min(before + need, (int64_t)c.n_pages + 1);
+      first[r] = pages_of(n, c.page_shift) - (int)min(before, (int64_t)c.n_pages + 1);
+    }
     carry += total;
   }
   __syncthreads();
   const int wanted = (int)min(carry, (int64_t)c.n_pages + 1);
-  const int found = free_pages(refs, c.n_pages, wanted, sums, [&](int rank, int page) {
+  const int found = free_pages(refs, c.n_pages, head, wanted, sums, [&](int rank, int page) {
     int lo = 0, hi = n_rows - 1;                     // first row with cum > rank
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
       if (cum[mid] > rank) hi = mid; else lo = mid + 1;
     }
-    const int at = pages_of(lens[lo], c.page_shift) + rank - (lo ? cum[lo - 1] : 0);
-    table[(int64_t)lo * c.width + at] = page;
+    table[(int64_t)lo * c.width + first[lo] + rank] = page;
     refs[page] = 1;
   });
   __syncthreads();
   for (int r = threadIdx.x; r < n_rows; r += PLAN_THREADS) {
+    if (n_rows > PLAN_THREADS) n = lens[r], m = add[r];
+    const int base = r ? cum[r - 1] : 0;
     int flag;
-    const int need = wants(r, flag), base = r ? cum[r - 1] : 0;
+    const int need = wants(n, m, flag);
     const bool fits = !flag && (need == 0 || cum[r] <= found);
     if (!flag && !fits) {
       atomicOr(&bits, CACHE_FULL);
       for (int k = base; k < found; ++k) {           // at most one row has got a part of its pages
-        int32_t* e = table + (int64_t)r * c.width + pages_of(lens[r], c.page_shift) + (k - base);
+        int32_t* e = table + (int64_t)r * c.width + first[r] + k;
         refs[*e] = 0;
         *e = -1;
       }
     }
-    lens_out[r] = lens[r] + (fits ? add[r] : 0);
+    lens_out[r] = n + (fits ? m : 0);
   }
   __syncthreads();
   if (threadIdx.x == 0 && bits) atomicOr(c.status, bits);
@@ -152,6 +159,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_select_plan_kernel(CacheVi
                                                                          int32_t* lens_out, int n_out, SelectPlan plan) {
   extern __shared__ int lds[];
   int *users = lds, *first = lds + n_in;
+  const int4 head = counts_of(refs, c.n_pages, (int)threadIdx.x * 4);
   __shared__ int sums[PLAN_WAVES];
   __shared__ int bits;
   if (threadIdx.x == 0) bits = 0;
@@ -203,7 +211,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_select_plan_kernel(CacheVi
   }
   for (int s = threadIdx.x; s < n_in; s += PLAN_THREADS) plan.users[s] = users[s];
   __syncthreads();
-  const int found = free_pages(refs, c.n_pages, wanted, sums, [&](int rank, int page) {
+  const int found = free_pages(refs, c.n_pages, head, wanted, sums, [&](int rank, int page) {
     plan.fresh[plan.copies[rank].y] = page;
     plan.copies[rank].y = page;
     refs[page] = 1;
@@ -220,16 +228,18 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_select_plan_kernel(CacheVi
   }
 }
 
+typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2v __attribute__((ext_vector_type(2)));
+
 // page copies over all layers: item i is 16 KB (or a page's rest) of one pool's copy of one page; nothing of it is read again soon, so it
 // is kept out of the way in the caches (248 MB of copies: 63 us, 75 without the hints)
-typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
 struct PageCopy {
   uint8_t *k, *v;
   int64_t layer_bytes;                               // of one pool
   int32_t page_bytes, layers;
 };
 constexpr int COPY_PIECE = 16384;
-template <class Pages>
+template <bool SHARED, class Pages>
 __device__ __forceinline__ void copy_pages(const PageCopy& a, int copies, int block, int blocks, Pages pages) {
   const int pieces = (a.page_bytes + COPY_PIECE - 1) / COPY_PIECE;
   const int64_t items = (int64_t)copies * a.layers * 2 * pieces;
@@ -248,7 +258,7 @@ __device__ __forceinline__ void copy_pages(const PageCopy& a, int copies, int bl
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
       const int at = threadIdx.x + e * APPLY_THREADS;
-      if (at < n / 16) x[e] = __builtin_nontemporal_load(in + at);
+      if (at < n / 16) x[e] = SHARED ? in[at] : __builtin_nontemporal_load(in + at);
     }
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
@@ -288,7 +298,7 @@ __global__ __launch_bounds__(APPLY_THREADS) void cache_select_apply_kernel(Cache
     return;
   }
   block -= n_in;
-  copy_pages(data, plan.count[0], block, gridDim.x - n_out - n_in, [&](int i, int& from, int& to) {
+  copy_pages<true>(data, plan.count[0], block, gridDim.x - n_out - n_in, [&](int i, int& from, int& to) {
     const int2 pair = plan.copies[i];
     from = pair.x;
     to = pair.y;
@@ -356,7 +366,7 @@ __global__ __launch_bounds__(APPLY_THREADS) void cache_compact_apply_kernel(Cach
     }
     return;
   }
-  copy_pages(data, plan.count[0], block - n_rows, gridDim.x - n_rows, [&](int i, int& from, int& to) {
+  copy_pages<false>(data, plan.count[0], block - n_rows, gridDim.x - n_rows, [&](int i, int& from, int& to) {
     from = plan.movers[i];
     to = plan.holes[i];
   });
@@ -418,14 +428,14 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a) {
   using Value = typename std::conditional<F8, uint8_t, uint16_t>::type;
   constexpr int PAD = F8 ? 20 : 18;                  // tokens of a channel's row in LDS, one word of them padding
   __shared__ __align__(16) Value tile[4][HD * PAD];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const CacheView& c = a.c;
   const int head = blockIdx.x % (unsigned)c.heads, unit = (int)(blockIdx.x / (unsigned)c.heads) * 4 + wave;       // a token's heads lie together
   if (unit >= a.units) return;
   int row = unit, t0 = row, fresh = 1, part = 0;
   if (a.cu) {
     // row r owns the numbers cu[r]/16 + 2 r ..., at least as many as it has blocks of 16 positions
-    row = last_not_above(a.n_rows, unit, [&](int r) { return (int64_t)(a.cu[r] >> 4) + 2ll * r; });
+    row = __builtin_amdgcn_readfirstlane(last_not_above(a.n_rows, unit, [&](int r) { return (int64_t)(a.cu[r] >> 4) + 2ll * r; }));
     t0 = a.cu[row];
     fresh = a.cu[row + 1] - t0;
     part = unit - ((t0 >> 4) + 2 * row);
@@ -437,7 +447,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a) {
   }
   const int begin = len - fresh;
   const int64_t at = (begin & ~15) + (int64_t)part * 16;       // position of the block
-  if (at >= len) return;
+  if (at >= len || fresh == 0) return;
   const int page = a.table[(int64_t)row * c.width + (at >> c.page_shift)];
   if ((unsigned)page >= (unsigned)c.n_pages) {
     if (lane == 0 && head == 0) atomicOr(c.status, CACHE_RANGE);
@@ -451,42 +461,43 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a) {
   constexpr int COLS = HD / 8 < 8 ? HD / 8 : 8, TOKENS = 64 / COLS, PASSES = 16 / TOKENS, ITERS = HD / 8 / COLS;
   const int i0 = lane / COLS, col = lane % COLS * 8;
   auto there = [&](int i) { return at + i >= begin && at + i < len; };      // position i of the block is new
-  uint4 kx[PASSES][ITERS], vx[PASSES][ITERS];
+  u32x4v kx[PASSES][ITERS], vx[PASSES][ITERS];
 #pragma unroll
-  for (int p = 0; p < PASSES; ++p)
-#pragma unroll
-    for (int it = 0; it < ITERS; ++it)
-      if (there(i0 + p * TOKENS)) {
-        const int64_t from = (t0 + (at + i0 + p * TOKENS - begin)) * a.token_stride + (int64_t)head * HD + col + it * COLS * 8;
-        kx[p][it] = *(const uint4*)(a.k_new + from);
-        vx[p][it] = *(const uint4*)(a.v_new + from);
-      }
-#pragma unroll
-  for (int p = 0; p < PASSES; ++p)
+  for (int p = 0; p < PASSES; ++p) {
+    // lanes without a new token read the row's first new one again, so that no load waits for a branch
+    const int i = i0 + p * TOKENS;
+    const int64_t from = (there(i) ? t0 + (at + i - begin) : t0) * a.token_stride + (int64_t)head * HD + col;
 #pragma unroll
     for (int it = 0; it < ITERS; ++it) {
-      const int i = i0 + p * TOKENS, ch = col + it * COLS * 8;
-      if (!there(i)) continue;
+      kx[p][it] = *(const u32x4v*)(a.k_new + from + it * COLS * 8);
+      vx[p][it] = *(const u32x4v*)(a.v_new + from + it * COLS * 8);
+    }
+  }
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    const int i = i0 + p * TOKENS;
+#pragma unroll
+    for (int it = 0; it < ITERS; ++it) {
+      const int ch = col + it * COLS * 8;
       const int64_t kt = to + (int64_t)(slot + i) * HD + ch;
       if constexpr (F8) {
-        auto codes = [](uint4 x, const Quotient& over) {
-          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        auto codes = [](u32x4v x, const Quotient& over) {
           float f[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] = over(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
-          return uint2{to_e4m3x4(f[0], f[1], f[2], f[3]), to_e4m3x4(f[4], f[5], f[6], f[7])};
+          for (int e = 0; e < 8; ++e) f[e] = over(e & 1 ? x[e >> 1] & 0xFFFF0000u : x[e >> 1] << 16);
+          return u32x2v{to_e4m3x4(f[0], f[1], f[2], f[3]), to_e4m3x4(f[4], f[5], f[6], f[7])};
         };
-        *(uint2*)((uint8_t*)a.k + kt) = codes(kx[p][it], ks);
-        const uint2 w = codes(vx[p][it], vs);
+        const u32x2v k = codes(kx[p][it], ks), v = codes(vx[p][it], vs);
+        if (there(i)) *(u32x2v*)((uint8_t*)a.k + kt) = k;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) t[(ch + e) * PAD + i] = (uint8_t)((e < 4 ? w.x : w.y) >> (8 * (e & 3)));
+        for (int e = 0; e < 8; ++e) t[(ch + e) * PAD + i] = (uint8_t)(v[e >> 2] >> (8 * (e & 3)));
       } else {
-        *(uint4*)((uint16_t*)a.k + kt) = kx[p][it];
-        const uint32_t w[4] = {vx[p][it].x, vx[p][it].y, vx[p][it].z, vx[p][it].w};
+        if (there(i)) *(u32x4v*)((uint16_t*)a.k + kt) = kx[p][it];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) t[(ch + e) * PAD + i] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+        for (int e = 0; e < 8; ++e) t[(ch + e) * PAD + i] = (uint16_t)(vx[p][it][e >> 1] >> (16 * (e & 1)));
       }
     }
+  }
   wave_lds_sync();
   const int64_t vrow = to + slot;                    // channel 0 of the block
   const int width = 1 << c.page_shift;
@@ -498,9 +509,8 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a) {
       for (int e = 0; e < (F8 ? 1 : 2); ++e) o[e] = uint4{s[4 * e], s[4 * e + 1], s[4 * e + 2], s[4 * e + 3]};
     }
   } else {
-    const int i = lane & 15;
-    for (int ch = lane >> 4; ch < HD; ch += 4)
-      if (there(i)) ((Value*)a.v)[vrow + (int64_t)ch * width + i] = t[ch * PAD + i];
+    for (int i = (int)max((int64_t)0, begin - at); i < 16 && at + i < len; ++i)
+      for (int ch = lane; ch < HD; ch += 64) ((Value*)a.v)[vrow + (int64_t)ch * width + i] = t[ch * PAD + i];
   }
 }
 
@@ -566,8 +576,8 @@ extern "C" pg_status pg_cache_reserve(const pg_cache* c, int32_t* table, const i
   PG_TRY(check_rows(n_rows, "pg_cache_reserve"));
   if (n_rows == 0) return PG_OK;
   if (!table || !lens || !add || !lens_out) return fail(PG_EINVAL, "pg_cache_reserve: null pointer");
-  PG_TRY(allow_lds((const void*)cache_reserve_kernel, (size_t)n_rows * sizeof(int)));
-  cache_reserve_kernel<<<dim3(1), dim3(PLAN_THREADS), (size_t)n_rows * sizeof(int), (hipStream_t)stream>>>(view_of(c), c->refs, table, lens,
+  PG_TRY(allow_lds((const void*)cache_reserve_kernel, (size_t)n_rows * 2 * sizeof(int)));
+  cache_reserve_kernel<<<dim3(1), dim3(PLAN_THREADS), (size_t)n_rows * 2 * sizeof(int), (hipStream_t)stream>>>(view_of(c), c->refs, table, lens,
                                                                                                           add, lens_out, n_rows);
   PG_LAUNCH_CHECK("cache_reserve_kernel");
   return PG_OK;
