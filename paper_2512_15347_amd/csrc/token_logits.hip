@@ -93,7 +93,8 @@ struct Stretch {
   static constexpr int TOKENS = G * PASS_TOKENS;
   uint32_t word[TOKENS];
   uint32_t ready[TOKENS / 32];                       // bit: word holds z
-  uint16_t seen[TOKENS];                             // tokens that occur in the history, in no particular order
+  static constexpr int LISTED = 1024;
+  uint16_t seen[LISTED];                             // tokens that occur in the history, in no particular order; of more all words are looked at
   int n_seen;
 };
 
@@ -144,7 +145,10 @@ __device__ __forceinline__ void prepare_stretch(const LogitArgs& a, const RowRul
   auto logit = [&](uint32_t at) { return BF16 ? bf16_to_f32(((const uint16_t*)d.logits)[row + at]) : ((const float*)d.logits)[row + at]; };
   auto count = [&](uint32_t at, int i) {
     const uint32_t old = i < q.prompt ? atomicOr(&s.word[at], IN_PROMPT) : atomicAdd(&s.word[at], 1u);
-    if ((old & ~HAS_BIAS) == 0) s.seen[atomicAdd(&s.n_seen, 1)] = (uint16_t)at;
+    if ((old & ~HAS_BIAS) == 0) {
+      const int k = atomicAdd(&s.n_seen, 1);
+      if (k < Stretch<G>::LISTED) s.seen[k] = (uint16_t)at;
+    }
   };
   auto finish = [&](uint32_t at, float z) {
     s.word[at] = __builtin_bit_cast(uint32_t, z);
@@ -173,9 +177,10 @@ __device__ __forceinline__ void prepare_stretch(const LogitArgs& a, const RowRul
     if (at < (uint32_t)n) atomicOr(&s.word[at], HAS_BIAS);
   }
   __syncthreads();
-  for (int k = threadIdx.x; k < s.n_seen; k += LOGIT_THREADS) {
-    const uint32_t at = s.seen[k], word = s.word[at];
-    if (!(word & HAS_BIAS)) finish(at, penalised(q, logit(at), word));
+  const bool listed = s.n_seen <= Stretch<G>::LISTED;
+  for (int k = threadIdx.x; k < (listed ? s.n_seen : n); k += LOGIT_THREADS) {
+    const uint32_t at = listed ? s.seen[k] : k, word = s.word[at];
+    if (word && !(word & HAS_BIAS)) finish(at, penalised(q, logit(at), word));
   }
   if (q.bias_lo < q.bias_hi) __syncthreads();        // the history's owners have looked for HAS_BIAS in words that become z here
   if (bias_at < (uint32_t)n && l.bias_before != l.bias_id) finish(bias_at, penalised(q, bias_x, s.word[bias_at]) + l.bias);
@@ -187,8 +192,16 @@ __device__ __forceinline__ void prepare_stretch(const LogitArgs& a, const RowRul
   if (threadIdx.x == 0) s.n_seen = 0;
 }
 
-// z of a group whose first token is number `at` of its stretch; tokens that are not allowed get -inf
-template <bool BF16, int G>
+template <int G>
+__device__ __forceinline__ void clear_group(int at, Stretch<G>& s) {
+  *(uint4*)(s.word + at) = *(uint4*)(s.word + at + 4) = uint4{0, 0, 0, 0};
+  ((uint8_t*)s.ready)[at >> 3] = 0;
+}
+
+// z of a group whose first token is number `at` of its stretch; tokens that are not allowed get -inf.  SKIP: waves whose tokens are all
+// allowed pass the masks over (draws, which the vector ALU bounds: 79 -> 75 us for 384 x 131073; adjusting gets slower with it, 35 -> 48 us
+// for 384 x 65537).
+template <bool BF16, int G, bool SKIP>
 __device__ __forceinline__ void group_logits(bool count, const Group<BF16>& x, int at, Stretch<G>& s, float* z) {
 #pragma unroll
   for (int e = 0; e < LANE_TOKENS; ++e) z[e] = x.logit(e);
@@ -196,13 +209,13 @@ __device__ __forceinline__ void group_logits(bool count, const Group<BF16>& x, i
     const uint32_t ready = ((const uint8_t*)s.ready)[at >> 3];
     if (ready) {
       const float4 w0 = *(const float4*)(s.word + at), w1 = *(const float4*)(s.word + at + 4);
-      *(uint4*)(s.word + at) = *(uint4*)(s.word + at + 4) = uint4{0, 0, 0, 0};
-      ((uint8_t*)s.ready)[at >> 3] = 0;
+      clear_group(at, s);
       const float w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
       for (int e = 0; e < LANE_TOKENS; ++e) z[e] = ready >> e & 1 ? w[e] : z[e];
     }
   }
+  if (SKIP && !__ballot(x.allowed != 0xFFu)) return;
 #pragma unroll
   for (int e = 0; e < LANE_TOKENS; ++e) z[e] = x.allowed >> e & 1 ? z[e] : -INFINITY;
 }
@@ -246,7 +259,7 @@ __global__ __launch_bounds__(LOGIT_THREADS) void logits_adjust_kernel(LogitArgs 
     const int64_t left = a.d.vocab - v;
     if (left <= 0) return;
     float z[8];
-    group_logits<BF16, G>(a.count, x, at, s, z);
+    group_logits<BF16, G, false>(a.count, x, at, s, z);
     if (left >= LANE_TOKENS) {
       __builtin_memcpy(to + v, z, 32);
     } else {
@@ -323,9 +336,12 @@ __global__ __launch_bounds__(LOGIT_THREADS, 6) void sample_range_kernel(LogitArg
   __syncthreads();
   Draw mine = no_draw();
   through_range<BF16, G>(a, q, r, s, [&](const Group<BF16>& x, int64_t v, int at) {
-    if (a.d.vocab - (v - (int)(threadIdx.x & 63) * LANE_TOKENS) <= 0) return;      // nothing of the wave's
+    if (!__ballot(x.allowed)) {                      // past the row's end, or in one of the long runs that a grammar leaves out
+      if (a.count) clear_group(at, s);
+      return;
+    }
     float y[8];
-    group_logits<BF16, G>(a.count, x, at, s, y);
+    group_logits<BF16, G, true>(a.count, x, at, s, y);
     if (greedy) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
