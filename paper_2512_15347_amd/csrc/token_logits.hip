@@ -304,14 +304,25 @@ __device__ __forceinline__ Draw wave_join(Draw a) {
   a.sum = wave_allsum(a.sum * exp_of(a.top - top));
   a.top = top;
   const float best = wave_max(a.score);
-  int token = a.score == best ? a.token : INT32_MAX;
-#pragma unroll
-  for (int d = 32; d; d >>= 1) token = min(token, __shfl_xor(token, d));
-  const uint64_t holder = __ballot(a.score == best && a.token == token);
-  a.y = holder ? __shfl(a.y, (int)__builtin_ctzll(holder)) : -INFINITY;
+  int token = INT32_MAX;
+  float y = -INFINITY;
+  for (uint64_t holders = __ballot(a.score == best && a.token != INT32_MAX); holders; holders &= holders - 1) {      // one, as a rule
+    const int lane = (int)__builtin_ctzll(holders), t = __builtin_amdgcn_readlane(a.token, lane);
+    if (t < token) {
+      token = t;
+      y = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, a.y), lane));
+    }
+  }
+  a.y = y;
   a.score = best;
   a.token = token;
   return a;
+}
+
+__device__ __forceinline__ void finish_draw(const Draw& a, int r, int32_t* token, float* logp) {
+  const bool bad = a.sum != a.sum, none = a.token == INT32_MAX;
+  token[r] = none || bad ? -1 : a.token;
+  logp[r] = bad ? __builtin_nanf("") : none ? -INFINITY : a.y - a.top - logf(a.sum);
 }
 
 // Few tokens can win: with E >= w (w the uniform variate of E = -log1p(-w)) a token's score y - ln E reaches a bound b only if
@@ -320,7 +331,8 @@ __device__ __forceinline__ Draw wave_join(Draw a) {
 // a token that the workgroup has seen, and only tokens that reach it get their score.
 template <bool BF16, int G>
 __global__ __launch_bounds__(LOGIT_THREADS, 6) void sample_range_kernel(LogitArgs a, const float* temperature, uint32_t k0, uint32_t k1,
-                                                                     uint32_t step, const int32_t* ids, Draw* parts) {
+                                                                     uint32_t step, const int32_t* ids, Draw* parts, int32_t* token,
+                                                                        float* logp) {
   extern __shared__ __align__(16) char lds[];
   Stretch<G>& s = *(Stretch<G>*)lds;
   __shared__ Draw waves[LOGIT_WAVES];
@@ -421,7 +433,8 @@ __global__ __launch_bounds__(LOGIT_THREADS, 6) void sample_range_kernel(LogitArg
   __syncthreads();
   if (threadIdx.x == 0) {
     for (int w = 1; w < LOGIT_WAVES; ++w) join(mine, waves[w]);
-    parts[(int64_t)r * gridDim.x + blockIdx.x] = mine;
+    if (gridDim.x == 1) finish_draw(mine, r, token, logp);
+    else parts[(int64_t)r * gridDim.x + blockIdx.x] = mine;
   }
 }
 
@@ -430,18 +443,15 @@ __global__ __launch_bounds__(WAVE) void sample_finish_kernel(const Draw* parts, 
   Draw mine = no_draw();
   for (int i = threadIdx.x; i < ranges; i += WAVE) join(mine, parts[(int64_t)r * ranges + i]);
   mine = wave_join(mine);
-  if (threadIdx.x == 0) {
-    const bool bad = mine.sum != mine.sum, none = mine.token == INT32_MAX;
-    token[r] = none || bad ? -1 : mine.token;
-    logp[r] = bad ? __builtin_nanf("") : none ? -INFINITY : mine.y - mine.top - logf(mine.sum);
-  }
+  if (threadIdx.x == 0) finish_draw(mine, r, token, logp);
 }
 
 // ---------------------------------------------------------------- host side
 
 // How a call is laid out: tokens of a counted stretch (2048 or 4096: a shorter one where there are few rows, so that more workgroups
 // share them) and of a workgroup, and workgroups a row.  `few`: workgroups that are enough; a draw's workgroup finds the bound that the tokens
-// have to reach anew, so it takes several stretches where that leaves so many.
+// have to reach anew, so it takes several stretches where that leaves so many.  (Whole rows of more than 2048 tokens in one workgroup, without
+// the second launch: 10.3 us for one row of 8192, 9.9 with it; 22.8 and 21.8 for 384 rows of 12288.)
 struct LogitGrid { int groups, range, workgroups; };
 static LogitGrid logit_grid(int64_t rows, int64_t vocab, int64_t few) {
   const int g = rows * ((vocab + 2 * PASS_TOKENS - 1) / (2 * PASS_TOKENS)) < 1024 ? 1 : 2;
@@ -450,7 +460,6 @@ static LogitGrid logit_grid(int64_t rows, int64_t vocab, int64_t few) {
   return LogitGrid{g, (int)(per * g * PASS_TOKENS), (int)((stretches + per - 1) / per)};
 }
 constexpr int64_t FEW_ADJUST = 8192, FEW_DRAW = 4096;
-
 static pg_status logit_args(const pg_logits* d, const char* who, LogitArgs& a) {
   if (!d) return fail(PG_EINVAL, "%s: desc is NULL", who);
   if (d->rows < 0 || d->vocab < 1 || (d->dtype != PG_LOGITS_F32 && d->dtype != PG_LOGITS_BF16))
@@ -520,8 +529,9 @@ extern "C" pg_status pg_sample_tokens(const pg_logits* desc, const float* temper
   const LogitGrid g = logit_grid(a.d.rows, a.d.vocab, FEW_DRAW);
   a.range = g.range;
   const dim3 grid((unsigned)g.workgroups, (unsigned)a.d.rows), block(LOGIT_THREADS);
-  PG_LOGIT_KERNEL(sample_range_kernel, g.groups, a, temperature, (uint32_t)seed, (uint32_t)(seed >> 32), step, ids, (Draw*)scratch);
+  PG_LOGIT_KERNEL(sample_range_kernel, g.groups, a, temperature, (uint32_t)seed, (uint32_t)(seed >> 32), step, ids, (Draw*)scratch, token, logp);
   PG_LAUNCH_CHECK("sample_range_kernel");
+  if (g.workgroups == 1) return PG_OK;
   sample_finish_kernel<<<dim3((unsigned)a.d.rows), dim3(WAVE), 0, s>>>((const Draw*)scratch, (int)grid.x, token, logp);
   PG_LAUNCH_CHECK("sample_finish_kernel");
   return PG_OK;
