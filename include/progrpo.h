@@ -355,7 +355,7 @@ enum { PG_CACHE_BF16 = 0, PG_CACHE_E4M3 = 1 };
  * Sequence r holds tokens 0 .. lens[r]-1; token t lies at slot t % page of page table[r * width + t / page].
  *   k: [layers, n_pages, heads, page, head_dim]      v: [layers, n_pages, heads, head_dim, page] (values transposed)
  * both 16-byte aligned, bf16 or 8-bit e4m3 codes (value = code * scale[layer, head]).  page 16, 32, 64 or 128;
- * head_dim 32, 64 or 128; width * page < 2^31.  Every table passed with a cache has `width` entries a row; entries
+ * head_dim 32, 64 or 128; width * page <= 2^30.  Every table passed with a cache has `width` entries a row; entries
  * past the last page of a row are not read (calls that write tables write -1 there).
  * refs[p]: rows that hold page p, 0 if it is free (any order of calls on one stream keeps it so).  A page that is
  * part filled belongs to one row.  Taking pages is deterministic: the free page of the lowest number first, in row order.
@@ -389,14 +389,14 @@ pg_status pg_cache_append(const pg_cache *cache, int32_t layer, const uint16_t *
                           int64_t token_stride, const int32_t *table, const int32_t *lens, const int32_t *cu,
                           int32_t n_rows, int32_t n_tokens, void *stream);
 
-/* int32 scratch of pg_cache_select (at most n_rows rows on either side) and pg_cache_compact. */
+/* int32 scratch of pg_cache_select (at most n_rows rows on either side) and pg_cache_compact; 8-byte aligned. */
 int64_t pg_cache_scratch_ints(const pg_cache *cache, int32_t n_rows);
 
 /* Fork, reorder and free: row r of (table_out, lens_out) is the sequence src[r] of (table_in, lens_in); src[r] == -1: an empty
  * row.  Whole pages are shared (refs += users - 1; a sequence without users gives its pages back), a part-filled last page stays
  * with the first of its users and is copied, in all layers, for the others, on pages that were free before the call.  A row whose
  * copy finds no page ends at its last whole page (status 4).  The new table replaces the old one, which must not be used
- * afterwards; the two must not overlap, nor the two arrays of lengths. */
+ * afterwards; the two must not overlap, nor the two arrays of lengths, nor src the new rows. */
 pg_status pg_cache_select(const pg_cache *cache, const int32_t *table_in, const int32_t *lens_in, int32_t n_in,
                           const int32_t *src, int32_t *table_out, int32_t *lens_out, int32_t n_out, int32_t *scratch,
                           void *stream);

@@ -158,7 +158,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void paged_attention_kernel(PagedArg
   if constexpr (EVEN) {
     ht = (int)(at / units);
     const int rest = (int)(at % units);
-    if (query < 0) {                                 // first query with cum > rest
+    if (query < 0 || rest == 0) {                    // the range, or a head, begins: first query with cum > rest
       int lo = 0, hi = a.n_q - 1;
       while (lo < hi) {
         const int mid = (lo + hi) >> 1;
@@ -166,7 +166,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void paged_attention_kernel(PagedArg
       }
       query = lo;
     } else {
-      do query = query + 1 < a.n_q ? query + 1 : 0;
+      do ++query;                                    // rest < units, which is the last one's cum
       while (lds_cum[query] <= rest);
     }
     query = __builtin_amdgcn_readfirstlane(query);

@@ -525,7 +525,7 @@ pg_status check_cache(const pg_cache* c, bool data, const char* who) {
     return fail(PG_ESHAPE, "%s: pages of %d tokens (16, 32, 64 or 128)", who, c->page);
   if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128)
     return fail(PG_ESHAPE, "%s: head width %d (32, 64 or 128)", who, c->head_dim);
-  if ((int64_t)c->width * c->page > INT32_MAX) return fail(PG_ESHAPE, "%s: a row of %d pages passes 2^31 tokens", who, c->width);
+  if ((int64_t)c->width * c->page > 1 << 30) return fail(PG_ESHAPE, "%s: a row of %d pages passes 2^30 tokens", who, c->width);
   if (c->n_pages > INT32_MAX - 8) return fail(PG_ESHAPE, "%s: too many pages", who);
   if ((int64_t)c->heads * c->page * c->head_dim > 1 << 30) return fail(PG_ESHAPE, "%s: a page of %d heads is too large", who, c->heads);
   if (!c->refs || !c->status) return fail(PG_EINVAL, "%s: refs or status is NULL", who);
@@ -637,6 +637,9 @@ extern "C" pg_status pg_cache_select(const pg_cache* c, const int32_t* table_in,
   };
   if (n_in && n_out && (overlap(table_in, (int64_t)n_in * c->width, table_out, (int64_t)n_out * c->width) || overlap(lens_in, n_in, lens_out, n_out)))
     return fail(PG_EINVAL, "pg_cache_select: the new rows overlap the old ones");
+  if (n_out && (overlap(src, n_out, table_out, (int64_t)n_out * c->width) || overlap(src, n_out, lens_out, n_out)))
+    return fail(PG_EINVAL, "pg_cache_select: the new rows overlap src");
+  if ((uintptr_t)scratch & 7) return fail(PG_ESHAPE, "pg_cache_select: scratch must be 8-byte aligned");
   hipStream_t s = (hipStream_t)stream;
   const SelectPlan plan = select_plan(scratch, n_in, n_out);
   PG_TRY(allow_lds((const void*)cache_select_plan_kernel, (size_t)n_in * 2 * sizeof(int)));

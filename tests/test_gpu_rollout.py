@@ -145,6 +145,29 @@ def test_attention_split_over_a_long_row(lib, n, f8):
         check_attention(lib, rng, cache, table, rows, lens, 8, 128, n, sharp=8.0)
 
 
+@pytest.mark.parametrize("rows,kv,group,hd,page,f8", [(30, 4, 3, 64, 16, False), (23, 3, 20, 128, 64, False), (17, 5, 2, 128, 32, True), (40, 2, 4, 32, 16, True)])
+def test_attention_in_even_ranges(lib, rows, kv, group, hd, page, f8):
+    """More units than ranges, so that a range covers several rows, some whole; empty rows at both ends and between; two tiles of heads."""
+    say(f"paged attention in even ranges: {rows} rows, {kv} x {group} heads of {hd}")
+    rng = np.random.default_rng([rows, kv, hd])
+    lens = rng.integers(1, 5000, size=rows)
+    lens[[0, 5, 6, rows - 1]] = 0
+    lens[7] = 9000
+    lens = lens.tolist()
+    cache, table, rows_ = make_cache(lib, rng, lens, kv, hd, page, f8)
+    assert lib.pg_paged_attention_workspace(cache, rows, kv * group, 9000) > 0
+    check_attention(lib, rng, cache, table, rows_, lens, kv * group, hd, 9000, sharp=2.0)
+
+
+def test_a_row_longer_than_said_and_than_the_page_numbers_in_lds(lib):
+    say("paged attention, 20000 tokens in pages of 16 by one workgroup")
+    rng = np.random.default_rng(12)
+    lens = [20000, 8192, 8193]
+    cache, table, rows = make_cache(lib, rng, lens, 1, 32, 16, False)
+    check_attention(lib, rng, cache, table, rows, lens, 2, 32, 1)
+    check_attention(lib, rng, cache, table, rows, lens, 2, 32, 20000)
+
+
 def test_attention_of_a_prompt_as_queries_of_growing_lengths(lib):
     """Rows of the table in any order and repeated; pages shared by several rows; the last of two layers."""
     say("paged attention with a row map")

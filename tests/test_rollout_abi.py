@@ -40,7 +40,7 @@ def cache(**change):
 
 BAD_CACHES = [(dict(layers=0), pg.PG_EINVAL), (dict(n_pages=0), pg.PG_EINVAL), (dict(heads=-1), pg.PG_EINVAL), (dict(width=0), pg.PG_EINVAL),
               (dict(dtype=2), pg.PG_EINVAL), (dict(page=8), pg.PG_ESHAPE), (dict(page=48), pg.PG_ESHAPE), (dict(head_dim=96), pg.PG_ESHAPE),
-              (dict(width=1 << 27), pg.PG_ESHAPE), (dict(refs=None), pg.PG_EINVAL), (dict(status=None), pg.PG_EINVAL),
+              (dict(width=1 << 27), pg.PG_ESHAPE), (dict(width=(1 << 26) + 1), pg.PG_ESHAPE), (dict(refs=None), pg.PG_EINVAL), (dict(status=None), pg.PG_EINVAL),
               (dict(refs=P + 4), pg.PG_ESHAPE), (dict(k_scale=P), pg.PG_EINVAL), (dict(k=None), pg.PG_EINVAL), (dict(v=P + 8), pg.PG_ESHAPE),
               (dict(heads=1 << 24), pg.PG_ESHAPE)]
 
@@ -80,6 +80,9 @@ def test_calls_on_the_cache_refuse_bad_arguments():
     assert f.pg_cache_select(c, P, P, 1, P, far, far, 1, None, None) == pg.PG_EINVAL
     assert f.pg_cache_select(c, P, P, 4, P, P + 32, far, 1, P, None) == pg.PG_EINVAL      # the tables overlap
     assert f.pg_cache_select(c, P, P, 4, P, far, P + 12, 1, P, None) == pg.PG_EINVAL      # the lengths overlap
+    assert f.pg_cache_select(c, P, P, 4, far, far + 64, 2 * far, 17, P, None) == pg.PG_EINVAL      # src and the new table overlap
+    assert f.pg_cache_select(c, P, P, 4, far, 2 * far, far + 4, 2, P, None) == pg.PG_EINVAL        # src and the new lengths
+    assert f.pg_cache_select(c, P, P, 1, 2 * P, far, 2 * far, 1, P + 4, None) == pg.PG_ESHAPE
     assert f.pg_cache_compact(c, P, P, -1, P, None) == pg.PG_EINVAL
     assert f.pg_cache_compact(c, P, P, 1, None, None) == pg.PG_EINVAL
     assert f.pg_cache_scratch_ints(c, 100) >= 4 + 3 * 100 and f.pg_cache_scratch_ints(None, 3) == 0
