@@ -31,6 +31,7 @@ constexpr int PA_HEADS = 16;                         // query heads of a tile: t
 
 constexpr int PA_PAGES = 512;                        // page numbers in LDS at a time
 constexpr int PA_EVEN_QUERIES = 2048;                // whose prefix sums are held in LDS
+constexpr int PA_RANGES = 512;                       // of an EVEN call: two workgroups a compute unit, what the registers of wide heads leave room for
 
 struct PagedArgs {
   CacheView c;
@@ -378,6 +379,7 @@ __global__ __launch_bounds__(PA_THREADS) void paged_join_kernel(PagedArgs a) {
   constexpr int LANES = HD / 4, PARTS = PA_THREADS / LANES;
   __shared__ __align__(16) float lds_o[PARTS][HD];
   __shared__ Piece lds_ml[PARTS];
+  __shared__ int lds_slot[PA_RANGES], lds_count;
   const int r0 = blockIdx.x, column = blockIdx.y, part = threadIdx.x / LANES, ch = threadIdx.x % LANES * 4;
   const int4 row = a.opened[r0];
   if (row.z == 0) return;
@@ -394,16 +396,31 @@ __global__ __launch_bounds__(PA_THREADS) void paged_join_kernel(PagedArgs a) {
     x = Piece{m, x.l * f + y.l * g};
     acc = acc * f + o * g;
   };
-  // pieces: the last of that range (its first, if it begins with the row), the first of all others
-#pragma unroll 4
-  for (int r = before + part; r < a.ranges; r += PARTS) {
+  // where the pieces lie, all looked up at once: the last of that range (its first, if it begins with the row), the first of all others
+  int mine = 0;
+  for (int r = before + threadIdx.x; r < a.ranges; r += PA_THREADS) {
     const int64_t start = a.starts[r];
-    if (start >= end) break;
-    if (start == a.starts[r + 1]) continue;
-    const int last = start < begin;
-    const float* p = a.parts + (((int64_t)r * 2 + last) * PA_HEADS + column) * (HD + 4);
-    const float2 ml = *(const float2*)p;
-    add(Piece{ml.x, ml.y}, *(const f32x4v*)(p + 4 + ch));
+    lds_slot[r - before] = start == a.starts[r + 1] ? -1 : 2 * r + (start < begin);
+    mine += start < end;
+  }
+  if (threadIdx.x == 0) lds_count = 0;
+  __syncthreads();
+  if (mine) atomicAdd(&lds_count, mine);
+  __syncthreads();
+  constexpr int AHEAD = 4;
+  for (int i = part; i < lds_count; i += AHEAD * PARTS) {
+    Piece y[AHEAD];
+    f32x4v o[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const int at = i + k * PARTS, slot = at < lds_count ? lds_slot[at] : -1;
+      const float* p = a.parts + ((int64_t)(slot < 0 ? lds_slot[0] : slot) * PA_HEADS + column) * (HD + 4);
+      const float2 ml = *(const float2*)p;
+      y[k] = Piece{slot < 0 ? -INFINITY : ml.x, ml.y};
+      o[k] = *(const f32x4v*)(p + 4 + ch);
+    }
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) add(y[k], o[k]);
   }
   *(f32x4v*)&lds_o[part][ch] = acc;
   if (ch == 0) lds_ml[part] = x;
@@ -416,10 +433,8 @@ __global__ __launch_bounds__(PA_THREADS) void paged_join_kernel(PagedArgs a) {
   if (a.lse && ch == 0) a.lse[(int64_t)row.x * a.heads_q + head] = x.l > 0.0f ? (x.m + log2f(x.l)) * 0.6931471805599453f : -INFINITY;
 }
 
-// Ranges of an EVEN call, 0 for WHOLE: two workgroups a compute unit are what the registers of the widest heads leave room for.  A row
-// alone takes about as many microseconds as it has units, and the prefix sums and the second launch of EVEN cost about eight; the rows
-// are taken to be half as long as the longest on average.
-constexpr int PA_RANGES = 512;
+// Ranges of an EVEN call, 0 for WHOLE.  A row alone takes about as many microseconds as it has units, and the prefix sums and the second
+// launch of EVEN cost about eight; the rows are taken to be half as long as the longest on average.
 static int ranges_of(const pg_cache* c, int64_t n_q, int heads_q, int max_len) {
   const int64_t items = n_q * c->heads * ((heads_q / c->heads + PA_HEADS - 1) / PA_HEADS), unit = c->dtype == PG_CACHE_E4M3 ? 256 : 128;
   const int64_t units = (max_len + unit - 1) / unit;
