@@ -18,6 +18,7 @@
 // workspace and a second launch joins them.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 #include "paged_cache.hpp"
 #include "operands.hpp"
 
@@ -246,7 +247,10 @@ __global__ __launch_bounds__(PA_THREADS, 2) void paged_attention_kernel(PagedArg
       load_keys(key0);
       load_values(key0);
     }
-    for (; key0 < tokens; key0 += PA_WAVES * S::KEYS) {
+    // MORE: a step follows, whose keys and values are asked for.  Under a branch inside the loop they made every wait for values wait for
+    // the keys of the next step, too: the compiler has to assume that nothing was asked for after the values.
+    auto work = [&](auto more) {
+      constexpr bool MORE = decltype(more)::value;
       const int next = key0 + PA_WAVES * S::KEYS;
       f32x4v s[2 * U];
 #pragma unroll
@@ -265,13 +269,15 @@ __global__ __launch_bounds__(PA_THREADS, 2) void paged_attention_kernel(PagedArg
           }
         }
       }
-      if (next < tokens) load_keys(next);
+      if constexpr (MORE) load_keys(next);
       const int there = tokens - key0;               // keys of the step that exist, if fewer than KEYS
       float top = -INFINITY;
 #pragma unroll
       for (int t = 0; t < 2 * U; ++t) {
         s[t] *= scale;
-        if (there < S::KEYS) {
+        // without a branch around it: where scores are first read behind one, this compiler has left out the wait states that a product's
+        // result needs, and read some of them too early
+        if constexpr (!MORE) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) s[t][i] = key_values + 4 * t + i < there ? s[t][i] : -INFINITY;
         }
@@ -304,7 +310,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void paged_attention_kernel(PagedArg
         for (int e = 0; e < 8; ++e) rest[e] = p[e] - (float)hi[u][e];
         lo[u] = as_bf16(uint4{pack_bf16x2(rest[0], rest[1]), pack_bf16x2(rest[2], rest[3]), pack_bf16x2(rest[4], rest[5]), pack_bf16x2(rest[6], rest[7])});
       }
-      if (there < S::KEYS) {                         // what lies behind the last token may be anything, NaN too
+      if (!MORE && there < S::KEYS) {                // what lies behind the last token may be anything, NaN too
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
           uint32_t w[4] = {vr[d].x, vr[d].y, vr[d].z, vr[d].w};
@@ -331,8 +337,11 @@ __global__ __launch_bounds__(PA_THREADS, 2) void paged_attention_kernel(PagedArg
           o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, lo[1], o[d], 0, 0, 0);
         }
       }
-      if (next < tokens) load_values(next);
-    }
+      if constexpr (MORE) load_values(next);
+      key0 = next;
+    };
+    while (key0 + PA_WAVES * S::KEYS < tokens) work(std::true_type{});
+    if (key0 < tokens) work(std::false_type{});
   }
   l = across_rows(l, [](float x, float y) { return x + y; });
 #pragma unroll
