@@ -16,6 +16,10 @@
 // holds workgroups, wherever a row begins or ends: rows of any lengths end together, and a workgroup streams through its range with one
 // start only.  A range has at most two rows that it does not cover whole, its first and its last; their pieces go to the
 // workspace and a second launch joins them.
+//
+// Measured: 384 rows of 1 to 4096 tokens, 32 / 8 heads of 128, codes (1.6 GB): 292 us, 5.6 TB/s, where a plain read of 4 GiB reaches 5.3
+// to 6.3; three rows of 65 to 131 thousand tokens in bf16 (0.65 GB): 126 us, of which the join takes 10; 48 rows of up to 1178 tokens with
+// heads of 64 (65 MB with the shared prompt counted once a row): 14 us; one row of 77 tokens: 4 us, and 8 with the call.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -32,7 +36,8 @@ constexpr int PA_HEADS = 16;                         // query heads of a tile: t
 
 constexpr int PA_PAGES = 512;                        // page numbers in LDS at a time
 constexpr int PA_EVEN_QUERIES = 2048;                // whose prefix sums are held in LDS
-constexpr int PA_RANGES = 512;                       // of an EVEN call: two workgroups a compute unit, what the registers of wide heads leave room for
+constexpr int PA_RANGES = 512;                       // of an EVEN call, at most: two workgroups a compute unit, what the registers of wide heads leave
+                                                     // room for (384 rows of up to 4096 tokens in codes: 296 us, 335 with 768 and 305 with 1024)
 
 struct PagedArgs {
   CacheView c;
@@ -45,8 +50,8 @@ struct PagedArgs {
   float scale_log2;
   uint16_t* out;
   float* lse;
-  int ranges;                                        // EVEN: workgroups, a multiple of 8
-  int64_t* starts;                                   // EVEN: first unit of each range and the end of the last, for the second launch
+  int ranges, log2_ranges;                           // EVEN: workgroups
+  int64_t* total;                                    // EVEN: units of all rows, heads and tiles, for the second launch
   int4* opened;                                      // EVEN: query, head tile, unit and units of the row that each range begins in
   float* parts;                                      // EVEN: [range][first, last][query head of the tile][HD + 4]: m, l, -, -, o'
 };
@@ -61,7 +66,7 @@ __device__ __forceinline__ int query_length(const PagedArgs& a, int query, int& 
   return 0;
 }
 // first unit of a range
-__device__ __forceinline__ int64_t range_start(int64_t total, int ranges, int r) { return total * r / ranges; }
+__device__ __forceinline__ int64_t range_start(int64_t total, int log2_ranges, int r) { return total * r >> log2_ranges; }
 
 __device__ __forceinline__ bf16x8 as_bf16(uint4 w) { return __builtin_bit_cast(bf16x8, w); }
 // eight codes -> eight bf16 (exact: e4m3 has three bits of fraction)
@@ -146,11 +151,10 @@ __global__ __launch_bounds__(PA_THREADS, 2) void paged_attention_kernel(PagedArg
       }
     __syncthreads();
     const int64_t total = (int64_t)units * a.c.heads * a.q_tiles;
-    at = range_start(total, a.ranges, range);
-    stop = range_start(total, a.ranges, range + 1);
+    at = range_start(total, a.log2_ranges, range);
+    stop = range_start(total, a.log2_ranges, range + 1);
     if (threadIdx.x == 0) {
-      a.starts[range] = at;
-      if (range == a.ranges - 1) a.starts[a.ranges] = stop;
+      if (range == 0) *a.total = total;
       if (at >= stop) a.opened[range] = int4{0, 0, 0, 0};
     }
   }
@@ -388,15 +392,17 @@ __global__ __launch_bounds__(PA_THREADS) void paged_join_kernel(PagedArgs a) {
   constexpr int LANES = HD / 4, PARTS = PA_THREADS / LANES;
   __shared__ __align__(16) float lds_o[PARTS][HD];
   __shared__ Piece lds_ml[PARTS];
-  __shared__ int lds_slot[PA_RANGES], lds_count;
   const int r0 = blockIdx.x, column = blockIdx.y, part = threadIdx.x / LANES, ch = threadIdx.x % LANES * 4;
   const int4 row = a.opened[r0];
+  const int64_t total = *a.total;
   if (row.z == 0) return;
-  const int64_t start0 = a.starts[r0], begin = start0 - row.z, end = begin + row.w;
+  const auto start = [&](int r) { return range_start(total, a.log2_ranges, r); };
+  const auto last_before = [&](int64_t unit) { return (int)((((uint64_t)unit << a.log2_ranges) - 1) / (uint64_t)total); };   // range, unit >= 1
+  const int64_t start0 = start(r0), begin = start0 - row.z, end = begin + row.w;
   const int tile = row.y % a.q_tiles, head = row.y / a.q_tiles * a.group + tile * PA_HEADS + column;
-  int before = r0 - 1;                               // the range that ends here; there are empty ones where units are few
-  while (a.starts[before] == start0) --before;
-  if (a.starts[before] > begin || column >= a.group - tile * PA_HEADS) return;
+  const int before = last_before(start0);            // the range that ends here; there are empty ones where units are few
+  if (start(before) > begin || column >= a.group - tile * PA_HEADS) return;
+  const int last = last_before(end);
   Piece x = {-INFINITY, 0.0f};
   f32x4v acc = {0.f, 0.f, 0.f, 0.f};
   auto add = [&](Piece y, f32x4v o) {
@@ -405,27 +411,17 @@ __global__ __launch_bounds__(PA_THREADS) void paged_join_kernel(PagedArgs a) {
     x = Piece{m, x.l * f + y.l * g};
     acc = acc * f + o * g;
   };
-  // where the pieces lie, all looked up at once: the last of that range (its first, if it begins with the row), the first of all others
-  int mine = 0;
-  for (int r = before + threadIdx.x; r < a.ranges; r += PA_THREADS) {
-    const int64_t start = a.starts[r];
-    lds_slot[r - before] = start == a.starts[r + 1] ? -1 : 2 * r + (start < begin);
-    mine += start < end;
-  }
-  if (threadIdx.x == 0) lds_count = 0;
-  __syncthreads();
-  if (mine) atomicAdd(&lds_count, mine);
-  __syncthreads();
+  // a range's piece of this row is its first, but for a range that begins before the row: there it is the last
   constexpr int AHEAD = 4;
-  for (int i = part; i < lds_count; i += AHEAD * PARTS) {
+  for (int i = before + part; i <= last; i += AHEAD * PARTS) {
     Piece y[AHEAD];
     f32x4v o[AHEAD];
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
-      const int at = i + k * PARTS, slot = at < lds_count ? lds_slot[at] : -1;
-      const float* p = a.parts + ((int64_t)(slot < 0 ? lds_slot[0] : slot) * PA_HEADS + column) * (HD + 4);
+      const int at = i + k * PARTS, r = at <= last ? at : before;
+      const float* p = a.parts + ((int64_t)(2 * r + (start(r) < begin)) * PA_HEADS + column) * (HD + 4);
       const float2 ml = *(const float2*)p;
-      y[k] = Piece{slot < 0 ? -INFINITY : ml.x, ml.y};
+      y[k] = Piece{at <= last && start(at) < start(at + 1) ? ml.x : -INFINITY, ml.y};
       o[k] = *(const f32x4v*)(p + 4 + ch);
     }
 #pragma unroll
@@ -442,14 +438,23 @@ __global__ __launch_bounds__(PA_THREADS) void paged_join_kernel(PagedArgs a) {
   if (a.lse && ch == 0) a.lse[(int64_t)row.x * a.heads_q + head] = x.l > 0.0f ? (x.m + log2f(x.l)) * 0.6931471805599453f : -INFINITY;
 }
 
-// Ranges of an EVEN call, 0 for WHOLE.  A row alone takes about as many microseconds as it has units, and the prefix sums and the second
-// launch of EVEN cost about eight; the rows are taken to be half as long as the longest on average.
+// Ranges of an EVEN call, 0 for WHOLE.  `span` is the longest row in units of heads of 128 channels, each of which takes a workgroup
+// alone 1.3 us; heads of 64 and 32 take 0.6 and 0.3, with codes 0.8 and 0.6 (a part of their steps does not depend on the width).
+// EVEN costs 7 us more (prefix sums, second launch), and an item's span some 1/200 of that of a workgroup alone once all items share the
+// device's bandwidth; longer rows are left waiting for at the end of a WHOLE call in any number, sooner where there
+// are more items than compute units.  WHOLE and EVEN in us, rows of 1 token up to the span, by items x span:  8 x 8: 13.7, 11.6;
+// 8 x 32: 45, 12.2;  32 x 8: 13.7, 11.8;  128 x 8: 14.1, 19.2;  128 x 16: 25.1, 25.0;  256 x 16: 27.8, 33.3;  384 x 8: 25.5, 28.4;
+// 384 x 14: 40, 37;  576 x 16: 77, 55;  768 x 14: 67, 69;  768 x 32: 178, 161;  1024 x 128: 822, 748;  3072 x 8: 157, 166;  3072 x 32: 575, 566;
+// and rows that are all of one length: 1024 x 13: 144, 155.
 static int ranges_of(const pg_cache* c, int64_t n_q, int heads_q, int max_len) {
   const int64_t items = n_q * c->heads * ((heads_q / c->heads + PA_HEADS - 1) / PA_HEADS), unit = c->dtype == PG_CACHE_E4M3 ? 256 : 128;
-  const int64_t units = (max_len + unit - 1) / unit;
-  if (n_q > PA_EVEN_QUERIES || units <= 8 + items * units / (2 * PA_RANGES)) return 0;
+  const int64_t units = (max_len + unit - 1) / unit,
+                span = units * (c->dtype == PG_CACHE_E4M3 ? (c->head_dim + 64) * 2 / 3 : c->head_dim);    // in 128ths
+  if (n_q > PA_EVEN_QUERIES || (span <= (items > 256 ? 12 : 16) * 128 && span <= 6 * 128 + items * span / 200)) return 0;
   if (n_q * ((int64_t)c->width * c->page / unit + 1) > 1 << 30) return 0;      // units are counted in 32 bits
-  return PA_RANGES;
+  int64_t ranges = 8;                                // no more than there are units: empty ones cost the join its time
+  while (ranges < PA_RANGES && ranges < items * units) ranges *= 2;
+  return (int)ranges;
 }
 
 static pg_status paged_sizes(const pg_cache* c, int32_t n_q, int32_t heads_q, int32_t max_len, const char* who) {
@@ -469,7 +474,7 @@ using namespace pg;
 extern "C" size_t pg_paged_attention_workspace(const pg_cache* c, int32_t n_q, int32_t heads_q, int32_t max_len) {
   if (paged_sizes(c, n_q, heads_q, max_len, "pg_paged_attention_workspace") != PG_OK) return 0;
   const int ranges = ranges_of(c, n_q, heads_q, max_len);
-  return ranges ? 16 + (size_t)ranges * (sizeof(int64_t) + sizeof(int4) + 2 * PA_HEADS * (c->head_dim + 4) * sizeof(float)) : 0;
+  return ranges ? 16 + (size_t)ranges * (sizeof(int4) + 2 * PA_HEADS * (c->head_dim + 4) * sizeof(float)) : 0;
 }
 
 extern "C" pg_status pg_paged_attention(const pg_cache* c, int32_t layer, const uint16_t* q, int64_t q_stride, const int32_t* table,
@@ -506,7 +511,8 @@ extern "C" pg_status pg_paged_attention(const pg_cache* c, int32_t layer, const 
   a.scale_log2 = (float)((scale == 0.0 ? 1.0 / std::sqrt((double)c->head_dim) : scale) * 1.4426950408889634);
   a.lse = lse;
   a.opened = (int4*)workspace; a.parts = (float*)(a.opened + a.ranges);
-  a.starts = (int64_t*)(a.parts + (size_t)a.ranges * 2 * PA_HEADS * (c->head_dim + 4));
+  a.total = (int64_t*)(a.parts + (size_t)a.ranges * 2 * PA_HEADS * (c->head_dim + 4));
+  while (1 << a.log2_ranges < a.ranges) ++a.log2_ranges;
   const dim3 block(PA_THREADS), join((unsigned)a.ranges, (unsigned)std::min(a.group, PA_HEADS));
   const dim3 grid = a.ranges ? dim3((unsigned)a.ranges) : dim3(1, (unsigned)(c->heads * a.q_tiles), (unsigned)n_q);
   hipStream_t s = (hipStream_t)stream;
