@@ -4,6 +4,11 @@
 // bias: for every 4096 tokens the row's history is counted in LDS (32 bits a token: integer sums, so their order does not matter), the
 // tokens that occur are worked out once each and left in LDS, and the groups pick them up by a bit.  So no counts are kept
 // between calls, and nothing but the history has to follow a member through a prune.  The logits are read once.
+//
+// Adjusting is bound by HBM, and by the barriers around the counts where there is a history: 384 x 65537 in bf16 takes 35 us without one
+// (4.3 TB/s), 49 with up to 2048 tokens of history a row, masks and lists.  Draws are bound by the vector ALU, of which 1024 SIMDs at
+// four cycles an instruction issue some 600 a nanosecond: 384 x 131073 takes 66 us without history, lists and masks, 96 with all of them (the
+// logits alone would be read in 20).
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
@@ -329,8 +334,9 @@ __device__ __forceinline__ void finish_draw(const Draw& a, int r, int32_t* token
 // w <= exp(y - b) = p exp(top - b), where p = exp(y - top) is what the softmax's sum needs anyway.  So a token costs its
 // Philox word, one exponential and one multiply-add; b is the best lower bound y - ln w - w (ln E <= ln w + w for w <= 1/2) of
 // a token that the workgroup has seen, and only tokens that reach it get their score.
+// Five waves a SIMD: six leave 80 registers, so that some of the history's are spilled (384 x 131073 in fp32: 100 us, 92 with five).
 template <bool BF16, int G>
-__global__ __launch_bounds__(LOGIT_THREADS, 6) void sample_range_kernel(LogitArgs a, const float* temperature, uint32_t k0, uint32_t k1,
+__global__ __launch_bounds__(LOGIT_THREADS, 5) void sample_range_kernel(LogitArgs a, const float* temperature, uint32_t k0, uint32_t k1,
                                                                      uint32_t step, const int32_t* ids, Draw* parts, int32_t* token,
                                                                         float* logp) {
   extern __shared__ __align__(16) char lds[];
@@ -449,17 +455,25 @@ __global__ __launch_bounds__(WAVE) void sample_finish_kernel(const Draw* parts, 
 // ---------------------------------------------------------------- host side
 
 // How a call is laid out: tokens of a counted stretch (2048 or 4096: a shorter one where there are few rows, so that more workgroups
-// share them) and of a workgroup, and workgroups a row.  `few`: workgroups that are enough; a draw's workgroup finds the bound that the tokens
-// have to reach anew, so it takes several stretches where that leaves so many.  (Whole rows of more than 2048 tokens in one workgroup, without
+// share them) and of a workgroup, and workgroups a row.  A draw's workgroup finds the bound that the tokens have to reach anew and looks
+// through the history once, so it takes as many stretches as let all workgroups be resident at once, five on each compute unit (this rule and
+// some 4096 workgroups, us, without a history in brackets: 384 x 65537: 60 and 70 (43 and 57); 384 x 131073: 93 and 93 (66 and 74);
+// 128 x 131073: 47 and 50 (34 and 39); 640 x 65537: 87 and 97 (53 and 71); 1000 x 65537: 111 and 125 (69 and 85)).  More rows than that
+// get some 4096 workgroups.  Adjusting keeps nothing but the history between stretches and gains nothing from longer ranges
+// (384 x 65537: 30 us with 8192 workgroups or fewer, 33 with 2048).  (Whole rows of more than 2048 tokens in one workgroup, without
 // the second launch: 10.3 us for one row of 8192, 9.9 with it; 22.8 and 21.8 for 384 rows of 12288.)
+constexpr int64_t RESIDENT_DRAWS = 1280;                  // of 256 lanes, five waves a SIMD
 struct LogitGrid { int groups, range, workgroups; };
-static LogitGrid logit_grid(int64_t rows, int64_t vocab, int64_t few) {
-  const int g = rows * ((vocab + 2 * PASS_TOKENS - 1) / (2 * PASS_TOKENS)) < 1024 ? 1 : 2;
+static LogitGrid logit_grid(int64_t rows, int64_t vocab, bool draw) {
+  // stretches of 2048 and 4096 in us: draws of 48 x 32001 (384 long stretches): 16.9, 16.6; 128 x 16384 (512): 18.1, 18.1; 48 x 65537 (816): 23.3,
+  // 20.2; adjusting 128 x 16384: 7.0, 7.7; 48 x 65537: 8.9, 9.7; 384 x 16384 (1536): 14.1, 12.3
+  const int g = rows * ((vocab + 2 * PASS_TOKENS - 1) / (2 * PASS_TOKENS)) < (draw ? 512 : 1024) ? 1 : 2;
   const int64_t stretches = (vocab + g * PASS_TOKENS - 1) / (g * PASS_TOKENS);
-  const int64_t per = std::min<int64_t>(stretches, std::max<int64_t>(1, rows * stretches / few));
+  const int64_t each = draw && rows ? RESIDENT_DRAWS / rows : 0;
+  const int64_t per = each ? (stretches + each - 1) / each
+                           : std::min<int64_t>(stretches, std::max<int64_t>(1, rows * stretches / (draw ? 4096 : 8192)));
   return LogitGrid{g, (int)(per * g * PASS_TOKENS), (int)((stretches + per - 1) / per)};
 }
-constexpr int64_t FEW_ADJUST = 8192, FEW_DRAW = 4096;
 static pg_status logit_args(const pg_logits* d, const char* who, LogitArgs& a) {
   if (!d) return fail(PG_EINVAL, "%s: desc is NULL", who);
   if (d->rows < 0 || d->vocab < 1 || (d->dtype != PG_LOGITS_F32 && d->dtype != PG_LOGITS_BF16))
@@ -505,7 +519,7 @@ extern "C" pg_status pg_logits_adjust(const pg_logits* desc, float* out, int64_t
   if ((uintptr_t)out & 3 || out_stride < a.d.vocab) return fail(PG_ESHAPE, "pg_logits_adjust: out rows %lld floats apart", (long long)out_stride);
   if ((const void*)out == a.d.logits && (a.d.dtype != PG_LOGITS_F32 || out_stride != a.d.stride))
     return fail(PG_EINVAL, "pg_logits_adjust: in place needs fp32 logits of the same stride");
-  const LogitGrid g = logit_grid(a.d.rows, a.d.vocab, FEW_ADJUST);
+  const LogitGrid g = logit_grid(a.d.rows, a.d.vocab, false);
   a.range = g.range;
   const dim3 grid((unsigned)g.workgroups, (unsigned)a.d.rows), block(LOGIT_THREADS);
   hipStream_t s = (hipStream_t)stream;
@@ -516,7 +530,7 @@ extern "C" pg_status pg_logits_adjust(const pg_logits* desc, float* out, int64_t
 
 extern "C" int64_t pg_sample_scratch_floats(int32_t rows, int32_t vocab) {
   if (rows < 1 || vocab < 1) return 0;
-  return (int64_t)rows * logit_grid(rows, vocab, FEW_DRAW).workgroups * (int64_t)(sizeof(Draw) / sizeof(float));
+  return (int64_t)rows * logit_grid(rows, vocab, true).workgroups * (int64_t)(sizeof(Draw) / sizeof(float));
 }
 
 extern "C" pg_status pg_sample_tokens(const pg_logits* desc, const float* temperature, uint64_t seed, uint32_t step, const int32_t* ids,
@@ -526,7 +540,7 @@ extern "C" pg_status pg_sample_tokens(const pg_logits* desc, const float* temper
   if (a.d.rows == 0) return PG_OK;
   if (!token || !logp || !scratch) return fail(PG_EINVAL, "pg_sample_tokens: null pointer");
   hipStream_t s = (hipStream_t)stream;
-  const LogitGrid g = logit_grid(a.d.rows, a.d.vocab, FEW_DRAW);
+  const LogitGrid g = logit_grid(a.d.rows, a.d.vocab, true);
   a.range = g.range;
   const dim3 grid((unsigned)g.workgroups, (unsigned)a.d.rows), block(LOGIT_THREADS);
   PG_LOGIT_KERNEL(sample_range_kernel, g.groups, a, temperature, (uint32_t)seed, (uint32_t)(seed >> 32), step, ids, (Draw*)scratch, token, logp);
