@@ -568,6 +568,27 @@ def test_drawn_tokens_and_log_probs(lib, R, V, H, masks, bias, dtype):
         assert abs(lp - ref.log_softmax_at(y, got)) <= 16 * U24 * size
 
 
+@pytest.mark.parametrize("R", [60, 380, 800, 1400])
+def test_a_draw_does_not_depend_on_the_rows_beside_it(lib, R):
+    """Rows of one stretch a workgroup, of two, whole ones, and more rows than are resident: each draws what it draws in a call of seven."""
+    say(f"draws of {R} rows")
+    rng = np.random.default_rng(R)
+    V, H = 24001, 300
+    t, more, rows = logits_case(rng, 7, V, torch.float32, H, 2)
+    T = torch.tensor([1.0, 0.0, 0.7, 1.3, 1.0, 1.0, 0.9], device=DEV)
+    at = torch.arange(R, device=DEV) % 7
+    one, one_p, many, many_p = (torch.full((n,), -5, dtype=k, device=DEV) for n in (7, R) for k in (torch.int32, torch.float32))
+    scratch = torch.empty(max(lib.pg_sample_scratch_floats(n, V) for n in (7, R)), device=DEV)
+    ids = torch.arange(7, dtype=torch.int32, device=DEV) * 11
+    lib.pg_sample_tokens(lib.Logits(t, **more), T, 5, 9, ids, one, one_p, scratch)
+    wide = {n: x if n == "allow" else x[at].contiguous() for n, x in more.items()}
+    lib.pg_sample_tokens(lib.Logits(t[at].contiguous(), **wide), T[at], 5, 9, ids[at], many, many_p, scratch)
+    assert torch.equal(many, one[at])                    # a token's score is its own
+    # each log-prob is within some ten roundings of values up to `size`, as above; sums are taken in another order
+    size = max(np.abs(z[np.isfinite(z)]).max(initial=0.0) for z in adjusted_rows(rows)) / 0.7 + 30 + 0.5 * H
+    assert ((many_p == one_p[at]) | ((many_p - one_p[at]).abs() <= 32 * U24 * size)).all()
+
+
 def test_draws_follow_the_softmax_and_the_ids(lib):
     say("draws' frequencies")
     R, V = 20000, 17
