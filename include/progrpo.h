@@ -414,7 +414,8 @@ pg_status pg_cache_check(const pg_cache *cache, void *stream);
  * q, out: bf16 [n_q, heads_q, head_dim], a query every q_stride / out_stride elements (multiples of 8, 16-byte aligned);
  * heads_q a multiple of cache->heads, query head j reads key/value head j / (heads_q / heads).  logits scaled by `scale`
  * (0: 1/sqrt(head_dim)).  lse (nullable) fp32 [n_q, heads_q]: natural logarithm of the softmax's denominator.  A query of no
- * tokens gives zeros and -inf.  max_len >= every length: sizes the split (longer rows are right too, but slower).  All sums in fp32.
+ * tokens, or whose scores are all -inf, gives zeros and -inf; NaN in a query, or in a key or value of
+ * its tokens, gives NaN in what it enters.  max_len >= every length: sizes the split (longer rows are right too, but slower).  All sums in fp32.
  * workspace: pg_paged_attention_workspace() bytes, 16-byte aligned (may be NULL where that is 0). */
 size_t pg_paged_attention_workspace(const pg_cache *cache, int32_t n_q, int32_t heads_q, int32_t max_len);
 pg_status pg_paged_attention(const pg_cache *cache, int32_t layer, const uint16_t *q, int64_t q_stride,

@@ -2,7 +2,8 @@
 //
 // For a query head with query q and keys k_j, values v_j (j < len):  s_j = scale <q, k_j>,  p_j = exp(s_j - m),  m = max s,
 // l = sum p_j,  o = sum p_j v_j / l,  lse = m + ln l, taken in pieces: two pieces (m, l, o') with o' = sum p_j v_j join as
-// m = max(m1, m2), l = l1 e^(m1-m) + l2 e^(m2-m), o' alike.
+// m = max(m1, m2), l = l1 e^(m1-m) + l2 e^(m2-m), o' alike.  m begins at the lowest finite number and the maximum passes NaN over, so m is
+// never -inf or NaN: a score of -inf has the weight 0 whatever came before it, and a NaN is in l and o' and stays there through every join.
 //
 // Every byte of the cache is read once and used for the G query heads of its key/value head only (G = 1 .. 16 products a value), so
 // the kernel is bound by HBM as long as enough loads are in flight.  Both products run on the matrix pipe, S^T = K Q^T and
@@ -21,6 +22,7 @@
 // to 6.3; three rows of 65 to 131 thousand tokens in bf16 (0.65 GB): 126 us, of which the join takes 10; 48 rows of up to 1178 tokens with
 // heads of 64 (65 MB with the shared prompt counted once a row): 14 us; one row of 77 tokens: 4 us, and 8 with the call.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <type_traits>
 #include "paged_cache.hpp"
@@ -95,6 +97,9 @@ __device__ __forceinline__ int channel_of(int j, int c) {
 }
 
 struct Piece { float m, l; };
+// what the sum of a softmax gives: nothing to divide by where no score has a weight, NaN where one was NaN
+__device__ __forceinline__ float over(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f; }
 
 template <int HD, bool F8, bool EVEN>
 __global__ __launch_bounds__(PA_THREADS, 2) void paged_attention_kernel(PagedArgs a) {
@@ -203,7 +208,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void paged_attention_kernel(PagedArg
   f32x4v o[DT];
 #pragma unroll
   for (int d = 0; d < DT; ++d) o[d] = f32x4v{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.0f;
+  float m = -FLT_MAX, l = 0.0f;
   const uint8_t* k_head = a.k + (int64_t)h * head_bytes;
   const uint8_t* v_head = a.v + (int64_t)h * head_bytes;
   // lane (r = n, c): key row r of tile t is key 8 U (r / 4) + 4 t + r % 4 of the step; it multiplies keys 8 U c ... 8 U c + 8 U - 1
@@ -364,18 +369,16 @@ __global__ __launch_bounds__(PA_THREADS, 2) void paged_attention_kernel(PagedArg
 #pragma unroll
     for (int w = 0; w < PA_WAVES; ++w) {
       const Piece p = lds_ml[w][head];
-      if (p.m > -INFINITY) {
-        const float f = __builtin_amdgcn_exp2f(p.m - top);
-        sum += p.l * f;
-        acc += *(const f32x4v*)&lds_o[w][head][ch] * f;
-      }
+      const float f = __builtin_amdgcn_exp2f(p.m - top);
+      sum += p.l * f;
+      acc += *(const f32x4v*)&lds_o[w][head][ch] * f;
     }
     acc *= v_scale;
     const int64_t item = (int64_t)query * a.heads_q + head0 + head;
     if (!EVEN || last_unit - first_unit == whole_units) {
-      acc *= sum > 0.0f ? 1.0f / sum : 0.0f;
+      acc *= over(sum);
       *(uint2*)(a.out + query * a.out_stride + (int64_t)(head0 + head) * HD + ch) = pack_bf16x4(float4{acc[0], acc[1], acc[2], acc[3]});
-      if (a.lse && ch == 0) a.lse[item] = sum > 0.0f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+      if (a.lse && ch == 0) a.lse[item] = lse_of(top, sum);
     } else {
       float* part = a.parts + (((int64_t)range * 2 + !opening) * PA_HEADS + head) * (HD + 4);
       *(f32x4v*)(part + 4 + ch) = acc;
@@ -406,7 +409,7 @@ __global__ __launch_bounds__(PA_THREADS) void paged_join_kernel(PagedArgs a) {
   Piece x = {-INFINITY, 0.0f};
   f32x4v acc = {0.f, 0.f, 0.f, 0.f};
   auto add = [&](Piece y, f32x4v o) {
-    if (!(y.m > -INFINITY)) return;
+    if (y.m == -INFINITY) return;                    // no piece
     const float m = fmaxf(x.m, y.m), f = __builtin_amdgcn_exp2f(x.m - m), g = __builtin_amdgcn_exp2f(y.m - m);
     x = Piece{m, x.l * f + y.l * g};
     acc = acc * f + o * g;
@@ -433,9 +436,9 @@ __global__ __launch_bounds__(PA_THREADS) void paged_join_kernel(PagedArgs a) {
   if (part) return;
 #pragma unroll
   for (int i = 1; i < PARTS; ++i) add(lds_ml[i], *(const f32x4v*)&lds_o[i][ch]);
-  acc *= x.l > 0.0f ? 1.0f / x.l : 0.0f;
+  acc *= over(x.l);
   *(uint2*)(a.out + row.x * a.out_stride + (int64_t)head * HD + ch) = pack_bf16x4(float4{acc[0], acc[1], acc[2], acc[3]});
-  if (a.lse && ch == 0) a.lse[(int64_t)row.x * a.heads_q + head] = x.l > 0.0f ? (x.m + log2f(x.l)) * 0.6931471805599453f : -INFINITY;
+  if (a.lse && ch == 0) a.lse[(int64_t)row.x * a.heads_q + head] = lse_of(x.m, x.l);
 }
 
 // Ranges of an EVEN call, 0 for WHOLE.  `span` is the longest row in units of heads of 128 channels, each of which takes a workgroup
