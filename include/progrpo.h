@@ -459,7 +459,8 @@ pg_status pg_logits_adjust(const pg_logits *desc, float *out, int64_t out_stride
  * Philox-4x32-10 block with counter (v div 4, step, ids[r], 2) and key (seed low, seed high); ids NULL: r.  The draw of a
  * trajectory depends on its id alone, not on where pruning has packed it.  temperature[r] == 0: argmax z, logp at temperature 1; NULL: 1.
  * Equal scores: the lowest token.  A row with nothing left: token -1, logp -inf.  A row with an allowed z that is NaN or +inf, or with
- * a temperature that is negative, infinite or NaN: token -1, logp NaN.  scratch: pg_sample_scratch_floats(rows, vocab) floats. */
+ * a temperature that is negative, infinite or NaN: token -1, logp NaN.  scratch: pg_sample_scratch_floats(rows, vocab) floats, which
+ * are enough for every call of no more rows and tokens, too. */
 int64_t pg_sample_scratch_floats(int32_t rows, int32_t vocab);
 pg_status pg_sample_tokens(const pg_logits *desc, const float *temperature, uint64_t seed, uint32_t step,
                            const int32_t *ids, int32_t *token, float *logp, float *scratch, void *stream);

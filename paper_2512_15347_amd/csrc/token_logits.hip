@@ -528,9 +528,13 @@ extern "C" pg_status pg_logits_adjust(const pg_logits* desc, float* out, int64_t
   return PG_OK;
 }
 
+// No less than any call of at most so many rows and tokens writes, though a call of fewer rows may have more workgroups: up to
+// RESIDENT_DRAWS rows have no more workgroups than that in all; above, where a row has `per` of its stretches a workgroup, they are fewer than
+// 8192 with per = 1, and with per >= 2 at most 4096 * 3/2 + rows (per is rounded down, the workgroups of a row up).
 extern "C" int64_t pg_sample_scratch_floats(int32_t rows, int32_t vocab) {
   if (rows < 1 || vocab < 1) return 0;
-  return (int64_t)rows * logit_grid(rows, vocab, true).workgroups * (int64_t)(sizeof(Draw) / sizeof(float));
+  const int64_t stretches = ((int64_t)vocab + PASS_TOKENS - 1) / PASS_TOKENS;
+  return std::min(rows * stretches, rows <= RESIDENT_DRAWS ? RESIDENT_DRAWS : 8192 + (int64_t)rows) * (int64_t)(sizeof(Draw) / sizeof(float));
 }
 
 extern "C" pg_status pg_sample_tokens(const pg_logits* desc, const float* temperature, uint64_t seed, uint32_t step, const int32_t* ids,
