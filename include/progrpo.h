@@ -416,7 +416,8 @@ pg_status pg_cache_check(const pg_cache *cache, void *stream);
  * (0: 1/sqrt(head_dim)).  lse (nullable) fp32 [n_q, heads_q]: natural logarithm of the softmax's denominator.  A query of no
  * tokens, or whose scores are all -inf, gives zeros and -inf; NaN in a query, or in a key or value of
  * its tokens, gives NaN in what it enters.  max_len >= every length: sizes the split (longer rows are right too, but slower).  All sums in fp32.
- * workspace: pg_paged_attention_workspace() bytes, 16-byte aligned (may be NULL where that is 0). */
+ * workspace: pg_paged_attention_workspace() bytes, 16-byte aligned (may be NULL where that is 0), which are enough for every call of
+ * no more queries and no larger max_len, too.  At most 65535 queries, and 2^24 of queries x key/value heads x tiles of 16 query heads. */
 size_t pg_paged_attention_workspace(const pg_cache *cache, int32_t n_q, int32_t heads_q, int32_t max_len);
 pg_status pg_paged_attention(const pg_cache *cache, int32_t layer, const uint16_t *q, int64_t q_stride,
                              const int32_t *table, int32_t n_rows, const int32_t *row_of, const int32_t *lens,

@@ -449,15 +449,30 @@ __global__ __launch_bounds__(PA_THREADS) void paged_join_kernel(PagedArgs a) {
 // 8 x 32: 45, 12.2;  32 x 8: 13.7, 11.8;  128 x 8: 14.1, 19.2;  128 x 16: 25.1, 25.0;  256 x 16: 27.8, 33.3;  384 x 8: 25.5, 28.4;
 // 384 x 14: 40, 37;  576 x 16: 77, 55;  768 x 14: 67, 69;  768 x 32: 178, 161;  1024 x 128: 822, 748;  3072 x 8: 157, 166;  3072 x 32: 575, 566;
 // and rows that are all of one length: 1024 x 13: 144, 155.
+struct PagedSplit {
+  int64_t item, unit, units, span;                   // items of a query; tokens of a unit, units of the longest row; span in 128ths
+  PagedSplit(const pg_cache* c, int heads_q, int max_len) {
+    item = c->heads * ((heads_q / c->heads + PA_HEADS - 1) / PA_HEADS);
+    unit = c->dtype == PG_CACHE_E4M3 ? 256 : 128;
+    units = (max_len + unit - 1) / unit;
+    span = units * (c->dtype == PG_CACHE_E4M3 ? (c->head_dim + 64) * 2 / 3 : c->head_dim);
+  }
+  bool long_rows(int64_t n_q) const { return span > (n_q * item > 256 ? 12 : 16) * 128; }
+  bool few_rows(int64_t n_q) const { return span > 6 * 128 + n_q * item * span / 200; }
+  int ranges(int64_t n_q) const {
+    int64_t r = 8;                                   // no more than there are units: empty ones cost the join its time
+    while (r < PA_RANGES && r < n_q * item * units) r *= 2;
+    return (int)r;
+  }
+};
 static int ranges_of(const pg_cache* c, int64_t n_q, int heads_q, int max_len) {
-  const int64_t items = n_q * c->heads * ((heads_q / c->heads + PA_HEADS - 1) / PA_HEADS), unit = c->dtype == PG_CACHE_E4M3 ? 256 : 128;
-  const int64_t units = (max_len + unit - 1) / unit,
-                span = units * (c->dtype == PG_CACHE_E4M3 ? (c->head_dim + 64) * 2 / 3 : c->head_dim);    // in 128ths
-  if (n_q > PA_EVEN_QUERIES || (span <= (items > 256 ? 12 : 16) * 128 && span <= 6 * 128 + items * span / 200)) return 0;
-  if (n_q * ((int64_t)c->width * c->page / unit + 1) > 1 << 30) return 0;      // units are counted in 32 bits
-  int64_t ranges = 8;                                // no more than there are units: empty ones cost the join its time
-  while (ranges < PA_RANGES && ranges < items * units) ranges *= 2;
-  return (int)ranges;
+  const PagedSplit s(c, heads_q, max_len);
+  if (n_q > PA_EVEN_QUERIES || !(s.long_rows(n_q) || s.few_rows(n_q))) return 0;
+  if (n_q * ((int64_t)c->width * c->page / s.unit + 1) > 1 << 30) return 0;    // units are counted in 32 bits
+  return s.ranges(n_q);
+}
+static size_t paged_bytes(const pg_cache* c, int ranges) {
+  return ranges ? 16 + (size_t)ranges * (sizeof(int4) + 2 * PA_HEADS * (c->head_dim + 4) * sizeof(float)) : 0;
 }
 
 static pg_status paged_sizes(const pg_cache* c, int32_t n_q, int32_t heads_q, int32_t max_len, const char* who) {
@@ -476,8 +491,11 @@ using namespace pg;
 
 extern "C" size_t pg_paged_attention_workspace(const pg_cache* c, int32_t n_q, int32_t heads_q, int32_t max_len) {
   if (paged_sizes(c, n_q, heads_q, max_len, "pg_paged_attention_workspace") != PG_OK) return 0;
-  const int ranges = ranges_of(c, n_q, heads_q, max_len);
-  return ranges ? 16 + (size_t)ranges * (sizeof(int4) + 2 * PA_HEADS * (c->head_dim + 4) * sizeof(float)) : 0;
+  // What any call of no more and no longer queries needs.  Some of them is cut into ranges if the one of most queries is, which has
+  // the lower bound on long rows, or one query alone, which are the fewest; it has the most ranges with as many queries as ranges are for.
+  const PagedSplit s(c, heads_q, max_len);
+  const int64_t most = std::min(n_q, PA_EVEN_QUERIES);
+  return n_q && (s.long_rows(most) || s.few_rows(1)) ? paged_bytes(c, s.ranges(most)) : 0;
 }
 
 extern "C" pg_status pg_paged_attention(const pg_cache* c, int32_t layer, const uint16_t* q, int64_t q_stride, const int32_t* table,
@@ -491,15 +509,16 @@ extern "C" pg_status pg_paged_attention(const pg_cache* c, int32_t layer, const 
   if (n_q == 0) return PG_OK;
   if (!q || !table || !lens || !out) return fail(PG_EINVAL, "%s: null pointer", who);
   if (n_rows < 1 || (!row_of && n_rows < n_q)) return fail(PG_EINVAL, "%s: a table of %d rows for %d queries", who, n_rows, n_q);
+  PagedArgs a{};
   const int64_t row = (int64_t)heads_q * c->head_dim;
   if (q_stride < row || out_stride < row || q_stride % 8 || out_stride % 8 || (((uintptr_t)q | (uintptr_t)out) & 15))
     return fail(PG_ESHAPE, "%s: queries and outputs must be 16-byte aligned, their strides (%lld, %lld) multiples of 8", who,
                 (long long)q_stride, (long long)out_stride);
-  const size_t need = pg_paged_attention_workspace(c, n_q, heads_q, max_len);
+  a.ranges = ranges_of(c, n_q, heads_q, max_len);
+  const size_t need = paged_bytes(c, a.ranges);
   if (need && (!workspace || workspace_bytes < need))
     return fail(PG_EWORKSPACE, "%s: %zu bytes of workspace, %zu given", who, need, workspace ? workspace_bytes : 0);
   if ((uintptr_t)workspace & 15) return fail(PG_ESHAPE, "%s: the workspace must be 16-byte aligned", who);
-  PagedArgs a{};
   a.c = view_of(c);
   const size_t layer_bytes = page_bytes(c) * c->n_pages;
   a.k = (const uint8_t*)c->k + layer * layer_bytes;
@@ -510,7 +529,6 @@ extern "C" pg_status pg_paged_attention(const pg_cache* c, int32_t layer, const 
   a.table = table; a.row_of = row_of; a.lens = lens; a.n_rows = n_rows;
   a.heads_q = heads_q; a.group = heads_q / c->heads; a.q_tiles = (a.group + PA_HEADS - 1) / PA_HEADS;
   a.n_q = n_q;
-  a.ranges = ranges_of(c, n_q, heads_q, max_len);
   a.scale_log2 = (float)((scale == 0.0 ? 1.0 / std::sqrt((double)c->head_dim) : scale) * 1.4426950408889634);
   a.lse = lse;
   a.opened = (int4*)workspace; a.parts = (float*)(a.opened + a.ranges);

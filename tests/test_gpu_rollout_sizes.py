@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from test_gpu_rollout import DEV, dev, say
+from test_gpu_rollout import DEV, say
 
 pytestmark = pytest.mark.gpu
 
@@ -23,3 +23,28 @@ def test_draws_stay_inside_the_scratch_of_the_largest_call(lib, most, vocab):
         assert (guard[size:] == 12345.0).all(), rows
         first = token.clone() if first is None else first
         assert torch.equal(token[:rows], first[:rows])
+
+
+def test_attention_stays_inside_the_workspace_of_the_largest_call(lib):
+    """2049 queries are one workgroup each, fewer and longer ones are cut into ranges."""
+    say("workspace of 2049 queries of 4096 tokens")
+    g = torch.Generator(device=DEV).manual_seed(1)
+    pool = lambda *s: torch.randn(s, device=DEV, generator=g).to(torch.bfloat16)  # noqa: E731
+    cache = lib.Cache(pool(1, 256, 1, 16, 128), pool(1, 256, 1, 128, 16), torch.ones(256, dtype=torch.int32, device=DEV), 256)
+    table = torch.arange(256, dtype=torch.int32, device=DEV)[None]
+    most = 2049
+    q, lens = pool(most, 2, 128), torch.arange(most, dtype=torch.int32, device=DEV) * 2
+    out, row_of = torch.empty_like(q), torch.zeros(most, dtype=torch.int32, device=DEV)
+    size = lib.pg_paged_attention_workspace(cache, most, 2, 4096)
+    guard = torch.full((size // 4 + 4096,), 12345.0, device=DEV)
+    first = None
+    for rows in (most, 2048, 512, 9, 1):
+        at = torch.arange(most - rows, most, device=DEV)                  # the longest ones
+        lib.pg_paged_attention(cache, 0, q[at], table, lens[at], out[:rows], 4096, guard[:size // 4], row_of=row_of[:rows])
+        assert (guard[size // 4:] == 12345.0).all(), rows
+        first = out.clone() if first is None else first
+        # the same sums cut in other places, both within (2^-15 + 2 far) max |v|, far = 4 hd 2^-24 sum |q k| / sqrt(hd) of scores in fp32 (sums up
+        # to 12, values up to 6 here), and then within a bf16 of each other
+        tol = 2 * (2.0 ** -15 + 2 * 4 * 128 * 2.0 ** -24 * 12) * 6
+        assert ((out[:rows].float() - first[at].float()).abs() <= 2.0 ** -7 * first[at].float().abs() + tol).all(), rows
+    lib.pg_cache_check(cache)
