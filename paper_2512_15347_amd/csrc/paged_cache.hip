@@ -240,12 +240,13 @@ typedef uint32_t u32x2v __attribute__((ext_vector_type(2)));
 struct PageCopy {
   uint8_t *k, *v;
   int64_t layer_bytes;                               // of one pool
-  int32_t page_bytes, layers;
+  uint32_t page_bytes;                               // up to 2^31
+  int32_t layers;
 };
 constexpr int COPY_PIECE = 16384;
 template <bool SHARED, class Pages>
 __device__ __forceinline__ void copy_pages(const PageCopy& a, int copies, int block, int blocks, Pages pages) {
-  const int pieces = (a.page_bytes + COPY_PIECE - 1) / COPY_PIECE;
+  const int pieces = (int)((a.page_bytes + COPY_PIECE - 1) / COPY_PIECE);
   const int64_t items = (int64_t)copies * a.layers * 2 * pieces;
   for (int64_t i = block; i < items; i += blocks) {
     const int piece = (int)(i % pieces);
@@ -254,7 +255,8 @@ __device__ __forceinline__ void copy_pages(const PageCopy& a, int copies, int bl
     int from, to;
     pages((int)((j >> 1) / a.layers), from, to);
     uint8_t* base = (pool ? a.v : a.k) + layer * a.layer_bytes;
-    const int lo = piece * COPY_PIECE, n = min(COPY_PIECE, a.page_bytes - lo);
+    const uint32_t lo = (uint32_t)piece * COPY_PIECE;
+    const int n = (int)min((uint32_t)COPY_PIECE, a.page_bytes - lo);
     const u32x4v* in = (const u32x4v*)(base + (int64_t)from * a.page_bytes + lo);
     u32x4v* out = (u32x4v*)(base + (int64_t)to * a.page_bytes + lo);
     constexpr int PER = COPY_PIECE / 16 / APPLY_THREADS;
@@ -554,7 +556,7 @@ static pg_status allow_lds(const void* kernel, size_t bytes) {
 
 static PageCopy copy_of(const pg_cache* c) {
   const int64_t bytes = (int64_t)page_bytes(c);
-  return PageCopy{(uint8_t*)c->k, (uint8_t*)c->v, bytes * c->n_pages, (int32_t)bytes, c->layers};
+  return PageCopy{(uint8_t*)c->k, (uint8_t*)c->v, bytes * c->n_pages, (uint32_t)bytes, c->layers};
 }
 // workgroups for the copies of at most `copies` pages
 static int copy_blocks(const pg_cache* c, int64_t copies) {

@@ -48,3 +48,31 @@ def test_attention_stays_inside_the_workspace_of_the_largest_call(lib):
         tol = 2 * (2.0 ** -15 + 2 * 4 * 128 * 2.0 ** -24 * 12) * 6
         assert ((out[:rows].float() - first[at].float()).abs() <= 2.0 ** -7 * first[at].float().abs() + tol).all(), rows
     lib.pg_cache_check(cache)
+
+
+@pytest.mark.parametrize("heads,page,head_dim", [(65536, 128, 128), (2097151, 16, 32)])
+def test_the_largest_pages_are_copied_and_moved(lib, heads, page, head_dim):
+    """2^31 bytes, and the most that is less: a fork's copy, and a move."""
+    say(f"pages of {heads * page * head_dim * 2} bytes")
+    z = lambda *s: torch.zeros(s, dtype=torch.bfloat16, device=DEV)  # noqa: E731
+    cache = lib.Cache(z(1, 3, heads, page, head_dim), z(1, 3, heads, head_dim, page), torch.zeros(3, dtype=torch.int32, device=DEV), 1)
+    lib.pg_cache_clear(cache)
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device=DEV)  # noqa: E731
+    table, lens = torch.full((1, 1), -1, dtype=torch.int32, device=DEV), ints(0)
+    lib.pg_cache_reserve(cache, table, lens, ints(5), lens)
+    gen = torch.Generator(device=DEV).manual_seed(heads)
+    for pool in (cache.k, cache.v):
+        pool[0, 0].view(torch.int16).random_(-2 ** 15, 2 ** 15, generator=gen)
+    scratch = torch.empty(lib.pg_cache_scratch_ints(cache, 2), dtype=torch.int32, device=DEV)
+    two, lens_two, last, lens_last = (torch.empty(s, dtype=torch.int32, device=DEV) for s in ((2, 1), (2,), (1, 1), (1,)))
+    lib.pg_cache_select(cache, table, lens, ints(0, 0), two, lens_two, scratch)
+    lib.pg_cache_check(cache)
+    same = lambda p, a, b: all(torch.equal(p[0, a, i::8].view(torch.int16), p[0, b, i::8].view(torch.int16)) for i in range(8))  # noqa: E731
+    assert two.tolist() == [[0], [1]] and same(cache.k, 0, 1) and same(cache.v, 0, 1)
+    lib.pg_cache_select(cache, two, lens_two, ints(1), last, lens_last, scratch)
+    for pool in (cache.k, cache.v):
+        pool[0, 0].zero_()
+    lib.pg_cache_compact(cache, last, lens_last, scratch)
+    lib.pg_cache_check(cache)
+    assert last.tolist() == [[0]] and cache.refs.tolist() == [1, 0, 0] and same(cache.k, 0, 1) and same(cache.v, 0, 1)
+    assert (cache.k[0, 0, -1].view(torch.int16) != 0).any() and (cache.k[0, 2, ::64] == 0).all()
