@@ -449,7 +449,7 @@ typedef struct pg_logits {
   int32_t n_bias;                 /* entries of bias_ids and bias_values */
   int32_t n_masks;                /* rows of allow */
   const uint32_t *allow;          /* [n_masks, ceil(vocab / 32)]: bit v % 32 of word v / 32 set = v is allowed */
-  const int32_t *allow_row;       /* [rows] mask of each row, -1: everything is allowed; NULL: mask r */
+  const int32_t *allow_row;       /* [rows] mask of each row, -1: everything is allowed, any other index that no mask has: nothing; NULL: mask r */
 } pg_logits;
 
 /* out[r, v] = z, fp32, a row every out_stride elements; out may be the logits themselves (fp32, equal strides). */

@@ -37,7 +37,8 @@ struct LogitArgs {
 // What one row needs.
 struct RowRules {
   float rep, freq, pres;
-  const uint8_t* allow;                              // NULL: everything; bit v % 8 of byte v / 8
+  const uint8_t* allow;                              // bit v % 8 of byte v / 8; NULL: `unmasked` for all of them
+  uint32_t unmasked;
   int bias_lo, bias_hi, made, prompt;
 };
 
@@ -56,6 +57,7 @@ __device__ __forceinline__ RowRules row_rules(const LogitArgs& a, int r) {
   q.pres = pres;
   const int mask = d.allow_row ? m : r;
   q.allow = d.allow && mask >= 0 && mask < d.n_masks ? (const uint8_t*)(d.allow + (int64_t)mask * a.words) : nullptr;
+  q.unmasked = d.allow && mask != -1 ? 0u : 0xFFu;   // an index that no mask has allows nothing
   q.bias_lo = max(0, lo);
   q.bias_hi = d.bias_offsets ? min(d.n_bias, hi) : 0;
   q.made = d.tokens ? min(max(made, 0), d.tokens_stride) : 0;
@@ -85,7 +87,7 @@ struct Group {
         else raw[e >> 1] = e & 1 ? raw[e >> 1] | x << 16 : x;
       }
     }
-    allowed = (q.allow ? q.allow[v >> 3] : 0xFFu) & (left >= LANE_TOKENS ? 0xFFu : (1u << left) - 1);
+    allowed = (q.allow ? q.allow[v >> 3] : q.unmasked) & (left >= LANE_TOKENS ? 0xFFu : (1u << left) - 1);
   }
   __device__ __forceinline__ float logit(int e) const {
     return __builtin_bit_cast(float, !BF16 ? raw[e] : e & 1 ? raw[e >> 1] & 0xFFFF0000u : raw[e >> 1] << 16);
