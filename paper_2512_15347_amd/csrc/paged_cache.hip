@@ -447,10 +447,11 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a) {
     part = unit - ((t0 >> 4) + 2 * row);
   }
   const int len = a.lens[row];
-  if (part < 0 || t0 < 0 || fresh < 0 || t0 + (int64_t)fresh > a.n_tokens || fresh > len || !length_fits(len, c)) {
+  if ((part < 0 && row) || t0 < 0 || fresh < 0 || t0 + (int64_t)fresh > a.n_tokens || fresh > len || !length_fits(len, c)) {
     if (lane == 0 && head == 0) atomicOr(c.status, CACHE_RANGE);
     return;
   }
+  if (part < 0) return;                              // a number of the tokens before the first row's
   const int begin = len - fresh;
   const int64_t at = (begin & ~15) + (int64_t)part * 16;       // position of the block
   if (at >= len || fresh == 0) return;
