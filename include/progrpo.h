@@ -359,8 +359,8 @@ enum { PG_CACHE_BF16 = 0, PG_CACHE_E4M3 = 1 };
  * past the last page of a row are not read (calls that write tables write -1 there).
  * refs[p]: rows that hold page p, 0 if it is free (any order of calls on one stream keeps it so).  A page that is
  * part filled belongs to one row.  Taking pages is deterministic: the free page of the lowest number first, in row order.
- * status[0] (sticky; pg_cache_check reports it): |= 4 a row got no page (pool or table width exhausted), |= 8 an
- * index, length or count out of range.  Kernels keep every access in bounds in both cases.
+ * status[0] (sticky; pg_cache_check reports it): |= 4 a row got no page (pool or table width exhausted, or tokens for a page that
+ * several rows hold), |= 8 an index, length or count out of range.  Kernels keep every access in bounds in both cases.
  */
 typedef struct pg_cache {
   int32_t layers, n_pages, heads, page, head_dim, dtype, width;
@@ -384,7 +384,10 @@ pg_status pg_cache_reserve(const pg_cache *cache, int32_t *table, const int32_t 
 /* Writes the keys and values of the LAST tokens of each row (lens counts them already): tokens cu[r] .. cu[r+1]-1 of
  * k_new / v_new are the last cu[r+1] - cu[r] of row r (cu: n_rows + 1 ascending offsets, cu[n_rows] == n_tokens; NULL: one token
  * a row).  k_new, v_new: bf16 [n_tokens, heads, head_dim], a token every token_stride elements (multiple of 8, so that slices
- * of a fused projection are taken as they are), 16-byte aligned.  e4m3 codes: round-to-nearest-even of x / scale, limited to +-448. */
+ * of a fused projection are taken as they are), 16-byte aligned.  e4m3 codes: round-to-nearest-even of x / scale, limited to +-448.
+ * A page that several rows hold is whole and stays as it is: tokens for it are left out (status 4).  A row that pg_cache_reserve
+ * refused has its old length and so no place for new tokens; in a page of its own they would replace its last ones.  Offsets cu of
+ * what the lengths grew by leave such rows out. */
 pg_status pg_cache_append(const pg_cache *cache, int32_t layer, const uint16_t *k_new, const uint16_t *v_new,
                           int64_t token_stride, const int32_t *table, const int32_t *lens, const int32_t *cu,
                           int32_t n_rows, int32_t n_tokens, void *stream);

@@ -422,7 +422,7 @@ struct AppendArgs {
   const float *k_scale, *v_scale;                    // of the layer, or NULL
   const uint16_t *k_new, *v_new;
   int64_t token_stride;
-  const int32_t *table, *lens, *cu;
+  const int32_t *table, *lens, *cu, *refs;
   int n_rows, n_tokens, units;
 };
 
@@ -460,6 +460,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a) {
     if (lane == 0 && head == 0) atomicOr(c.status, CACHE_RANGE);
     return;
   }
+  const int users = a.refs[page];
   const int slot = (int)at & ((1 << c.page_shift) - 1);
   const int64_t to = (((int64_t)page * c.heads + head) << c.page_shift) * HD;
   const Quotient ks(F8 && a.k_scale ? a.k_scale[head] : 1.0f), vs(F8 && a.v_scale ? a.v_scale[head] : 1.0f);
@@ -479,6 +480,10 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a) {
       kx[p][it] = *(const u32x4v*)(a.k_new + from + it * COLS * 8);
       vx[p][it] = *(const u32x4v*)(a.v_new + from + it * COLS * 8);
     }
+  }
+  if (users > 1) {                                   // whole, and others read it: the row has no place for these tokens
+    if (lane == 0 && head == 0) atomicOr(c.status, CACHE_FULL);
+    return;
   }
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
@@ -612,7 +617,7 @@ extern "C" pg_status pg_cache_append(const pg_cache* c, int32_t layer, const uin
   a.k_scale = c->k_scale ? c->k_scale + (int64_t)layer * c->heads : nullptr;
   a.v_scale = c->v_scale ? c->v_scale + (int64_t)layer * c->heads : nullptr;
   a.k_new = k_new; a.v_new = v_new; a.token_stride = token_stride;
-  a.table = table; a.lens = lens; a.cu = cu; a.n_rows = n_rows; a.n_tokens = n_tokens; a.units = (int)units;
+  a.table = table; a.lens = lens; a.cu = cu; a.refs = c->refs; a.n_rows = n_rows; a.n_tokens = n_tokens; a.units = (int)units;
   const dim3 grid((unsigned)blocks), block(256);
   hipStream_t s = (hipStream_t)stream;
   const bool f8 = c->dtype == PG_CACHE_E4M3;
