@@ -78,7 +78,7 @@ def sample_groups(decoder, prompts, members, steps, schedule, seed, token_reward
 
     token_reward: fp32 [vocab]; a sequence's proxy reward is the mean over its drawn tokens.  penalties: (repetition, frequency, presence).
     allow: int32 [1, words] mask of tokens that may be drawn.  Returns survivors' ids, tokens, rewards and advantages, and logp [steps,
-    groups * members] by original id (NaN where pruned)."""
+    groups * members] by original id (NaN where pruned).  Raises PgError if pages ran out or a member had nothing to draw from."""
     dev, c, P = token_reward.device, decoder.cfg, len(prompts)
     if min(len(p) for p in prompts) < 1 or max(len(p) for p in prompts) + steps > c["max_len"] + 1:
         raise ValueError("prompts of at least one token that leave room for the steps are needed")
@@ -115,6 +115,7 @@ def sample_groups(decoder, prompts, members, steps, schedule, seed, token_reward
     offsets = ints(np.arange(P + 1) * members)
     logp, score = torch.full((steps, M), math.nan, device=dev), torch.zeros(M, device=dev)
     keep = dict(schedule)
+    undrawn = torch.zeros((), dtype=torch.bool, device=dev)             # some member had nothing to draw from
     for step in range(steps):
         n = ids.shape[0]
         more = {}
@@ -128,7 +129,8 @@ def sample_groups(decoder, prompts, members, steps, schedule, seed, token_reward
         token, lp = torch.empty(n, dtype=torch.int32, device=dev), torch.empty(n, device=dev)
         draw = torch.empty(desc.scratch, device=dev)
         pg.pg_sample_tokens(desc, torch.full((n,), float(temperature), device=dev), seed, step, ids, token, lp, draw)
-        drawn = token.clamp_min(0).long()                # a row with nothing to draw from: its log-prob says so
+        undrawn |= (token < 0).any()
+        drawn = token.clamp_min(0).long()
         logp[step, ids.long()] = lp
         score += (token_reward[drawn] - score) / (step + 1)
         history.scatter_(1, (n_prompt + step).long()[:, None], drawn.int()[:, None])
@@ -148,6 +150,8 @@ def sample_groups(decoder, prompts, members, steps, schedule, seed, token_reward
     adv = torch.empty_like(score)
     pg.pg_group_advantages(score, offsets, P, adv_eps, adv)
     pg.pg_cache_check(cache)
+    if undrawn:
+        raise pg.PgError(pg.PG_EINVAL, "a member had no token to draw: a mask that allows none, or logits that are no numbers")
     return dict(ids=ids, tokens=history, lens=n_prompt + steps, rewards=score, advantages=adv, logp=logp, offsets=offsets)
 
 
