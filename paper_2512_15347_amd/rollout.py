@@ -78,7 +78,8 @@ def sample_groups(decoder, prompts, members, steps, schedule, seed, token_reward
 
     token_reward: fp32 [vocab]; a sequence's proxy reward is the mean over its drawn tokens.  penalties: (repetition, frequency, presence).
     allow: int32 [1, words] mask of tokens that may be drawn.  Returns survivors' ids, tokens, rewards and advantages, and logp [steps,
-    groups * members] by original id (NaN where pruned).  Raises PgError if pages ran out or a member had nothing to draw from."""
+    groups * members] by original id (NaN where pruned).  Raises PgError if pages ran out, a member had nothing to draw from or
+    a reward at a checkpoint was no number."""
     dev, c, P = token_reward.device, decoder.cfg, len(prompts)
     if min(len(p) for p in prompts) < 1 or max(len(p) for p in prompts) + steps > c["max_len"] + 1:
         raise ValueError("prompts of at least one token that leave room for the steps are needed")
@@ -116,6 +117,7 @@ def sample_groups(decoder, prompts, members, steps, schedule, seed, token_reward
     logp, score = torch.full((steps, M), math.nan, device=dev), torch.zeros(M, device=dev)
     keep = dict(schedule)
     undrawn = torch.zeros((), dtype=torch.bool, device=dev)             # some member had nothing to draw from
+    status = torch.zeros(4, dtype=torch.int32, device=dev)              # of all selections
     for step in range(steps):
         n = ids.shape[0]
         more = {}
@@ -137,7 +139,7 @@ def sample_groups(decoder, prompts, members, steps, schedule, seed, token_reward
         if step in keep:                                 # checkpoint: the members whose rewards vary most go on
             k = keep[step]
             sel = torch.empty(P * k, dtype=torch.int32, device=dev)
-            status, new_offsets = torch.zeros(4, dtype=torch.int32, device=dev), torch.empty(P + 1, dtype=torch.int32, device=dev)
+            new_offsets = torch.empty(P + 1, dtype=torch.int32, device=dev)
             pg.pg_ovf_select(score, offsets, ints([k] * P), P, torch.empty(P, dtype=torch.int64, device=dev), sel, new_offsets, status,
                              torch.empty(pg.pg_ovf_scratch_ints(P), dtype=torch.int32, device=dev))
             table, lens = take(sel, table, lens)
@@ -152,6 +154,8 @@ def sample_groups(decoder, prompts, members, steps, schedule, seed, token_reward
     pg.pg_cache_check(cache)
     if undrawn:
         raise pg.PgError(pg.PG_EINVAL, "a member had no token to draw: a mask that allows none, or logits that are no numbers")
+    if int(status[0]):
+        raise pg.PgError(pg.PG_ENAN, "a non-finite proxy reward reached the selection")
     return dict(ids=ids, tokens=history, lens=n_prompt + steps, rewards=score, advantages=adv, logp=logp, offsets=offsets)
 
 

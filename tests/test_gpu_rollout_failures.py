@@ -1,4 +1,4 @@
-"""The token policy's funnel where a member cannot draw: the run says so."""
+"""The token policy's funnel where a member cannot draw, or a reward is no number: the run says so."""
 import math
 
 import pytest
@@ -34,3 +34,13 @@ def test_logits_of_nan_are_an_error(lib, weights):
     with pytest.raises(lib.PgError) as e:
         rollout.sample_groups(decoder, [[5, 6]], 4, 3, [], 1, torch.ones(CFG["vocab"], device=DEV))
     assert e.value.status == lib.PG_EINVAL
+
+
+def test_a_reward_of_nan_at_a_checkpoint_is_an_error(lib, weights):
+    from paper_2512_15347_amd import rollout
+    print("rewards of NaN", flush=True)
+    for schedule in ([(0, 3), (2, 2)], [(2, 2)]):           # the first of two checkpoints, or the only one
+        decoder = rollout.Decoder(CFG, weights, rows=8)
+        with pytest.raises(lib.PgError) as e:
+            rollout.sample_groups(decoder, [[5, 6], [9]], 4, 4, schedule, 1, torch.full((CFG["vocab"],), math.nan, device=DEV))
+        assert e.value.status == lib.PG_ENAN
