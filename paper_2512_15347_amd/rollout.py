@@ -74,7 +74,8 @@ class Decoder:
 
 
 def sample_groups(decoder, prompts, members, steps, schedule, seed, token_reward, temperature=1.0, penalties=None, allow=None, adv_eps=1e-6):
-    """prompts: list of token lists; schedule: [(step, k)], after which step k members of every group are kept (falling counts).
+    """prompts: list of token lists; schedule: [(step, k)], after which step k members of every group are kept (counts that fall with the
+    steps, in any order).
 
     token_reward: fp32 [vocab]; a sequence's proxy reward is the mean over its drawn tokens.  penalties: (repetition, frequency, presence).
     allow: int32 [1, words] mask of tokens that may be drawn.  Returns survivors' ids, tokens, rewards and advantages, and logp [steps,
@@ -83,8 +84,9 @@ def sample_groups(decoder, prompts, members, steps, schedule, seed, token_reward
     dev, c, P = token_reward.device, decoder.cfg, len(prompts)
     if min(len(p) for p in prompts) < 1 or max(len(p) for p in prompts) + steps > c["max_len"] + 1:
         raise ValueError("prompts of at least one token that leave room for the steps are needed")
-    if any(not 0 < k <= n for (_, k), n in zip(schedule, [members] + [k for _, k in schedule])) or members > 64:
-        raise ValueError("schedule: counts fall from the group's members, at most 64")
+    keep, counts = dict(schedule), [members] + [k for _, k in sorted(schedule)]
+    if len(keep) < len(schedule) or any(not 0 < k <= n for n, k in zip(counts, counts[1:])) or members > 64:
+        raise ValueError("schedule: at most one count a step, falling from the group's members, at most 64")
     ints = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).to(dev)  # noqa: E731
     cache, width, M = decoder.cache, decoder.width, P * members
     pg.pg_cache_clear(cache)
@@ -115,7 +117,6 @@ def sample_groups(decoder, prompts, members, steps, schedule, seed, token_reward
     logits, history, n_prompt = logits[rows].contiguous(), history[rows].contiguous(), n_prompt[rows].contiguous()
     offsets = ints(np.arange(P + 1) * members)
     logp, score = torch.full((steps, M), math.nan, device=dev), torch.zeros(M, device=dev)
-    keep = dict(schedule)
     undrawn = torch.zeros((), dtype=torch.bool, device=dev)             # some member had nothing to draw from
     status = torch.zeros(4, dtype=torch.int32, device=dev)              # of all selections
     for step in range(steps):
