@@ -84,6 +84,8 @@ def sample_groups(decoder, prompts, members, steps, schedule, seed, token_reward
     dev, c, P = token_reward.device, decoder.cfg, len(prompts)
     if min(len(p) for p in prompts) < 1 or max(len(p) for p in prompts) + steps > c["max_len"] + 1:
         raise ValueError("prompts of at least one token that leave room for the steps are needed")
+    if token_reward.shape != (c["vocab"],) or not all(0 <= t < c["vocab"] for p in prompts for t in p):
+        raise ValueError("tokens of the prompts outside the vocabulary, or rewards for another one")
     keep, counts = dict(schedule), [members] + [k for _, k in sorted(schedule)]
     if len(keep) < len(schedule) or any(not 0 < k <= n for n, k in zip(counts, counts[1:])) or members > 64:
         raise ValueError("schedule: at most one count a step, falling from the group's members, at most 64")

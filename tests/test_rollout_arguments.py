@@ -24,3 +24,12 @@ def test_schedules_that_are_no_funnel(schedule):
 def test_schedules_in_any_order(schedule):
     with pytest.raises(AttributeError):                                # accepted: the next thing asked for is the decoder's cache
         call([[1, 2]], 12, 20, schedule)
+
+
+def test_tokens_and_rewards_that_do_not_fit_the_vocabulary():
+    for prompts in ([[1, 2], [3, 50]], [[-1]]):
+        with pytest.raises(ValueError):
+            call(prompts, 4, 3, [])
+    for reward in (torch.ones(49), torch.ones(51), torch.ones(50, 1)):
+        with pytest.raises(ValueError):
+            rollout.sample_groups(DECODER, [[1]], 4, 3, [], 1, reward)
