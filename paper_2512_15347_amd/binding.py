@@ -489,6 +489,9 @@ class _Types:
     def __getattr__(self, name):
         import torch
         self.int32, self.float32, self.bfloat16 = torch.int32, torch.float32, torch.bfloat16
+        # what is read as bf16 and as codes, the bits alone among them
+        self.pairs = frozenset((torch.bfloat16, torch.int16, torch.uint16))
+        self.codes = frozenset((torch.float8_e4m3fn, torch.int8, torch.uint8))
         return self.__dict__[name]
 
 
@@ -520,21 +523,22 @@ def _rows(t, heads, head_dim):
     """Address and row stride (in elements) of [rows, heads, head_dim] in bf16 whose rows may be slices of longer ones."""
     rows, n, d = t.shape
     s0, s1, s2 = t.stride()
-    assert n == heads and d == head_dim and t.element_size() == 2 and s2 == 1 and (s1 == d or n == 1), \
-        f"[rows, {heads}, {head_dim}] in 16 bits with contiguous heads wanted: {t.dtype} {tuple(t.shape)}, strides {t.stride()}"
+    assert n == heads and d == head_dim and (t.dtype is _types.bfloat16 or t.dtype in _types.pairs) and s2 == 1 and (s1 == d or n == 1), \
+        f"[rows, {heads}, {head_dim}] in bf16 with contiguous heads wanted: {t.dtype} {tuple(t.shape)}, strides {t.stride()}"
     return t.data_ptr(), s0 if rows > 1 else max(s0, n * d)
 
 
 class Cache:
     """Device tensors of a paged cache (the caller's) + the filled pg_cache.
 
-    k: [layers, pages, heads, page, head_dim], v: [layers, pages, heads, head_dim, page], both bf16 (or 16-bit patterns) or uint8
-    codes; refs: int32 [pages]; width: entries of a table's row."""
+    k: [layers, pages, heads, page, head_dim], v: [layers, pages, heads, head_dim, page], both bf16 (or 16-bit integers: its bits) or
+    e4m3 codes (or 8-bit integers); refs: int32 [pages]; width: entries of a table's row."""
 
     def __init__(self, k, v, refs, width, k_scale=None, v_scale=None, status=None):
         import torch
         layers, n_pages, heads, page, head_dim = k.shape
-        assert tuple(v.shape) == (layers, n_pages, heads, head_dim, page) and k.element_size() == v.element_size() <= 2
+        assert tuple(v.shape) == (layers, n_pages, heads, head_dim, page)
+        assert any(k.dtype in kind and v.dtype in kind for kind in (_types.pairs, _types.codes)), f"pools of {k.dtype} and {v.dtype}"
         self.k, self.v, self.refs, self.k_scale, self.v_scale = k, v, refs, k_scale, v_scale
         self.status = torch.zeros(4, dtype=torch.int32, device=k.device) if status is None else status
         c = pg_cache()
@@ -651,7 +655,7 @@ def pg_sample_scratch_floats(rows, vocab):
 
 def pg_sample_tokens(desc, temperature, seed, step, ids, token, logp, scratch, stream=None):
     n = desc.rows
-    assert scratch.numel() >= desc.scratch
+    assert scratch.numel() * scratch.element_size() >= 4 * desc.scratch
     _check(_lib.pg_sample_tokens(desc.ref, _f32s(temperature, n), seed, step, _i32s(ids, n), _i32s(token, n), _f32s(logp, n), _ptr(scratch),
                                  _stream(stream)))
 
