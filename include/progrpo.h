@@ -455,7 +455,8 @@ typedef struct pg_logits {
   const int32_t *allow_row;       /* [rows] mask of each row, -1: everything is allowed, any other index that no mask has: nothing; NULL: mask r */
 } pg_logits;
 
-/* out[r, v] = z, fp32, a row every out_stride elements; out may be the logits themselves (fp32, equal strides). */
+/* out[r, v] = z, fp32, a row every out_stride elements; out may be the logits themselves (fp32, equal strides), and
+ * overlaps them in no other way. */
 pg_status pg_logits_adjust(const pg_logits *desc, float *out, int64_t out_stride, void *stream);
 
 /* Draws token[r] from softmax(y), y = z * (1 / temperature[r]), and logp[r] = y[token] - ln sum exp(y), in one pass over the logits:

@@ -500,6 +500,18 @@ static pg_status logit_args(const pg_logits* d, const char* who, LogitArgs& a) {
   return PG_OK;
 }
 
+// Whether one of `rows` intervals of `b` bytes from q on, each `q_step` after the one before, meets one of `a` bytes from p on (a <= p_step).
+static bool rows_overlap(uintptr_t p, int64_t p_step, int64_t a, uintptr_t q, int64_t q_step, int64_t b, int64_t rows) {
+  if (p + (rows - 1) * p_step + a <= q || q + (rows - 1) * q_step + b <= p) return false;
+  for (int64_t r = 0; r < rows; ++r) {
+    const int64_t lo = (int64_t)(q - p) + r * q_step;
+    const int64_t i = lo >= 0 ? lo / p_step : -1;    // the last that begins at or before it
+    if (i >= 0 && i < rows && lo < i * p_step + a) return true;
+    if (i + 1 < rows && (i + 1) * p_step < lo + b) return true;
+  }
+  return false;
+}
+
 // launches F<bf16, groups>
 #define PG_LOGIT_KERNEL(F, groups, ...)                                                                                          \
   do {                                                                                                                           \
@@ -521,6 +533,10 @@ extern "C" pg_status pg_logits_adjust(const pg_logits* desc, float* out, int64_t
   if ((uintptr_t)out & 3 || out_stride < a.d.vocab) return fail(PG_ESHAPE, "pg_logits_adjust: out rows %lld floats apart", (long long)out_stride);
   if ((const void*)out == a.d.logits && (a.d.dtype != PG_LOGITS_F32 || out_stride != a.d.stride))
     return fail(PG_EINVAL, "pg_logits_adjust: in place needs fp32 logits of the same stride");
+  const int64_t elt = a.d.dtype == PG_LOGITS_BF16 ? 2 : 4;
+  if ((const void*)out != a.d.logits && rows_overlap((uintptr_t)a.d.logits, a.d.stride * elt, a.d.vocab * elt, (uintptr_t)out, out_stride * 4,
+                                                     a.d.vocab * 4ll, a.d.rows))
+    return fail(PG_EINVAL, "pg_logits_adjust: out overlaps the logits");
   const LogitGrid g = logit_grid(a.d.rows, a.d.vocab, false);
   a.range = g.range;
   const dim3 grid((unsigned)g.workgroups, (unsigned)a.d.rows), block(LOGIT_THREADS);

@@ -1,4 +1,4 @@
-"""Mask indices that no mask has."""
+"""Mask indices that no mask has, and outputs beside the logits."""
 import math
 
 import pytest
@@ -29,3 +29,21 @@ def test_an_index_that_no_mask_has_allows_nothing(lib, vocab, dtype):
                 assert torch.equal(out[r], x[r].float()) and 0 <= int(token[r]) < vocab and math.isfinite(float(logp[r]))
             else:
                 assert (out[r] == -math.inf).all() and int(token[r]) == -1 and float(logp[r]) == -math.inf
+
+
+def test_rows_between_the_logits_rows_may_be_written(lib):
+    """Columns of one allocation, above and below, and blocks side by side."""
+    say("adjusting into the other half of the rows")
+    g = torch.Generator(device=DEV).manual_seed(3)
+    wide = torch.randn(5, 2 * 3001, device=DEV, generator=g)
+    keep = wide.clone()
+    for lo, to in ((0, 3001), (3001, 0)):
+        x, out = wide[:, lo:lo + 3001], wide[:, to:to + 3001]
+        lib.pg_logits_adjust(lib.Logits(x), out)
+        assert torch.equal(out, x) and torch.equal(x, keep[:, :3001])
+    two = torch.randn(10, 3001, device=DEV, generator=g)
+    keep = two.clone()
+    lib.pg_logits_adjust(lib.Logits(two[5:]), two[:5])
+    assert torch.equal(two[:5], keep[5:]) and torch.equal(two[5:], keep[5:])
+    lib.pg_logits_adjust(lib.Logits(two[0::2]), two[1::2])
+    assert torch.equal(two[1::2], two[0::2])
