@@ -71,6 +71,10 @@ __device__ __forceinline__ int query_length(const PagedArgs& a, int query, int& 
 __device__ __forceinline__ int64_t range_start(int64_t total, int log2_ranges, int r) { return total * r >> log2_ranges; }
 
 __device__ __forceinline__ bf16x8 as_bf16(uint4 w) { return __builtin_bit_cast(bf16x8, w); }
+// a and b cut to bf16
+__device__ __forceinline__ uint32_t upper_halves(float a, float b) {
+  return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, a), 0x07060302u);
+}
 // eight codes -> eight bf16 (exact: e4m3 has three bits of fraction)
 __device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t a, uint32_t b) {
   const auto x0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)a, false), x1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)a, true);
@@ -303,7 +307,8 @@ __global__ __launch_bounds__(PA_THREADS, 2) void paged_attention_kernel(PagedArg
         for (int d = 0; d < DT; ++d) o[d] *= shrink;
       }
       // a probability is kept as the sum of two bf16: the matrix pipe has time for both, and 8 bits alone would make the output's error
-      // 1.4 times as large
+      // 1.4 times as large.  Where values may be infinite (codes are not), both parts have to be positive, or infinity would meet a 0 or its
+      // opposite: the first is the probability cut to 8 bits, not rounded, and the second at least the smallest normal number
       bf16x8 hi[U], lo[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -313,10 +318,15 @@ __global__ __launch_bounds__(PA_THREADS, 2) void paged_attention_kernel(PagedArg
           p[e] = __builtin_amdgcn_exp2f(s[2 * u + (e >> 2)][e & 3] - m);
           l += p[e];
         }
-        const uint4 w = {pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])};
-        hi[u] = as_bf16(w);
+        if constexpr (F8) {
+          hi[u] = as_bf16(uint4{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])});
 #pragma unroll
-        for (int e = 0; e < 8; ++e) rest[e] = p[e] - (float)hi[u][e];
+          for (int e = 0; e < 8; ++e) rest[e] = p[e] - (float)hi[u][e];
+        } else {
+          hi[u] = as_bf16(uint4{upper_halves(p[0], p[1]), upper_halves(p[2], p[3]), upper_halves(p[4], p[5]), upper_halves(p[6], p[7])});
+#pragma unroll
+          for (int e = 0; e < 8; ++e) rest[e] = fmaxf(p[e] - (float)hi[u][e], FLT_MIN);
+        }
         lo[u] = as_bf16(uint4{pack_bf16x2(rest[0], rest[1]), pack_bf16x2(rest[2], rest[3]), pack_bf16x2(rest[4], rest[5]), pack_bf16x2(rest[6], rest[7])});
       }
       if (!MORE && there < S::KEYS) {                // what lies behind the last token may be anything, NaN too

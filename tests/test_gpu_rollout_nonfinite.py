@@ -115,3 +115,15 @@ def test_a_score_of_plus_infinity_gives_nan(lib):
     c.q[:, :, 2] = 1.0
     c.put(0, 2, 150, 2, math.inf)
     c.check(False)
+
+
+@pytest.mark.parametrize("lens,hd,page,f8,ranges", [f for f in FORMS if not f[3]])
+def test_an_infinite_value_is_an_infinite_output(lib, lens, hd, page, f8, ranges):
+    """Of the only token, whose probability is 1, of the last and of one in the middle; in its channel alone."""
+    say(f"infinite values, rows {lens}, head width {hd}")
+    for value, at in ((math.inf, lambda n: n - 1), (-math.inf, lambda n: n // 2), (math.inf, lambda n: 0)):
+        c = Case(lib, lens, hd, page, f8, 6)
+        for r, n in enumerate(lens):
+            if n:
+                c.put(1, r, at(n), 9, value)
+        c.check(ranges)
