@@ -515,7 +515,8 @@ extern "C" pg_status pg_paged_attention(const pg_cache* c, int32_t layer, const 
   const char* who = "pg_paged_attention";
   PG_TRY(paged_sizes(c, n_q, heads_q, max_len, who));
   if (layer < 0 || layer >= c->layers) return fail(PG_EINVAL, "%s: layer %d of %d", who, layer, c->layers);
-  if (!std::isfinite(scale)) return fail(PG_EINVAL, "%s: scale is not finite", who);
+  const float scale_log2 = (float)((scale == 0.0 ? 1.0 / std::sqrt((double)c->head_dim) : scale) * 1.4426950408889634);
+  if (!std::isfinite(scale_log2)) return fail(PG_EINVAL, "%s: scale is not finite in 32 bits", who);
   if (n_q == 0) return PG_OK;
   if (!q || !table || !lens || !out) return fail(PG_EINVAL, "%s: null pointer", who);
   if (n_rows < 1 || (!row_of && n_rows < n_q)) return fail(PG_EINVAL, "%s: a table of %d rows for %d queries", who, n_rows, n_q);
@@ -539,7 +540,7 @@ extern "C" pg_status pg_paged_attention(const pg_cache* c, int32_t layer, const 
   a.table = table; a.row_of = row_of; a.lens = lens; a.n_rows = n_rows;
   a.heads_q = heads_q; a.group = heads_q / c->heads; a.q_tiles = (a.group + PA_HEADS - 1) / PA_HEADS;
   a.n_q = n_q;
-  a.scale_log2 = (float)((scale == 0.0 ? 1.0 / std::sqrt((double)c->head_dim) : scale) * 1.4426950408889634);
+  a.scale_log2 = scale_log2;
   a.lse = lse;
   a.opened = (int4*)workspace; a.parts = (float*)(a.opened + a.ranges);
   a.total = (int64_t*)(a.parts + (size_t)a.ranges * 2 * PA_HEADS * (c->head_dim + 4));
