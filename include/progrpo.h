@@ -384,7 +384,8 @@ pg_status pg_cache_reserve(const pg_cache *cache, int32_t *table, const int32_t 
 /* Writes the keys and values of the LAST tokens of each row (lens counts them already): tokens cu[r] .. cu[r+1]-1 of
  * k_new / v_new are the last cu[r+1] - cu[r] of row r (cu: n_rows + 1 ascending offsets, cu[n_rows] == n_tokens; NULL: one token
  * a row).  k_new, v_new: bf16 [n_tokens, heads, head_dim], a token every token_stride elements (multiple of 8, so that slices
- * of a fused projection are taken as they are), 16-byte aligned.  e4m3 codes: round-to-nearest-even of x / scale, limited to +-448.
+ * of a fused projection are taken as they are), 16-byte aligned.  e4m3 codes: round-to-nearest-even of the fp32 quotient x / scale,
+ * limited to +-448.
  * A page that several rows hold is whole and stays as it is: tokens for it are left out (status 4).  A row that pg_cache_reserve
  * refused has its old length and so no place for new tokens; in a page of its own they would replace its last ones.  Offsets cu of
  * what the lengths grew by leave such rows out. */
@@ -418,7 +419,8 @@ pg_status pg_cache_check(const pg_cache *cache, void *stream);
  * heads_q a multiple of cache->heads, query head j reads key/value head j / (heads_q / heads).  logits scaled by `scale`
  * (0: 1/sqrt(head_dim)).  lse (nullable) fp32 [n_q, heads_q]: natural logarithm of the softmax's denominator.  A query of no
  * tokens, or whose scores are all -inf, gives zeros and -inf; NaN in a query, or in a key or value of
- * its tokens, gives NaN in what it enters.  max_len >= every length: sizes the split (longer rows are right too, but slower).  All sums in fp32.
+ * its tokens, gives NaN in what it enters.  Long rows are cut into pieces that depend on the call's other rows, and an output's last bits with them.
+ * max_len >= every length: sizes the split (longer rows are right too, but slower).  All sums in fp32.
  * workspace: pg_paged_attention_workspace() bytes, 16-byte aligned (may be NULL where that is 0), which are enough for every call of
  * no more queries and no larger max_len, too.  At most 65535 queries, and 2^24 of queries x key/value heads x tiles of 16 query heads. */
 size_t pg_paged_attention_workspace(const pg_cache *cache, int32_t n_q, int32_t heads_q, int32_t max_len);
@@ -461,8 +463,8 @@ pg_status pg_logits_adjust(const pg_logits *desc, float *out, int64_t out_stride
 
 /* Draws token[r] from softmax(y), y = z * (1 / temperature[r]), and logp[r] = y[token] - ln sum exp(y), in one pass over the logits:
  * token = argmax_v y_v - ln E_v, E_v = -log1p(-min((n + 1/2) 2^-32, 1 - 2^-24)) exponential variates from word n = (v mod 4) of the
- * Philox-4x32-10 block with counter (v div 4, step, ids[r], 2) and key (seed low, seed high); ids NULL: r.  The draw of a
- * trajectory depends on its id alone, not on where pruning has packed it.  temperature[r] == 0: argmax z, logp at temperature 1; NULL: 1.
+ * Philox-4x32-10 block with counter (v div 4, step, ids[r], 2) and key (seed low, seed high); ids NULL: r.  For equal
+ * logits the draw of a trajectory depends on its id alone, not on where pruning has packed it.  temperature[r] == 0: argmax z, logp at temperature 1; NULL: 1.
  * Equal scores: the lowest token.  A row with nothing left: token -1, logp -inf.  A row with an allowed z that is NaN or +inf, or with
  * a temperature that is negative, infinite or NaN: token -1, logp NaN.  scratch: pg_sample_scratch_floats(rows, vocab) floats, which
  * are enough for every call of no more rows and tokens, too. */

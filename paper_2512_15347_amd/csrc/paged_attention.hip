@@ -18,7 +18,7 @@
 // start only.  A range has at most two rows that it does not cover whole, its first and its last; their pieces go to the
 // workspace and a second launch joins them.
 //
-// Measured: 384 rows of 1 to 4096 tokens, 32 / 8 heads of 128, codes (1.6 GB): 292 us, 5.6 TB/s, where a plain read of 4 GiB reaches 5.3
+// Measured: 384 rows of 1 to 4096 tokens, 32 / 8 heads of 128, codes (1.6 GB): 293 us, 5.5 TB/s, where a plain read of 4 GiB reaches 5.3
 // to 6.3; three rows of 65 to 131 thousand tokens in bf16 (0.65 GB): 126 us, of which the join takes 10; 48 rows of up to 1178 tokens with
 // heads of 64 (65 MB with the shared prompt counted once a row): 14 us; one row of 77 tokens: 4 us, and 8 with the call.
 #include <algorithm>

@@ -7,7 +7,7 @@
 //
 // Measured: a plan takes 2.8 to 7.4 us (latency: four to six dependent loads and barriers); 376 part-filled pages of twelve layers copied for
 // a fork 26 us (148 MB written, the eight source pages come from the caches: the write rate of the device is 6.9 TB/s); 530 MB of pages moved
-// 200 us (5.3 TB/s read and written, where a plain copy reaches 4.8); 135 thousand tokens of eight heads of 128 appended as codes 190 us (4.4 TB/s).
+// 200 us (5.3 TB/s read and written, where a plain copy of 4 GiB reaches 4.8 to 5.6 by its grid); 135 thousand tokens of eight heads of 128 appended as codes 192 us (4.3 TB/s).
 #include <cmath>
 #include <type_traits>
 #include "paged_cache.hpp"

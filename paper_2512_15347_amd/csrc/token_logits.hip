@@ -1,13 +1,13 @@
 // Logits of a token policy: penalties, biases and grammar masks, and the draw of a token with its log-prob.
 //
 // A workgroup takes a range of one row's vocabulary and goes through it in groups of eight tokens a lane.  Few tokens have a penalty or a
-// bias: for every 4096 tokens the row's history is counted in LDS (32 bits a token: integer sums, so their order does not matter), the
+// bias: for every 2048 or 4096 tokens the row's history is counted in LDS (32 bits a token: integer sums, so their order does not matter), the
 // tokens that occur are worked out once each and left in LDS, and the groups pick them up by a bit.  So no counts are kept
 // between calls, and nothing but the history has to follow a member through a prune.  The logits are read once.
 //
-// Adjusting is bound by HBM, and by the barriers around the counts where there is a history: 384 x 65537 in bf16 takes 35 us without one
-// (4.3 TB/s), 49 with up to 2048 tokens of history a row, masks and lists.  Draws are bound by the vector ALU, of which 1024 SIMDs at
-// four cycles an instruction issue some 600 a nanosecond: 384 x 131073 takes 66 us without history, lists and masks, 96 with all of them (the
+// Adjusting is bound by HBM, and by the barriers around the counts where there is a history: 384 x 65537 in bf16 takes 35 us with nothing to adjust
+// (4.4 TB/s), 49 with up to 2048 tokens of history a row, masks and lists.  Draws are bound by the vector ALU, of which 1024 SIMDs at
+// four cycles an instruction issue some 600 a nanosecond: 384 x 131073 takes 67 us without history, lists and masks, 97 with all of them (the
 // logits alone would be read in 20).
 #include <algorithm>
 #include <cfloat>
@@ -462,7 +462,7 @@ __global__ __launch_bounds__(WAVE) void sample_finish_kernel(const Draw* parts, 
 // some 4096 workgroups, us, without a history in brackets: 384 x 65537: 60 and 70 (43 and 57); 384 x 131073: 93 and 93 (66 and 74);
 // 128 x 131073: 47 and 50 (34 and 39); 640 x 65537: 87 and 97 (53 and 71); 1000 x 65537: 111 and 125 (69 and 85)).  More rows than that
 // get some 4096 workgroups.  Adjusting keeps nothing but the history between stretches and gains nothing from longer ranges
-// (384 x 65537: 30 us with 8192 workgroups or fewer, 33 with 2048).  (Whole rows of more than 2048 tokens in one workgroup, without
+// (384 x 65537 in bf16, nothing to adjust: 35 us by this rule, a stretch each, and 44 with 2048 workgroups).  (Whole rows of more than 2048 tokens in one workgroup, without
 // the second launch: 10.3 us for one row of 8192, 9.9 with it; 22.8 and 21.8 for 384 rows of 12288.)
 constexpr int64_t RESIDENT_DRAWS = 1280;                  // of 256 lanes, five waves a SIMD
 struct LogitGrid { int groups, range, workgroups; };
