@@ -226,9 +226,9 @@ def _own_policy(s):
 
 def _own_distill(s):
     pg, d = _descriptor(s)
-    teacher = dict(tail=bool(s["case"]["tail"]), temperature=s["temperature"])
-    pg.pg_distill_loss(d, s["teacher_ids"], s["teacher_logp"], s["loss"], s["scratch"], stats=s["stats"], **teacher)
-    pg.pg_distill_backward(d, s["teacher_ids"], s["teacher_logp"], s["stats"], s["g_loss"], s["d_logits"], **teacher)
+    pg.pg_distill_loss(d, s["teacher_ids"], s["teacher_logp"], s["loss"], s["scratch"], tail=bool(s["case"]["tail"]),
+                       temperature=s["temperature"], stats=s["stats"])
+    pg.pg_distill_backward(d, s["teacher_ids"], s["teacher_logp"], s["stats"], s["g_loss"], s["d_logits"], temperature=s["temperature"])
     return dict(loss=s["loss"], d_logits=s["d_logits"])
 
 
