@@ -472,6 +472,71 @@ int64_t pg_sample_scratch_floats(int32_t rows, int32_t vocab);
 pg_status pg_sample_tokens(const pg_logits *desc, const float *temperature, uint64_t seed, uint32_t step,
                            const int32_t *ids, int32_t *token, float *logp, float *scratch, void *stream);
 
+/* ---- what a token policy learns from: log-probs of given tokens, distillation, the clipped objective ----
+ *
+ * Rows of logits as pg_logits describes them: logits, allow and allow_row; tokens and bias_offsets have to be NULL (pg_logits_adjust first).
+ * As in a draw y = z / temperature[r] (0 or NULL: 1) over the allowed tokens and p = softmax(y); a token that is not allowed, or whose logit is
+ * -inf, has p = 0 and gradient 0.  A row with an allowed logit that is NaN or +inf, or with a temperature that is negative, infinite or
+ * NaN, gives NaN.  All sums in fp32 or more.  Every result follows from its row alone, but that long rows are cut into pieces
+ * by the call's number of rows, and the last bits with them.
+ * Gradients are with respect to the logits as they lie there, in their type, rounded once; d_logits may be the logits themselves
+ * (equal strides) and overlaps them in no other way. */
+
+/* Alternatives of a row, tokens of a teacher's list, floats of a row that the forward pass leaves for the backward one. */
+#define PG_TOP_MAX 64
+#define PG_DISTILL_MAX 256
+#define PG_LOGPROB_STATS 4
+#define PG_DISTILL_STATS 8
+
+/* logp[r] = ln p of target[r]; entropy[r] = -sum p ln p; top_ids, top_logp [rows, n_top]: the most likely tokens in falling order
+ * (equal logits: the lowest token first) and their log-probs, -1 and -inf past the last token whose logit is above -inf.  Every output may be NULL.
+ * target[r] == -1: a row that is left out and not read (logp and entropy 0, no alternatives, gradient 0); any other index that no token has:
+ * logp NaN.  target NULL: no row is left out, and logp has to be NULL.  A row with nothing left: logp -inf, entropy 0.  A bad row: NaN, and
+ * -1 and NaN for its alternatives.  stats: [rows, PG_LOGPROB_STATS], for the backward pass; stats[r][0] + stats[r][1] is the natural logarithm of
+ * the softmax's denominator of y (the largest y, and what the others add).
+ * scratch: pg_logprob_scratch_floats() floats, 8-byte aligned, which are enough for every call of no more rows, tokens and alternatives, too. */
+int64_t pg_logprob_scratch_floats(int32_t rows, int32_t vocab, int32_t n_top);
+pg_status pg_token_logprobs(const pg_logits *desc, const float *temperature, const int32_t *target, float *logp, float *entropy,
+                            float *stats, int32_t n_top, int32_t *top_ids, float *top_logp, float *scratch, void *stream);
+
+/* d_logits[r, v] = 1/T [g_logp[r] (1[v = target[r]] - p_v) - g_entropy[r] p_v (ln p_v + entropy)], a row every d_stride elements; desc,
+ * temperature, target and stats as the forward pass had them.  g_logp or g_entropy NULL: 0.  A row whose two are 0 is not read. */
+pg_status pg_token_logprobs_backward(const pg_logits *desc, const float *temperature, const int32_t *target, const float *stats,
+                                     const float *g_logp, const float *g_entropy, void *d_logits, int64_t d_stride, void *stream);
+
+/* Divergence from a teacher of whose distribution only the k most likely tokens are known: teacher_ids, teacher_logp [rows, k] as
+ * pg_token_logprobs gives them at the same temperature (any order; ids that no token has are passed over; of equal ids the first counts).
+ *   PG_DISTILL_TOP:   q = exp(teacher_logp) over their sum (so that any shift of a row's values does), loss = sum q (ln q - ln p)
+ *   PG_DISTILL_TAIL:  q = exp(teacher_logp), and what is missing to 1 is one more outcome, that of all other allowed tokens together:
+ *                     loss = the sum above + q_rest (ln q_rest - ln p_rest); without other tokens (or q_rest <= 0) q_rest = 0
+ * A row without a listed token, with nothing left, or (PG_DISTILL_TOP) with a list of -inf alone: loss 0, gradient 0.  q > 0 for a token with
+ * p = 0: loss +inf.  A value of a listed token that is NaN or +inf: NaN.  stats: [rows, PG_DISTILL_STATS], for the backward pass (may be NULL).
+ * scratch: pg_distill_scratch_floats() floats, enough for every call of no more rows and tokens, too. */
+enum { PG_DISTILL_TOP = 0, PG_DISTILL_TAIL = 1 };
+int64_t pg_distill_scratch_floats(int32_t rows, int32_t vocab);
+pg_status pg_distill_loss(const pg_logits *desc, const float *temperature, int32_t mode, const int32_t *teacher_ids,
+                          const float *teacher_logp, int32_t k, float *loss, float *stats, float *scratch, void *stream);
+
+/* d_logits[r, v] = g_loss[r] d loss[r] / d logits[r, v]; the other arguments as the forward pass had them.  A row whose g_loss is 0 is not
+ * read. */
+pg_status pg_distill_backward(const pg_logits *desc, const float *temperature, const int32_t *teacher_ids, const float *teacher_logp,
+                              int32_t k, const float *stats, const float *g_loss, void *d_logits, int64_t d_stride, void *stream);
+
+/* The clipped objective of Eq. 20 over tokens, and its gradient, for sequences r of tokens cu[r] .. cu[r+1]-1 (cu: n_seq + 1 ascending offsets,
+ * no larger than n_tokens; fp32 arrays of n_tokens):
+ *   rho = exp(logp - logp_old),  x = logp_ref - logp,  k = exp(x) - x - 1
+ *   objective[r] = w sum_t [min(rho A, clip(rho, 1 - clip_low, 1 + clip_high) A) - kl_coef k],   A = adv[r], w = weight[r] (NULL: 1 / length)
+ *   g_logp[t] = w [rho A unless that was cut + kl_coef (exp(x) - 1)]
+ * kl[r]: mean of k; clipped[r]: tokens whose gradient was cut (rho above 1 + clip_high with A > 0, or below 1 - clip_low with A < 0).
+ * logp_ref NULL: k = 0.  Every output may be NULL.  A sequence of no tokens gives zeros; tokens past cu[n_seq] are left as they are.
+ * g_logp may be one of the inputs of that length.  clip_low in [0, 1], clip_high >= 0 (infinite: no bound); cuts are decided in fp64.
+ * max_len >= every length: sizes the split (longer sequences are right too, but slower).  scratch: pg_surrogate_scratch_floats() floats,
+ * enough for every call of no more sequences and no larger max_len, too (may be NULL where that is 0). */
+int64_t pg_surrogate_scratch_floats(int32_t n_seq, int32_t max_len);
+pg_status pg_token_surrogate(const float *logp, const float *logp_old, const float *logp_ref, const float *adv, const float *weight,
+                             const int32_t *cu, int32_t n_seq, int32_t n_tokens, int32_t max_len, double clip_low, double clip_high,
+                             double kl_coef, float *objective, float *kl, int32_t *clipped, float *g_logp, float *scratch, void *stream);
+
 /* ---- measurement hooks (process-wide, not thread-safe) ----
  * Between pg_profile_begin and pg_profile_end every launch of the heavy kernels is bracketed by a
  * pair of HIP events on the stream it is launched on (at most max_records launches are recorded).

@@ -133,6 +133,14 @@ _SIGNATURES = {
     "pg_logits_adjust": (_i32, [_lp, _vp, _i64, _vp]),
     "pg_sample_scratch_floats": (_i64, [_i32, _i32]),
     "pg_sample_tokens": (_i32, [_lp, _vp, _u64, _u32, _vp, _vp, _vp, _vp, _vp]),
+    "pg_logprob_scratch_floats": (_i64, [_i32, _i32, _i32]),
+    "pg_token_logprobs": (_i32, [_lp, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _vp]),
+    "pg_token_logprobs_backward": (_i32, [_lp, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp]),
+    "pg_distill_scratch_floats": (_i64, [_i32, _i32]),
+    "pg_distill_loss": (_i32, [_lp, _vp, _i32, _vp, _vp, _i32, _vp, _vp, _vp, _vp]),
+    "pg_distill_backward": (_i32, [_lp, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _i64, _vp]),
+    "pg_surrogate_scratch_floats": (_i64, [_i32, _i32]),
+    "pg_token_surrogate": (_i32, [_vp] * 6 + [_i32] * 3 + [_f64] * 3 + [_vp] * 6),
     "pg_profile_begin": (_i32, [_i32]),
     "pg_profile_read": (_i32, [_i32, _dp, _dp, C.POINTER(_i64)]),
     "pg_profile_end": (_i32, []),
@@ -658,6 +666,78 @@ def pg_sample_tokens(desc, temperature, seed, step, ids, token, logp, scratch, s
     assert scratch.numel() * scratch.element_size() >= 4 * desc.scratch
     _check(_lib.pg_sample_tokens(desc.ref, _f32s(temperature, n), seed, step, _i32s(ids, n), _i32s(token, n), _f32s(logp, n), _ptr(scratch),
                                  _stream(stream)))
+
+
+# ---------------------------------------------------------------- what a token policy learns from
+
+PG_TOP_MAX, PG_DISTILL_MAX = 64, 256
+PG_LOGPROB_STATS, PG_DISTILL_STATS = 4, 8
+PG_DISTILL_TOP, PG_DISTILL_TAIL = 0, 1
+
+
+def _gradient(desc, d_logits):
+    """Address and row stride of the gradient of desc's logits, which has their type."""
+    rows, vocab = desc.rows, desc.vocab
+    s0, s1 = d_logits.stride()
+    if d_logits.shape != (rows, vocab) or d_logits.dtype is not desc.keep[0].dtype or (vocab > 1 and s1 != 1):
+        _wanted(d_logits, str(desc.keep[0].dtype), (rows, vocab))
+    return d_logits.data_ptr(), s0 if rows > 1 else max(s0, vocab)
+
+
+def _scratch(scratch, floats):
+    assert scratch is not None and scratch.is_contiguous() and scratch.numel() * scratch.element_size() >= 4 * floats if floats else True, \
+        f"scratch of {floats} floats wanted"
+    return None if scratch is None else scratch.data_ptr()
+
+
+def pg_logprob_scratch_floats(rows, vocab, n_top=0):
+    return int(_lib.pg_logprob_scratch_floats(rows, vocab, n_top))
+
+
+def pg_token_logprobs(desc, target, logp, scratch, temperature=None, entropy=None, stats=None, top_ids=None, top_logp=None, stream=None):
+    n = desc.rows
+    top = 0 if top_ids is None and top_logp is None else (top_logp if top_ids is None else top_ids).shape[1]
+    _check(_lib.pg_token_logprobs(desc.ref, _f32s(temperature, n), _i32s(target, n), _f32s(logp, n), _f32s(entropy, n),
+                                  _f32s(stats, n, PG_LOGPROB_STATS), top, _i32s(top_ids, n, top), _f32s(top_logp, n, top),
+                                  _scratch(scratch, pg_logprob_scratch_floats(n, desc.vocab, top)), _stream(stream)))
+
+
+def pg_token_logprobs_backward(desc, target, stats, d_logits, g_logp=None, g_entropy=None, temperature=None, stream=None):
+    n = desc.rows
+    to, stride = _gradient(desc, d_logits)
+    _check(_lib.pg_token_logprobs_backward(desc.ref, _f32s(temperature, n), _i32s(target, n), _f32s(stats, n, PG_LOGPROB_STATS), _f32s(g_logp, n),
+                                           _f32s(g_entropy, n), to, stride, _stream(stream)))
+
+
+def pg_distill_scratch_floats(rows, vocab):
+    return int(_lib.pg_distill_scratch_floats(rows, vocab))
+
+
+def pg_distill_loss(desc, teacher_ids, teacher_logp, loss, scratch, tail=False, temperature=None, stats=None, stream=None):
+    n, k = desc.rows, teacher_ids.shape[1]
+    _check(_lib.pg_distill_loss(desc.ref, _f32s(temperature, n), PG_DISTILL_TAIL if tail else PG_DISTILL_TOP, _i32s(teacher_ids, n, k),
+                                _f32s(teacher_logp, n, k), k, _f32s(loss, n), _f32s(stats, n, PG_DISTILL_STATS),
+                                _scratch(scratch, pg_distill_scratch_floats(n, desc.vocab)), _stream(stream)))
+
+
+def pg_distill_backward(desc, teacher_ids, teacher_logp, stats, g_loss, d_logits, temperature=None, stream=None):
+    n, k = desc.rows, teacher_ids.shape[1]
+    to, stride = _gradient(desc, d_logits)
+    _check(_lib.pg_distill_backward(desc.ref, _f32s(temperature, n), _i32s(teacher_ids, n, k), _f32s(teacher_logp, n, k), k,
+                                    _f32s(stats, n, PG_DISTILL_STATS), _f32s(g_loss, n), to, stride, _stream(stream)))
+
+
+def pg_surrogate_scratch_floats(n_seq, max_len):
+    return int(_lib.pg_surrogate_scratch_floats(n_seq, max_len))
+
+
+def pg_token_surrogate(logp, logp_old, adv, cu, objective, g_logp, clip_low, clip_high, max_len, scratch=None, logp_ref=None, kl_coef=0.0,
+                       weight=None, kl=None, clipped=None, stream=None):
+    n, tokens = adv.shape[0], logp.shape[0]
+    _check(_lib.pg_token_surrogate(_f32s(logp, tokens), _f32s(logp_old, tokens), _f32s(logp_ref, tokens), _f32s(adv, n), _f32s(weight, n),
+                                   _i32s(cu, n + 1), n, tokens, max_len, clip_low, clip_high, kl_coef, _f32s(objective, n), _f32s(kl, n),
+                                   _i32s(clipped, n), _f32s(g_logp, tokens), _scratch(scratch, pg_surrogate_scratch_floats(n, max_len)),
+                                   _stream(stream)))
 
 
 def pg_mfma_probe(blocks, iters, operand_scale, out, stream=None):

@@ -15,24 +15,16 @@
 #include "common.hpp"
 #include "operands.hpp"
 #include "philox.hpp"
+#include "token_logits.hpp"
 
 namespace pg {
 
 constexpr int LOGIT_THREADS = 256;
 constexpr int LOGIT_WAVES = LOGIT_THREADS / WAVE;
-constexpr int LANE_TOKENS = 8;                       // a group: 16 or 32 bytes, two Philox blocks, one byte of a mask
 constexpr int PASS_TOKENS = LOGIT_THREADS * LANE_TOKENS;
 constexpr uint32_t STREAM_TOKEN = 2u;
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 // LDS word of a token: how often it is in the output, and whether it is in the prompt or has a bias; then its z
 constexpr uint32_t IN_PROMPT = 1u << 31, HAS_BIAS = 1u << 30, COUNT = HAS_BIAS - 1;
-
-struct LogitArgs {
-  pg_logits d;
-  int words;                                         // of a mask
-  int range;                                         // tokens of a workgroup, a multiple of the counted stretch
-  bool count;                                        // there is a history or a bias list
-};
 
 // What one row needs.
 struct RowRules {
@@ -476,11 +468,11 @@ static LogitGrid logit_grid(int64_t rows, int64_t vocab, bool draw) {
                            : std::min<int64_t>(stretches, std::max<int64_t>(1, rows * stretches / (draw ? 4096 : 8192)));
   return LogitGrid{g, (int)(per * g * PASS_TOKENS), (int)((stretches + per - 1) / per)};
 }
-static pg_status logit_args(const pg_logits* d, const char* who, LogitArgs& a) {
+pg_status logit_args(const pg_logits* d, const char* who, LogitArgs& a, int32_t max_rows) {
   if (!d) return fail(PG_EINVAL, "%s: desc is NULL", who);
   if (d->rows < 0 || d->vocab < 1 || (d->dtype != PG_LOGITS_F32 && d->dtype != PG_LOGITS_BF16))
     return fail(PG_EINVAL, "%s: %d rows of %d tokens, dtype %d", who, d->rows, d->vocab, d->dtype);
-  if (d->rows > 65535) return fail(PG_ESHAPE, "%s: %d rows (at most 65535)", who, d->rows);
+  if (d->rows > max_rows) return fail(PG_ESHAPE, "%s: %d rows (at most %d)", who, d->rows, max_rows);
   if (d->vocab > 1 << 30 || d->rows * ((d->vocab + PASS_TOKENS - 1ll) / PASS_TOKENS) >= 1 << 24)
     return fail(PG_ESHAPE, "%s: %d rows of %d tokens pass 2^24 workgroups", who, d->rows, d->vocab);
   if (d->rows && !d->logits) return fail(PG_EINVAL, "%s: logits is NULL", who);
@@ -500,8 +492,7 @@ static pg_status logit_args(const pg_logits* d, const char* who, LogitArgs& a) {
   return PG_OK;
 }
 
-// Whether one of `rows` intervals of `b` bytes from q on, each `q_step` after the one before, meets one of `a` bytes from p on (a <= p_step).
-static bool rows_overlap(uintptr_t p, int64_t p_step, int64_t a, uintptr_t q, int64_t q_step, int64_t b, int64_t rows) {
+bool rows_overlap(uintptr_t p, int64_t p_step, int64_t a, uintptr_t q, int64_t q_step, int64_t b, int64_t rows) {
   if (p + (rows - 1) * p_step + a <= q || q + (rows - 1) * q_step + b <= p) return false;
   for (int64_t r = 0; r < rows; ++r) {
     const int64_t lo = (int64_t)(q - p) + r * q_step;
@@ -527,7 +518,7 @@ using namespace pg;
 
 extern "C" pg_status pg_logits_adjust(const pg_logits* desc, float* out, int64_t out_stride, void* stream) {
   LogitArgs a{};
-  PG_TRY(logit_args(desc, "pg_logits_adjust", a));
+  PG_TRY(logit_args(desc, "pg_logits_adjust", a, 65535));
   if (a.d.rows == 0) return PG_OK;
   if (!out) return fail(PG_EINVAL, "pg_logits_adjust: out is NULL");
   if ((uintptr_t)out & 3 || out_stride < a.d.vocab) return fail(PG_ESHAPE, "pg_logits_adjust: out rows %lld floats apart", (long long)out_stride);
@@ -558,7 +549,7 @@ extern "C" int64_t pg_sample_scratch_floats(int32_t rows, int32_t vocab) {
 extern "C" pg_status pg_sample_tokens(const pg_logits* desc, const float* temperature, uint64_t seed, uint32_t step, const int32_t* ids,
                                       int32_t* token, float* logp, float* scratch, void* stream) {
   LogitArgs a{};
-  PG_TRY(logit_args(desc, "pg_sample_tokens", a));
+  PG_TRY(logit_args(desc, "pg_sample_tokens", a, 65535));
   if (a.d.rows == 0) return PG_OK;
   if (!token || !logp || !scratch) return fail(PG_EINVAL, "pg_sample_tokens: null pointer");
   hipStream_t s = (hipStream_t)stream;
