@@ -102,7 +102,7 @@ def surrogate(logp, old, adv, clip_low, clip_high, ref=None, kl_coef=0.0, weight
     if n == 0:
         return dict(objective=0.0, kl=0.0, clipped=0, g_logp=np.zeros(0))
     w = 1.0 / n if weight is None else float(weight)
-    with np.errstate(over="ignore"):
+    with np.errstate(over="ignore", invalid="ignore"):
         rho = np.exp(logp - old)
         a = float(adv)
         cut = (rho > 1 + clip_high) & (a > 0) | (rho < 1 - clip_low) & (a < 0)
@@ -112,6 +112,6 @@ def surrogate(logp, old, adv, clip_low, clip_high, ref=None, kl_coef=0.0, weight
         kl = np.zeros(n)
         if ref is not None:
             x = np.asarray(ref, dtype=np.float64) - logp
-            kl = np.expm1(x) - x
+            kl = np.where(np.expm1(x) == np.inf, np.inf, np.expm1(x) - x)
             term, g = term - kl_coef * kl, g + kl_coef * np.expm1(x)
     return dict(objective=w * term.sum(), kl=kl.mean(), clipped=int(cut.sum()), g_logp=w * g)

@@ -5,8 +5,10 @@
 // teacher's list is compared, S over the tokens that are not on it.  Then ln p = (z - m) / T - ln S and the entropy is ln S - U / (S T), a
 // sum of terms of one sign.  Differences to m are exact where it matters, so that a row may be shifted by any amount; m and ln S are kept apart
 // for the backward pass for the same reason.
+#include <algorithm>
 #include <cfloat>
 #include <cmath>
+#include <type_traits>
 #include "common.hpp"
 #include "operands.hpp"
 #include "token_logits.hpp"
@@ -15,6 +17,7 @@ namespace pg {
 
 constexpr int LOSS_THREADS = 256;
 constexpr int LOSS_WAVES = LOSS_THREADS / WAVE;
+constexpr int LOSS_TOKENS = LOSS_THREADS * LANE_TOKENS;                 // one group a lane
 constexpr float FAR = 200.0f;                        // exp(-FAR) is 0 in fp32
 
 struct LossArgs {
@@ -74,28 +77,172 @@ __device__ __forceinline__ void join(Sums& a, Sums b, const LossRow& q) {
   a.s += b.s;
   a.u += b.u;
 }
-__device__ __forceinline__ void take(Sums& a, float z, const LossRow& q) {
-  if (z > a.m) move_to(a, z, q);
-  const float t = z - a.m, e = exp2_of(t * q.c);
-  a.s += e;
-  a.u += e * fmaxf(t, q.lim);
+__device__ __forceinline__ float lanes_max(float v) {
+  for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  return v;
 }
-
+__device__ __forceinline__ Sums wave_sums(Sums a, const LossRow& q) {
+  move_to(a, lanes_max(a.m), q);
+  a.s = wave_allsum(a.s);
+  a.u = wave_allsum(a.u);
+  return a;
+}
 __device__ __forceinline__ Sums block_sums(Sums a, const LossRow& q, Sums* waves) {
-  for (int o = 32; o; o >>= 1) {
-    const Sums b{__shfl_xor(a.m, o), __shfl_xor(a.s, o), __shfl_xor(a.u, o)};
-    join(a, b, q);
-  }
-  __syncthreads();
+  a = wave_sums(a, q);
   if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = a;
   __syncthreads();
   a = waves[0];
+#pragma unroll
   for (int w = 1; w < LOSS_WAVES; ++w) join(a, waves[w], q);
   return a;
 }
 
-// Whether (z, v) comes before (y, w) among alternatives.
+// A lane's group of eight tokens, from any address that is a multiple of their size (the hardware takes unaligned 16-byte loads).
+template <bool BF16>
+struct Lot {
+  uint32_t raw[BF16 ? 4 : 8];
+  __device__ __forceinline__ void load(const char* p) { __builtin_memcpy(raw, p, BF16 ? 16 : 32); }
+  __device__ __forceinline__ void load(const char* p, int64_t left) {
+    if (left >= LANE_TOKENS) return load(p);
+#pragma unroll
+    for (int e = 0; e < LANE_TOKENS; ++e) {
+      const uint32_t x = e >= left ? 0u : BF16 ? ((const uint16_t*)p)[e] : ((const uint32_t*)p)[e];
+      if (!BF16) raw[e] = x;
+      else raw[e >> 1] = e & 1 ? raw[e >> 1] | x << 16 : x;
+    }
+  }
+  __device__ __forceinline__ float logit(int e) const {
+    return __builtin_bit_cast(float, !BF16 ? raw[e] : e & 1 ? raw[e >> 1] & 0xFFFF0000u : raw[e >> 1] << 16);
+  }
+};
+__device__ __forceinline__ uint32_t up_to(int64_t left) { return left >= LANE_TOKENS ? 0xFFu : left <= 0 ? 0u : (1u << left) - 1; }
+
+// The workgroup's range of a row, G groups a lane at a time: each(logits, first token of group g = v + g * LOSS_TOKENS), with -inf where a token
+// is not allowed, is past the range or is struck out (strike(g): bits of the tokens that are).
+template <bool BF16, int G, class Strike, class Each>
+__device__ __forceinline__ void through(const LossArgs& a, const LossRow& q, int64_t first, int64_t end, Strike strike, Each each) {
+  constexpr int ELT = BF16 ? 2 : 4;
+  const char* row = (const char*)a.l.d.logits + q.at * ELT;
+#pragma unroll 1
+  for (int64_t base = first; base < end; base += G * LOSS_TOKENS) {
+    const int64_t v = base + threadIdx.x * LANE_TOKENS;
+    Lot<BF16> x[G];
+    uint32_t bits[G];
+    if (base + G * LOSS_TOKENS <= end) {
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        x[g].load(row + (v + g * LOSS_TOKENS) * ELT);
+        bits[g] = q.allow ? q.allow[(v + g * LOSS_TOKENS) >> 3] : q.unmasked;
+      }
+    } else {
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const int64_t left = end - (v + g * LOSS_TOKENS);
+        bits[g] = up_to(left);
+        if (left > 0) {
+          x[g].load(row + (v + g * LOSS_TOKENS) * ELT, left);
+          bits[g] &= q.allow ? q.allow[(v + g * LOSS_TOKENS) >> 3] : q.unmasked;
+        }
+      }
+    }
+    uint32_t all = 0xFFu;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      bits[g] &= ~strike(v + g * LOSS_TOKENS);
+      all &= bits[g];
+    }
+    float z[G * LANE_TOKENS];
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int e = 0; e < LANE_TOKENS; ++e) z[g * LANE_TOKENS + e] = x[g].logit(e);
+    if (__ballot(all != 0xFFu)) {
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int e = 0; e < LANE_TOKENS; ++e) z[g * LANE_TOKENS + e] = bits[g] >> e & 1 ? z[g * LANE_TOKENS + e] : -INFINITY;
+    }
+    each(z, base);
+  }
+}
+
+// Adds N logits to the sums; the sums move to a new largest logit once for all of them.
+template <int N, bool ENTROPY>
+__device__ __forceinline__ void take(Sums& a, const float* z, float top, const LossRow& q) {
+  if (top > a.m) move_to(a, top, q);
+  float s = 0.0f, u = 0.0f;
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    const float t = z[e] - a.m, p = exp2_of(t * q.c);
+    s += p;
+    if (ENTROPY) u = __builtin_fmaf(p, fmaxf(t, q.lim), u);
+  }
+  a.s += s;
+  a.u += u;
+}
+
+// How a call is laid out: groups a lane takes at a time, tokens of a workgroup, workgroups of a row.
+struct LossGrid {
+  int groups, range, pieces;
+};
+
+// ---------------------------------------------------------------- alternatives
+// The n best tokens lie in the n stretches of CHUNK tokens whose largest logits come first (equal ones in the order of their tokens): each of
+// these has a token that comes before all others of the stretches that come after.  So the pass over the logits leaves the largest logit of each
+// stretch, the stretches are chosen from these, and their tokens are looked at again.
+constexpr int CHUNK = 4 * LANE_TOKENS;
+
+// Whether (z, v) comes before (y, w).
 __device__ __forceinline__ bool before(float z, int v, float y, int w) { return z > y || (z == y && v < w); }
+__device__ __forceinline__ float lane_of(float x, int lane) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
+}
+__device__ __forceinline__ int from_left(int x) { return __builtin_amdgcn_update_dpp(x, x, 0x138, 0xF, 0xF, false); }      // lane i - 1's
+
+// The best entries that a wave has seen, lane i the i-th.
+struct Best {
+  float z;
+  int v;
+  __device__ __forceinline__ void clear() {
+    z = -INFINITY;
+    v = INT32_MAX;
+  }
+  // every lane offers one (none: -inf); the first n are kept
+  __device__ __forceinline__ void offer(float cz, int cv, int n) {
+    const int lane = threadIdx.x & 63;
+    uint64_t left = __ballot(cz > -INFINITY) & __ballot(before(cz, cv, lane_of(z, n - 1), __builtin_amdgcn_readlane(v, n - 1)));
+    while (left) {
+      const int from = (int)__builtin_ctzll(left);
+      const float y = lane_of(cz, from);
+      const int w = __builtin_amdgcn_readlane(cv, from);
+      const int place = __builtin_popcountll(__ballot(before(z, v, y, w)));
+      const float up_z = __builtin_bit_cast(float, from_left(__builtin_bit_cast(int, z)));
+      const int up_v = from_left(v);
+      z = lane < place ? z : lane == place ? y : up_z;
+      v = lane < place ? v : lane == place ? w : up_v;
+      left &= left - 1;
+      left &= __ballot(before(cz, cv, lane_of(z, n - 1), __builtin_amdgcn_readlane(v, n - 1)));
+    }
+  }
+};
+struct TopLds {
+  float z[LOSS_WAVES][WAVE];
+  int v[LOSS_WAVES][WAVE];
+};
+// The best of all waves' lists, in wave 0 and in row 0 of the LDS.
+__device__ __forceinline__ void join_lists(Best& b, int n, TopLds& s) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __syncthreads();                                   // the lists before have been read
+  s.z[wave][lane] = b.z;
+  s.v[wave][lane] = b.v;
+  __syncthreads();
+  if (wave == 0) {
+    for (int w = 1; w < LOSS_WAVES; ++w) b.offer(lane < n ? s.z[w][lane] : -INFINITY, s.v[w][lane], n);
+    s.z[0][lane] = b.z;
+    s.v[0][lane] = b.v;
+  }
+  __syncthreads();
+}
 
 struct LogprobOut {
   const int32_t* target;
@@ -103,198 +250,415 @@ struct LogprobOut {
   int n_top;
   int32_t* top_ids;
   float* top_logp;
+  Sums* parts;                                       // [rows, pieces]
+  float* chunks;                                     // [rows, n_chunks]: the largest logit of each
+  int n_chunks;
 };
 
+// What the whole row's sums give; all lanes of a workgroup, or (no alternatives) of a wave.
 template <bool BF16>
-__global__ __launch_bounds__(LOSS_THREADS) void logprob_kernel(LossArgs a, LogprobOut o) {
-  __shared__ Sums waves[LOSS_WAVES];
-  __shared__ float best_z[LOSS_WAVES];
-  __shared__ int best_v[LOSS_WAVES];
-  const int r = blockIdx.x, vocab = a.l.d.vocab;
-  const LossRow q = loss_row(a, r);
-  const int target = o.target ? o.target[r] : 0;
-  const bool gone = target == -1;
-  Sums mine = no_sums();
-  if (!gone)
-    for (int v = threadIdx.x; v < vocab; v += LOSS_THREADS) take(mine, open_logit<BF16>(a, q, v), q);
-  mine = block_sums(mine, q, waves);
-  const bool bad = mine.s != mine.s, none = mine.s == 0.0f;
-  const float ln_s = none ? 0.0f : logf(mine.s);
+__device__ __forceinline__ void finish_logprob(const LossArgs& a, const LogprobOut& o, const LossRow& q, int r, int target, const Sums& sum, TopLds* s) {
+  const int vocab = a.l.d.vocab, lane = threadIdx.x & 63;
+  const bool gone = target == -1, bad = sum.s != sum.s, none = sum.s == 0.0f;
+  const float ln_s = none ? 0.0f : logf(sum.s);
   if (threadIdx.x == 0) {
-    const float h = gone || none ? 0.0f : ln_s - q.inv * (mine.u / mine.s);
+    const float h = none ? 0.0f : ln_s - q.inv * (sum.u / sum.s);
     if (o.entropy) o.entropy[r] = h;
     if (o.logp) {
       float l = __builtin_nanf("");
       if (gone) l = 0.0f;
-      else if (target >= 0 && target < vocab && !bad) l = none ? -INFINITY : (open_logit<BF16>(a, q, target) - mine.m) * q.inv - ln_s;
+      else if (target >= 0 && target < vocab && !bad) l = none ? -INFINITY : (open_logit<BF16>(a, q, target) - sum.m) * q.inv - ln_s;
       o.logp[r] = l;
     }
-    if (o.stats) *(float4*)(o.stats + 4ll * r) = float4{none ? -INFINITY : mine.m * q.inv, ln_s, h, mine.m};
+    if (o.stats) *(float4*)(o.stats + 4ll * r) = float4{none ? -INFINITY : sum.m * q.inv, ln_s, h, sum.m};
   }
-  float last_z = INFINITY;
-  int last_v = -1;
-  for (int i = 0; i < o.n_top; ++i) {
-    float z = -INFINITY;
-    int at = INT32_MAX;
-    if (!gone && !bad)
-      for (int v = threadIdx.x; v < vocab; v += LOSS_THREADS) {
-        const float x = open_logit<BF16>(a, q, v);
-        if (before(last_z, last_v, x, v) && before(x, v, z, at)) {
-          z = x;
-          at = v;
+  if (!s) return;
+  const int n = o.n_top, wave = threadIdx.x >> 6;
+  Best best;
+  best.clear();
+  if (!gone && !bad) {
+    const float* largest = o.chunks + (int64_t)r * o.n_chunks;
+    for (int c = threadIdx.x; c - lane < o.n_chunks; c += LOSS_THREADS) best.offer(c < o.n_chunks ? largest[c] : -INFINITY, c, n);
+    join_lists(best, n, *s);
+    const float least = s->z[0][n - 1];
+    best.clear();
+    for (int i = 2 * wave; i < n; i += 2 * LOSS_WAVES) {
+      const int at = i + (lane >> 5);
+      const int64_t v = at < n && s->v[0][at] != INT32_MAX ? (int64_t)s->v[0][at] * CHUNK + (lane & 31) : vocab;
+      const float z = v < vocab ? open_logit<BF16>(a, q, v) : -INFINITY;
+      best.offer(z >= least ? z : -INFINITY, (int)v, n);
+    }
+    join_lists(best, n, *s);
+  }
+  if (wave == 0 && lane < n) {
+    const bool there = best.z > -INFINITY;
+    if (o.top_ids) o.top_ids[(int64_t)r * n + lane] = there ? best.v : -1;
+    if (o.top_logp) o.top_logp[(int64_t)r * n + lane] = bad ? __builtin_nanf("") : there ? (best.z - sum.m) * q.inv - ln_s : -INFINITY;
+  }
+}
+
+template <bool BF16, int G, bool TOP>
+__global__ __launch_bounds__(LOSS_THREADS) void logprob_kernel(LossArgs a, LossGrid grid, LogprobOut o) {
+  __shared__ Sums waves[LOSS_WAVES];
+  __shared__ TopLds lists;
+  const int r = blockIdx.x / grid.pieces, piece = blockIdx.x - r * grid.pieces, lane = threadIdx.x & 63;
+  const LossRow q = loss_row(a, r);
+  const int target = o.target ? o.target[r] : 0;
+  Sums mine = no_sums();
+  if (target != -1) {
+    const int64_t first = (int64_t)piece * grid.range, end = min(first + grid.range, (int64_t)a.l.d.vocab);
+    through<BF16, G>(a, q, first, end, [](int64_t) { return 0u; }, [&](const float* z, int64_t base) {
+      float top[G], all = -INFINITY;
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        top[g] = z[g * LANE_TOKENS];
+#pragma unroll
+        for (int e = 1; e < LANE_TOKENS; ++e) top[g] = fmaxf(top[g], z[g * LANE_TOKENS + e]);
+        all = fmaxf(all, top[g]);
+      }
+      take<G * LANE_TOKENS, true>(mine, z, all, q);
+      if (TOP) {
+        auto moved = [](float x, auto ctrl) {
+          const int w = __builtin_bit_cast(int, x);
+          return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(w, w, decltype(ctrl)::value, 0xF, 0xF, false));
+        };
+        float* to = o.chunks + (int64_t)r * o.n_chunks;
+        const int place = (int)(base / CHUNK) + (int)(threadIdx.x >> 2);
+#pragma unroll
+        for (int g = 0; g < G; ++g) {                // four adjacent lanes have a stretch
+          float t = fmaxf(top[g], moved(top[g], std::integral_constant<int, 0xB1>{}));
+          t = fmaxf(t, moved(t, std::integral_constant<int, 0x4E>{}));
+          const int c = place + g * (LOSS_TOKENS / CHUNK);
+          if ((lane & 3) == g % 4 && c < o.n_chunks) to[c] = t;
         }
       }
-    for (int k = 32; k; k >>= 1) {
-      const float y = __shfl_xor(z, k);
-      const int w = __shfl_xor(at, k);
-      if (before(y, w, z, at)) {
-        z = y;
-        at = w;
-      }
-    }
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) {
-      best_z[threadIdx.x >> 6] = z;
-      best_v[threadIdx.x >> 6] = at;
-    }
-    __syncthreads();
-    for (int w = 0; w < LOSS_WAVES; ++w)
-      if (before(best_z[w], best_v[w], z, at)) {
-        z = best_z[w];
-        at = best_v[w];
-      }
-    const bool there = z > -INFINITY;
-    last_z = z;
-    last_v = at;
-    if (threadIdx.x == 0) {
-      if (o.top_ids) o.top_ids[(int64_t)r * o.n_top + i] = there ? at : -1;
-      if (o.top_logp) o.top_logp[(int64_t)r * o.n_top + i] = bad ? __builtin_nanf("") : there ? (z - mine.m) * q.inv - ln_s : -INFINITY;
-    }
+    });
   }
+  const Sums sum = block_sums(mine, q, waves);
+  if (grid.pieces > 1) {
+    if (threadIdx.x == 0) o.parts[blockIdx.x] = sum;
+    return;
+  }
+  if (TOP) __threadfence_block();
+  finish_logprob<BF16>(a, o, q, r, target, sum, TOP ? &lists : nullptr);
 }
 
-template <bool BF16>
-__device__ __forceinline__ void put(void* to, int64_t at, float v) {
-  if (BF16) ((uint16_t*)to)[at] = (uint16_t)pack_bf16x2(v, 0.0f);
-  else ((float*)to)[at] = v;
+template <bool BF16, bool TOP>
+__global__ __launch_bounds__(LOSS_THREADS) void logprob_finish_kernel(LossArgs a, LossGrid grid, LogprobOut o) {
+  __shared__ TopLds lists;
+  const int r = blockIdx.x;
+  const LossRow q = loss_row(a, r);
+  Sums sum = no_sums();
+  for (int i = threadIdx.x & 63; i < grid.pieces; i += WAVE) join(sum, o.parts[(int64_t)r * grid.pieces + i], q);
+  sum = wave_sums(sum, q);
+  finish_logprob<BF16>(a, o, q, r, o.target ? o.target[r] : 0, sum, TOP ? &lists : nullptr);
 }
 
+// Writes the gradient of a group, in the logits' type.
 template <bool BF16>
-__global__ __launch_bounds__(LOSS_THREADS) void logprob_backward_kernel(LossArgs a, const int32_t* target, const float* stats, const float* g_logp,
-                                                                        const float* g_entropy, void* out, int64_t out_stride) {
-  const int r = blockIdx.x, vocab = a.l.d.vocab;
+__device__ __forceinline__ void put(char* to, const float* d, int64_t left) {
+  if (left >= LANE_TOKENS) {
+    if (BF16) {
+      const uint32_t w[4] = {pack_bf16x2(d[0], d[1]), pack_bf16x2(d[2], d[3]), pack_bf16x2(d[4], d[5]), pack_bf16x2(d[6], d[7])};
+      __builtin_memcpy(to, w, 16);
+    } else {
+      __builtin_memcpy(to, d, 32);
+    }
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < LANE_TOKENS; ++e)
+    if (e < left) {
+      if (BF16) ((uint16_t*)to)[e] = (uint16_t)pack_bf16x2(d[e], 0.0f);
+      else ((float*)to)[e] = d[e];
+    }
+}
+
+// The gradient is p (c0 + c1 (z - m)) with two numbers of the row, and g / T more at the target.
+template <bool BF16, int G>
+__global__ __launch_bounds__(LOSS_THREADS) void logprob_backward_kernel(LossArgs a, int pieces, const int32_t* target, const float* stats,
+                                                                        const float* g_logp, const float* g_entropy, void* out, int64_t out_stride) {
+  constexpr int ELT = BF16 ? 2 : 4;
+  const int r = blockIdx.x / pieces, piece = blockIdx.x - r * pieces;
+  const int64_t vocab = a.l.d.vocab, first = (int64_t)piece * (G * LOSS_TOKENS);
   const LossRow q = loss_row(a, r);
   const int t = target ? target[r] : 0;
   float g = g_logp ? g_logp[r] : 0.0f;
   const float ge = g_entropy ? g_entropy[r] : 0.0f;
-  const bool still = t == -1 || (g == 0.0f && ge == 0.0f);
-  if (g_logp && (t < 0 || t >= vocab)) g = __builtin_nanf("");
-  const float ln_s = stats[4ll * r + 1], h = stats[4ll * r + 2], m = stats[4ll * r + 3];
-  const float c0 = q.inv * (-g - ge * (h - ln_s)), c1 = -q.inv * ge * q.inv, at_target = q.inv * g;
-  for (int v = threadIdx.x; v < vocab; v += LOSS_THREADS) {
-    float d = 0.0f;
-    if (!still) {
-      const float z = open_logit<BF16>(a, q, v), x = fmaxf(z - m, q.lim);
-      if (z != -INFINITY) d = exp2_of(x * q.c - ln_s * LOG2E) * (c1 * x + c0) + (v == t ? at_target : 0.0f);
+  char* to = (char*)out + (int64_t)r * out_stride * ELT;
+  if (t == -1 || (g == 0.0f && ge == 0.0f)) {
+    const float nothing[LANE_TOKENS] = {};
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
+      const int64_t v = first + i * LOSS_TOKENS + threadIdx.x * LANE_TOKENS;
+      put<BF16>(to + v * ELT, nothing, vocab - v);
     }
-    put<BF16>(out, (int64_t)r * out_stride + v, d);
+    return;
   }
+  if (g_logp && (t < 0 || t >= vocab)) g = __builtin_nanf("");
+  const float4 s = *(const float4*)(stats + 4ll * r);
+  const float ln_s = s.y, h = s.z, m = s.w;
+  const float c0 = q.inv * (-g - ge * (h - ln_s)), c1 = -q.inv * ge * q.inv, at_target = q.inv * g, less = ln_s * LOG2E;
+  through<BF16, G>(a, q, first, min(first + G * LOSS_TOKENS, vocab), [](int64_t) { return 0u; }, [&](const float* z, int64_t base) {
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
+      const int64_t v = base + i * LOSS_TOKENS + threadIdx.x * LANE_TOKENS;
+      float d[LANE_TOKENS];
+#pragma unroll
+      for (int e = 0; e < LANE_TOKENS; ++e) {
+        const float x = fmaxf(z[i * LANE_TOKENS + e] - m, q.lim);
+        const float p = exp2_of(__builtin_fmaf(x, q.c, -less));
+        d[e] = p * __builtin_fmaf(c1, x, c0);
+        if (z[i * LANE_TOKENS + e] == -INFINITY) d[e] = 0.0f;
+      }
+      const int64_t at = t - v;
+      if (at >= 0 && at < LANE_TOKENS) {
+#pragma unroll
+        for (int e = 0; e < LANE_TOKENS; ++e)
+          if (e == at && z[i * LANE_TOKENS + e] != -INFINITY) d[e] += at_target;
+      }
+      put<BF16>(to + v * ELT, d, vocab - v);
+    }
+  });
 }
 
 // ---------------------------------------------------------------- distillation
 
-// Entry i of a row's list counts: its token exists, and no entry before it has the same.
-__device__ __forceinline__ bool first_of(const int32_t* ids, int i, int vocab) {
-  const int id = ids[i];
-  if (id < 0 || id >= vocab) return false;
-  for (int j = 0; j < i; ++j)
-    if (ids[j] == id) return false;
-  return true;
-}
-__device__ __forceinline__ bool is_listed(const int32_t* ids, int k, int v) {
-  for (int j = 0; j < k; ++j)
-    if (ids[j] == v) return true;
-  return false;
+constexpr int LIST_LANES = PG_DISTILL_MAX / WAVE;     // entries of a wave's lane
+constexpr int LIST_SLOTS = 4 * PG_DISTILL_MAX;       // a quarter full at most
+static_assert(LIST_SLOTS == 1 << 10 && PG_DISTILL_MAX == LOSS_THREADS, "ten bits of a hash, an entry a lane");
+constexpr int LIST_RANGE = 1 << 17;                  // tokens of a workgroup at most: one bit each in LDS
+
+// Which entries of a row's list count: the first of each token that exists.  A table of tokens in LDS with the first entry that has each.
+struct ListLds {
+  int token[LIST_SLOTS], first[LIST_SLOTS];
+};
+__device__ __forceinline__ uint32_t entries_that_count(const int* id, int k, int vocab, ListLds& s) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < LIST_SLOTS / WAVE; ++i) {
+    s.token[i * WAVE + lane] = -1;
+    s.first[i * WAVE + lane] = INT32_MAX;
+  }
+  wave_lds_sync();
+  int slot[LIST_LANES];
+#pragma unroll
+  for (int i = 0; i < LIST_LANES; ++i) {
+    slot[i] = -1;
+    const int at = i * WAVE + lane;
+    if (at < k && id[i] >= 0 && id[i] < vocab) {
+      int h = (int)((uint32_t)id[i] * 2654435761u >> 22);
+      for (int tries = 0; tries < LIST_SLOTS; ++tries, h = (h + 1) & (LIST_SLOTS - 1)) {
+        const int old = atomicCAS(&s.token[h], -1, id[i]);
+        if (old == -1 || old == id[i]) break;
+      }
+      slot[i] = h;
+      atomicMin(&s.first[h], at);
+    }
+  }
+  wave_lds_sync();
+  uint32_t count = 0;
+#pragma unroll
+  for (int i = 0; i < LIST_LANES; ++i)
+    if (slot[i] >= 0 && s.first[slot[i]] == i * WAVE + lane) count |= 1u << i;
+  return count;
 }
 
+__device__ __forceinline__ double lanes_sum(double v) {
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+__device__ __forceinline__ double lanes_max(double v) {
+  for (int o = 32; o; o >>= 1) v = fmax(v, __shfl_xor(v, o));
+  return v;
+}
+
+struct DistillArgs {
+  int mode, k;
+  const int32_t* ids;
+  const float* logp;
+  float *loss, *stats;
+  Sums* parts;                                       // [rows, pieces]
+};
+
+// From the sums over what is not listed to the loss: the lanes of one wave.  In fp64: it is a few hundred values, and what
+// is left over (1 - sum q, Q p_rest - q_rest) is a difference.
 template <bool BF16>
-__global__ __launch_bounds__(LOSS_THREADS) void distill_kernel(LossArgs a, int mode, const int32_t* teacher_ids, const float* teacher_logp, int k,
-                                                               float* loss, float* stats) {
-  __shared__ Sums waves[LOSS_WAVES];
-  const int r = blockIdx.x, vocab = a.l.d.vocab;
-  const LossRow q = loss_row(a, r);
-  const int32_t* ids = teacher_ids + (int64_t)r * k;
-  const float* t = teacher_logp + (int64_t)r * k;
-  Sums mine = no_sums();
-  for (int v = threadIdx.x; v < vocab; v += LOSS_THREADS)
-    if (!is_listed(ids, k, v)) take(mine, open_logit<BF16>(a, q, v), q);
-  const Sums rest = block_sums(mine, q, waves);
-  if (threadIdx.x) return;
-  double m = rest.m, most = -INFINITY;
-  int n = 0;
-  for (int i = 0; i < k; ++i)
-    if (first_of(ids, i, vocab)) {
-      ++n;
-      m = fmax(m, (double)open_logit<BF16>(a, q, ids[i]));
-      most = fmax(most, (double)t[i]);
+__device__ __forceinline__ void finish_distill(const LossArgs& a, const DistillArgs& o, const LossRow& q, int r, const Sums& rest, ListLds& s) {
+  const int lane = threadIdx.x & 63, vocab = a.l.d.vocab;
+  int id[LIST_LANES];
+  float t[LIST_LANES], z[LIST_LANES];
+#pragma unroll
+  for (int i = 0; i < LIST_LANES; ++i) {
+    const int at = i * WAVE + lane;
+    id[i] = at < o.k ? o.ids[(int64_t)r * o.k + at] : -1;
+    t[i] = at < o.k ? o.logp[(int64_t)r * o.k + at] : -INFINITY;
+    z[i] = id[i] >= 0 && id[i] < vocab ? open_logit<BF16>(a, q, id[i]) : -INFINITY;
+  }
+  const uint32_t count = entries_that_count(id, o.k, vocab, s);
+  float m = rest.m, most = -INFINITY;
+  bool wrong = false;
+#pragma unroll
+  for (int i = 0; i < LIST_LANES; ++i)
+    if (count >> i & 1) {
+      m = fmaxf(m, z[i]);
+      most = fmaxf(most, t[i]);
+      wrong |= !(t[i] < INFINITY);
     }
-  double s = rest.s * exp((rest.m - m) * q.inv), sum_q = 0.0, bad = 0.0;
-  for (int i = 0; i < k; ++i)
-    if (first_of(ids, i, vocab)) {
-      s += exp((open_logit<BF16>(a, q, ids[i]) - m) * q.inv);
-      if (!(t[i] < INFINITY)) bad = __builtin_nan("");
-      sum_q += exp(mode == PG_DISTILL_TOP ? t[i] - most : (double)t[i]);
+  m = lanes_max(m);
+  most = lanes_max(most);
+  const double bad = __ballot(wrong) ? __builtin_nan("") : 0.0;
+  const bool top = o.mode == PG_DISTILL_TOP;
+  double s_all = 0.0, sum_q = 0.0;
+#pragma unroll
+  for (int i = 0; i < LIST_LANES; ++i)
+    if (count >> i & 1) {
+      s_all += exp(((double)z[i] - m) * q.inv);
+      sum_q += exp(top ? (double)t[i] - most : (double)t[i]);
     }
-  const bool active = n && s != 0.0 && !(mode == PG_DISTILL_TOP && most == -INFINITY && bad == 0.0);
-  double total = 0.0, q_rest = 0.0, all = 0.0, t0 = 0.0, p_rest = 0.0;
+  const bool others = rest.s != 0.0f;
+  s_all = lanes_sum(s_all) + (others ? rest.s * exp(((double)rest.m - m) * q.inv) : 0.0);
+  sum_q = lanes_sum(sum_q);
+  const bool active = __ballot(count != 0) && s_all != 0.0 && !(top && most == -INFINITY && bad == 0.0);
+  double total = 0.0, q_rest = 0.0, p_rest = 0.0, all = 0.0, t0 = 0.0;
   if (active) {
-    t0 = mode == PG_DISTILL_TOP ? most + log(sum_q) : 0.0;
-    const double ln_rest = (rest.m - m) * q.inv + log((double)rest.s) - log(s);
-    if (rest.s != 0.0f) p_rest = exp(ln_rest);
-    if (mode == PG_DISTILL_TAIL && rest.s != 0.0f) q_rest = fmax(0.0, 1.0 - sum_q);
-    total = bad;
-    for (int i = 0; i < k; ++i)
-      if (first_of(ids, i, vocab)) {
+    const double ln_s = log(s_all), ln_rest = ((double)rest.m - m) * q.inv + log((double)rest.s) - ln_s;
+    t0 = top ? most + log(sum_q) : 0.0;
+    if (others) p_rest = exp(ln_rest);
+    if (!top && others) q_rest = fmax(0.0, 1.0 - sum_q);
+#pragma unroll
+    for (int i = 0; i < LIST_LANES; ++i)
+      if (count >> i & 1) {
         const double lq = t[i] - t0, w = exp(lq);
-        if (w > 0.0) total += w * (lq - ((open_logit<BF16>(a, q, ids[i]) - m) * q.inv - log(s)));
+        if (w > 0.0) total += w * (lq - (((double)z[i] - m) * q.inv - ln_s));
         all += w;
       }
+    total = lanes_sum(total) + bad;
+    all = lanes_sum(all) + q_rest + bad;
     if (q_rest > 0.0) total += q_rest * (log(q_rest) - ln_rest);
-    all += q_rest + bad;
   }
-  loss[r] = (float)total;
-  if (stats) {
-    float* x = stats + (int64_t)r * PG_DISTILL_STATS;
-    x[0] = (float)m;
-    x[1] = (float)log(s);
-    x[2] = rest.m;
-    x[3] = rest.s == 0.0f ? 0.0f : logf(rest.s);
-    x[4] = (float)(all * p_rest - q_rest);
-    x[5] = (float)t0;
-    x[6] = (float)all;
-    x[7] = active ? 1.0f : 0.0f;
+  if (lane) return;
+  o.loss[r] = (float)total;
+  if (o.stats) {
+    float4* x = (float4*)(o.stats + (int64_t)r * PG_DISTILL_STATS);
+    x[0] = float4{m, (float)log(s_all), rest.m, others ? logf(rest.s) : 0.0f};
+    x[1] = float4{(float)(all * p_rest - q_rest), (float)t0, (float)all, active ? 1.0f : 0.0f};
+  }
+}
+
+template <bool BF16, int G>
+__global__ __launch_bounds__(LOSS_THREADS) void distill_kernel(LossArgs a, LossGrid grid, DistillArgs o) {
+  __shared__ Sums waves[LOSS_WAVES];
+  extern __shared__ uint32_t listed[];               // a bit for each token of the range, or (the end) the table of the list
+  const int r = blockIdx.x / grid.pieces, piece = blockIdx.x - r * grid.pieces;
+  const LossRow q = loss_row(a, r);
+  const int64_t first = (int64_t)piece * grid.range, end = min(first + grid.range, (int64_t)a.l.d.vocab);
+  for (int i = threadIdx.x; i < (int)((end - first + 31) / 32); i += LOSS_THREADS) listed[i] = 0;
+  const int id = (int)threadIdx.x < o.k ? o.ids[(int64_t)r * o.k + threadIdx.x] : -1;
+  __syncthreads();
+  if (id >= first && id < end) atomicOr(&listed[(id - first) >> 5], 1u << ((id - first) & 31));
+  __syncthreads();
+  Sums mine = no_sums();
+  auto strike = [&](int64_t v) { return v < end ? (uint32_t)((const uint8_t*)listed)[(v - first) >> 3] : 0u; };
+  through<BF16, G>(a, q, first, end, strike, [&](const float* z, int64_t) {
+    float top = z[0];
+#pragma unroll
+    for (int e = 1; e < G * LANE_TOKENS; ++e) top = fmaxf(top, z[e]);
+    take<G * LANE_TOKENS, false>(mine, z, top, q);
+  });
+  const Sums rest = block_sums(mine, q, waves);
+  if (grid.pieces > 1) {
+    if (threadIdx.x == 0) o.parts[blockIdx.x] = rest;
+  } else {
+    __syncthreads();                                 // the bits have been read
+    if (threadIdx.x < WAVE) finish_distill<BF16>(a, o, q, r, rest, *(ListLds*)listed);
   }
 }
 
 template <bool BF16>
-__global__ __launch_bounds__(LOSS_THREADS) void distill_backward_kernel(LossArgs a, const int32_t* teacher_ids, const float* teacher_logp, int k,
-                                                                        const float* stats, const float* g_loss, void* out, int64_t out_stride) {
-  const int r = blockIdx.x, vocab = a.l.d.vocab;
+__global__ __launch_bounds__(WAVE) void distill_finish_kernel(LossArgs a, LossGrid grid, DistillArgs o) {
+  __shared__ ListLds list;
+  const int r = blockIdx.x;
   const LossRow q = loss_row(a, r);
-  const int32_t* ids = teacher_ids + (int64_t)r * k;
-  const float* x = stats + (int64_t)r * PG_DISTILL_STATS;
-  const float g = x[7] == 0.0f ? 0.0f : g_loss[r], scale = g * q.inv;
-  for (int v = threadIdx.x; v < vocab; v += LOSS_THREADS) {
-    float d = 0.0f;
-    const float z = g != 0.0f ? open_logit<BF16>(a, q, v) : -INFINITY;
-    if (z != -INFINITY) {
-      int at = -1;
-      for (int j = k - 1; j >= 0; --j) at = ids[j] == v ? j : at;
-      d = at < 0 ? scale * x[4] * exp2_of(fmaxf(z - x[2], q.lim) * q.c - x[3] * LOG2E)
-                 : scale * (x[6] * exp2_of(fmaxf(z - x[0], q.lim) * q.c - x[1] * LOG2E) - expf(teacher_logp[(int64_t)r * k + at] - x[5]));
+  Sums rest = no_sums();
+  for (int i = threadIdx.x; i < grid.pieces; i += WAVE) join(rest, o.parts[(int64_t)r * grid.pieces + i], q);
+  finish_distill<BF16>(a, o, q, r, wave_sums(rest, q), list);
+}
+
+// What is not listed has the gradient g / T (Q p_rest - q_rest) of its share of p_rest; a listed token is written by the lane that holds its
+// entry, and by no other.
+template <bool BF16, int G>
+__global__ __launch_bounds__(LOSS_THREADS) void distill_backward_kernel(LossArgs a, int pieces, DistillArgs o, const float* g_loss, void* out,
+                                                                        int64_t out_stride) {
+  constexpr int ELT = BF16 ? 2 : 4, RANGE = G * LOSS_TOKENS;
+  __shared__ uint32_t listed[RANGE / 32];
+  __shared__ int token[PG_DISTILL_MAX];
+  __shared__ int twice;
+  const int r = blockIdx.x / pieces, piece = blockIdx.x - r * pieces;
+  const int64_t vocab = a.l.d.vocab, first = (int64_t)piece * RANGE, end = min(first + RANGE, vocab);
+  const LossRow q = loss_row(a, r);
+  const float4 s0 = ((const float4*)(o.stats + (int64_t)r * PG_DISTILL_STATS))[0], s1 = ((const float4*)(o.stats + (int64_t)r * PG_DISTILL_STATS))[1];
+  const float g = s1.w == 0.0f ? 0.0f : g_loss[r];
+  char* to = (char*)out + (int64_t)r * out_stride * ELT;
+  if (g == 0.0f) {
+    const float nothing[LANE_TOKENS] = {};
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
+      const int64_t v = first + i * LOSS_TOKENS + threadIdx.x * LANE_TOKENS;
+      put<BF16>(to + v * ELT, nothing, vocab - v);
     }
-    put<BF16>(out, (int64_t)r * out_stride + v, d);
+    return;
   }
+  const bool entry = (int)threadIdx.x < o.k;
+  const int id = entry ? o.ids[(int64_t)r * o.k + threadIdx.x] : -1;
+  const float t = entry ? o.logp[(int64_t)r * o.k + threadIdx.x] : 0.0f;
+  const bool mine = id >= first && id < end;
+  const float scale = g * q.inv;
+  if (threadIdx.x < RANGE / 32) listed[threadIdx.x] = 0;
+  if (threadIdx.x == 0) twice = 0;
+  token[threadIdx.x] = id;
+  __syncthreads();
+  if (mine) {
+    const uint32_t bit = 1u << ((id - first) & 31);
+    if (atomicOr(&listed[(id - first) >> 5], bit) & bit) twice = 1;
+  }
+  __syncthreads();
+  bool writes = mine;
+  if (twice && mine)
+    for (int i = 0; i < (int)threadIdx.x; ++i) writes &= token[i] != id;       // the first of equal ids counts
+  if (writes) {
+    const float z = open_logit<BF16>(a, q, id);
+    const float p = exp2_of(__builtin_fmaf(fmaxf(z - s0.x, q.lim), q.c, -s0.y * LOG2E));
+    const float d = z == -INFINITY ? 0.0f : scale * (s1.z * p - expf(t - s1.y));
+    if (BF16) ((uint16_t*)to)[id] = (uint16_t)pack_bf16x2(d, 0.0f);
+    else ((float*)to)[id] = d;
+  }
+  const float c = scale * s1.x, less = s0.w * LOG2E;
+  auto strike = [&](int64_t v) { return v < end ? (uint32_t)((const uint8_t*)listed)[(v - first) >> 3] : 0u; };
+  through<BF16, G>(a, q, first, end, strike, [&](const float* z, int64_t base) {
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
+      const int64_t v = base + i * LOSS_TOKENS + threadIdx.x * LANE_TOKENS;
+      float d[LANE_TOKENS];
+#pragma unroll
+      for (int e = 0; e < LANE_TOKENS; ++e) {
+        const float x = z[i * LANE_TOKENS + e];
+        d[e] = c * exp2_of(__builtin_fmaf(fmaxf(x - s0.z, q.lim), q.c, -less));
+        if (x == -INFINITY) d[e] = 0.0f;
+      }
+      const uint32_t others = strike(v);
+      if (!others) {
+        put<BF16>(to + v * ELT, d, vocab - v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < LANE_TOKENS; ++e)
+          if (v + e < vocab && !(others >> e & 1)) {
+            if (BF16) ((uint16_t*)to)[v + e] = (uint16_t)pack_bf16x2(d[e], 0.0f);
+            else ((float*)to)[v + e] = d[e];
+          }
+      }
+    }
+  });
 }
 
 // ---------------------------------------------------------------- the clipped objective
@@ -307,47 +671,91 @@ struct SurrogateArgs {
   float at_lo, at_hi, kl_coef;
   float *objective, *kl, *g_logp;
   int32_t* clipped;
+  int pieces, piece;                                 // workgroups of a sequence, tokens of each but the last
+  float* parts;                                      // [sequences, pieces, 4]
 };
 
+// What a sequence's sums give.
+__device__ __forceinline__ void finish_surrogate(const SurrogateArgs& a, int r, int n, double sum, double kl, int cuts) {
+  const float w = a.weight ? a.weight[r] : 1.0f / (float)max(n, 1);
+  if (a.objective) a.objective[r] = n ? (float)(w * sum) : 0.0f;
+  if (a.kl) a.kl[r] = (float)(kl / max(n, 1));
+  if (a.clipped) a.clipped[r] = cuts;
+}
+
 __global__ __launch_bounds__(LOSS_THREADS) void surrogate_tokens_kernel(SurrogateArgs a) {
-  __shared__ double sums[2][LOSS_THREADS];
-  __shared__ int counts[LOSS_THREADS];
-  const int r = blockIdx.x;
+  __shared__ float sums[LOSS_WAVES][2];
+  __shared__ int counts[LOSS_WAVES];
+  const int r = blockIdx.x / a.pieces, piece = blockIdx.x - r * a.pieces;
   const int from = min(max(a.cu[r], 0), a.n_tokens), to = min(max(a.cu[r + 1], from), a.n_tokens), n = to - from;
   const float A = a.adv[r], w = a.weight ? a.weight[r] : 1.0f / (float)max(n, 1);
-  double sum = 0.0, kl = 0.0;
+  const int64_t first = from + (int64_t)piece * a.piece, end = piece + 1 < a.pieces ? min(first + a.piece, (int64_t)to) : to;
+  float sum = 0.0f, kl = 0.0f;
   int cuts = 0;
-  for (int i = from + threadIdx.x; i < to; i += LOSS_THREADS) {
+  for (int64_t i = first + threadIdx.x; i < end; i += LOSS_THREADS) {
     const float l = a.logp[i];
     const double d = (double)l - (double)a.old[i];
     const bool cut = A > 0.0f ? d > a.hi : A < 0.0f && d < a.lo;
     const float ra = A == 0.0f ? 0.0f : expf((float)d) * A;
     float g = cut ? 0.0f : ra, value = cut ? (A > 0.0f ? a.at_hi : a.at_lo) * A : ra;
     if (a.ref) {
+      // e^x - x - 1: near 0 x^2 / 2 (1 + x / 3 (1 + x / 4 (...))), whose terms past the eighth are 2^-26 of it at x = 1/2
       const float x = a.ref[i] - l;
-      const double e = expm1((double)x);
-      const float k = (float)(e - x);
+      float k = 1.0f;
+#pragma unroll
+      for (int j = 10; j > 2; --j) k = __builtin_fmaf(k, x * (1.0f / j), 1.0f);
+      k *= 0.5f * x * x;
+      float slope = k + x;
+      if (!(fabsf(x) < 0.5f)) {
+        const float e = expf(x);
+        k = e == INFINITY ? e : e - x - 1.0f;
+        slope = e - 1.0f;
+      }
       kl += k;
       value -= a.kl_coef * k;
-      g += a.kl_coef * (float)e;
+      g += a.kl_coef * slope;
     }
     sum += value;
     cuts += cut;
     if (a.g_logp) a.g_logp[i] = w * g;
   }
-  sums[0][threadIdx.x] = sum;
-  sums[1][threadIdx.x] = kl;
-  counts[threadIdx.x] = cuts;
+  sum = wave_allsum(sum);
+  kl = wave_allsum(kl);
+  for (int o = 32; o; o >>= 1) cuts += __shfl_xor(cuts, o);
+  if ((threadIdx.x & 63) == 0) {
+    sums[threadIdx.x >> 6][0] = sum;
+    sums[threadIdx.x >> 6][1] = kl;
+    counts[threadIdx.x >> 6] = cuts;
+  }
   __syncthreads();
   if (threadIdx.x) return;
-  for (int i = 1; i < LOSS_THREADS; ++i) {
-    sum += sums[0][i];
-    kl += sums[1][i];
+  double all = 0.0, all_kl = 0.0;
+  cuts = 0;
+#pragma unroll
+  for (int i = 0; i < LOSS_WAVES; ++i) {
+    all += sums[i][0];
+    all_kl += sums[i][1];
     cuts += counts[i];
   }
-  if (a.objective) a.objective[r] = (float)(w * sum);
-  if (a.kl) a.kl[r] = (float)(kl / max(n, 1));
-  if (a.clipped) a.clipped[r] = cuts;
+  if (a.pieces == 1) finish_surrogate(a, r, n, all, all_kl, cuts);
+  else *(float4*)(a.parts + 4ll * blockIdx.x) = float4{(float)all, (float)all_kl, __builtin_bit_cast(float, cuts), 0.0f};
+}
+
+__global__ __launch_bounds__(WAVE) void surrogate_finish_kernel(SurrogateArgs a) {
+  const int r = blockIdx.x;
+  const int from = min(max(a.cu[r], 0), a.n_tokens), n = min(max(a.cu[r + 1], from), a.n_tokens) - from;
+  double sum = 0.0, kl = 0.0;
+  int cuts = 0;
+  for (int i = threadIdx.x; i < a.pieces; i += WAVE) {
+    const float4 p = *(const float4*)(a.parts + 4 * ((int64_t)r * a.pieces + i));
+    sum += p.x;
+    kl += p.y;
+    cuts += __builtin_bit_cast(int, p.z);
+  }
+  sum = lanes_sum(sum);
+  kl = lanes_sum(kl);
+  for (int o = 32; o; o >>= 1) cuts += __shfl_xor(cuts, o);
+  if (threadIdx.x == 0) finish_surrogate(a, r, n, sum, kl, cuts);
 }
 
 // ---------------------------------------------------------------- host side
@@ -369,13 +777,39 @@ static pg_status check_gradient(const LossArgs& a, const void* out, int64_t out_
   return PG_OK;
 }
 
-// launches F<bf16>
-#define PG_LOSS_KERNEL(F, grid, ...)                                                                            \
-  do {                                                                                                          \
-    if (a.l.d.dtype == PG_LOGITS_BF16) F<true><<<dim3(grid), dim3(LOSS_THREADS), 0, (hipStream_t)stream>>>(__VA_ARGS__); \
-    else F<false><<<dim3(grid), dim3(LOSS_THREADS), 0, (hipStream_t)stream>>>(__VA_ARGS__);                     \
-    PG_LAUNCH_CHECK(#F);                                                                                        \
+static int64_t stretches_of(int64_t vocab) { return (vocab + LOSS_TOKENS - 1) / LOSS_TOKENS; }
+
+// Workgroups of a pass over the logits: as many as fill the chip a few times over; what a row's finish has to join stays short.
+constexpr int64_t LOSS_WORKGROUPS = 4096;
+static LossGrid loss_grid(int64_t rows, int64_t vocab) {
+  const int64_t stretches = stretches_of(vocab);
+  const int groups = rows * ((stretches + 3) / 4) >= 1024 ? 4 : 1;
+  const int64_t passes = (stretches + groups - 1) / groups, each = std::max<int64_t>(1, LOSS_WORKGROUPS / rows);
+  const int64_t per = std::min<int64_t>((passes + each - 1) / each, LIST_RANGE / (groups * LOSS_TOKENS));
+  return LossGrid{groups, (int)(per * groups * LOSS_TOKENS), (int)((passes + per - 1) / per)};
+}
+// No fewer than any call of at most so many rows and tokens has: a row has no more than its share of LOSS_WORKGROUPS, or one for LIST_RANGE tokens.
+static int64_t most_parts(int64_t rows, int64_t vocab) {
+  return std::min(rows * stretches_of(vocab), std::max(LOSS_WORKGROUPS, rows * ((vocab + LIST_RANGE - 1) / LIST_RANGE)));
+}
+static int n_chunks(int64_t vocab) { return (int)((vocab + CHUNK - 1) / CHUNK); }
+static int64_t part_floats(int64_t rows, int64_t vocab) { return (most_parts(rows, vocab) * (int64_t)(sizeof(Sums) / sizeof(float)) + 3) / 4 * 4; }
+
+// launches F<bf16, ...> with `lds` bytes
+#define PG_LOSS_LAUNCH(blocks, threads, lds, F, ...)                                                         \
+  do {                                                                                                       \
+    F<<<dim3((unsigned)(blocks)), dim3(threads), lds, (hipStream_t)stream>>>(__VA_ARGS__);                   \
+    PG_LAUNCH_CHECK(#F);                                                                                     \
   } while (0)
+
+// f(whether the logits are bf16, groups a lane takes at a time), as types
+template <class F>
+static pg_status with_kind(const LossArgs& a, int groups, F f) {
+  const auto four = std::integral_constant<int, 4>{};
+  const auto one = std::integral_constant<int, 1>{};
+  if (a.l.d.dtype == PG_LOGITS_BF16) return groups == 4 ? f(std::true_type{}, four) : f(std::true_type{}, one);
+  return groups == 4 ? f(std::false_type{}, four) : f(std::false_type{}, one);
+}
 
 }  // namespace pg
 
@@ -383,7 +817,7 @@ using namespace pg;
 
 extern "C" int64_t pg_logprob_scratch_floats(int32_t rows, int32_t vocab, int32_t n_top) {
   if (rows < 1 || vocab < 1 || n_top < 0) return 0;
-  return 0;
+  return part_floats(rows, vocab) + (n_top ? (int64_t)rows * n_chunks(vocab) : 0);
 }
 
 extern "C" pg_status pg_token_logprobs(const pg_logits* desc, const float* temperature, const int32_t* target, float* logp, float* entropy,
@@ -391,25 +825,47 @@ extern "C" pg_status pg_token_logprobs(const pg_logits* desc, const float* tempe
   LossArgs a{};
   PG_TRY(loss_args(desc, temperature, "pg_token_logprobs", a));
   if (n_top < 0 || n_top > PG_TOP_MAX) return fail(n_top < 0 ? PG_EINVAL : PG_ESHAPE, "pg_token_logprobs: %d alternatives (at most %d)", n_top, PG_TOP_MAX);
-  if (a.l.d.rows == 0) return PG_OK;
+  const int64_t rows = a.l.d.rows;
+  if (rows == 0) return PG_OK;
   if (logp && !target) return fail(PG_EINVAL, "pg_token_logprobs: logp without targets");
   if ((uintptr_t)stats & 15) return fail(PG_ESHAPE, "pg_token_logprobs: stats are not 16-byte aligned");
-  const LogprobOut o{target, logp, entropy, stats, n_top, top_ids, top_logp};
-  PG_LOSS_KERNEL(logprob_kernel, (unsigned)a.l.d.rows, a, o);
-  return PG_OK;
+  if (!scratch) return fail(PG_EINVAL, "pg_token_logprobs: scratch is NULL");
+  if ((uintptr_t)scratch & 7) return fail(PG_ESHAPE, "pg_token_logprobs: scratch is not 8-byte aligned");
+  const LossGrid g = loss_grid(rows, a.l.d.vocab);
+  const bool top = n_top && (top_ids || top_logp);
+  const LogprobOut o{target, logp, entropy, stats, n_top, top_ids, top_logp, (Sums*)scratch, scratch + part_floats(rows, a.l.d.vocab), n_chunks(a.l.d.vocab)};
+  return with_kind(a, g.groups, [&](auto bf, auto groups) {
+    constexpr bool BF = decltype(bf)::value;
+    constexpr int G = decltype(groups)::value;
+    if (top) PG_LOSS_LAUNCH(rows * g.pieces, LOSS_THREADS, 0, (logprob_kernel<BF, G, true>), a, g, o);
+    else PG_LOSS_LAUNCH(rows * g.pieces, LOSS_THREADS, 0, (logprob_kernel<BF, G, false>), a, g, o);
+    if (g.pieces == 1) return PG_OK;
+    if (top) PG_LOSS_LAUNCH(rows, LOSS_THREADS, 0, (logprob_finish_kernel<BF, true>), a, g, o);
+    else PG_LOSS_LAUNCH(rows, WAVE, 0, (logprob_finish_kernel<BF, false>), a, g, o);
+    return PG_OK;
+  });
 }
+
+// A gradient's workgroup takes four groups a lane once, or (few rows) one.
+static int gradient_groups(int64_t rows, int64_t vocab) { return rows * ((stretches_of(vocab) + 3) / 4) >= 1024 ? 4 : 1; }
 
 extern "C" pg_status pg_token_logprobs_backward(const pg_logits* desc, const float* temperature, const int32_t* target, const float* stats,
                                                 const float* g_logp, const float* g_entropy, void* d_logits, int64_t d_stride, void* stream) {
   LossArgs a{};
   PG_TRY(loss_args(desc, temperature, "pg_token_logprobs_backward", a));
-  if (a.l.d.rows == 0) return PG_OK;
+  const int64_t rows = a.l.d.rows;
+  if (rows == 0) return PG_OK;
   if (!stats) return fail(PG_EINVAL, "pg_token_logprobs_backward: stats is NULL");
   if ((uintptr_t)stats & 15) return fail(PG_ESHAPE, "pg_token_logprobs_backward: stats are not 16-byte aligned");
   if (g_logp && !target) return fail(PG_EINVAL, "pg_token_logprobs_backward: a gradient of log-probs without targets");
   PG_TRY(check_gradient(a, d_logits, d_stride, "pg_token_logprobs_backward"));
-  PG_LOSS_KERNEL(logprob_backward_kernel, (unsigned)a.l.d.rows, a, target, stats, g_logp, g_entropy, d_logits, d_stride);
-  return PG_OK;
+  return with_kind(a, gradient_groups(rows, a.l.d.vocab), [&](auto bf, auto groups) {
+    constexpr int G = decltype(groups)::value;
+    const int pieces = (int)((stretches_of(a.l.d.vocab) + G - 1) / G);
+    PG_LOSS_LAUNCH(rows * pieces, LOSS_THREADS, 0, (logprob_backward_kernel<decltype(bf)::value, G>), a, pieces, target, stats, g_logp, g_entropy, d_logits,
+                   d_stride);
+    return PG_OK;
+  });
 }
 
 static pg_status distill_args(const LossArgs& a, const int32_t* ids, const float* logp, int32_t k, const float* stats, const char* who) {
@@ -420,10 +876,7 @@ static pg_status distill_args(const LossArgs& a, const int32_t* ids, const float
   return PG_OK;
 }
 
-extern "C" int64_t pg_distill_scratch_floats(int32_t rows, int32_t vocab) {
-  if (rows < 1 || vocab < 1) return 0;
-  return 0;
-}
+extern "C" int64_t pg_distill_scratch_floats(int32_t rows, int32_t vocab) { return rows < 1 || vocab < 1 ? 0 : part_floats(rows, vocab); }
 
 extern "C" pg_status pg_distill_loss(const pg_logits* desc, const float* temperature, int32_t mode, const int32_t* teacher_ids,
                                      const float* teacher_logp, int32_t k, float* loss, float* stats, float* scratch, void* stream) {
@@ -431,10 +884,19 @@ extern "C" pg_status pg_distill_loss(const pg_logits* desc, const float* tempera
   PG_TRY(loss_args(desc, temperature, "pg_distill_loss", a));
   if (mode != PG_DISTILL_TOP && mode != PG_DISTILL_TAIL) return fail(PG_EINVAL, "pg_distill_loss: mode %d", mode);
   PG_TRY(distill_args(a, teacher_ids, teacher_logp, k, stats, "pg_distill_loss"));
-  if (a.l.d.rows == 0) return PG_OK;
-  if (!loss) return fail(PG_EINVAL, "pg_distill_loss: loss is NULL");
-  PG_LOSS_KERNEL(distill_kernel, (unsigned)a.l.d.rows, a, mode, teacher_ids, teacher_logp, k, loss, stats);
-  return PG_OK;
+  const int64_t rows = a.l.d.rows;
+  if (rows == 0) return PG_OK;
+  if (!loss || !scratch) return fail(PG_EINVAL, "pg_distill_loss: null pointer");
+  if ((uintptr_t)scratch & 7) return fail(PG_ESHAPE, "pg_distill_loss: scratch is not 8-byte aligned");
+  const LossGrid g = loss_grid(rows, a.l.d.vocab);
+  const DistillArgs o{mode, k, teacher_ids, teacher_logp, loss, stats, (Sums*)scratch};
+  const size_t lds = std::max<size_t>(std::min<int64_t>(g.range, (a.l.d.vocab + 31) / 32 * 32) / 8, g.pieces == 1 ? sizeof(ListLds) : 0);
+  return with_kind(a, g.groups, [&](auto bf, auto groups) {
+    constexpr bool BF = decltype(bf)::value;
+    PG_LOSS_LAUNCH(rows * g.pieces, LOSS_THREADS, lds, (distill_kernel<BF, decltype(groups)::value>), a, g, o);
+    if (g.pieces > 1) PG_LOSS_LAUNCH(rows, WAVE, 0, distill_finish_kernel<BF>, a, g, o);
+    return PG_OK;
+  });
 }
 
 extern "C" pg_status pg_distill_backward(const pg_logits* desc, const float* temperature, const int32_t* teacher_ids, const float* teacher_logp,
@@ -442,16 +904,29 @@ extern "C" pg_status pg_distill_backward(const pg_logits* desc, const float* tem
   LossArgs a{};
   PG_TRY(loss_args(desc, temperature, "pg_distill_backward", a));
   PG_TRY(distill_args(a, teacher_ids, teacher_logp, k, stats, "pg_distill_backward"));
-  if (a.l.d.rows == 0) return PG_OK;
+  const int64_t rows = a.l.d.rows;
+  if (rows == 0) return PG_OK;
   if (!stats || !g_loss) return fail(PG_EINVAL, "pg_distill_backward: null pointer");
   PG_TRY(check_gradient(a, d_logits, d_stride, "pg_distill_backward"));
-  PG_LOSS_KERNEL(distill_backward_kernel, (unsigned)a.l.d.rows, a, teacher_ids, teacher_logp, k, stats, g_loss, d_logits, d_stride);
-  return PG_OK;
+  const DistillArgs o{0, k, teacher_ids, teacher_logp, nullptr, const_cast<float*>(stats), nullptr};
+  return with_kind(a, gradient_groups(rows, a.l.d.vocab), [&](auto bf, auto groups) {
+    constexpr int G = decltype(groups)::value;
+    const int pieces = (int)((stretches_of(a.l.d.vocab) + G - 1) / G);
+    PG_LOSS_LAUNCH(rows * pieces, LOSS_THREADS, 0, (distill_backward_kernel<decltype(bf)::value, G>), a, pieces, o, g_loss, d_logits, d_stride);
+    return PG_OK;
+  });
+}
+
+// A sequence of up to 4096 tokens is one workgroup's; longer ones are cut into pieces of 1024 tokens or more, some 4096 in all.
+constexpr int64_t SURROGATE_WHOLE = 4096, SURROGATE_PIECE = 1024, SURROGATE_WORKGROUPS = 4096;
+static int64_t surrogate_pieces(int64_t n_seq, int64_t max_len) {
+  if (max_len <= SURROGATE_WHOLE) return 1;
+  return std::min((max_len + SURROGATE_PIECE - 1) / SURROGATE_PIECE, std::max<int64_t>(1, SURROGATE_WORKGROUPS / n_seq));
 }
 
 extern "C" int64_t pg_surrogate_scratch_floats(int32_t n_seq, int32_t max_len) {
-  if (n_seq < 1 || max_len < 1) return 0;
-  return 0;
+  if (n_seq < 1 || max_len <= SURROGATE_WHOLE) return 0;
+  return 4 * std::min<int64_t>(n_seq * ((max_len + SURROGATE_PIECE - 1) / SURROGATE_PIECE), SURROGATE_WORKGROUPS);
 }
 
 extern "C" pg_status pg_token_surrogate(const float* logp, const float* logp_old, const float* logp_ref, const float* adv, const float* weight,
@@ -464,9 +939,12 @@ extern "C" pg_status pg_token_surrogate(const float* logp, const float* logp_old
     return fail(PG_EINVAL, "pg_token_surrogate: clip %g below and %g above, kl_coef %g", clip_low, clip_high, kl_coef);
   if (n_seq == 0) return PG_OK;
   if (!adv || !cu || (n_tokens && (!logp || !logp_old))) return fail(PG_EINVAL, "pg_token_surrogate: null pointer");
+  const int pieces = (int)surrogate_pieces(n_seq, max_len);
+  if (pieces > 1 && !scratch) return fail(PG_EINVAL, "pg_token_surrogate: scratch is NULL");
+  if (pieces > 1 && (uintptr_t)scratch & 15) return fail(PG_ESHAPE, "pg_token_surrogate: scratch is not 16-byte aligned");
   const SurrogateArgs a{logp, logp_old, logp_ref, adv, weight, cu, n_tokens, std::log1p(-clip_low), std::log1p(clip_high), (float)(1.0 - clip_low),
-                        (float)(1.0 + clip_high), (float)kl_coef, objective, kl, g_logp, clipped};
-  surrogate_tokens_kernel<<<dim3((unsigned)n_seq), dim3(LOSS_THREADS), 0, (hipStream_t)stream>>>(a);
-  PG_LAUNCH_CHECK("surrogate_tokens_kernel");
+                        (float)(1.0 + clip_high), (float)kl_coef, objective, kl, g_logp, clipped, pieces, (int)(((int64_t)max_len + pieces - 1) / pieces), scratch};
+  PG_LOSS_LAUNCH((int64_t)n_seq * pieces, LOSS_THREADS, 0, surrogate_tokens_kernel, a);
+  if (pieces > 1) PG_LOSS_LAUNCH(n_seq, WAVE, 0, surrogate_finish_kernel, a);
   return PG_OK;
 }
