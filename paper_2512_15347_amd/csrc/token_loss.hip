@@ -1,8 +1,8 @@
 // What a token policy learns from: log-probs of given tokens with entropy and alternatives, the divergence from a teacher's most likely
 // tokens, the clipped objective of sequences, and their gradients.
 //
-// Of a row only three sums are needed, all relative to its largest logit m: S = sum exp((z - m) / T), U = sum exp((z - m) / T) (z - m) and, where a
-// teacher's list is compared, S over the tokens that are not on it.  Then ln p = (z - m) / T - ln S and the entropy is ln S - U / (S T), a
+// Of a row only three sums are needed, all relative to its largest logit m: S = sum exp((z - m) / T), U = sum exp((z - m) / T) (z - m) / T and, where
+// a teacher's list is compared, S over the tokens that are not on it.  Then ln p = (z - m) / T - ln S and the entropy is ln S - U / S, a
 // sum of terms of one sign.  Differences to m are exact where it matters, so that a row may be shifted by any amount; m and ln S are kept apart
 // for the backward pass for the same reason.
 #include <algorithm>
@@ -18,7 +18,7 @@ namespace pg {
 constexpr int LOSS_THREADS = 256;
 constexpr int LOSS_WAVES = LOSS_THREADS / WAVE;
 constexpr int LOSS_TOKENS = LOSS_THREADS * LANE_TOKENS;                 // one group a lane
-constexpr float FAR = 200.0f;                        // exp(-FAR) is 0 in fp32
+constexpr float FAR = 300.0f;                        // 2^-FAR is 0 in fp32
 
 struct LossArgs {
   LogitArgs l;
@@ -28,23 +28,26 @@ struct LossArgs {
 // What one row needs.
 struct LossRow {
   int64_t at;                                        // its first logit
+  int shift;                                         // slot t, of which eight are 16 aligned bytes, has token t - shift
   const uint8_t* allow;                              // bit v % 8 of byte v / 8; NULL: `unmasked` for all of them
   uint32_t unmasked;
   float inv;                                         // 1 / temperature, NaN for one that is no temperature
   float c;                                           // the same in base 2
-  float lim;                                         // z - m below which p is 0
+  float lim;                                         // z - m below which p is 0: (z - m) c < -FAR
 };
+template <bool BF16>
 __device__ __forceinline__ LossRow loss_row(const LossArgs& a, int r) {
   const pg_logits& d = a.l.d;
   LossRow q;
   q.at = (int64_t)r * d.stride;
+  q.shift = BF16 ? (int)((uintptr_t)d.logits / 2 + (uint64_t)q.at) & (LANE_TOKENS - 1) : 0;
   const int mask = d.allow_row ? d.allow_row[r] : r;
   q.allow = d.allow && mask >= 0 && mask < d.n_masks ? (const uint8_t*)(d.allow + (int64_t)mask * a.l.words) : nullptr;
   q.unmasked = d.allow && mask != -1 ? 0u : 0xFFu;   // an index that no mask has allows nothing
   const float t = a.temperature ? a.temperature[r] : 1.0f;
   q.inv = !(t >= 0.0f && t < INFINITY) ? __builtin_nanf("") : t == 0.0f ? 1.0f : 1.0f / t;
   q.c = q.inv * LOG2E;
-  q.lim = -FAR * (t > 0.0f && t < INFINITY ? t : 1.0f);
+  q.lim = -FAR * LN2 * (t > 0.0f && t < INFINITY ? t : 1.0f);
   return q;
 }
 __device__ __forceinline__ bool allowed(const LossRow& q, int64_t v) { return (q.allow ? (uint32_t)q.allow[v >> 3] : q.unmasked) >> (v & 7) & 1; }
@@ -58,15 +61,15 @@ __device__ __forceinline__ float open_logit(const LossArgs& a, const LossRow& q,
   return allowed(q, v) ? logit_at<BF16>(a, q, v) : -INFINITY;
 }
 
-// Sums of a lane, a wave or a range; NaN in s once a logit was NaN or +inf.
+// Sums of a lane, a wave or a range, with x = (z - m) c in base 2: s = sum 2^x, u = sum 2^x x; NaN in s once a logit was NaN or +inf.
 struct Sums {
   float m, s, u;
 };
 __device__ __forceinline__ Sums no_sums() { return Sums{-FLT_MAX, 0.0f, 0.0f}; }
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ void move_to(Sums& a, float m, const LossRow& q) {
-  const float t = a.m - m, f = exp2_of(t * q.c);
-  a.u = f * (a.u + fmaxf(t, q.lim) * a.s);
+  const float x = (a.m - m) * q.c, f = exp2_of(x);
+  a.u = f * (a.u + fmaxf(x, -FAR) * a.s);
   a.s = f * a.s;
   a.m = m;
 }
@@ -97,88 +100,166 @@ __device__ __forceinline__ Sums block_sums(Sums a, const LossRow& q, Sums* waves
   return a;
 }
 
-// A lane's group of eight tokens, from any address that is a multiple of their size (the hardware takes unaligned 16-byte loads).
-template <bool BF16>
-struct Lot {
-  uint32_t raw[BF16 ? 4 : 8];
-  __device__ __forceinline__ void load(const char* p) { __builtin_memcpy(raw, p, BF16 ? 16 : 32); }
-  __device__ __forceinline__ void load(const char* p, int64_t left) {
-    if (left >= LANE_TOKENS) return load(p);
-#pragma unroll
-    for (int e = 0; e < LANE_TOKENS; ++e) {
-      const uint32_t x = e >= left ? 0u : BF16 ? ((const uint16_t*)p)[e] : ((const uint32_t*)p)[e];
-      if (!BF16) raw[e] = x;
-      else raw[e >> 1] = e & 1 ? raw[e >> 1] | x << 16 : x;
-    }
-  }
-  __device__ __forceinline__ float logit(int e) const {
-    return __builtin_bit_cast(float, !BF16 ? raw[e] : e & 1 ? raw[e >> 1] & 0xFFFF0000u : raw[e >> 1] << 16);
-  }
-};
-__device__ __forceinline__ uint32_t up_to(int64_t left) { return left >= LANE_TOKENS ? 0xFFu : left <= 0 ? 0u : (1u << left) - 1; }
+// A lane's part of one pass over a range: G groups of eight slots and which of their tokens count: those that are in the row and in the range,
+// allowed and not struck out.  16-byte loads may be unaligned, but in bf16, where a row may begin between two 4-byte words, they are a third
+// slower then (4096 x 131073, the forward pass: 311 us, LATER with slots); in fp32 it makes no difference.
+template <bool BF16, int G>
+struct Pass {
+  static constexpr int ELT = BF16 ? 2 : 4;
+  uint32_t raw[G][BF16 ? 4 : 8];
+  uint32_t bits[G];
 
-// The workgroup's range of a row, G groups a lane at a time: each(logits, first token of group g = v + g * LOSS_TOKENS), with -inf where a token
-// is not allowed, is past the range or is struck out (strike(g): bits of the tokens that are).
-template <bool BF16, int G, class Strike, class Each>
-__device__ __forceinline__ void through(const LossArgs& a, const LossRow& q, int64_t first, int64_t end, Strike strike, Each each) {
-  constexpr int ELT = BF16 ? 2 : 4;
-  const char* row = (const char*)a.l.d.logits + q.at * ELT;
-#pragma unroll 1
-  for (int64_t base = first; base < end; base += G * LOSS_TOKENS) {
-    const int64_t v = base + threadIdx.x * LANE_TOKENS;
-    Lot<BF16> x[G];
-    uint32_t bits[G];
-    if (base + G * LOSS_TOKENS <= end) {
-#pragma unroll
-      for (int g = 0; g < G; ++g) {
-        x[g].load(row + (v + g * LOSS_TOKENS) * ELT);
-        bits[g] = q.allow ? q.allow[(v + g * LOSS_TOKENS) >> 3] : q.unmasked;
-      }
+  // whether the group at slot t lies in the row
+  static __device__ __forceinline__ bool inside(const LossRow& q, int64_t t, int64_t vocab) { return t >= q.shift && t - q.shift + LANE_TOKENS <= vocab; }
+  static __device__ __forceinline__ uint32_t mask_bits(const LossArgs& a, const LossRow& q, int64_t t, bool whole) {
+    if (!q.allow) return q.unmasked;
+    if (q.shift == 0) return q.allow[t >> 3];
+    const int64_t byte = (t - q.shift) >> 3;         // the first token's, -1 before the row
+    uint16_t two = 0;
+    if (whole) {
+      __builtin_memcpy(&two, q.allow + byte, 2);
     } else {
-#pragma unroll
-      for (int g = 0; g < G; ++g) {
-        const int64_t left = end - (v + g * LOSS_TOKENS);
-        bits[g] = up_to(left);
-        if (left > 0) {
-          x[g].load(row + (v + g * LOSS_TOKENS) * ELT, left);
-          bits[g] &= q.allow ? q.allow[(v + g * LOSS_TOKENS) >> 3] : q.unmasked;
-        }
-      }
+      if (byte >= 0) two = q.allow[byte];
+      if (byte + 1 < 4 * a.l.words) two |= (uint16_t)(q.allow[byte + 1] << 8);
     }
-    uint32_t all = 0xFFu;
+    return two >> (LANE_TOKENS - q.shift) & 0xFFu;
+  }
+  __device__ __forceinline__ void load(const LossArgs& a, const LossRow& q, const char* row, int64_t t, int64_t end, bool whole) {
+    const int64_t vocab = a.l.d.vocab;
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      bits[g] &= ~strike(v + g * LOSS_TOKENS);
-      all &= bits[g];
+      const int64_t at = t + g * LOSS_TOKENS, v = at - q.shift;
+      const char* p = row + v * ELT;
+      bits[g] = 0;
+      if (whole || (at < end && inside(q, at, vocab))) {
+        __builtin_memcpy(raw[g], __builtin_assume_aligned(p, BF16 ? 16 : 4), BF16 ? 16 : 32);
+        bits[g] = mask_bits(a, q, at, true);
+      } else {
+        uint32_t there = 0;
+#pragma unroll
+        for (int e = 0; e < LANE_TOKENS; ++e) {
+          const bool in = at < end && v + e >= 0 && v + e < vocab;
+          const uint32_t x = !in ? 0u : BF16 ? ((const uint16_t*)p)[e] : ((const uint32_t*)p)[e];
+          there |= (uint32_t)in << e;
+          if (!BF16) raw[g][e] = x;
+          else raw[g][e >> 1] = e & 1 ? raw[g][e >> 1] | x << 16 : x;
+        }
+        if (there) bits[g] = mask_bits(a, q, at, false) & there;
+      }
     }
-    float z[G * LANE_TOKENS];
+  }
+  __device__ __forceinline__ float raw_logit(int g, int e) const {
+    return __builtin_bit_cast(float, !BF16 ? raw[g][e] : e & 1 ? raw[g][e >> 1] & 0xFFFF0000u : raw[g][e >> 1] << 16);
+  }
+  // HOLES: -inf for what does not count
+  template <bool HOLES>
+  __device__ __forceinline__ float logit(int g, int e) const {
+    return HOLES && !(bits[g] >> e & 1) ? -INFINITY : raw_logit(g, e);
+  }
+  template <bool HOLES>
+  __device__ __forceinline__ float largest(int g) const {
+    float top = logit<HOLES>(g, 0);
 #pragma unroll
-    for (int g = 0; g < G; ++g)
+    for (int e = 1; e < LANE_TOKENS; ++e) top = fmaxf(top, logit<HOLES>(g, e));
+    return top;
+  }
+};
+
+// Goes through slots first .. end - 1 of a row: each(pass, its first slot of this lane, whether some of the wave's tokens do not count) for passes
+// that have a token that counts, none(first slot) for the others.  strike(t): bits of the group at slot t that are struck out.
+template <bool BF16, int G, class Strike, class Each, class None>
+__device__ __forceinline__ void through(const LossArgs& a, const LossRow& q, int64_t first, int64_t end, Strike strike, Each each, None none) {
+  const char* row = (const char*)a.l.d.logits + q.at * (BF16 ? 2 : 4);
+#pragma unroll 1
+  for (int64_t base = first; base < end; base += G * LOSS_TOKENS) {
+    const int64_t t = base + threadIdx.x * LANE_TOKENS;
+    Pass<BF16, G> x;
+    if (base >= q.shift && base + G * LOSS_TOKENS <= min(end, a.l.d.vocab + (int64_t)q.shift)) x.load(a, q, row, t, end, true);
+    else x.load(a, q, row, t, end, false);
+    uint32_t all = 0xFFu, some = 0;
 #pragma unroll
-      for (int e = 0; e < LANE_TOKENS; ++e) z[g * LANE_TOKENS + e] = x[g].logit(e);
-    if (__ballot(all != 0xFFu)) {
-#pragma unroll
-      for (int g = 0; g < G; ++g)
-#pragma unroll
-        for (int e = 0; e < LANE_TOKENS; ++e) z[g * LANE_TOKENS + e] = bits[g] >> e & 1 ? z[g * LANE_TOKENS + e] : -INFINITY;
+    for (int g = 0; g < G; ++g) {
+      x.bits[g] &= ~strike(t + g * LOSS_TOKENS);
+      all &= x.bits[g];
+      some |= x.bits[g];
     }
-    each(z, base);
+    const bool holes = __ballot(all != 0xFFu);
+    if (holes && !__ballot(some != 0)) none(t);
+    else each(x, t, holes);
   }
 }
 
-// Adds N logits to the sums; the sums move to a new largest logit once for all of them.
-template <int N, bool ENTROPY>
-__device__ __forceinline__ void take(Sums& a, const float* z, float top, const LossRow& q) {
-  if (top > a.m) move_to(a, top, q);
+// What a wave has summed: every lane the sums of its own tokens, relative to one logit m for all of them, which is some logit of the wave's
+// and at most a little less than the largest: 2^x stays within 2^6.
+struct WaveSums {
+  Sums sums;
+  bool clamp;                                        // there are logits of -inf
+};
+
+// What does not count has x = -FAR.
+template <bool HOLES, bool CLAMP, bool ENTROPY, class P, int G>
+__device__ __forceinline__ void add_near(const P& x, float r, const LossRow& q, float& s, float& u) {
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    float y[LANE_TOKENS], p[LANE_TOKENS];
+#pragma unroll
+    for (int e = 0; e < LANE_TOKENS; ++e) {
+      y[e] = __builtin_fmaf(x.raw_logit(g, e), q.c, -r);
+      if (HOLES) {
+        const uint32_t counts = (uint32_t)__builtin_amdgcn_sbfe((int)x.bits[g], e, 1);
+        y[e] = __builtin_bit_cast(float, (counts & __builtin_bit_cast(uint32_t, y[e])) | (~counts & __builtin_bit_cast(uint32_t, -FAR)));
+      }
+      p[e] = exp2_of(y[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < LANE_TOKENS; ++e) {
+      s += p[e];
+      if (ENTROPY) u = __builtin_fmaf(p[e], CLAMP ? fmaxf(y[e], -FAR) : y[e], u);
+    }
+  }
+}
+
+// Adds a pass to the sums.  As a rule m stays, and x = z c - r is one operation, with r = m c as rounded; what r is off, d, is known and goes into
+// the sums afterwards.  Where a lane's sum shows that m is too small (or that there is a NaN), where nothing has been seen yet, or where r is no
+// number of fp32, the pass is gone through again: m becomes the largest logit of the wave's, and x = (z - m) c.
+template <bool ENTROPY, bool BF16, int G>
+__device__ __forceinline__ void take(WaveSums& a, const Pass<BF16, G>& x, bool holes, const LossRow& q) {
+  using P = Pass<BF16, G>;
+  const float m = a.sums.m, r = m * q.c;
+  if (fabsf(r) < INFINITY) {
+    float s = 0.0f, u = 0.0f;
+    if (ENTROPY && a.clamp) add_near<true, true, ENTROPY, P, G>(x, r, q, s, u);
+    else if (holes) add_near<true, false, ENTROPY, P, G>(x, r, q, s, u);
+    else add_near<false, false, ENTROPY, P, G>(x, r, q, s, u);
+    if (!__ballot(!(s <= 64.0f && u == u))) {
+      const float d = __builtin_fmaf(m, q.c, -r), f = exp2_of(-d);
+      s *= f;
+      a.sums.s += s;
+      if (ENTROPY) a.sums.u += u * f - d * s;
+      return;
+    }
+  }
+  float top = -INFINITY, low = INFINITY;
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    top = fmaxf(top, x.template largest<true>(g));
+#pragma unroll
+    for (int e = 0; e < LANE_TOKENS; ++e) low = fminf(low, x.raw_logit(g, e));
+  }
+  a.clamp |= __ballot(low == -INFINITY) != 0;
+  top = lanes_max(top);
+  if (top > m) move_to(a.sums, top, q);
   float s = 0.0f, u = 0.0f;
 #pragma unroll
-  for (int e = 0; e < N; ++e) {
-    const float t = z[e] - a.m, p = exp2_of(t * q.c);
-    s += p;
-    if (ENTROPY) u = __builtin_fmaf(p, fmaxf(t, q.lim), u);
-  }
-  a.s += s;
-  a.u += u;
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int e = 0; e < LANE_TOKENS; ++e) {
+      const float y = (x.template logit<true>(g, e) - a.sums.m) * q.c, p = exp2_of(y);
+      s += p;
+      if (ENTROPY) u = __builtin_fmaf(p, fmaxf(y, -FAR), u);
+    }
+  a.sums.s += s;
+  a.sums.u += u;
 }
 
 // How a call is laid out: groups a lane takes at a time, tokens of a workgroup, workgroups of a row.
@@ -187,61 +268,152 @@ struct LossGrid {
 };
 
 // ---------------------------------------------------------------- alternatives
-// The n best tokens lie in the n stretches of CHUNK tokens whose largest logits come first (equal ones in the order of their tokens): each of
+// The n best tokens lie in the n stretches of CHUNK slots whose largest logits come first (equal ones in the order of their tokens): each of
 // these has a token that comes before all others of the stretches that come after.  So the pass over the logits leaves the largest logit of each
 // stretch, the stretches are chosen from these, and their tokens are looked at again.
-constexpr int CHUNK = 4 * LANE_TOKENS;
+constexpr int CHUNK = 4 * LANE_TOKENS;               // of four adjacent lanes
 
-// Whether (z, v) comes before (y, w).
-__device__ __forceinline__ bool before(float z, int v, float y, int w) { return z > y || (z == y && v < w); }
-__device__ __forceinline__ float lane_of(float x, int lane) {
-  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
+// Its bits in the order of the numbers; -0 and 0 are equal.
+__device__ __forceinline__ uint32_t ordered(float z) {
+  const int bits = __builtin_bit_cast(int, z + 0.0f);
+  return (uint32_t)bits ^ ((uint32_t)(bits >> 31) | 0x80000000u);
 }
-__device__ __forceinline__ int from_left(int x) { return __builtin_amdgcn_update_dpp(x, x, 0x138, 0xF, 0xF, false); }      // lane i - 1's
+// A logit and where it comes from in one number, the larger the earlier it comes among alternatives; 0 for -inf.  All others are distinct.
+__device__ __forceinline__ uint64_t key_of(float z, int at) {
+  if (!(z > -INFINITY)) return 0;
+  return (uint64_t)ordered(z) << 32 | (uint32_t)~at;
+}
+__device__ __forceinline__ float logit_of(uint64_t key) {
+  const uint32_t bits = (uint32_t)(key >> 32);
+  return __builtin_bit_cast(float, bits & 0x80000000u ? bits ^ 0x80000000u : ~bits);
+}
+__device__ __forceinline__ int place_of(uint64_t key) { return (int)~(uint32_t)key; }
 
-// The best entries that a wave has seen, lane i the i-th.
-struct Best {
-  float z;
-  int v;
-  __device__ __forceinline__ void clear() {
-    z = -INFINITY;
-    v = INT32_MAX;
-  }
-  // every lane offers one (none: -inf); the first n are kept
-  __device__ __forceinline__ void offer(float cz, int cv, int n) {
-    const int lane = threadIdx.x & 63;
-    uint64_t left = __ballot(cz > -INFINITY) & __ballot(before(cz, cv, lane_of(z, n - 1), __builtin_amdgcn_readlane(v, n - 1)));
-    while (left) {
-      const int from = (int)__builtin_ctzll(left);
-      const float y = lane_of(cz, from);
-      const int w = __builtin_amdgcn_readlane(cv, from);
-      const int place = __builtin_popcountll(__ballot(before(z, v, y, w)));
-      const float up_z = __builtin_bit_cast(float, from_left(__builtin_bit_cast(int, z)));
-      const int up_v = from_left(v);
-      z = lane < place ? z : lane == place ? y : up_z;
-      v = lane < place ? v : lane == place ? w : up_v;
-      left &= left - 1;
-      left &= __ballot(before(cz, cv, lane_of(z, n - 1), __builtin_amdgcn_readlane(v, n - 1)));
-    }
-  }
-};
 struct TopLds {
-  float z[LOSS_WAVES][WAVE];
-  int v[LOSS_WAVES][WAVE];
+  static constexpr int CANDIDATES = 4 * LOSS_THREADS;
+  uint64_t lane[LOSS_THREADS], candidate[CANDIDATES], best[PG_TOP_MAX], least;
+  float top[LOSS_THREADS];
+  uint32_t bound;
+  int count;
 };
-// The best of all waves' lists, in wave 0 and in row 0 of the LDS.
-__device__ __forceinline__ void join_lists(Best& b, int n, TopLds& s) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  __syncthreads();                                   // the lists before have been read
-  s.z[wave][lane] = b.z;
-  s.v[wave][lane] = b.v;
+
+// Before and after the collection of candidates; s.best is the n largest of them in falling order (0: there are no more).
+__device__ __forceinline__ void no_candidates(TopLds& s) {
+  __syncthreads();                                   // what was there has been read
+  if (threadIdx.x < PG_TOP_MAX) s.best[threadIdx.x] = 0;
+  if (threadIdx.x == 0) {
+    s.count = 0;
+    s.least = 1;
+    s.bound = ~0u;
+  }
+}
+__device__ __forceinline__ void candidate(uint64_t key, TopLds& s) {
+  const int at = atomicAdd(&s.count, 1);
+  if (at < TopLds::CANDIDATES) s.candidate[at] = key;
+}
+__device__ __forceinline__ bool rank_candidates(int n, TopLds& s) {
   __syncthreads();
-  if (wave == 0) {
-    for (int w = 1; w < LOSS_WAVES; ++w) b.offer(lane < n ? s.z[w][lane] : -INFINITY, s.v[w][lane], n);
-    s.z[0][lane] = b.z;
-    s.v[0][lane] = b.v;
+  const int m = s.count;
+  if (m > TopLds::CANDIDATES) return false;
+  for (int k = threadIdx.x; k < m; k += LOSS_THREADS) {
+    const uint64_t key = s.candidate[k];
+    int rank = 0;
+#pragma unroll 4
+    for (int i = 0; i < m; ++i) rank += s.candidate[i] > key;
+    if (rank < n) s.best[rank] = key;
   }
   __syncthreads();
+  return true;
+}
+
+// The n-th largest of the lanes' values: n of them, at least, reach it.
+__device__ __forceinline__ float nth_of_lanes(float top, int n, TopLds& s) {
+  s.top[threadIdx.x] = top;
+  __syncthreads();
+  int rank = 0;
+#pragma unroll 16
+  for (int i = 0; i < LOSS_THREADS / 4; ++i) {
+    const float4 t = ((const float4*)s.top)[i];
+    rank += (t.x > top) + (t.y > top) + (t.z > top) + (t.w > top);
+  }
+  if (rank < n) atomicMin(&s.bound, ordered(top));
+  __syncthreads();
+  return logit_of((uint64_t)s.bound << 32);
+}
+
+// The n largest of the keys item(0) .. item(N - 1) where too many reach a bound on their logits alone.  Of the largest keys of the lanes the
+// n-th is a bound that takes equal logits apart; where the lanes that have the largest keys have too many of them, n rounds of a maximum.
+template <class Item>
+__device__ __forceinline__ void select_by_key(int N, int n, TopLds& s, Item item) {
+  const int me = threadIdx.x;
+  uint64_t most = 0;
+  for (int i = me; i < N; i += LOSS_THREADS) most = max(most, item(i));
+  no_candidates(s);
+  s.lane[me] = most;
+  __syncthreads();
+  int rank = 0;
+  for (int i = 0; i < LOSS_THREADS; ++i) rank += s.lane[i] > most;
+  if (most && rank == n - 1) s.least = most;
+  __syncthreads();
+  const uint64_t least = s.least;
+  for (int i = me; i < N; i += LOSS_THREADS) {
+    const uint64_t key = item(i);
+    if (key >= least) candidate(key, s);
+  }
+  if (rank_candidates(n, s)) return;
+  uint64_t last = ~0ull;
+  for (int k = 0; k < n && last; ++k) {
+    most = 0;
+    for (int i = me; i < N; i += LOSS_THREADS) {
+      const uint64_t key = item(i);
+      if (key < last) most = max(most, key);
+    }
+    __syncthreads();
+    s.lane[me] = most;
+    __syncthreads();
+    for (int i = 0; i < LOSS_THREADS; ++i) most = max(most, s.lane[i]);
+    if (me == 0) s.best[k] = most;
+    last = most;
+  }
+  __syncthreads();
+}
+
+// The n best tokens of a row, from the largest logits of its stretches, to s.best: all lanes of a workgroup.
+template <bool BF16>
+__device__ __forceinline__ void alternatives(const LossArgs& a, const LossRow& q, const float* largest, int n, TopLds& s) {
+  constexpr int KEPT = 20;                           // stretches a lane has in registers: 163840 tokens
+  const int me = threadIdx.x, vocab = a.l.d.vocab, N = (vocab + q.shift + CHUNK - 1) / CHUNK;
+  no_candidates(s);
+  float z[KEPT], top = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < KEPT; ++k) z[k] = me + k * LOSS_THREADS < N ? largest[me + k * LOSS_THREADS] : -INFINITY;
+#pragma unroll
+  for (int k = 0; k < KEPT; ++k) top = fmaxf(top, z[k]);
+  for (int i = me + KEPT * LOSS_THREADS; i < N; i += LOSS_THREADS) top = fmaxf(top, largest[i]);
+  const float bound = nth_of_lanes(top, n, s);
+#pragma unroll
+  for (int k = 0; k < KEPT; ++k)
+    if (z[k] >= bound && z[k] > -INFINITY) candidate(key_of(z[k], me + k * LOSS_THREADS), s);
+  for (int i = me + KEPT * LOSS_THREADS; i < N; i += LOSS_THREADS)
+    if (largest[i] >= bound && largest[i] > -INFINITY) candidate(key_of(largest[i], i), s);
+  if (!rank_candidates(n, s)) select_by_key(N, n, s, [&](int i) { return key_of(largest[i], i); });
+  // four lanes look at a stretch again, eight tokens each
+  const uint64_t chunk = me / 4 < n ? s.best[me / 4] : 0;
+  const float least = logit_of(s.best[n - 1]);       // NaN for 0: nothing is below it
+  Pass<BF16, 1> x;
+  const int64_t slot = chunk ? (int64_t)place_of(chunk) * CHUNK + (me & 3) * LANE_TOKENS : (int64_t)vocab + q.shift;
+  x.load(a, q, (const char*)a.l.d.logits + q.at * (BF16 ? 2 : 4), slot, (int64_t)vocab + q.shift, false);
+  const int v = (int)(slot - q.shift);
+  uint64_t key[LANE_TOKENS];
+  no_candidates(s);
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < LANE_TOKENS; ++e) {
+    const float y = x.template logit<true>(0, e);
+    key[e] = y < least ? 0 : key_of(y, v + e);
+    if (key[e]) candidate(key[e], s);
+  }
+  if (!rank_candidates(n, s)) select_by_key(LOSS_THREADS * LANE_TOKENS, n, s, [&](int i) { return key[i / LOSS_THREADS]; });
 }
 
 struct LogprobOut {
@@ -257,43 +429,31 @@ struct LogprobOut {
 
 // What the whole row's sums give; all lanes of a workgroup, or (no alternatives) of a wave.
 template <bool BF16>
-__device__ __forceinline__ void finish_logprob(const LossArgs& a, const LogprobOut& o, const LossRow& q, int r, int target, const Sums& sum, TopLds* s) {
-  const int vocab = a.l.d.vocab, lane = threadIdx.x & 63;
+__device__ __forceinline__ void finish_logprob(const LossArgs& a, const LogprobOut& o, const LossRow& q, int r, int target, float at_target, const Sums& sum,
+                                               TopLds* s) {
   const bool gone = target == -1, bad = sum.s != sum.s, none = sum.s == 0.0f;
   const float ln_s = none ? 0.0f : logf(sum.s);
   if (threadIdx.x == 0) {
-    const float h = none ? 0.0f : ln_s - q.inv * (sum.u / sum.s);
+    const float h = none ? 0.0f : ln_s - LN2 * (sum.u / sum.s);
     if (o.entropy) o.entropy[r] = h;
     if (o.logp) {
       float l = __builtin_nanf("");
       if (gone) l = 0.0f;
-      else if (target >= 0 && target < vocab && !bad) l = none ? -INFINITY : (open_logit<BF16>(a, q, target) - sum.m) * q.inv - ln_s;
+      else if (target >= 0 && target < a.l.d.vocab && !bad) l = none ? -INFINITY : (at_target - sum.m) * q.inv - ln_s;
       o.logp[r] = l;
     }
     if (o.stats) *(float4*)(o.stats + 4ll * r) = float4{none ? -INFINITY : sum.m * q.inv, ln_s, h, sum.m};
   }
   if (!s) return;
-  const int n = o.n_top, wave = threadIdx.x >> 6;
-  Best best;
-  best.clear();
-  if (!gone && !bad) {
-    const float* largest = o.chunks + (int64_t)r * o.n_chunks;
-    for (int c = threadIdx.x; c - lane < o.n_chunks; c += LOSS_THREADS) best.offer(c < o.n_chunks ? largest[c] : -INFINITY, c, n);
-    join_lists(best, n, *s);
-    const float least = s->z[0][n - 1];
-    best.clear();
-    for (int i = 2 * wave; i < n; i += 2 * LOSS_WAVES) {
-      const int at = i + (lane >> 5);
-      const int64_t v = at < n && s->v[0][at] != INT32_MAX ? (int64_t)s->v[0][at] * CHUNK + (lane & 31) : vocab;
-      const float z = v < vocab ? open_logit<BF16>(a, q, v) : -INFINITY;
-      best.offer(z >= least ? z : -INFINITY, (int)v, n);
-    }
-    join_lists(best, n, *s);
+  const int n = o.n_top;
+  uint64_t key = 0;
+  if (!gone && !bad && !none) {
+    alternatives<BF16>(a, q, o.chunks + (int64_t)r * o.n_chunks, n, *s);
+    key = (int)threadIdx.x < n ? s->best[threadIdx.x] : 0;
   }
-  if (wave == 0 && lane < n) {
-    const bool there = best.z > -INFINITY;
-    if (o.top_ids) o.top_ids[(int64_t)r * n + lane] = there ? best.v : -1;
-    if (o.top_logp) o.top_logp[(int64_t)r * n + lane] = bad ? __builtin_nanf("") : there ? (best.z - sum.m) * q.inv - ln_s : -INFINITY;
+  if ((int)threadIdx.x < n) {
+    if (o.top_ids) o.top_ids[(int64_t)r * n + threadIdx.x] = key ? place_of(key) : -1;
+    if (o.top_logp) o.top_logp[(int64_t)r * n + threadIdx.x] = bad ? __builtin_nanf("") : key ? (logit_of(key) - sum.m) * q.inv - ln_s : -INFINITY;
   }
 }
 
@@ -302,65 +462,71 @@ __global__ __launch_bounds__(LOSS_THREADS) void logprob_kernel(LossArgs a, LossG
   __shared__ Sums waves[LOSS_WAVES];
   __shared__ TopLds lists;
   const int r = blockIdx.x / grid.pieces, piece = blockIdx.x - r * grid.pieces, lane = threadIdx.x & 63;
-  const LossRow q = loss_row(a, r);
+  const LossRow q = loss_row<BF16>(a, r);
   const int target = o.target ? o.target[r] : 0;
-  Sums mine = no_sums();
+  const float at_target = target >= 0 && target < a.l.d.vocab ? open_logit<BF16>(a, q, target) : 0.0f;       // asked for early
+  WaveSums mine{no_sums(), false};
   if (target != -1) {
-    const int64_t first = (int64_t)piece * grid.range, end = min(first + grid.range, (int64_t)a.l.d.vocab);
-    through<BF16, G>(a, q, first, end, [](int64_t) { return 0u; }, [&](const float* z, int64_t base) {
-      float top[G], all = -INFINITY;
-#pragma unroll
-      for (int g = 0; g < G; ++g) {
-        top[g] = z[g * LANE_TOKENS];
-#pragma unroll
-        for (int e = 1; e < LANE_TOKENS; ++e) top[g] = fmaxf(top[g], z[g * LANE_TOKENS + e]);
-        all = fmaxf(all, top[g]);
-      }
-      take<G * LANE_TOKENS, true>(mine, z, all, q);
+    const int64_t first = (int64_t)piece * grid.range, end = min(first + grid.range, (int64_t)a.l.d.vocab + q.shift);
+    float* chunks = o.chunks + (int64_t)r * o.n_chunks;
+    auto leave = [&](int64_t t, int g, float top) {
+      const int c = (int)(t / CHUNK) + g * (LOSS_TOKENS / CHUNK);
+      if ((lane & 3) == g % 4 && c < o.n_chunks) chunks[c] = top;
+    };
+    through<BF16, G>(a, q, first, end, [](int64_t) { return 0u; }, [&](const Pass<BF16, G>& x, int64_t t, bool holes) {
+      take<true>(mine, x, holes, q);
       if (TOP) {
-        auto moved = [](float x, auto ctrl) {
-          const int w = __builtin_bit_cast(int, x);
+        auto moved = [](float y, auto ctrl) {
+          const int w = __builtin_bit_cast(int, y);
           return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(w, w, decltype(ctrl)::value, 0xF, 0xF, false));
         };
-        float* to = o.chunks + (int64_t)r * o.n_chunks;
-        const int place = (int)(base / CHUNK) + (int)(threadIdx.x >> 2);
 #pragma unroll
-        for (int g = 0; g < G; ++g) {                // four adjacent lanes have a stretch
-          float t = fmaxf(top[g], moved(top[g], std::integral_constant<int, 0xB1>{}));
-          t = fmaxf(t, moved(t, std::integral_constant<int, 0x4E>{}));
-          const int c = place + g * (LOSS_TOKENS / CHUNK);
-          if ((lane & 3) == g % 4 && c < o.n_chunks) to[c] = t;
+        for (int g = 0; g < G; ++g) {
+          float top = holes ? x.template largest<true>(g) : x.template largest<false>(g);
+          top = fmaxf(top, moved(top, std::integral_constant<int, 0xB1>{}));
+          top = fmaxf(top, moved(top, std::integral_constant<int, 0x4E>{}));
+          leave(t, g, top);
         }
       }
+    }, [&](int64_t t) {
+      if (TOP)
+        for (int g = 0; g < G; ++g) leave(t, g, -INFINITY);
     });
   }
-  const Sums sum = block_sums(mine, q, waves);
+  const Sums sum = block_sums(mine.sums, q, waves);
   if (grid.pieces > 1) {
     if (threadIdx.x == 0) o.parts[blockIdx.x] = sum;
     return;
   }
   if (TOP) __threadfence_block();
-  finish_logprob<BF16>(a, o, q, r, target, sum, TOP ? &lists : nullptr);
+  finish_logprob<BF16>(a, o, q, r, target, at_target, sum, TOP ? &lists : nullptr);
 }
 
 template <bool BF16, bool TOP>
 __global__ __launch_bounds__(LOSS_THREADS) void logprob_finish_kernel(LossArgs a, LossGrid grid, LogprobOut o) {
   __shared__ TopLds lists;
   const int r = blockIdx.x;
-  const LossRow q = loss_row(a, r);
+  const LossRow q = loss_row<BF16>(a, r);
+  const int target = o.target ? o.target[r] : 0;
+  const float at_target = target >= 0 && target < a.l.d.vocab ? open_logit<BF16>(a, q, target) : 0.0f;
   Sums sum = no_sums();
   for (int i = threadIdx.x & 63; i < grid.pieces; i += WAVE) join(sum, o.parts[(int64_t)r * grid.pieces + i], q);
   sum = wave_sums(sum, q);
-  finish_logprob<BF16>(a, o, q, r, o.target ? o.target[r] : 0, sum, TOP ? &lists : nullptr);
+  finish_logprob<BF16>(a, o, q, r, target, at_target, sum, TOP ? &lists : nullptr);
 }
 
-// Writes the gradient of a group, in the logits' type.
-template <bool BF16>
-__device__ __forceinline__ void put(char* to, const float* d, int64_t left) {
-  if (left >= LANE_TOKENS) {
+// Writes the gradient of the tokens v .. v + 7 that are in the row, but for those of `others`, in the logits' type.  PAST: not to be kept in the
+// caches.
+template <bool BF16, bool PAST>
+__device__ __forceinline__ void put(char* row, int64_t v, int64_t vocab, const float* d, uint32_t others = 0) {
+  char* to = row + v * (BF16 ? 2 : 4);
+  if (v >= 0 && v + LANE_TOKENS <= vocab && !others) {
     if (BF16) {
       const uint32_t w[4] = {pack_bf16x2(d[0], d[1]), pack_bf16x2(d[2], d[3]), pack_bf16x2(d[4], d[5]), pack_bf16x2(d[6], d[7])};
-      __builtin_memcpy(to, w, 16);
+      typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(2)));
+      const Words x{w[0], w[1], w[2], w[3]};
+      if (PAST) __builtin_nontemporal_store(x, (Words*)to);
+      else *(Words*)to = x;
     } else {
       __builtin_memcpy(to, d, 32);
     }
@@ -368,58 +534,63 @@ __device__ __forceinline__ void put(char* to, const float* d, int64_t left) {
   }
 #pragma unroll
   for (int e = 0; e < LANE_TOKENS; ++e)
-    if (e < left) {
+    if (v + e >= 0 && v + e < vocab && !(others >> e & 1)) {
       if (BF16) ((uint16_t*)to)[e] = (uint16_t)pack_bf16x2(d[e], 0.0f);
       else ((float*)to)[e] = d[e];
     }
 }
+template <bool BF16, bool PAST, int G>
+__device__ __forceinline__ void put_zeros(char* row, int64_t v, int64_t vocab) {
+  const float nothing[LANE_TOKENS] = {};
+#pragma unroll
+  for (int i = 0; i < G; ++i) put<BF16, PAST>(row, v + i * LOSS_TOKENS, vocab, nothing);
+}
 
 // The gradient is p (c0 + c1 (z - m)) with two numbers of the row, and g / T more at the target.
-template <bool BF16, int G>
+template <bool BF16, int G, bool PAST>
 __global__ __launch_bounds__(LOSS_THREADS) void logprob_backward_kernel(LossArgs a, int pieces, const int32_t* target, const float* stats,
                                                                         const float* g_logp, const float* g_entropy, void* out, int64_t out_stride) {
   constexpr int ELT = BF16 ? 2 : 4;
-  const int r = blockIdx.x / pieces, piece = blockIdx.x - r * pieces;
+  const int block = gridDim.x - 1 - blockIdx.x, r = block / pieces, piece = block - r * pieces;
   const int64_t vocab = a.l.d.vocab, first = (int64_t)piece * (G * LOSS_TOKENS);
-  const LossRow q = loss_row(a, r);
+  const LossRow q = loss_row<BF16>(a, r);
   const int t = target ? target[r] : 0;
   float g = g_logp ? g_logp[r] : 0.0f;
   const float ge = g_entropy ? g_entropy[r] : 0.0f;
   char* to = (char*)out + (int64_t)r * out_stride * ELT;
-  if (t == -1 || (g == 0.0f && ge == 0.0f)) {
-    const float nothing[LANE_TOKENS] = {};
-#pragma unroll
-    for (int i = 0; i < G; ++i) {
-      const int64_t v = first + i * LOSS_TOKENS + threadIdx.x * LANE_TOKENS;
-      put<BF16>(to + v * ELT, nothing, vocab - v);
-    }
-    return;
-  }
+  auto clear = [&](int64_t slot) { put_zeros<BF16, PAST, G>(to, slot - q.shift, vocab); };
+  if (t == -1 || (g == 0.0f && ge == 0.0f)) return clear(first + threadIdx.x * LANE_TOKENS);
   if (g_logp && (t < 0 || t >= vocab)) g = __builtin_nanf("");
   const float4 s = *(const float4*)(stats + 4ll * r);
   const float ln_s = s.y, h = s.z, m = s.w;
   const float c0 = q.inv * (-g - ge * (h - ln_s)), c1 = -q.inv * ge * q.inv, at_target = q.inv * g, less = ln_s * LOG2E;
-  through<BF16, G>(a, q, first, min(first + G * LOSS_TOKENS, vocab), [](int64_t) { return 0u; }, [&](const float* z, int64_t base) {
+  const bool odd = !(fabsf(c0) < INFINITY && fabsf(c1) < INFINITY && less == less);        // 0 times these is no 0
+  auto each = [&](const Pass<BF16, G>& x, int64_t slot, auto all) {
+    constexpr bool HOLES = !decltype(all)::value;
 #pragma unroll
     for (int i = 0; i < G; ++i) {
-      const int64_t v = base + i * LOSS_TOKENS + threadIdx.x * LANE_TOKENS;
+      const int64_t v = slot + i * LOSS_TOKENS - q.shift;
       float d[LANE_TOKENS];
 #pragma unroll
       for (int e = 0; e < LANE_TOKENS; ++e) {
-        const float x = fmaxf(z[i * LANE_TOKENS + e] - m, q.lim);
-        const float p = exp2_of(__builtin_fmaf(x, q.c, -less));
-        d[e] = p * __builtin_fmaf(c1, x, c0);
-        if (z[i * LANE_TOKENS + e] == -INFINITY) d[e] = 0.0f;
+        const float z = x.template logit<HOLES>(i, e), y = fmaxf(z - m, q.lim);
+        d[e] = exp2_of(__builtin_fmaf(y, q.c, -less)) * __builtin_fmaf(c1, y, c0);
+        if (HOLES && z == -INFINITY) d[e] = 0.0f;
       }
       const int64_t at = t - v;
       if (at >= 0 && at < LANE_TOKENS) {
 #pragma unroll
         for (int e = 0; e < LANE_TOKENS; ++e)
-          if (e == at && z[i * LANE_TOKENS + e] != -INFINITY) d[e] += at_target;
+          if (e == at && x.template logit<true>(i, e) != -INFINITY) d[e] += at_target;
       }
-      put<BF16>(to + v * ELT, d, vocab - v);
+      put<BF16, PAST>(to, v, vocab, d);
     }
-  });
+  };
+  const int64_t end = min(first + G * LOSS_TOKENS, vocab + q.shift);
+  through<BF16, G>(a, q, first, end, [](int64_t) { return 0u; }, [&](const Pass<BF16, G>& x, int64_t slot, bool holes) {
+    if (holes || odd) each(x, slot, std::false_type{});
+    else each(x, slot, std::true_type{});
+  }, clear);
 }
 
 // ---------------------------------------------------------------- distillation
@@ -551,22 +722,18 @@ __global__ __launch_bounds__(LOSS_THREADS) void distill_kernel(LossArgs a, LossG
   __shared__ Sums waves[LOSS_WAVES];
   extern __shared__ uint32_t listed[];               // a bit for each token of the range, or (the end) the table of the list
   const int r = blockIdx.x / grid.pieces, piece = blockIdx.x - r * grid.pieces;
-  const LossRow q = loss_row(a, r);
-  const int64_t first = (int64_t)piece * grid.range, end = min(first + grid.range, (int64_t)a.l.d.vocab);
+  const LossRow q = loss_row<BF16>(a, r);
+  const int64_t first = (int64_t)piece * grid.range, end = min(first + grid.range, (int64_t)a.l.d.vocab + q.shift);
   for (int i = threadIdx.x; i < (int)((end - first + 31) / 32); i += LOSS_THREADS) listed[i] = 0;
   const int id = (int)threadIdx.x < o.k ? o.ids[(int64_t)r * o.k + threadIdx.x] : -1;
+  const int64_t slot = (int64_t)id + q.shift;
   __syncthreads();
-  if (id >= first && id < end) atomicOr(&listed[(id - first) >> 5], 1u << ((id - first) & 31));
+  if (id >= 0 && slot >= first && slot < end) atomicOr(&listed[(slot - first) >> 5], 1u << ((slot - first) & 31));
   __syncthreads();
-  Sums mine = no_sums();
-  auto strike = [&](int64_t v) { return v < end ? (uint32_t)((const uint8_t*)listed)[(v - first) >> 3] : 0u; };
-  through<BF16, G>(a, q, first, end, strike, [&](const float* z, int64_t) {
-    float top = z[0];
-#pragma unroll
-    for (int e = 1; e < G * LANE_TOKENS; ++e) top = fmaxf(top, z[e]);
-    take<G * LANE_TOKENS, false>(mine, z, top, q);
-  });
-  const Sums rest = block_sums(mine, q, waves);
+  WaveSums mine{no_sums(), false};
+  auto strike = [&](int64_t t) { return t < end ? (uint32_t)((const uint8_t*)listed)[(t - first) >> 3] : 0u; };
+  through<BF16, G>(a, q, first, end, strike, [&](const Pass<BF16, G>& x, int64_t, bool holes) { take<false>(mine, x, holes, q); }, [](int64_t) {});
+  const Sums rest = block_sums(mine.sums, q, waves);
   if (grid.pieces > 1) {
     if (threadIdx.x == 0) o.parts[blockIdx.x] = rest;
   } else {
@@ -579,7 +746,7 @@ template <bool BF16>
 __global__ __launch_bounds__(WAVE) void distill_finish_kernel(LossArgs a, LossGrid grid, DistillArgs o) {
   __shared__ ListLds list;
   const int r = blockIdx.x;
-  const LossRow q = loss_row(a, r);
+  const LossRow q = loss_row<BF16>(a, r);
   Sums rest = no_sums();
   for (int i = threadIdx.x; i < grid.pieces; i += WAVE) join(rest, o.parts[(int64_t)r * grid.pieces + i], q);
   finish_distill<BF16>(a, o, q, r, wave_sums(rest, q), list);
@@ -587,40 +754,33 @@ __global__ __launch_bounds__(WAVE) void distill_finish_kernel(LossArgs a, LossGr
 
 // What is not listed has the gradient g / T (Q p_rest - q_rest) of its share of p_rest; a listed token is written by the lane that holds its
 // entry, and by no other.
-template <bool BF16, int G>
+template <bool BF16, int G, bool PAST>
 __global__ __launch_bounds__(LOSS_THREADS) void distill_backward_kernel(LossArgs a, int pieces, DistillArgs o, const float* g_loss, void* out,
                                                                         int64_t out_stride) {
   constexpr int ELT = BF16 ? 2 : 4, RANGE = G * LOSS_TOKENS;
   __shared__ uint32_t listed[RANGE / 32];
   __shared__ int token[PG_DISTILL_MAX];
   __shared__ int twice;
-  const int r = blockIdx.x / pieces, piece = blockIdx.x - r * pieces;
-  const int64_t vocab = a.l.d.vocab, first = (int64_t)piece * RANGE, end = min(first + RANGE, vocab);
-  const LossRow q = loss_row(a, r);
+  const int block = gridDim.x - 1 - blockIdx.x, r = block / pieces, piece = block - r * pieces;
+  const LossRow q = loss_row<BF16>(a, r);
+  const int64_t vocab = a.l.d.vocab, first = (int64_t)piece * RANGE, end = min(first + RANGE, vocab + q.shift);
   const float4 s0 = ((const float4*)(o.stats + (int64_t)r * PG_DISTILL_STATS))[0], s1 = ((const float4*)(o.stats + (int64_t)r * PG_DISTILL_STATS))[1];
   const float g = s1.w == 0.0f ? 0.0f : g_loss[r];
   char* to = (char*)out + (int64_t)r * out_stride * ELT;
-  if (g == 0.0f) {
-    const float nothing[LANE_TOKENS] = {};
-#pragma unroll
-    for (int i = 0; i < G; ++i) {
-      const int64_t v = first + i * LOSS_TOKENS + threadIdx.x * LANE_TOKENS;
-      put<BF16>(to + v * ELT, nothing, vocab - v);
-    }
-    return;
-  }
+  if (g == 0.0f) return put_zeros<BF16, PAST, G>(to, first + threadIdx.x * LANE_TOKENS - q.shift, vocab);
   const bool entry = (int)threadIdx.x < o.k;
   const int id = entry ? o.ids[(int64_t)r * o.k + threadIdx.x] : -1;
   const float t = entry ? o.logp[(int64_t)r * o.k + threadIdx.x] : 0.0f;
-  const bool mine = id >= first && id < end;
+  const int64_t place = (int64_t)id + q.shift - first;
+  const bool mine = id >= 0 && place >= 0 && place < end - first;
   const float scale = g * q.inv;
   if (threadIdx.x < RANGE / 32) listed[threadIdx.x] = 0;
   if (threadIdx.x == 0) twice = 0;
   token[threadIdx.x] = id;
   __syncthreads();
   if (mine) {
-    const uint32_t bit = 1u << ((id - first) & 31);
-    if (atomicOr(&listed[(id - first) >> 5], bit) & bit) twice = 1;
+    const uint32_t bit = 1u << (place & 31);
+    if (atomicOr(&listed[place >> 5], bit) & bit) twice = 1;
   }
   __syncthreads();
   bool writes = mine;
@@ -634,30 +794,30 @@ __global__ __launch_bounds__(LOSS_THREADS) void distill_backward_kernel(LossArgs
     else ((float*)to)[id] = d;
   }
   const float c = scale * s1.x, less = s0.w * LOG2E;
-  auto strike = [&](int64_t v) { return v < end ? (uint32_t)((const uint8_t*)listed)[(v - first) >> 3] : 0u; };
-  through<BF16, G>(a, q, first, end, strike, [&](const float* z, int64_t base) {
+  auto strike = [&](int64_t t) { return t < end ? (uint32_t)((const uint8_t*)listed)[(t - first) >> 3] : 0u; };
+  const bool odd = !(fabsf(c) < INFINITY && less == less);
+  auto each = [&](const Pass<BF16, G>& x, int64_t slot, auto all) {
+    constexpr bool HOLES = !decltype(all)::value;
 #pragma unroll
     for (int i = 0; i < G; ++i) {
-      const int64_t v = base + i * LOSS_TOKENS + threadIdx.x * LANE_TOKENS;
+      const int64_t v = slot + i * LOSS_TOKENS - q.shift;
       float d[LANE_TOKENS];
 #pragma unroll
       for (int e = 0; e < LANE_TOKENS; ++e) {
-        const float x = z[i * LANE_TOKENS + e];
-        d[e] = c * exp2_of(__builtin_fmaf(fmaxf(x - s0.z, q.lim), q.c, -less));
-        if (x == -INFINITY) d[e] = 0.0f;
+        const float z = x.template logit<HOLES>(i, e);
+        d[e] = c * exp2_of(__builtin_fmaf(fmaxf(z - s0.z, q.lim), q.c, -less));
+        if (HOLES && z == -INFINITY) d[e] = 0.0f;
       }
-      const uint32_t others = strike(v);
-      if (!others) {
-        put<BF16>(to + v * ELT, d, vocab - v);
-      } else {
-#pragma unroll
-        for (int e = 0; e < LANE_TOKENS; ++e)
-          if (v + e < vocab && !(others >> e & 1)) {
-            if (BF16) ((uint16_t*)to)[v + e] = (uint16_t)pack_bf16x2(d[e], 0.0f);
-            else ((float*)to)[v + e] = d[e];
-          }
-      }
+      put<BF16, PAST>(to, v, vocab, d, HOLES ? strike(v + q.shift) : 0u);
     }
+  };
+  // a pass without a token that counts may have listed ones among those that are not allowed
+  through<BF16, G>(a, q, first, end, strike, [&](const Pass<BF16, G>& x, int64_t slot, bool holes) {
+    if (holes || odd) each(x, slot, std::false_type{});
+    else each(x, slot, std::true_type{});
+  }, [&](int64_t slot) {
+    Pass<BF16, G> nothing{};
+    each(nothing, slot, std::false_type{});
   });
 }
 
@@ -777,12 +937,19 @@ static pg_status check_gradient(const LossArgs& a, const void* out, int64_t out_
   return PG_OK;
 }
 
-static int64_t stretches_of(int64_t vocab) { return (vocab + LOSS_TOKENS - 1) / LOSS_TOKENS; }
+// The most slots that a row of this call has, and that one of any call with so many tokens has.
+static int64_t slots_of(const LossArgs& a) {
+  const pg_logits& d = a.l.d;
+  if (d.dtype != PG_LOGITS_BF16) return d.vocab;
+  return d.vocab + (d.rows > 1 && d.stride % LANE_TOKENS ? LANE_TOKENS - 1 : (int64_t)((uintptr_t)d.logits / 2 % LANE_TOKENS));
+}
+static int64_t most_slots(int64_t vocab) { return vocab + LANE_TOKENS - 1; }
+static int64_t stretches_of(int64_t slots) { return (slots + LOSS_TOKENS - 1) / LOSS_TOKENS; }
 
 // Workgroups of a pass over the logits: as many as fill the chip a few times over; what a row's finish has to join stays short.
-constexpr int64_t LOSS_WORKGROUPS = 4096;
-static LossGrid loss_grid(int64_t rows, int64_t vocab) {
-  const int64_t stretches = stretches_of(vocab);
+constexpr int64_t LOSS_WORKGROUPS = 16384;
+static LossGrid loss_grid(const LossArgs& a) {
+  const int64_t rows = a.l.d.rows, stretches = stretches_of(slots_of(a));
   const int groups = rows * ((stretches + 3) / 4) >= 1024 ? 4 : 1;
   const int64_t passes = (stretches + groups - 1) / groups, each = std::max<int64_t>(1, LOSS_WORKGROUPS / rows);
   const int64_t per = std::min<int64_t>((passes + each - 1) / each, LIST_RANGE / (groups * LOSS_TOKENS));
@@ -790,9 +957,10 @@ static LossGrid loss_grid(int64_t rows, int64_t vocab) {
 }
 // No fewer than any call of at most so many rows and tokens has: a row has no more than its share of LOSS_WORKGROUPS, or one for LIST_RANGE tokens.
 static int64_t most_parts(int64_t rows, int64_t vocab) {
-  return std::min(rows * stretches_of(vocab), std::max(LOSS_WORKGROUPS, rows * ((vocab + LIST_RANGE - 1) / LIST_RANGE)));
+  const int64_t slots = most_slots(vocab);
+  return std::min(rows * stretches_of(slots), std::max(LOSS_WORKGROUPS, rows * ((slots + LIST_RANGE - 1) / LIST_RANGE)));
 }
-static int n_chunks(int64_t vocab) { return (int)((vocab + CHUNK - 1) / CHUNK); }
+static int n_chunks(int64_t vocab) { return (int)((most_slots(vocab) + CHUNK - 1) / CHUNK); }
 static int64_t part_floats(int64_t rows, int64_t vocab) { return (most_parts(rows, vocab) * (int64_t)(sizeof(Sums) / sizeof(float)) + 3) / 4 * 4; }
 
 // launches F<bf16, ...> with `lds` bytes
@@ -831,7 +999,7 @@ extern "C" pg_status pg_token_logprobs(const pg_logits* desc, const float* tempe
   if ((uintptr_t)stats & 15) return fail(PG_ESHAPE, "pg_token_logprobs: stats are not 16-byte aligned");
   if (!scratch) return fail(PG_EINVAL, "pg_token_logprobs: scratch is NULL");
   if ((uintptr_t)scratch & 7) return fail(PG_ESHAPE, "pg_token_logprobs: scratch is not 8-byte aligned");
-  const LossGrid g = loss_grid(rows, a.l.d.vocab);
+  const LossGrid g = loss_grid(a);
   const bool top = n_top && (top_ids || top_logp);
   const LogprobOut o{target, logp, entropy, stats, n_top, top_ids, top_logp, (Sums*)scratch, scratch + part_floats(rows, a.l.d.vocab), n_chunks(a.l.d.vocab)};
   return with_kind(a, g.groups, [&](auto bf, auto groups) {
@@ -846,8 +1014,10 @@ extern "C" pg_status pg_token_logprobs(const pg_logits* desc, const float* tempe
   });
 }
 
+static bool past_the_caches(const LossArgs& a) { return a.l.d.dtype == PG_LOGITS_BF16 && (int64_t)a.l.d.rows * a.l.d.vocab * 2 > 256ll << 20; }
+
 // A gradient's workgroup takes four groups a lane once, or (few rows) one.
-static int gradient_groups(int64_t rows, int64_t vocab) { return rows * ((stretches_of(vocab) + 3) / 4) >= 1024 ? 4 : 1; }
+static int gradient_groups(const LossArgs& a) { return a.l.d.rows * ((stretches_of(slots_of(a)) + 3) / 4) >= 1024 ? 4 : 1; }
 
 extern "C" pg_status pg_token_logprobs_backward(const pg_logits* desc, const float* temperature, const int32_t* target, const float* stats,
                                                 const float* g_logp, const float* g_entropy, void* d_logits, int64_t d_stride, void* stream) {
@@ -859,11 +1029,13 @@ extern "C" pg_status pg_token_logprobs_backward(const pg_logits* desc, const flo
   if ((uintptr_t)stats & 15) return fail(PG_ESHAPE, "pg_token_logprobs_backward: stats are not 16-byte aligned");
   if (g_logp && !target) return fail(PG_EINVAL, "pg_token_logprobs_backward: a gradient of log-probs without targets");
   PG_TRY(check_gradient(a, d_logits, d_stride, "pg_token_logprobs_backward"));
-  return with_kind(a, gradient_groups(rows, a.l.d.vocab), [&](auto bf, auto groups) {
+  return with_kind(a, gradient_groups(a), [&](auto bf, auto groups) {
+    constexpr bool BF = decltype(bf)::value;
     constexpr int G = decltype(groups)::value;
-    const int pieces = (int)((stretches_of(a.l.d.vocab) + G - 1) / G);
-    PG_LOSS_LAUNCH(rows * pieces, LOSS_THREADS, 0, (logprob_backward_kernel<decltype(bf)::value, G>), a, pieces, target, stats, g_logp, g_entropy, d_logits,
-                   d_stride);
+    const int64_t blocks = rows * ((stretches_of(slots_of(a)) + G - 1) / G);
+    const int pieces = (int)(blocks / rows);
+    if (past_the_caches(a)) PG_LOSS_LAUNCH(blocks, LOSS_THREADS, 0, (logprob_backward_kernel<BF, G, BF>), a, pieces, target, stats, g_logp, g_entropy, d_logits, d_stride);
+    else PG_LOSS_LAUNCH(blocks, LOSS_THREADS, 0, (logprob_backward_kernel<BF, G, false>), a, pieces, target, stats, g_logp, g_entropy, d_logits, d_stride);
     return PG_OK;
   });
 }
@@ -888,9 +1060,9 @@ extern "C" pg_status pg_distill_loss(const pg_logits* desc, const float* tempera
   if (rows == 0) return PG_OK;
   if (!loss || !scratch) return fail(PG_EINVAL, "pg_distill_loss: null pointer");
   if ((uintptr_t)scratch & 7) return fail(PG_ESHAPE, "pg_distill_loss: scratch is not 8-byte aligned");
-  const LossGrid g = loss_grid(rows, a.l.d.vocab);
+  const LossGrid g = loss_grid(a);
   const DistillArgs o{mode, k, teacher_ids, teacher_logp, loss, stats, (Sums*)scratch};
-  const size_t lds = std::max<size_t>(std::min<int64_t>(g.range, (a.l.d.vocab + 31) / 32 * 32) / 8, g.pieces == 1 ? sizeof(ListLds) : 0);
+  const size_t lds = std::max<size_t>(std::min<int64_t>(g.range, (slots_of(a) + 31) / 32 * 32) / 8, g.pieces == 1 ? sizeof(ListLds) : 0);
   return with_kind(a, g.groups, [&](auto bf, auto groups) {
     constexpr bool BF = decltype(bf)::value;
     PG_LOSS_LAUNCH(rows * g.pieces, LOSS_THREADS, lds, (distill_kernel<BF, decltype(groups)::value>), a, g, o);
@@ -909,10 +1081,13 @@ extern "C" pg_status pg_distill_backward(const pg_logits* desc, const float* tem
   if (!stats || !g_loss) return fail(PG_EINVAL, "pg_distill_backward: null pointer");
   PG_TRY(check_gradient(a, d_logits, d_stride, "pg_distill_backward"));
   const DistillArgs o{0, k, teacher_ids, teacher_logp, nullptr, const_cast<float*>(stats), nullptr};
-  return with_kind(a, gradient_groups(rows, a.l.d.vocab), [&](auto bf, auto groups) {
+  return with_kind(a, gradient_groups(a), [&](auto bf, auto groups) {
+    constexpr bool BF = decltype(bf)::value;
     constexpr int G = decltype(groups)::value;
-    const int pieces = (int)((stretches_of(a.l.d.vocab) + G - 1) / G);
-    PG_LOSS_LAUNCH(rows * pieces, LOSS_THREADS, 0, (distill_backward_kernel<decltype(bf)::value, G>), a, pieces, o, g_loss, d_logits, d_stride);
+    const int64_t blocks = rows * ((stretches_of(slots_of(a)) + G - 1) / G);
+    const int pieces = (int)(blocks / rows);
+    if (past_the_caches(a)) PG_LOSS_LAUNCH(blocks, LOSS_THREADS, 0, (distill_backward_kernel<BF, G, BF>), a, pieces, o, g_loss, d_logits, d_stride);
+    else PG_LOSS_LAUNCH(blocks, LOSS_THREADS, 0, (distill_backward_kernel<BF, G, false>), a, pieces, o, g_loss, d_logits, d_stride);
     return PG_OK;
   });
 }

@@ -268,6 +268,17 @@ def test_ascending_and_descending_logits(lib, vocab):
     check_logprobs(got, z, False, target, n_top=64, g=np.ones(4), ge=np.ones(4))
 
 
+def test_large_logits_that_all_lie_in_the_same_places(lib):
+    """In every 256 stretches of 32 tokens the same 63 have nearly all of the mass."""
+    rng = np.random.default_rng(4)
+    vocab = 300001
+    z = rounded(rng.standard_normal((2, vocab)) * 0.5 + 10.0 * (np.arange(vocab) // 32 % 256 < 63), False)
+    z[1] = rounded(np.floor(z[1] * 4) / 4, False)          # and many equal ones
+    target = np.array([0, 300000])
+    for n_top in (1, 63, 64):
+        check_logprobs(run_logprobs(lib, z, False, target, n_top=n_top), z, False, target, n_top=n_top)
+
+
 def test_any_output_may_be_left_out(lib):
     rng = np.random.default_rng(5)
     z = make_logits(rng, 3, 5000, False)
