@@ -86,5 +86,16 @@ __device__ __forceinline__ float across_rows(float v, Op op) {
 __device__ __forceinline__ float wave_allsum(float v) {
   return across_rows(head_sum(v, true), [](float x, float y) { return x + y; });
 }
+// largest of the wave, the same in every lane
+template <int CTRL>
+__device__ __forceinline__ int permuted(int w) { return __builtin_amdgcn_update_dpp(w, w, CTRL, 0xF, 0xF, false); }
+__device__ __forceinline__ float wave_max(float v) {
+  auto f = [](int w) { return __builtin_bit_cast(float, w); };
+  v = fmaxf(v, f(permuted<0xB1>(__builtin_bit_cast(int, v))));
+  v = fmaxf(v, f(permuted<0x4E>(__builtin_bit_cast(int, v))));
+  v = fmaxf(v, f(permuted<0x141>(__builtin_bit_cast(int, v))));
+  v = fmaxf(v, f(permuted<0x140>(__builtin_bit_cast(int, v))));
+  return across_rows(v, [](float x, float y) { return fmaxf(x, y); });
+}
 
 }  // namespace pg

@@ -288,16 +288,6 @@ __device__ __forceinline__ void join(Draw& a, const Draw& b) {
     a.y = b.y;
   }
 }
-template <int CTRL>
-__device__ __forceinline__ int permuted(int w) { return __builtin_amdgcn_update_dpp(w, w, CTRL, 0xF, 0xF, false); }
-__device__ __forceinline__ float wave_max(float v) {
-  auto f = [](int w) { return __builtin_bit_cast(float, w); };
-  v = fmaxf(v, f(permuted<0xB1>(__builtin_bit_cast(int, v))));
-  v = fmaxf(v, f(permuted<0x4E>(__builtin_bit_cast(int, v))));
-  v = fmaxf(v, f(permuted<0x141>(__builtin_bit_cast(int, v))));
-  v = fmaxf(v, f(permuted<0x140>(__builtin_bit_cast(int, v))));
-  return across_rows(v, [](float x, float y) { return fmaxf(x, y); });
-}
 __device__ __forceinline__ Draw wave_join(Draw a) {
   const float top = wave_max(a.top);
   a.sum = wave_allsum(a.sum * exp_of(a.top - top));

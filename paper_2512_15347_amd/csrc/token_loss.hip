@@ -23,6 +23,7 @@ constexpr float FAR = 300.0f;                        // 2^-FAR is 0 in fp32
 struct LossArgs {
   LogitArgs l;
   const float* temperature;
+  int64_t span;                                      // elements from the first row's first logit to the last row's last
 };
 
 // What one row needs.
@@ -80,18 +81,16 @@ __device__ __forceinline__ void join(Sums& a, Sums b, const LossRow& q) {
   a.s += b.s;
   a.u += b.u;
 }
-__device__ __forceinline__ float lanes_max(float v) {
-  for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-  return v;
-}
 __device__ __forceinline__ Sums wave_sums(Sums a, const LossRow& q) {
-  move_to(a, lanes_max(a.m), q);
+  move_to(a, wave_max(a.m), q);
   a.s = wave_allsum(a.s);
   a.u = wave_allsum(a.u);
   return a;
 }
+// The workgroup's, from lanes that have the same m throughout a wave.
 __device__ __forceinline__ Sums block_sums(Sums a, const LossRow& q, Sums* waves) {
-  a = wave_sums(a, q);
+  a.s = wave_allsum(a.s);
+  a.u = wave_allsum(a.u);
   if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = a;
   __syncthreads();
   a = waves[0];
@@ -100,56 +99,83 @@ __device__ __forceinline__ Sums block_sums(Sums a, const LossRow& q, Sums* waves
   return a;
 }
 
+// Keeps the compiler from unpacking all groups of a pass before it works on the first: eight waves a SIMD instead of five.
+__device__ __forceinline__ void one_group_at_a_time() { __builtin_amdgcn_sched_barrier(0); }
+
 // A lane's part of one pass over a range: G groups of eight slots and which of their tokens count: those that are in the row and in the range,
 // allowed and not struck out.  16-byte loads may be unaligned, but in bf16, where a row may begin between two 4-byte words, they are a third
-// slower then (4096 x 131073, the forward pass: 311 us, LATER with slots); in fp32 it makes no difference.
+// slower then (4096 x 131073, the forward pass: 311 us, 222 with slots); in fp32 it makes no difference.
+typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(4)));
+
 template <bool BF16, int G>
 struct Pass {
   static constexpr int ELT = BF16 ? 2 : 4;
   uint32_t raw[G][BF16 ? 4 : 8];
   uint32_t bits[G];
 
-  // whether the group at slot t lies in the row
-  static __device__ __forceinline__ bool inside(const LossRow& q, int64_t t, int64_t vocab) { return t >= q.shift && t - q.shift + LANE_TOKENS <= vocab; }
-  static __device__ __forceinline__ uint32_t mask_bits(const LossArgs& a, const LossRow& q, int64_t t, bool whole) {
-    if (!q.allow) return q.unmasked;
-    if (q.shift == 0) return q.allow[t >> 3];
-    const int64_t byte = (t - q.shift) >> 3;         // the first token's, -1 before the row
-    uint16_t two = 0;
-    if (whole) {
-      __builtin_memcpy(&two, q.allow + byte, 2);
-    } else {
-      if (byte >= 0) two = q.allow[byte];
-      if (byte + 1 < 4 * a.l.words) two |= (uint16_t)(q.allow[byte + 1] << 8);
-    }
-    return two >> (LANE_TOKENS - q.shift) & 0xFFu;
-  }
-  __device__ __forceinline__ void load(const LossArgs& a, const LossRow& q, const char* row, int64_t t, int64_t end, bool whole) {
-    const int64_t vocab = a.l.d.vocab;
+  // Slots base + g LOSS_TOKENS + 8 lane .. of which all have tokens; the masks' bits alone are left out where there are none.
+  template <bool MASKS>
+  __device__ __forceinline__ void load_whole(const LossArgs& a, const LossRow& q, int base) {
+    const char* p = (const char*)a.l.d.logits + (q.at + base - q.shift) * ELT;       // the wave's; a lane adds 32 bits
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int i = 0; i < (BF16 ? 4 : 8); i += 4) {
+        const Words x = __builtin_nontemporal_load((const Words*)(p + g * (LOSS_TOKENS * ELT) + threadIdx.x * (LANE_TOKENS * ELT) + 4 * i));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) raw[g][i + j] = x[j];
+      }
+    if (!MASKS) return;
+    const uint8_t* m = q.allow + ((base - q.shift) >> 3);
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      const int64_t at = t + g * LOSS_TOKENS, v = at - q.shift;
-      const char* p = row + v * ELT;
-      bits[g] = 0;
-      if (whole || (at < end && inside(q, at, vocab))) {
-        __builtin_memcpy(raw[g], __builtin_assume_aligned(p, BF16 ? 16 : 4), BF16 ? 16 : 32);
-        bits[g] = mask_bits(a, q, at, true);
+      const uint8_t* at = m + g * (LOSS_TOKENS / LANE_TOKENS) + threadIdx.x;
+      if (q.shift == 0) {
+        bits[g] = *at;
       } else {
-        uint32_t there = 0;
+        uint16_t two;
+        __builtin_memcpy(&two, at, 2);
+        bits[g] = two >> (LANE_TOKENS - q.shift) & 0xFFu;
+      }
+    }
+  }
+  // Of slots up to `end`.  A group at an end of its row is read with what lies beside it in the logits' span; only the first row's first and the last
+  // row's last may have nothing there.
+  __device__ __forceinline__ void load_part(const LossArgs& a, const LossRow& q, int base, int end) {
+    const int vocab = a.l.d.vocab;
 #pragma unroll
-        for (int e = 0; e < LANE_TOKENS; ++e) {
-          const bool in = at < end && v + e >= 0 && v + e < vocab;
-          const uint32_t x = !in ? 0u : BF16 ? ((const uint16_t*)p)[e] : ((const uint32_t*)p)[e];
-          there |= (uint32_t)in << e;
-          if (!BF16) raw[g][e] = x;
-          else raw[g][e >> 1] = e & 1 ? raw[g][e >> 1] | x << 16 : x;
+    for (int g = 0; g < G; ++g) {
+      const int at = base + g * LOSS_TOKENS + (int)threadIdx.x * LANE_TOKENS, v = at - q.shift;
+      const char* p = (const char*)a.l.d.logits + (q.at + v) * ELT;
+      bits[g] = 0;
+      if (at < end && v < vocab) {
+        uint32_t there = v < 0 ? 0xFFu << -v & 0xFFu : 0xFFu;
+        if (v > vocab - LANE_TOKENS) there &= (1u << (vocab - v)) - 1;
+        if (q.at + v >= 0 && q.at + v + LANE_TOKENS <= a.span) {
+          __builtin_memcpy(raw[g], __builtin_assume_aligned(p, BF16 ? 16 : 4), BF16 ? 16 : 32);
+        } else {
+#pragma unroll
+          for (int e = 0; e < LANE_TOKENS; ++e) {
+            const uint32_t x = !(there >> e & 1) ? 0u : BF16 ? ((const uint16_t*)p)[e] : ((const uint32_t*)p)[e];
+            if (!BF16) raw[g][e] = x;
+            else raw[g][e >> 1] = e & 1 ? raw[g][e >> 1] | x << 16 : x;
+          }
         }
-        if (there) bits[g] = mask_bits(a, q, at, false) & there;
+        if (q.allow) {
+          const int byte = v >> 3;                   // the first token's, -1 before the row
+          const uint32_t lo = byte >= 0 ? q.allow[byte] : 0u, hi = byte + 1 < 4 * a.l.words ? q.allow[byte + 1] : 0u;
+          there &= (lo | hi << 8) >> (v & 7);
+        }
+        bits[g] = there;
       }
     }
   }
   __device__ __forceinline__ float raw_logit(int g, int e) const {
     return __builtin_bit_cast(float, !BF16 ? raw[g][e] : e & 1 ? raw[g][e >> 1] & 0xFFFF0000u : raw[g][e >> 1] << 16);
+  }
+  __device__ __forceinline__ void all_count() {
+#pragma unroll
+    for (int g = 0; g < G; ++g) bits[g] = 0xFFu;
   }
   // HOLES: -inf for what does not count
   template <bool HOLES>
@@ -163,37 +189,65 @@ struct Pass {
     for (int e = 1; e < LANE_TOKENS; ++e) top = fmaxf(top, logit<HOLES>(g, e));
     return top;
   }
-};
-
-// Goes through slots first .. end - 1 of a row: each(pass, its first slot of this lane, whether some of the wave's tokens do not count) for passes
-// that have a token that counts, none(first slot) for the others.  strike(t): bits of the group at slot t that are struck out.
-template <bool BF16, int G, class Strike, class Each, class None>
-__device__ __forceinline__ void through(const LossArgs& a, const LossRow& q, int64_t first, int64_t end, Strike strike, Each each, None none) {
-  const char* row = (const char*)a.l.d.logits + q.at * (BF16 ? 2 : 4);
-#pragma unroll 1
-  for (int64_t base = first; base < end; base += G * LOSS_TOKENS) {
-    const int64_t t = base + threadIdx.x * LANE_TOKENS;
-    Pass<BF16, G> x;
-    if (base >= q.shift && base + G * LOSS_TOKENS <= min(end, a.l.d.vocab + (int64_t)q.shift)) x.load(a, q, row, t, end, true);
-    else x.load(a, q, row, t, end, false);
-    uint32_t all = 0xFFu, some = 0;
+  // of the wave's, the same in every lane
+  __device__ __forceinline__ float largest(bool holes) const {
+    float top = -INFINITY;
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      x.bits[g] &= ~strike(t + g * LOSS_TOKENS);
-      all &= x.bits[g];
-      some |= x.bits[g];
+      top = fmaxf(top, holes ? largest<true>(g) : largest<false>(g));
+      one_group_at_a_time();
     }
-    const bool holes = __ballot(all != 0xFFu);
-    if (holes && !__ballot(some != 0)) none(t);
-    else each(x, t, holes);
+    return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, wave_max(top))));
+  }
+};
+
+// Goes through slots first .. end - 1 of a row: each(pass, its first slot, whether some of the wave's tokens do not count) for passes that have a
+// token that counts, none(first slot) for the others; `first` is a multiple of LOSS_TOKENS.  strike(t): bits of the group at slot t that are
+// struck out, if STRIKES.
+template <bool BF16, int G, bool STRIKES, class Strike, class Each, class None>
+__device__ __forceinline__ void through(const LossArgs& a, const LossRow& q, int first, int end, Strike strike, Each each, None none) {
+  const int whole = min(end, a.l.d.vocab + q.shift) - G * LOSS_TOKENS;         // the last pass of which all slots have tokens
+#pragma unroll 1
+  for (int base = first; base < end; base += G * LOSS_TOKENS) {
+    Pass<BF16, G> x;
+    bool holes = false;
+    if (!q.allow && !q.unmasked) {
+      none(base);
+      continue;
+    }
+    if (base >= q.shift && base <= whole) {
+      if (q.allow) x.template load_whole<true>(a, q, base);
+      else x.template load_whole<false>(a, q, base);
+    } else {
+      x.load_part(a, q, base, end);
+      holes = true;
+    }
+    if (STRIKES || holes || q.allow) {
+      uint32_t all = 0xFFu, some = 0;
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        if (!q.allow && !holes) x.bits[g] = 0xFFu;
+        if (STRIKES) x.bits[g] &= ~strike(base + g * LOSS_TOKENS + (int)threadIdx.x * LANE_TOKENS);
+        all &= x.bits[g];
+        some |= x.bits[g];
+      }
+      holes = __ballot(all != 0xFFu);
+      if (holes && !__ballot(some != 0)) {
+        none(base);
+        continue;
+      }
+    }
+    each(x, base, holes);
   }
 }
+constexpr auto no_strike = [](int) { return 0u; };
 
 // What a wave has summed: every lane the sums of its own tokens, relative to one logit m for all of them, which is some logit of the wave's
 // and at most a little less than the largest: 2^x stays within 2^6.
 struct WaveSums {
   Sums sums;
   bool clamp;                                        // there are logits of -inf
+  __device__ __forceinline__ WaveSums() : sums(no_sums()), clamp(false) {}
 };
 
 // What does not count has x = -FAR.
@@ -216,19 +270,24 @@ __device__ __forceinline__ void add_near(const P& x, float r, const LossRow& q, 
       s += p[e];
       if (ENTROPY) u = __builtin_fmaf(p[e], CLAMP ? fmaxf(y[e], -FAR) : y[e], u);
     }
+    one_group_at_a_time();
   }
 }
 
 // Adds a pass to the sums.  As a rule m stays, and x = z c - r is one operation, with r = m c as rounded; what r is off, d, is known and goes into
-// the sums afterwards.  Where a lane's sum shows that m is too small (or that there is a NaN), where nothing has been seen yet, or where r is no
-// number of fp32, the pass is gone through again: m becomes the largest logit of the wave's, and x = (z - m) c.
+// the sums afterwards.  Where a lane's sum shows that m is too small (or that there is a NaN), or where r is so large that d is, too, the pass is gone through
+// again: m becomes the largest logit of the wave's, and x = (z - m) c.
 template <bool ENTROPY, bool BF16, int G>
-__device__ __forceinline__ void take(WaveSums& a, const Pass<BF16, G>& x, bool holes, const LossRow& q) {
+__device__ __forceinline__ void take(WaveSums& a, Pass<BF16, G>& x, bool holes, const LossRow& q) {
   using P = Pass<BF16, G>;
+  if (a.sums.m == -FLT_MAX) a.sums.m = fmaxf(a.sums.m, x.largest(holes));        // nothing but zeros has been summed
   const float m = a.sums.m, r = m * q.c;
-  if (fabsf(r) < INFINITY) {
+  if (fabsf(r) < 16777216.0f) {                      // d is at most 1/2
     float s = 0.0f, u = 0.0f;
-    if (ENTROPY && a.clamp) add_near<true, true, ENTROPY, P, G>(x, r, q, s, u);
+    if (ENTROPY && a.clamp) {
+      if (!holes) x.all_count();
+      add_near<true, true, ENTROPY, P, G>(x, r, q, s, u);
+    }
     else if (holes) add_near<true, false, ENTROPY, P, G>(x, r, q, s, u);
     else add_near<false, false, ENTROPY, P, G>(x, r, q, s, u);
     if (!__ballot(!(s <= 64.0f && u == u))) {
@@ -239,15 +298,14 @@ __device__ __forceinline__ void take(WaveSums& a, const Pass<BF16, G>& x, bool h
       return;
     }
   }
-  float top = -INFINITY, low = INFINITY;
+  if (!holes) x.all_count();
+  float low = INFINITY;
 #pragma unroll
-  for (int g = 0; g < G; ++g) {
-    top = fmaxf(top, x.template largest<true>(g));
+  for (int g = 0; g < G; ++g)
 #pragma unroll
     for (int e = 0; e < LANE_TOKENS; ++e) low = fminf(low, x.raw_logit(g, e));
-  }
   a.clamp |= __ballot(low == -INFINITY) != 0;
-  top = lanes_max(top);
+  const float top = x.largest(holes);
   if (top > m) move_to(a.sums, top, q);
   float s = 0.0f, u = 0.0f;
 #pragma unroll
@@ -257,21 +315,35 @@ __device__ __forceinline__ void take(WaveSums& a, const Pass<BF16, G>& x, bool h
       const float y = (x.template logit<true>(g, e) - a.sums.m) * q.c, p = exp2_of(y);
       s += p;
       if (ENTROPY) u = __builtin_fmaf(p, fmaxf(y, -FAR), u);
+      if (e + 1 == LANE_TOKENS) one_group_at_a_time();
     }
   a.sums.s += s;
   a.sums.u += u;
 }
 
-// How a call is laid out: groups a lane takes at a time, tokens of a workgroup, workgroups of a row.
+// How a pass over the logits is laid out.  Rows are stretches of LOSS_TOKENS slots each, and a workgroup takes the next `share` of all rows'
+// stretches: so that all workgroups are resident at once and end together.  What it sums of row r goes to part r + its own number.
 struct LossGrid {
-  int groups, range, pieces;
+  int stretches, share, workgroups;
 };
+struct Part {
+  int r, from, to;                                   // stretches of row r
+  __device__ __forceinline__ Part(const LossGrid& g, int at, int stop) : r(at / g.stretches), from(at - r * g.stretches), to(min(g.stretches, from + stop - at)) {}
+};
+// The sums of row r: of a wave's lanes, from the parts; false where one workgroup has had it all.
+__device__ __forceinline__ bool parts_of(const LossGrid& g, int r, const Sums* parts, const LossRow& q, Sums& sum) {
+  const int first = r * g.stretches / g.share, last = ((r + 1) * g.stretches - 1) / g.share;
+  sum = no_sums();
+  for (int w = first + (int)(threadIdx.x & 63); w <= last; w += WAVE) join(sum, parts[r + w], q);
+  sum = wave_sums(sum, q);
+  return first < last;
+}
 
 // ---------------------------------------------------------------- alternatives
 // The n best tokens lie in the n stretches of CHUNK slots whose largest logits come first (equal ones in the order of their tokens): each of
 // these has a token that comes before all others of the stretches that come after.  So the pass over the logits leaves the largest logit of each
 // stretch, the stretches are chosen from these, and their tokens are looked at again.
-constexpr int CHUNK = 4 * LANE_TOKENS;               // of four adjacent lanes
+constexpr int CHUNK_LANES = 8, CHUNK = CHUNK_LANES * LANE_TOKENS;
 
 // Its bits in the order of the numbers; -0 and 0 are equal.
 __device__ __forceinline__ uint32_t ordered(float z) {
@@ -381,7 +453,8 @@ __device__ __forceinline__ void select_by_key(int N, int n, TopLds& s, Item item
 // The n best tokens of a row, from the largest logits of its stretches, to s.best: all lanes of a workgroup.
 template <bool BF16>
 __device__ __forceinline__ void alternatives(const LossArgs& a, const LossRow& q, const float* largest, int n, TopLds& s) {
-  constexpr int KEPT = 20;                           // stretches a lane has in registers: 163840 tokens
+  constexpr int KEPT = 10;                           // stretches a lane has in registers: 163840 tokens
+  constexpr int AGAIN = PG_TOP_MAX * CHUNK_LANES / LOSS_THREADS;
   const int me = threadIdx.x, vocab = a.l.d.vocab, N = (vocab + q.shift + CHUNK - 1) / CHUNK;
   no_candidates(s);
   float z[KEPT], top = -INFINITY;
@@ -397,23 +470,29 @@ __device__ __forceinline__ void alternatives(const LossArgs& a, const LossRow& q
   for (int i = me + KEPT * LOSS_THREADS; i < N; i += LOSS_THREADS)
     if (largest[i] >= bound && largest[i] > -INFINITY) candidate(key_of(largest[i], i), s);
   if (!rank_candidates(n, s)) select_by_key(N, n, s, [&](int i) { return key_of(largest[i], i); });
-  // four lanes look at a stretch again, eight tokens each
-  const uint64_t chunk = me / 4 < n ? s.best[me / 4] : 0;
+  // the lanes look at these stretches again, eight tokens each
   const float least = logit_of(s.best[n - 1]);       // NaN for 0: nothing is below it
-  Pass<BF16, 1> x;
-  const int64_t slot = chunk ? (int64_t)place_of(chunk) * CHUNK + (me & 3) * LANE_TOKENS : (int64_t)vocab + q.shift;
-  x.load(a, q, (const char*)a.l.d.logits + q.at * (BF16 ? 2 : 4), slot, (int64_t)vocab + q.shift, false);
-  const int v = (int)(slot - q.shift);
-  uint64_t key[LANE_TOKENS];
+  const int end = vocab + q.shift;
+  uint64_t key[AGAIN * LANE_TOKENS];
+  Pass<BF16, 1> x[AGAIN];
+#pragma unroll
+  for (int k = 0; k < AGAIN; ++k) {
+    const int i = (me + k * LOSS_THREADS) / CHUNK_LANES;
+    const uint64_t chunk = i < n ? s.best[i] : 0;
+    const int slot = chunk ? place_of(chunk) * CHUNK + me % CHUNK_LANES * LANE_TOKENS : end;
+    x[k].load_part(a, q, slot - me * LANE_TOKENS, end);
+#pragma unroll
+    for (int e = 0; e < LANE_TOKENS; ++e) key[k * LANE_TOKENS + e] = slot - q.shift + e;
+  }
   no_candidates(s);
   __syncthreads();
 #pragma unroll
-  for (int e = 0; e < LANE_TOKENS; ++e) {
-    const float y = x.template logit<true>(0, e);
-    key[e] = y < least ? 0 : key_of(y, v + e);
+  for (int e = 0; e < AGAIN * LANE_TOKENS; ++e) {
+    const float y = x[e / LANE_TOKENS].template logit<true>(0, e % LANE_TOKENS);
+    key[e] = y < least ? 0 : key_of(y, (int)key[e]);
     if (key[e]) candidate(key[e], s);
   }
-  if (!rank_candidates(n, s)) select_by_key(LOSS_THREADS * LANE_TOKENS, n, s, [&](int i) { return key[i / LOSS_THREADS]; });
+  if (!rank_candidates(n, s)) select_by_key(LOSS_THREADS * LANE_TOKENS * AGAIN, n, s, [&](int i) { return key[i / LOSS_THREADS]; });
 }
 
 struct LogprobOut {
@@ -422,7 +501,7 @@ struct LogprobOut {
   int n_top;
   int32_t* top_ids;
   float* top_logp;
-  Sums* parts;                                       // [rows, pieces]
+  Sums* parts;                                       // [rows + workgroups]
   float* chunks;                                     // [rows, n_chunks]: the largest logit of each
   int n_chunks;
 };
@@ -458,48 +537,46 @@ __device__ __forceinline__ void finish_logprob(const LossArgs& a, const LogprobO
 }
 
 template <bool BF16, int G, bool TOP>
-__global__ __launch_bounds__(LOSS_THREADS) void logprob_kernel(LossArgs a, LossGrid grid, LogprobOut o) {
+__global__ __launch_bounds__(LOSS_THREADS, TOP ? 6 : 8) void logprob_kernel(LossArgs a, LossGrid grid, LogprobOut o) {
   __shared__ Sums waves[LOSS_WAVES];
-  __shared__ TopLds lists;
-  const int r = blockIdx.x / grid.pieces, piece = blockIdx.x - r * grid.pieces, lane = threadIdx.x & 63;
-  const LossRow q = loss_row<BF16>(a, r);
-  const int target = o.target ? o.target[r] : 0;
-  const float at_target = target >= 0 && target < a.l.d.vocab ? open_logit<BF16>(a, q, target) : 0.0f;       // asked for early
-  WaveSums mine{no_sums(), false};
-  if (target != -1) {
-    const int64_t first = (int64_t)piece * grid.range, end = min(first + grid.range, (int64_t)a.l.d.vocab + q.shift);
-    float* chunks = o.chunks + (int64_t)r * o.n_chunks;
-    auto leave = [&](int64_t t, int g, float top) {
-      const int c = (int)(t / CHUNK) + g * (LOSS_TOKENS / CHUNK);
-      if ((lane & 3) == g % 4 && c < o.n_chunks) chunks[c] = top;
-    };
-    through<BF16, G>(a, q, first, end, [](int64_t) { return 0u; }, [&](const Pass<BF16, G>& x, int64_t t, bool holes) {
-      take<true>(mine, x, holes, q);
-      if (TOP) {
-        auto moved = [](float y, auto ctrl) {
-          const int w = __builtin_bit_cast(int, y);
-          return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(w, w, decltype(ctrl)::value, 0xF, 0xF, false));
-        };
+  const int stop = min((int)(blockIdx.x + 1) * grid.share, a.l.d.rows * grid.stretches), lane = threadIdx.x & 63;
+  for (int at = blockIdx.x * grid.share; at < stop;) {
+    const Part part(grid, at, stop);
+    const int r = part.r;
+    const LossRow q = loss_row<BF16>(a, r);
+    const int target = o.target ? o.target[r] : 0;
+    WaveSums mine;
+    if (target != -1) {
+      float* chunks = o.chunks + (int64_t)r * o.n_chunks;
+      const int end = min(part.to * LOSS_TOKENS, a.l.d.vocab + q.shift);
+      auto leave = [&](int base, int g, float top) { // a pass may reach past the part's end
+        const int c = base / CHUNK + g * (LOSS_TOKENS / CHUNK) + (int)threadIdx.x / CHUNK_LANES;
+        if (lane % CHUNK_LANES == g && c * CHUNK < end) chunks[c] = top;
+      };
+      through<BF16, G, false>(a, q, part.from * LOSS_TOKENS, end, no_strike, [&](Pass<BF16, G>& x, int base, bool holes) {
+        if (TOP) {
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-          float top = holes ? x.template largest<true>(g) : x.template largest<false>(g);
-          top = fmaxf(top, moved(top, std::integral_constant<int, 0xB1>{}));
-          top = fmaxf(top, moved(top, std::integral_constant<int, 0x4E>{}));
-          leave(t, g, top);
+          for (int g = 0; g < G; ++g) {
+            float top = holes ? x.template largest<true>(g) : x.template largest<false>(g);
+            top = fmaxf(top, __builtin_bit_cast(float, permuted<0xB1>(__builtin_bit_cast(int, top))));
+            top = fmaxf(top, __builtin_bit_cast(float, permuted<0x4E>(__builtin_bit_cast(int, top))));
+            top = fmaxf(top, __builtin_bit_cast(float, permuted<0x141>(__builtin_bit_cast(int, top))));
+            leave(base, g, top);
+          }
         }
-      }
-    }, [&](int64_t t) {
-      if (TOP)
-        for (int g = 0; g < G; ++g) leave(t, g, -INFINITY);
-    });
+        take<true>(mine, x, holes, q);
+      }, [&](int base) {
+        if (TOP)
+          for (int g = 0; g < G; ++g) leave(base, g, -INFINITY);
+      });
+    }
+    const Sums sum = block_sums(mine.sums, q, waves);
+    if (!TOP && part.from == 0 && part.to == grid.stretches)
+      finish_logprob<BF16>(a, o, q, r, target, target >= 0 && target < a.l.d.vocab ? open_logit<BF16>(a, q, target) : 0.0f, sum, nullptr);
+    else if (threadIdx.x == 0) o.parts[r + blockIdx.x] = sum;
+    at += part.to - part.from;
+    if (at < stop) __syncthreads();                  // the waves' sums have been read
   }
-  const Sums sum = block_sums(mine.sums, q, waves);
-  if (grid.pieces > 1) {
-    if (threadIdx.x == 0) o.parts[blockIdx.x] = sum;
-    return;
-  }
-  if (TOP) __threadfence_block();
-  finish_logprob<BF16>(a, o, q, r, target, at_target, sum, TOP ? &lists : nullptr);
 }
 
 template <bool BF16, bool TOP>
@@ -509,24 +586,22 @@ __global__ __launch_bounds__(LOSS_THREADS) void logprob_finish_kernel(LossArgs a
   const LossRow q = loss_row<BF16>(a, r);
   const int target = o.target ? o.target[r] : 0;
   const float at_target = target >= 0 && target < a.l.d.vocab ? open_logit<BF16>(a, q, target) : 0.0f;
-  Sums sum = no_sums();
-  for (int i = threadIdx.x & 63; i < grid.pieces; i += WAVE) join(sum, o.parts[(int64_t)r * grid.pieces + i], q);
-  sum = wave_sums(sum, q);
-  finish_logprob<BF16>(a, o, q, r, target, at_target, sum, TOP ? &lists : nullptr);
+  Sums sum;
+  if (parts_of(grid, r, o.parts, q, sum) || TOP) finish_logprob<BF16>(a, o, q, r, target, at_target, sum, TOP ? &lists : nullptr);
 }
 
 // Writes the gradient of the tokens v .. v + 7 that are in the row, but for those of `others`, in the logits' type.  PAST: not to be kept in the
 // caches.
 template <bool BF16, bool PAST>
-__device__ __forceinline__ void put(char* row, int64_t v, int64_t vocab, const float* d, uint32_t others = 0) {
-  char* to = row + v * (BF16 ? 2 : 4);
+__device__ __forceinline__ void put(char* row, int v, int vocab, const float* d, uint32_t others = 0) {
+  char* to = row + (int64_t)v * (BF16 ? 2 : 4);
   if (v >= 0 && v + LANE_TOKENS <= vocab && !others) {
     if (BF16) {
       const uint32_t w[4] = {pack_bf16x2(d[0], d[1]), pack_bf16x2(d[2], d[3]), pack_bf16x2(d[4], d[5]), pack_bf16x2(d[6], d[7])};
-      typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(2)));
-      const Words x{w[0], w[1], w[2], w[3]};
-      if (PAST) __builtin_nontemporal_store(x, (Words*)to);
-      else *(Words*)to = x;
+      typedef uint32_t Unaligned __attribute__((ext_vector_type(4), aligned(2)));
+      const Unaligned x{w[0], w[1], w[2], w[3]};
+      if (PAST) __builtin_nontemporal_store(x, (Unaligned*)to);
+      else *(Unaligned*)to = x;
     } else {
       __builtin_memcpy(to, d, 32);
     }
@@ -540,7 +615,7 @@ __device__ __forceinline__ void put(char* row, int64_t v, int64_t vocab, const f
     }
 }
 template <bool BF16, bool PAST, int G>
-__device__ __forceinline__ void put_zeros(char* row, int64_t v, int64_t vocab) {
+__device__ __forceinline__ void put_zeros(char* row, int v, int vocab) {
   const float nothing[LANE_TOKENS] = {};
 #pragma unroll
   for (int i = 0; i < G; ++i) put<BF16, PAST>(row, v + i * LOSS_TOKENS, vocab, nothing);
@@ -552,24 +627,24 @@ __global__ __launch_bounds__(LOSS_THREADS) void logprob_backward_kernel(LossArgs
                                                                         const float* g_logp, const float* g_entropy, void* out, int64_t out_stride) {
   constexpr int ELT = BF16 ? 2 : 4;
   const int block = gridDim.x - 1 - blockIdx.x, r = block / pieces, piece = block - r * pieces;
-  const int64_t vocab = a.l.d.vocab, first = (int64_t)piece * (G * LOSS_TOKENS);
+  const int vocab = a.l.d.vocab, first = piece * (G * LOSS_TOKENS);
   const LossRow q = loss_row<BF16>(a, r);
   const int t = target ? target[r] : 0;
   float g = g_logp ? g_logp[r] : 0.0f;
   const float ge = g_entropy ? g_entropy[r] : 0.0f;
   char* to = (char*)out + (int64_t)r * out_stride * ELT;
-  auto clear = [&](int64_t slot) { put_zeros<BF16, PAST, G>(to, slot - q.shift, vocab); };
-  if (t == -1 || (g == 0.0f && ge == 0.0f)) return clear(first + threadIdx.x * LANE_TOKENS);
+  auto clear = [&](int base) { put_zeros<BF16, PAST, G>(to, base + (int)threadIdx.x * LANE_TOKENS - q.shift, vocab); };
+  if (t == -1 || (g == 0.0f && ge == 0.0f)) return clear(first);
   if (g_logp && (t < 0 || t >= vocab)) g = __builtin_nanf("");
   const float4 s = *(const float4*)(stats + 4ll * r);
   const float ln_s = s.y, h = s.z, m = s.w;
   const float c0 = q.inv * (-g - ge * (h - ln_s)), c1 = -q.inv * ge * q.inv, at_target = q.inv * g, less = ln_s * LOG2E;
   const bool odd = !(fabsf(c0) < INFINITY && fabsf(c1) < INFINITY && less == less);        // 0 times these is no 0
-  auto each = [&](const Pass<BF16, G>& x, int64_t slot, auto all) {
+  auto each = [&](const Pass<BF16, G>& x, int base, auto all) {
     constexpr bool HOLES = !decltype(all)::value;
 #pragma unroll
     for (int i = 0; i < G; ++i) {
-      const int64_t v = slot + i * LOSS_TOKENS - q.shift;
+      const int v = base + i * LOSS_TOKENS + (int)threadIdx.x * LANE_TOKENS - q.shift;
       float d[LANE_TOKENS];
 #pragma unroll
       for (int e = 0; e < LANE_TOKENS; ++e) {
@@ -577,19 +652,22 @@ __global__ __launch_bounds__(LOSS_THREADS) void logprob_backward_kernel(LossArgs
         d[e] = exp2_of(__builtin_fmaf(y, q.c, -less)) * __builtin_fmaf(c1, y, c0);
         if (HOLES && z == -INFINITY) d[e] = 0.0f;
       }
-      const int64_t at = t - v;
+      const int at = t - v;
       if (at >= 0 && at < LANE_TOKENS) {
 #pragma unroll
         for (int e = 0; e < LANE_TOKENS; ++e)
-          if (e == at && x.template logit<true>(i, e) != -INFINITY) d[e] += at_target;
+          if (e == at && x.template logit<HOLES>(i, e) != -INFINITY) d[e] += at_target;
       }
       put<BF16, PAST>(to, v, vocab, d);
     }
   };
-  const int64_t end = min(first + G * LOSS_TOKENS, vocab + q.shift);
-  through<BF16, G>(a, q, first, end, [](int64_t) { return 0u; }, [&](const Pass<BF16, G>& x, int64_t slot, bool holes) {
-    if (holes || odd) each(x, slot, std::false_type{});
-    else each(x, slot, std::true_type{});
+  through<BF16, G, false>(a, q, first, min(first + G * LOSS_TOKENS, vocab + q.shift), no_strike, [&](Pass<BF16, G>& x, int base, bool holes) {
+    if (holes || odd) {
+      if (!holes) x.all_count();
+      each(x, base, std::false_type{});
+    } else {
+      each(x, base, std::true_type{});
+    }
   }, clear);
 }
 
@@ -598,7 +676,7 @@ __global__ __launch_bounds__(LOSS_THREADS) void logprob_backward_kernel(LossArgs
 constexpr int LIST_LANES = PG_DISTILL_MAX / WAVE;     // entries of a wave's lane
 constexpr int LIST_SLOTS = 4 * PG_DISTILL_MAX;       // a quarter full at most
 static_assert(LIST_SLOTS == 1 << 10 && PG_DISTILL_MAX == LOSS_THREADS, "ten bits of a hash, an entry a lane");
-constexpr int LIST_RANGE = 1 << 17;                  // tokens of a workgroup at most: one bit each in LDS
+constexpr int LIST_RANGE = 1 << 17;                  // slots whose bits LDS holds at a time
 
 // Which entries of a row's list count: the first of each token that exists.  A table of tokens in LDS with the first entry that has each.
 struct ListLds {
@@ -639,17 +717,13 @@ __device__ __forceinline__ double lanes_sum(double v) {
   for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
   return v;
 }
-__device__ __forceinline__ double lanes_max(double v) {
-  for (int o = 32; o; o >>= 1) v = fmax(v, __shfl_xor(v, o));
-  return v;
-}
 
 struct DistillArgs {
   int mode, k;
   const int32_t* ids;
   const float* logp;
   float *loss, *stats;
-  Sums* parts;                                       // [rows, pieces]
+  Sums* parts;                                       // [rows + workgroups]
 };
 
 // From the sums over what is not listed to the loss: the lanes of one wave.  In fp64: it is a few hundred values, and what
@@ -676,8 +750,8 @@ __device__ __forceinline__ void finish_distill(const LossArgs& a, const DistillA
       most = fmaxf(most, t[i]);
       wrong |= !(t[i] < INFINITY);
     }
-  m = lanes_max(m);
-  most = lanes_max(most);
+  m = wave_max(m);
+  most = wave_max(most);
   const double bad = __ballot(wrong) ? __builtin_nan("") : 0.0;
   const bool top = o.mode == PG_DISTILL_TOP;
   double s_all = 0.0, sum_q = 0.0;
@@ -718,27 +792,32 @@ __device__ __forceinline__ void finish_distill(const LossArgs& a, const DistillA
 }
 
 template <bool BF16, int G>
-__global__ __launch_bounds__(LOSS_THREADS) void distill_kernel(LossArgs a, LossGrid grid, DistillArgs o) {
+__global__ __launch_bounds__(LOSS_THREADS, 8) void distill_kernel(LossArgs a, LossGrid grid, DistillArgs o) {
   __shared__ Sums waves[LOSS_WAVES];
-  extern __shared__ uint32_t listed[];               // a bit for each token of the range, or (the end) the table of the list
-  const int r = blockIdx.x / grid.pieces, piece = blockIdx.x - r * grid.pieces;
-  const LossRow q = loss_row<BF16>(a, r);
-  const int64_t first = (int64_t)piece * grid.range, end = min(first + grid.range, (int64_t)a.l.d.vocab + q.shift);
-  for (int i = threadIdx.x; i < (int)((end - first + 31) / 32); i += LOSS_THREADS) listed[i] = 0;
-  const int id = (int)threadIdx.x < o.k ? o.ids[(int64_t)r * o.k + threadIdx.x] : -1;
-  const int64_t slot = (int64_t)id + q.shift;
-  __syncthreads();
-  if (id >= 0 && slot >= first && slot < end) atomicOr(&listed[(slot - first) >> 5], 1u << ((slot - first) & 31));
-  __syncthreads();
-  WaveSums mine{no_sums(), false};
-  auto strike = [&](int64_t t) { return t < end ? (uint32_t)((const uint8_t*)listed)[(t - first) >> 3] : 0u; };
-  through<BF16, G>(a, q, first, end, strike, [&](const Pass<BF16, G>& x, int64_t, bool holes) { take<false>(mine, x, holes, q); }, [](int64_t) {});
-  const Sums rest = block_sums(mine.sums, q, waves);
-  if (grid.pieces > 1) {
-    if (threadIdx.x == 0) o.parts[blockIdx.x] = rest;
-  } else {
-    __syncthreads();                                 // the bits have been read
-    if (threadIdx.x < WAVE) finish_distill<BF16>(a, o, q, r, rest, *(ListLds*)listed);
+  extern __shared__ uint32_t listed[];               // a bit for each slot of the row's part
+  const int stop = min((int)(blockIdx.x + 1) * grid.share, a.l.d.rows * grid.stretches);
+  for (int at = blockIdx.x * grid.share; at < stop;) {
+    const Part part(grid, at, stop);
+    const int r = part.r;
+    const int id = (int)threadIdx.x < o.k ? o.ids[(int64_t)r * o.k + threadIdx.x] : -1;
+    const LossRow q = loss_row<BF16>(a, r);
+    WaveSums mine;
+    for (int from = part.from; from < part.to; from += LIST_RANGE / LOSS_TOKENS) {
+      const int to = min(part.to, from + LIST_RANGE / LOSS_TOKENS);
+      const int first = from * LOSS_TOKENS, end = min(to * LOSS_TOKENS, a.l.d.vocab + q.shift);
+      for (int i = threadIdx.x; i < (to - from) * (LOSS_TOKENS / 32); i += LOSS_THREADS) listed[i] = 0;
+      __syncthreads();
+      const int place = (id < a.l.d.vocab ? id : -1) + q.shift - first;
+      if (id >= 0 && place >= 0 && place < end - first) atomicOr(&listed[place >> 5], 1u << (place & 31));
+      __syncthreads();
+      auto strike = [&](int t) { return t < end ? (uint32_t)((const uint8_t*)listed)[(t - first) >> 3] : 0u; };
+      through<BF16, G, true>(a, q, first, end, strike, [&](Pass<BF16, G>& x, int, bool holes) { take<false>(mine, x, holes, q); }, [](int) {});
+      __syncthreads();                               // the bits have been read
+    }
+    const Sums rest = block_sums(mine.sums, q, waves);
+    if (threadIdx.x == 0) o.parts[r + blockIdx.x] = rest;
+    at += part.to - part.from;
+    if (at < stop) __syncthreads();                  // the waves' sums have been read
   }
 }
 
@@ -747,9 +826,9 @@ __global__ __launch_bounds__(WAVE) void distill_finish_kernel(LossArgs a, LossGr
   __shared__ ListLds list;
   const int r = blockIdx.x;
   const LossRow q = loss_row<BF16>(a, r);
-  Sums rest = no_sums();
-  for (int i = threadIdx.x; i < grid.pieces; i += WAVE) join(rest, o.parts[(int64_t)r * grid.pieces + i], q);
-  finish_distill<BF16>(a, o, q, r, wave_sums(rest, q), list);
+  Sums rest;
+  parts_of(grid, r, o.parts, q, rest);
+  finish_distill<BF16>(a, o, q, r, rest, list);
 }
 
 // What is not listed has the gradient g / T (Q p_rest - q_rest) of its share of p_rest; a listed token is written by the lane that holds its
@@ -763,16 +842,16 @@ __global__ __launch_bounds__(LOSS_THREADS) void distill_backward_kernel(LossArgs
   __shared__ int twice;
   const int block = gridDim.x - 1 - blockIdx.x, r = block / pieces, piece = block - r * pieces;
   const LossRow q = loss_row<BF16>(a, r);
-  const int64_t vocab = a.l.d.vocab, first = (int64_t)piece * RANGE, end = min(first + RANGE, vocab + q.shift);
+  const int vocab = a.l.d.vocab, first = piece * RANGE, end = min(first + RANGE, vocab + q.shift);
   const float4 s0 = ((const float4*)(o.stats + (int64_t)r * PG_DISTILL_STATS))[0], s1 = ((const float4*)(o.stats + (int64_t)r * PG_DISTILL_STATS))[1];
   const float g = s1.w == 0.0f ? 0.0f : g_loss[r];
   char* to = (char*)out + (int64_t)r * out_stride * ELT;
-  if (g == 0.0f) return put_zeros<BF16, PAST, G>(to, first + threadIdx.x * LANE_TOKENS - q.shift, vocab);
+  if (g == 0.0f) return put_zeros<BF16, PAST, G>(to, first + (int)threadIdx.x * LANE_TOKENS - q.shift, vocab);
   const bool entry = (int)threadIdx.x < o.k;
   const int id = entry ? o.ids[(int64_t)r * o.k + threadIdx.x] : -1;
   const float t = entry ? o.logp[(int64_t)r * o.k + threadIdx.x] : 0.0f;
-  const int64_t place = (int64_t)id + q.shift - first;
-  const bool mine = id >= 0 && place >= 0 && place < end - first;
+  const int place = (id < vocab ? id : -1) + q.shift - first;
+  const bool mine = id >= 0 && id < vocab && place >= 0 && place < end - first;
   const float scale = g * q.inv;
   if (threadIdx.x < RANGE / 32) listed[threadIdx.x] = 0;
   if (threadIdx.x == 0) twice = 0;
@@ -794,13 +873,13 @@ __global__ __launch_bounds__(LOSS_THREADS) void distill_backward_kernel(LossArgs
     else ((float*)to)[id] = d;
   }
   const float c = scale * s1.x, less = s0.w * LOG2E;
-  auto strike = [&](int64_t t) { return t < end ? (uint32_t)((const uint8_t*)listed)[(t - first) >> 3] : 0u; };
+  auto strike = [&](int t) { return t < end ? (uint32_t)((const uint8_t*)listed)[(t - first) >> 3] : 0u; };
   const bool odd = !(fabsf(c) < INFINITY && less == less);
-  auto each = [&](const Pass<BF16, G>& x, int64_t slot, auto all) {
+  auto each = [&](const Pass<BF16, G>& x, int base, auto all) {
     constexpr bool HOLES = !decltype(all)::value;
 #pragma unroll
     for (int i = 0; i < G; ++i) {
-      const int64_t v = slot + i * LOSS_TOKENS - q.shift;
+      const int v = base + i * LOSS_TOKENS + (int)threadIdx.x * LANE_TOKENS - q.shift;
       float d[LANE_TOKENS];
 #pragma unroll
       for (int e = 0; e < LANE_TOKENS; ++e) {
@@ -812,12 +891,12 @@ __global__ __launch_bounds__(LOSS_THREADS) void distill_backward_kernel(LossArgs
     }
   };
   // a pass without a token that counts may have listed ones among those that are not allowed
-  through<BF16, G>(a, q, first, end, strike, [&](const Pass<BF16, G>& x, int64_t slot, bool holes) {
-    if (holes || odd) each(x, slot, std::false_type{});
-    else each(x, slot, std::true_type{});
-  }, [&](int64_t slot) {
+  through<BF16, G, true>(a, q, first, end, strike, [&](const Pass<BF16, G>& x, int base, bool holes) {
+    if (holes || odd) each(x, base, std::false_type{});
+    else each(x, base, std::true_type{});
+  }, [&](int base) {
     Pass<BF16, G> nothing{};
-    each(nothing, slot, std::false_type{});
+    each(nothing, base, std::false_type{});
   });
 }
 
@@ -924,6 +1003,7 @@ static pg_status loss_args(const pg_logits* desc, const float* temperature, cons
   PG_TRY(logit_args(desc, who, a.l, 1 << 23));
   if (desc->tokens || desc->bias_offsets) return fail(PG_EINVAL, "%s: logits with a history or biases (pg_logits_adjust first)", who);
   a.temperature = temperature;
+  a.span = desc->rows ? (desc->rows - 1) * desc->stride + desc->vocab : 0;
   return PG_OK;
 }
 static pg_status check_gradient(const LossArgs& a, const void* out, int64_t out_stride, const char* who) {
@@ -946,19 +1026,18 @@ static int64_t slots_of(const LossArgs& a) {
 static int64_t most_slots(int64_t vocab) { return vocab + LANE_TOKENS - 1; }
 static int64_t stretches_of(int64_t slots) { return (slots + LOSS_TOKENS - 1) / LOSS_TOKENS; }
 
-// Workgroups of a pass over the logits: as many as fill the chip a few times over; what a row's finish has to join stays short.
-constexpr int64_t LOSS_WORKGROUPS = 16384;
-static LossGrid loss_grid(const LossArgs& a) {
-  const int64_t rows = a.l.d.rows, stretches = stretches_of(slots_of(a));
-  const int groups = rows * ((stretches + 3) / 4) >= 1024 ? 4 : 1;
-  const int64_t passes = (stretches + groups - 1) / groups, each = std::max<int64_t>(1, LOSS_WORKGROUPS / rows);
-  const int64_t per = std::min<int64_t>((passes + each - 1) / each, LIST_RANGE / (groups * LOSS_TOKENS));
-  return LossGrid{groups, (int)(per * groups * LOSS_TOKENS), (int)((passes + per - 1) / per)};
+// As many workgroups as are resident at once, if there is a stretch for each; short rows are no more than 8 to a workgroup, which goes
+// through them one after another.
+constexpr int64_t LOSS_WORKGROUPS = 2048, TOP_WORKGROUPS = 1536, ROWS_OF_ONE = 8;
+constexpr int PASS_GROUPS = 2;
+static LossGrid loss_grid(const LossArgs& a, bool top) {
+  const int64_t rows = a.l.d.rows, stretches = stretches_of(slots_of(a)), all = rows * stretches;
+  const int64_t most = top ? TOP_WORKGROUPS : LOSS_WORKGROUPS, share = std::min((all + most - 1) / most, ROWS_OF_ONE * stretches);
+  return LossGrid{(int)stretches, (int)share, (int)((all + share - 1) / share)};
 }
-// No fewer than any call of at most so many rows and tokens has: a row has no more than its share of LOSS_WORKGROUPS, or one for LIST_RANGE tokens.
+// No fewer than any call of at most so many rows and tokens has: a part for each row, and one more for each workgroup.
 static int64_t most_parts(int64_t rows, int64_t vocab) {
-  const int64_t slots = most_slots(vocab);
-  return std::min(rows * stretches_of(slots), std::max(LOSS_WORKGROUPS, rows * ((slots + LIST_RANGE - 1) / LIST_RANGE)));
+  return rows + std::min(rows * stretches_of(most_slots(vocab)), std::max(LOSS_WORKGROUPS, (rows + ROWS_OF_ONE - 1) / ROWS_OF_ONE));
 }
 static int n_chunks(int64_t vocab) { return (int)((most_slots(vocab) + CHUNK - 1) / CHUNK); }
 static int64_t part_floats(int64_t rows, int64_t vocab) { return (most_parts(rows, vocab) * (int64_t)(sizeof(Sums) / sizeof(float)) + 3) / 4 * 4; }
@@ -970,13 +1049,10 @@ static int64_t part_floats(int64_t rows, int64_t vocab) { return (most_parts(row
     PG_LAUNCH_CHECK(#F);                                                                                     \
   } while (0)
 
-// f(whether the logits are bf16, groups a lane takes at a time), as types
+// f(whether the logits are bf16), as a type
 template <class F>
-static pg_status with_kind(const LossArgs& a, int groups, F f) {
-  const auto four = std::integral_constant<int, 4>{};
-  const auto one = std::integral_constant<int, 1>{};
-  if (a.l.d.dtype == PG_LOGITS_BF16) return groups == 4 ? f(std::true_type{}, four) : f(std::true_type{}, one);
-  return groups == 4 ? f(std::false_type{}, four) : f(std::false_type{}, one);
+static pg_status with_kind(const LossArgs& a, F f) {
+  return a.l.d.dtype == PG_LOGITS_BF16 ? f(std::true_type{}) : f(std::false_type{});
 }
 
 }  // namespace pg
@@ -999,25 +1075,32 @@ extern "C" pg_status pg_token_logprobs(const pg_logits* desc, const float* tempe
   if ((uintptr_t)stats & 15) return fail(PG_ESHAPE, "pg_token_logprobs: stats are not 16-byte aligned");
   if (!scratch) return fail(PG_EINVAL, "pg_token_logprobs: scratch is NULL");
   if ((uintptr_t)scratch & 7) return fail(PG_ESHAPE, "pg_token_logprobs: scratch is not 8-byte aligned");
-  const LossGrid g = loss_grid(a);
   const bool top = n_top && (top_ids || top_logp);
+  const LossGrid g = loss_grid(a, top);
   const LogprobOut o{target, logp, entropy, stats, n_top, top_ids, top_logp, (Sums*)scratch, scratch + part_floats(rows, a.l.d.vocab), n_chunks(a.l.d.vocab)};
-  return with_kind(a, g.groups, [&](auto bf, auto groups) {
+  return with_kind(a, [&](auto bf) {
     constexpr bool BF = decltype(bf)::value;
-    constexpr int G = decltype(groups)::value;
-    if (top) PG_LOSS_LAUNCH(rows * g.pieces, LOSS_THREADS, 0, (logprob_kernel<BF, G, true>), a, g, o);
-    else PG_LOSS_LAUNCH(rows * g.pieces, LOSS_THREADS, 0, (logprob_kernel<BF, G, false>), a, g, o);
-    if (g.pieces == 1) return PG_OK;
+    if (top) PG_LOSS_LAUNCH(g.workgroups, LOSS_THREADS, 0, (logprob_kernel<BF, PASS_GROUPS, true>), a, g, o);
+    else PG_LOSS_LAUNCH(g.workgroups, LOSS_THREADS, 0, (logprob_kernel<BF, PASS_GROUPS, false>), a, g, o);
     if (top) PG_LOSS_LAUNCH(rows, LOSS_THREADS, 0, (logprob_finish_kernel<BF, true>), a, g, o);
-    else PG_LOSS_LAUNCH(rows, WAVE, 0, (logprob_finish_kernel<BF, false>), a, g, o);
+    else if (g.share % g.stretches) PG_LOSS_LAUNCH(rows, WAVE, 0, (logprob_finish_kernel<BF, false>), a, g, o);
     return PG_OK;
   });
 }
 
 static bool past_the_caches(const LossArgs& a) { return a.l.d.dtype == PG_LOGITS_BF16 && (int64_t)a.l.d.rows * a.l.d.vocab * 2 > 256ll << 20; }
 
-// A gradient's workgroup takes four groups a lane once, or (few rows) one.
-static int gradient_groups(const LossArgs& a) { return a.l.d.rows * ((stretches_of(slots_of(a)) + 3) / 4) >= 1024 ? 4 : 1; }
+// A gradient's workgroup goes through one pass, of four groups a lane in bf16 and of one in fp32 or where there are few rows.
+static bool large_passes(const LossArgs& a) { return a.l.d.dtype == PG_LOGITS_BF16 && a.l.d.rows * ((stretches_of(slots_of(a)) + 3) / 4) >= 1024; }
+// f(whether the logits are bf16, groups a lane takes, whether the gradient goes past the caches), as types
+template <class F>
+static pg_status with_gradient(const LossArgs& a, F f) {
+  const auto four = std::integral_constant<int, 4>{};
+  const auto one = std::integral_constant<int, 1>{};
+  if (a.l.d.dtype != PG_LOGITS_BF16) return f(std::false_type{}, one, std::false_type{});
+  if (!large_passes(a)) return f(std::true_type{}, one, std::false_type{});
+  return past_the_caches(a) ? f(std::true_type{}, four, std::true_type{}) : f(std::true_type{}, four, std::false_type{});
+}
 
 extern "C" pg_status pg_token_logprobs_backward(const pg_logits* desc, const float* temperature, const int32_t* target, const float* stats,
                                                 const float* g_logp, const float* g_entropy, void* d_logits, int64_t d_stride, void* stream) {
@@ -1029,13 +1112,10 @@ extern "C" pg_status pg_token_logprobs_backward(const pg_logits* desc, const flo
   if ((uintptr_t)stats & 15) return fail(PG_ESHAPE, "pg_token_logprobs_backward: stats are not 16-byte aligned");
   if (g_logp && !target) return fail(PG_EINVAL, "pg_token_logprobs_backward: a gradient of log-probs without targets");
   PG_TRY(check_gradient(a, d_logits, d_stride, "pg_token_logprobs_backward"));
-  return with_kind(a, gradient_groups(a), [&](auto bf, auto groups) {
-    constexpr bool BF = decltype(bf)::value;
+  return with_gradient(a, [&](auto bf, auto groups, auto past) {
     constexpr int G = decltype(groups)::value;
-    const int64_t blocks = rows * ((stretches_of(slots_of(a)) + G - 1) / G);
-    const int pieces = (int)(blocks / rows);
-    if (past_the_caches(a)) PG_LOSS_LAUNCH(blocks, LOSS_THREADS, 0, (logprob_backward_kernel<BF, G, BF>), a, pieces, target, stats, g_logp, g_entropy, d_logits, d_stride);
-    else PG_LOSS_LAUNCH(blocks, LOSS_THREADS, 0, (logprob_backward_kernel<BF, G, false>), a, pieces, target, stats, g_logp, g_entropy, d_logits, d_stride);
+    const int pieces = (int)((stretches_of(slots_of(a)) + G - 1) / G);
+    PG_LOSS_LAUNCH(rows * pieces, LOSS_THREADS, 0, (logprob_backward_kernel<decltype(bf)::value, G, decltype(past)::value>), a, pieces, target, stats, g_logp, g_entropy, d_logits, d_stride);
     return PG_OK;
   });
 }
@@ -1060,13 +1140,13 @@ extern "C" pg_status pg_distill_loss(const pg_logits* desc, const float* tempera
   if (rows == 0) return PG_OK;
   if (!loss || !scratch) return fail(PG_EINVAL, "pg_distill_loss: null pointer");
   if ((uintptr_t)scratch & 7) return fail(PG_ESHAPE, "pg_distill_loss: scratch is not 8-byte aligned");
-  const LossGrid g = loss_grid(a);
+  const LossGrid g = loss_grid(a, false);
   const DistillArgs o{mode, k, teacher_ids, teacher_logp, loss, stats, (Sums*)scratch};
-  const size_t lds = std::max<size_t>(std::min<int64_t>(g.range, (slots_of(a) + 31) / 32 * 32) / 8, g.pieces == 1 ? sizeof(ListLds) : 0);
-  return with_kind(a, g.groups, [&](auto bf, auto groups) {
+  const size_t lds = std::min({g.stretches, g.share, LIST_RANGE / LOSS_TOKENS}) * (LOSS_TOKENS / 8);
+  return with_kind(a, [&](auto bf) {
     constexpr bool BF = decltype(bf)::value;
-    PG_LOSS_LAUNCH(rows * g.pieces, LOSS_THREADS, lds, (distill_kernel<BF, decltype(groups)::value>), a, g, o);
-    if (g.pieces > 1) PG_LOSS_LAUNCH(rows, WAVE, 0, distill_finish_kernel<BF>, a, g, o);
+    PG_LOSS_LAUNCH(g.workgroups, LOSS_THREADS, lds, (distill_kernel<BF, PASS_GROUPS>), a, g, o);
+    PG_LOSS_LAUNCH(rows, WAVE, 0, distill_finish_kernel<BF>, a, g, o);
     return PG_OK;
   });
 }
@@ -1081,13 +1161,10 @@ extern "C" pg_status pg_distill_backward(const pg_logits* desc, const float* tem
   if (!stats || !g_loss) return fail(PG_EINVAL, "pg_distill_backward: null pointer");
   PG_TRY(check_gradient(a, d_logits, d_stride, "pg_distill_backward"));
   const DistillArgs o{0, k, teacher_ids, teacher_logp, nullptr, const_cast<float*>(stats), nullptr};
-  return with_kind(a, gradient_groups(a), [&](auto bf, auto groups) {
-    constexpr bool BF = decltype(bf)::value;
+  return with_gradient(a, [&](auto bf, auto groups, auto past) {
     constexpr int G = decltype(groups)::value;
-    const int64_t blocks = rows * ((stretches_of(slots_of(a)) + G - 1) / G);
-    const int pieces = (int)(blocks / rows);
-    if (past_the_caches(a)) PG_LOSS_LAUNCH(blocks, LOSS_THREADS, 0, (distill_backward_kernel<BF, G, BF>), a, pieces, o, g_loss, d_logits, d_stride);
-    else PG_LOSS_LAUNCH(blocks, LOSS_THREADS, 0, (distill_backward_kernel<BF, G, false>), a, pieces, o, g_loss, d_logits, d_stride);
+    const int pieces = (int)((stretches_of(slots_of(a)) + G - 1) / G);
+    PG_LOSS_LAUNCH(rows * pieces, LOSS_THREADS, 0, (distill_backward_kernel<decltype(bf)::value, G, decltype(past)::value>), a, pieces, o, g_loss, d_logits, d_stride);
     return PG_OK;
   });
 }

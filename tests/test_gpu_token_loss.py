@@ -314,6 +314,53 @@ def test_entropys_gradient_without_targets(lib):
         near(d[r].double().cpu().numpy(), want, tol * (1 + 2.0 ** -7) + store_tol(want, True), f"row {r}")
 
 
+@pytest.mark.parametrize("bf", [False, True], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab,k", [(700, 24001, 64), (3000, 5000, 7), (150, 65537, 200), (2049, 2048, 33), (5000, 300, 256)])
+def test_rows_whose_pieces_do_not_end_with_them(lib, rows, vocab, k, bf):
+    """Many rows of several pieces each, shared out to workgroups: every row is right."""
+    gen = torch.Generator(device=DEV).manual_seed(rows)
+    z = torch.randn(rows, vocab, device=DEV, generator=gen) * 3
+    z = z.to(torch.bfloat16) if bf else z
+    target = torch.randint(0, vocab, (rows,), device=DEV, generator=gen).to(torch.int32)
+    desc, n = lib.Logits(z), 20
+    f = lambda *s: torch.full(s, 99.0, device=DEV)  # noqa: E731
+    scratch = f(lib.pg_logprob_scratch_floats(rows, vocab, n))
+    ln = torch.log_softmax(z.double(), 1)
+    t = target.long()[:, None]
+    tol = float((vocab / 256 + 64) * U + 120 * U)          # |y - top| and entropies stay below 26
+    order = torch.sort(z.float(), dim=1, descending=True, stable=True)[1][:, :n]
+    for top in (False, True):
+        logp, entropy, stats = f(rows), f(rows), f(rows, 4)
+        ids, values = torch.zeros(rows, n, dtype=torch.int32, device=DEV), f(rows, n)
+        lib.pg_token_logprobs(desc, target, logp, scratch, entropy=entropy, stats=stats, **(dict(top_ids=ids, top_logp=values) if top else {}))
+        assert (logp.double() - ln.gather(1, t)[:, 0]).abs().max() < tol
+        assert (entropy.double() + (ln.exp() * ln).sum(1)).abs().max() < 12 * tol
+        if top:
+            assert torch.equal(ids.long(), order) and (values.double() - ln.gather(1, order)).abs().max() < tol
+    g = torch.randn(rows, device=DEV, generator=gen)
+    d = torch.empty_like(z)
+    lib.pg_token_logprobs_backward(desc, target, stats, d, g_logp=g)
+    want = -g.double()[:, None] * ln.exp()
+    want.scatter_add_(1, t, g.double()[:, None])
+    assert ((d.double() - want).abs() - want.abs() * (2.0 ** -8 if bf else U)).max() < 5 * tol
+    # a list of tokens of every kind of row
+    ids = torch.argsort(torch.rand(rows, vocab, device=DEV, generator=gen), dim=1)[:, :k].to(torch.int32).contiguous()
+    q = torch.log_softmax(torch.randn(rows, vocab, device=DEV, generator=gen) * 3, 1).gather(1, ids.long()).contiguous()
+    loss, stats = f(rows), f(rows, lib.PG_DISTILL_STATS)
+    lib.pg_distill_loss(desc, ids, q, loss, scratch, tail=True, stats=stats)
+    w, p = q.double().exp(), ln.exp().scatter(1, ids.long(), 0.0).sum(1)
+    q_rest = (1 - w.sum(1)).clamp_min(0)
+    want = (w * (q.double() - ln.gather(1, ids.long()))).sum(1)
+    want += torch.where(q_rest > 0, q_rest * (q_rest.log() - p.log()), 0.0) if k < vocab else 0.0
+    assert (loss.double() - want).abs().max() < 3 * tol
+    lib.pg_distill_backward(desc, ids, q, stats, g, d)
+    everything = (w.sum(1) + q_rest)[:, None]
+    want = ln.exp() * (everything - torch.where(p > 0, q_rest / p, 0.0)[:, None])
+    want.scatter_(1, ids.long(), everything * ln.exp().gather(1, ids.long()) - w)
+    want *= g.double()[:, None]
+    assert ((d.double() - want).abs() - want.abs() * (2.0 ** -8 if bf else U)).max() < 5 * tol
+
+
 def test_more_rows_than_a_grid_has_in_one_direction(lib):
     """And short ones: every row is right, the last included."""
     rows, vocab = 70001, 11
