@@ -363,8 +363,9 @@ __device__ __forceinline__ int place_of(uint64_t key) { return (int)~(uint32_t)k
 
 struct TopLds {
   static constexpr int CANDIDATES = 4 * LOSS_THREADS;
-  uint64_t lane[LOSS_THREADS], candidate[CANDIDATES], best[PG_TOP_MAX], least;
-  float top[LOSS_THREADS];
+  static constexpr int AT_ONCE = 16;                 // the list is compared so many at a time, zeros behind it
+  uint64_t lane[LOSS_THREADS], candidate[CANDIDATES + AT_ONCE], best[PG_TOP_MAX], least;
+  float top[LOSS_THREADS / 2];
   uint32_t bound;
   int count;
 };
@@ -379,36 +380,58 @@ __device__ __forceinline__ void no_candidates(TopLds& s) {
     s.bound = ~0u;
   }
 }
-__device__ __forceinline__ void candidate(uint64_t key, TopLds& s) {
-  const int at = atomicAdd(&s.count, 1);
-  if (at < TopLds::CANDIDATES) s.candidate[at] = key;
+// Of a lane's N keys those that are not 0, with one request for their places.
+template <int N>
+__device__ __forceinline__ void candidates(const uint64_t* key, TopLds& s) {
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) n += key[i] != 0;
+  if (!n) return;
+  int at = atomicAdd(&s.count, n);
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (key[i]) {
+      if (at < TopLds::CANDIDATES) s.candidate[at] = key[i];
+      ++at;
+    }
 }
 __device__ __forceinline__ bool rank_candidates(int n, TopLds& s) {
   __syncthreads();
   const int m = s.count;
   if (m > TopLds::CANDIDATES) return false;
+  if (threadIdx.x < TopLds::AT_ONCE) s.candidate[m + threadIdx.x] = 0;
+  __syncthreads();
   for (int k = threadIdx.x; k < m; k += LOSS_THREADS) {
     const uint64_t key = s.candidate[k];
     int rank = 0;
-#pragma unroll 4
-    for (int i = 0; i < m; ++i) rank += s.candidate[i] > key;
+    for (int i = 0; i < m; i += TopLds::AT_ONCE)
+#pragma unroll
+      for (int j = 0; j < TopLds::AT_ONCE; ++j) rank += s.candidate[i + j] > key;
     if (rank < n) s.best[rank] = key;
   }
   __syncthreads();
   return true;
 }
 
-// The n-th largest of the lanes' values: n of them, at least, reach it.
+// A bound that n of the lanes' values, at least, reach, and hardly more: the n-th largest among the largest of two or four adjacent lanes each.
 __device__ __forceinline__ float nth_of_lanes(float top, int n, TopLds& s) {
-  s.top[threadIdx.x] = top;
+  static_assert(PG_TOP_MAX <= LOSS_THREADS / 4, "half of the pairs at most");
+  const int each = n <= LOSS_THREADS / 8 ? 4 : 2;
+  top = fmaxf(top, __builtin_bit_cast(float, permuted<0xB1>(__builtin_bit_cast(int, top))));
+  if (each == 4) top = fmaxf(top, __builtin_bit_cast(float, permuted<0x4E>(__builtin_bit_cast(int, top))));
+  if (threadIdx.x % each == 0) s.top[threadIdx.x / each] = top;
   __syncthreads();
-  int rank = 0;
-#pragma unroll 16
-  for (int i = 0; i < LOSS_THREADS / 4; ++i) {
-    const float4 t = ((const float4*)s.top)[i];
-    rank += (t.x > top) + (t.y > top) + (t.z > top) + (t.w > top);
+  if ((int)threadIdx.x < LOSS_THREADS / each) {
+    top = s.top[threadIdx.x];
+    int rank = 0;
+    for (int i = 0; i < LOSS_THREADS / each / 4; i += 16)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const float4 t = ((const float4*)s.top)[i + j];
+        rank += (t.x > top) + (t.y > top) + (t.z > top) + (t.w > top);
+      }
+    if (rank < n) atomicMin(&s.bound, ordered(top));
   }
-  if (rank < n) atomicMin(&s.bound, ordered(top));
   __syncthreads();
   return logit_of((uint64_t)s.bound << 32);
 }
@@ -429,8 +452,8 @@ __device__ __forceinline__ void select_by_key(int N, int n, TopLds& s, Item item
   __syncthreads();
   const uint64_t least = s.least;
   for (int i = me; i < N; i += LOSS_THREADS) {
-    const uint64_t key = item(i);
-    if (key >= least) candidate(key, s);
+    const uint64_t key = item(i), mine = key >= least ? key : 0;
+    candidates<1>(&mine, s);
   }
   if (rank_candidates(n, s)) return;
   uint64_t last = ~0ull;
@@ -450,25 +473,37 @@ __device__ __forceinline__ void select_by_key(int N, int n, TopLds& s, Item item
   __syncthreads();
 }
 
+// The first stretches' largest logits of a lane, asked for early.
+struct Kept {
+  static constexpr int N = 10;                       // 163840 tokens of a row
+  float z[N];
+  __device__ __forceinline__ void load(const float* largest, int chunks) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) z[k] = (int)threadIdx.x + k * LOSS_THREADS < chunks ? largest[threadIdx.x + k * LOSS_THREADS] : -INFINITY;
+  }
+};
+__device__ __forceinline__ int chunks_of(const LossArgs& a, const LossRow& q) { return (a.l.d.vocab + q.shift + CHUNK - 1) / CHUNK; }
+
 // The n best tokens of a row, from the largest logits of its stretches, to s.best: all lanes of a workgroup.
 template <bool BF16>
-__device__ __forceinline__ void alternatives(const LossArgs& a, const LossRow& q, const float* largest, int n, TopLds& s) {
-  constexpr int KEPT = 10;                           // stretches a lane has in registers: 163840 tokens
+__device__ __forceinline__ void alternatives(const LossArgs& a, const LossRow& q, const Kept& kept, const float* largest, int n, TopLds& s) {
+  constexpr int KEPT = Kept::N;
   constexpr int AGAIN = PG_TOP_MAX * CHUNK_LANES / LOSS_THREADS;
-  const int me = threadIdx.x, vocab = a.l.d.vocab, N = (vocab + q.shift + CHUNK - 1) / CHUNK;
+  const int me = threadIdx.x, vocab = a.l.d.vocab, N = chunks_of(a, q);
   no_candidates(s);
-  float z[KEPT], top = -INFINITY;
+  float top = -INFINITY;
 #pragma unroll
-  for (int k = 0; k < KEPT; ++k) z[k] = me + k * LOSS_THREADS < N ? largest[me + k * LOSS_THREADS] : -INFINITY;
-#pragma unroll
-  for (int k = 0; k < KEPT; ++k) top = fmaxf(top, z[k]);
+  for (int k = 0; k < KEPT; ++k) top = fmaxf(top, kept.z[k]);
   for (int i = me + KEPT * LOSS_THREADS; i < N; i += LOSS_THREADS) top = fmaxf(top, largest[i]);
   const float bound = nth_of_lanes(top, n, s);
+  uint64_t mine[KEPT];
 #pragma unroll
-  for (int k = 0; k < KEPT; ++k)
-    if (z[k] >= bound && z[k] > -INFINITY) candidate(key_of(z[k], me + k * LOSS_THREADS), s);
-  for (int i = me + KEPT * LOSS_THREADS; i < N; i += LOSS_THREADS)
-    if (largest[i] >= bound && largest[i] > -INFINITY) candidate(key_of(largest[i], i), s);
+  for (int k = 0; k < KEPT; ++k) mine[k] = kept.z[k] >= bound ? key_of(kept.z[k], me + k * LOSS_THREADS) : 0;
+  candidates<KEPT>(mine, s);
+  for (int i = me + KEPT * LOSS_THREADS; i < N; i += LOSS_THREADS) {
+    const uint64_t one = largest[i] >= bound ? key_of(largest[i], i) : 0;
+    candidates<1>(&one, s);
+  }
   if (!rank_candidates(n, s)) select_by_key(N, n, s, [&](int i) { return key_of(largest[i], i); });
   // the lanes look at these stretches again, eight tokens each
   const float least = logit_of(s.best[n - 1]);       // NaN for 0: nothing is below it
@@ -490,8 +525,8 @@ __device__ __forceinline__ void alternatives(const LossArgs& a, const LossRow& q
   for (int e = 0; e < AGAIN * LANE_TOKENS; ++e) {
     const float y = x[e / LANE_TOKENS].template logit<true>(0, e % LANE_TOKENS);
     key[e] = y < least ? 0 : key_of(y, (int)key[e]);
-    if (key[e]) candidate(key[e], s);
   }
+  candidates<AGAIN * LANE_TOKENS>(key, s);
   if (!rank_candidates(n, s)) select_by_key(LOSS_THREADS * LANE_TOKENS * AGAIN, n, s, [&](int i) { return key[i / LOSS_THREADS]; });
 }
 
@@ -506,10 +541,10 @@ struct LogprobOut {
   int n_chunks;
 };
 
-// What the whole row's sums give; all lanes of a workgroup, or (no alternatives) of a wave.
+// What the whole row's sums give; all lanes of a workgroup, or (s NULL: no alternatives) of a wave.
 template <bool BF16>
 __device__ __forceinline__ void finish_logprob(const LossArgs& a, const LogprobOut& o, const LossRow& q, int r, int target, float at_target, const Sums& sum,
-                                               TopLds* s) {
+                                               const Kept& kept, TopLds* s) {
   const bool gone = target == -1, bad = sum.s != sum.s, none = sum.s == 0.0f;
   const float ln_s = none ? 0.0f : logf(sum.s);
   if (threadIdx.x == 0) {
@@ -527,7 +562,7 @@ __device__ __forceinline__ void finish_logprob(const LossArgs& a, const LogprobO
   const int n = o.n_top;
   uint64_t key = 0;
   if (!gone && !bad && !none) {
-    alternatives<BF16>(a, q, o.chunks + (int64_t)r * o.n_chunks, n, *s);
+    alternatives<BF16>(a, q, kept, o.chunks + (int64_t)r * o.n_chunks, n, *s);
     key = (int)threadIdx.x < n ? s->best[threadIdx.x] : 0;
   }
   if ((int)threadIdx.x < n) {
@@ -536,9 +571,11 @@ __device__ __forceinline__ void finish_logprob(const LossArgs& a, const LogprobO
   }
 }
 
-template <bool BF16, int G, bool TOP>
-__global__ __launch_bounds__(LOSS_THREADS, TOP ? 6 : 8) void logprob_kernel(LossArgs a, LossGrid grid, LogprobOut o) {
+// WHOLE: every workgroup has one row, and no launch comes after this one.
+template <bool BF16, int G, bool TOP, bool WHOLE>
+__global__ __launch_bounds__(LOSS_THREADS, WHOLE ? 2 : TOP ? 6 : 8) void logprob_kernel(LossArgs a, LossGrid grid, LogprobOut o) {
   __shared__ Sums waves[LOSS_WAVES];
+  __shared__ std::conditional_t<WHOLE && TOP, TopLds, char> lists;
   const int stop = min((int)(blockIdx.x + 1) * grid.share, a.l.d.rows * grid.stretches), lane = threadIdx.x & 63;
   for (int at = blockIdx.x * grid.share; at < stop;) {
     const Part part(grid, at, stop);
@@ -571,9 +608,19 @@ __global__ __launch_bounds__(LOSS_THREADS, TOP ? 6 : 8) void logprob_kernel(Loss
       });
     }
     const Sums sum = block_sums(mine.sums, q, waves);
-    if (!TOP && part.from == 0 && part.to == grid.stretches)
-      finish_logprob<BF16>(a, o, q, r, target, target >= 0 && target < a.l.d.vocab ? open_logit<BF16>(a, q, target) : 0.0f, sum, nullptr);
-    else if (threadIdx.x == 0) o.parts[r + blockIdx.x] = sum;
+    if (WHOLE || (!TOP && part.from == 0 && part.to == grid.stretches)) {
+      const float at_target = target >= 0 && target < a.l.d.vocab ? open_logit<BF16>(a, q, target) : 0.0f;
+      Kept kept;
+      if constexpr (WHOLE && TOP) {
+        kept.load(o.chunks + (int64_t)r * o.n_chunks, chunks_of(a, q));
+        finish_logprob<BF16>(a, o, q, r, target, at_target, sum, kept, &lists);
+      } else {
+        finish_logprob<BF16>(a, o, q, r, target, at_target, sum, kept, nullptr);
+      }
+    } else if (threadIdx.x == 0) {
+      o.parts[r + blockIdx.x] = sum;
+    }
+    if (WHOLE) return;
     at += part.to - part.from;
     if (at < stop) __syncthreads();                  // the waves' sums have been read
   }
@@ -586,8 +633,10 @@ __global__ __launch_bounds__(LOSS_THREADS) void logprob_finish_kernel(LossArgs a
   const LossRow q = loss_row<BF16>(a, r);
   const int target = o.target ? o.target[r] : 0;
   const float at_target = target >= 0 && target < a.l.d.vocab ? open_logit<BF16>(a, q, target) : 0.0f;
+  Kept kept;
+  if (TOP && target != -1) kept.load(o.chunks + (int64_t)r * o.n_chunks, chunks_of(a, q));
   Sums sum;
-  if (parts_of(grid, r, o.parts, q, sum) || TOP) finish_logprob<BF16>(a, o, q, r, target, at_target, sum, TOP ? &lists : nullptr);
+  if (parts_of(grid, r, o.parts, q, sum) || TOP) finish_logprob<BF16>(a, o, q, r, target, at_target, sum, kept, TOP ? &lists : nullptr);
 }
 
 // Writes the gradient of the tokens v .. v + 7 that are in the row, but for those of `others`, in the logits' type.  PAST: not to be kept in the
@@ -791,10 +840,10 @@ __device__ __forceinline__ void finish_distill(const LossArgs& a, const DistillA
   }
 }
 
-template <bool BF16, int G>
-__global__ __launch_bounds__(LOSS_THREADS, 8) void distill_kernel(LossArgs a, LossGrid grid, DistillArgs o) {
+template <bool BF16, int G, bool WHOLE>
+__global__ __launch_bounds__(LOSS_THREADS, WHOLE ? 2 : 8) void distill_kernel(LossArgs a, LossGrid grid, DistillArgs o) {
   __shared__ Sums waves[LOSS_WAVES];
-  extern __shared__ uint32_t listed[];               // a bit for each slot of the row's part
+  extern __shared__ uint32_t listed[];               // a bit for each slot of the row's part; WHOLE: then the table of the list
   const int stop = min((int)(blockIdx.x + 1) * grid.share, a.l.d.rows * grid.stretches);
   for (int at = blockIdx.x * grid.share; at < stop;) {
     const Part part(grid, at, stop);
@@ -815,6 +864,10 @@ __global__ __launch_bounds__(LOSS_THREADS, 8) void distill_kernel(LossArgs a, Lo
       __syncthreads();                               // the bits have been read
     }
     const Sums rest = block_sums(mine.sums, q, waves);
+    if (WHOLE) {
+      if (threadIdx.x < WAVE) finish_distill<BF16>(a, o, q, r, rest, *(ListLds*)listed);
+      return;
+    }
     if (threadIdx.x == 0) o.parts[r + blockIdx.x] = rest;
     at += part.to - part.from;
     if (at < stop) __syncthreads();                  // the waves' sums have been read
@@ -922,25 +975,21 @@ __device__ __forceinline__ void finish_surrogate(const SurrogateArgs& a, int r, 
   if (a.clipped) a.clipped[r] = cuts;
 }
 
-__global__ __launch_bounds__(LOSS_THREADS) void surrogate_tokens_kernel(SurrogateArgs a) {
-  __shared__ float sums[LOSS_WAVES][2];
-  __shared__ int counts[LOSS_WAVES];
-  const int r = blockIdx.x / a.pieces, piece = blockIdx.x - r * a.pieces;
-  const int from = min(max(a.cu[r], 0), a.n_tokens), to = min(max(a.cu[r + 1], from), a.n_tokens), n = to - from;
-  const float A = a.adv[r], w = a.weight ? a.weight[r] : 1.0f / (float)max(n, 1);
-  const int64_t first = from + (int64_t)piece * a.piece, end = piece + 1 < a.pieces ? min(first + a.piece, (int64_t)to) : to;
-  float sum = 0.0f, kl = 0.0f;
-  int cuts = 0;
-  for (int64_t i = first + threadIdx.x; i < end; i += LOSS_THREADS) {
-    const float l = a.logp[i];
-    const double d = (double)l - (double)a.old[i];
-    const bool cut = A > 0.0f ? d > a.hi : A < 0.0f && d < a.lo;
+// One token's part of the objective, of the divergence and of the gradient; whether it was cut.
+struct Token {
+  float value, k, g;
+  bool cut;
+  __device__ __forceinline__ Token(const SurrogateArgs& a, float A, float l, float old, float ref) {
+    const double d = (double)l - (double)old;
+    cut = A > 0.0f ? d > a.hi : A < 0.0f && d < a.lo;
     const float ra = A == 0.0f ? 0.0f : expf((float)d) * A;
-    float g = cut ? 0.0f : ra, value = cut ? (A > 0.0f ? a.at_hi : a.at_lo) * A : ra;
+    g = cut ? 0.0f : ra;
+    value = cut ? (A > 0.0f ? a.at_hi : a.at_lo) * A : ra;
+    k = 0.0f;
     if (a.ref) {
       // e^x - x - 1: near 0 x^2 / 2 (1 + x / 3 (1 + x / 4 (...))), whose terms past the eighth are 2^-26 of it at x = 1/2
-      const float x = a.ref[i] - l;
-      float k = 1.0f;
+      const float x = ref - l;
+      k = 1.0f;
 #pragma unroll
       for (int j = 10; j > 2; --j) k = __builtin_fmaf(k, x * (1.0f / j), 1.0f);
       k *= 0.5f * x * x;
@@ -950,13 +999,42 @@ __global__ __launch_bounds__(LOSS_THREADS) void surrogate_tokens_kernel(Surrogat
         k = e == INFINITY ? e : e - x - 1.0f;
         slope = e - 1.0f;
       }
-      kl += k;
       value -= a.kl_coef * k;
       g += a.kl_coef * slope;
     }
-    sum += value;
-    cuts += cut;
-    if (a.g_logp) a.g_logp[i] = w * g;
+  }
+};
+
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void surrogate_tokens_kernel(SurrogateArgs a) {
+  constexpr int AT_ONCE = 4;                         // tokens of a lane whose loads are under way together
+  __shared__ float sums[THREADS / WAVE][2];
+  __shared__ int counts[THREADS / WAVE];
+  const int r = blockIdx.x / a.pieces, piece = blockIdx.x - r * a.pieces;
+  const float A = a.adv[r], weight = a.weight ? a.weight[r] : 0.0f;
+  const int from = min(max(a.cu[r], 0), a.n_tokens), to = min(max(a.cu[r + 1], from), a.n_tokens), n = to - from;
+  const float w = a.weight ? weight : 1.0f / (float)max(n, 1);
+  const int64_t first = from + (int64_t)piece * a.piece, end = piece + 1 < a.pieces ? min(first + a.piece, (int64_t)to) : to;
+  float sum = 0.0f, kl = 0.0f;
+  int cuts = 0;
+  for (int64_t i = first + threadIdx.x; i < end; i += AT_ONCE * THREADS) {
+    float l[AT_ONCE], old[AT_ONCE], ref[AT_ONCE];
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int64_t at = min(i + j * THREADS, end - 1);
+      l[j] = a.logp[at];
+      old[j] = a.old[at];
+      ref[j] = a.ref ? a.ref[at] : 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j)
+      if (i + j * THREADS < end) {
+        const Token t(a, A, l[j], old[j], ref[j]);
+        sum += t.value;
+        kl += t.k;
+        cuts += t.cut;
+        if (a.g_logp) a.g_logp[i + j * THREADS] = w * t.g;
+      }
   }
   sum = wave_allsum(sum);
   kl = wave_allsum(kl);
@@ -971,7 +1049,7 @@ __global__ __launch_bounds__(LOSS_THREADS) void surrogate_tokens_kernel(Surrogat
   double all = 0.0, all_kl = 0.0;
   cuts = 0;
 #pragma unroll
-  for (int i = 0; i < LOSS_WAVES; ++i) {
+  for (int i = 0; i < THREADS / WAVE; ++i) {
     all += sums[i][0];
     all_kl += sums[i][1];
     cuts += counts[i];
@@ -1029,10 +1107,12 @@ static int64_t stretches_of(int64_t slots) { return (slots + LOSS_TOKENS - 1) / 
 // As many workgroups as are resident at once, if there is a stretch for each; short rows are no more than 8 to a workgroup, which goes
 // through them one after another.
 constexpr int64_t LOSS_WORKGROUPS = 2048, TOP_WORKGROUPS = 1536, ROWS_OF_ONE = 8;
-constexpr int PASS_GROUPS = 2;
+constexpr int PASS_GROUPS = 2, WHOLE_GROUPS = 4, WHOLE_STRETCHES = 8;
+// Few short rows are a workgroup's each, with four groups a lane at a time, in one launch.
+static bool whole_rows(int64_t rows, int64_t stretches) { return stretches <= WHOLE_STRETCHES && rows * stretches <= LOSS_WORKGROUPS; }
 static LossGrid loss_grid(const LossArgs& a, bool top) {
-  const int64_t rows = a.l.d.rows, stretches = stretches_of(slots_of(a)), all = rows * stretches;
-  const int64_t most = top ? TOP_WORKGROUPS : LOSS_WORKGROUPS, share = std::min((all + most - 1) / most, ROWS_OF_ONE * stretches);
+  const int64_t rows = a.l.d.rows, stretches = stretches_of(slots_of(a)), all = rows * stretches, most = top ? TOP_WORKGROUPS : LOSS_WORKGROUPS;
+  const int64_t share = whole_rows(rows, stretches) ? stretches : std::min((all + most - 1) / most, ROWS_OF_ONE * stretches);
   return LossGrid{(int)stretches, (int)share, (int)((all + share - 1) / share)};
 }
 // No fewer than any call of at most so many rows and tokens has: a part for each row, and one more for each workgroup.
@@ -1080,8 +1160,13 @@ extern "C" pg_status pg_token_logprobs(const pg_logits* desc, const float* tempe
   const LogprobOut o{target, logp, entropy, stats, n_top, top_ids, top_logp, (Sums*)scratch, scratch + part_floats(rows, a.l.d.vocab), n_chunks(a.l.d.vocab)};
   return with_kind(a, [&](auto bf) {
     constexpr bool BF = decltype(bf)::value;
-    if (top) PG_LOSS_LAUNCH(g.workgroups, LOSS_THREADS, 0, (logprob_kernel<BF, PASS_GROUPS, true>), a, g, o);
-    else PG_LOSS_LAUNCH(g.workgroups, LOSS_THREADS, 0, (logprob_kernel<BF, PASS_GROUPS, false>), a, g, o);
+    if (whole_rows(rows, g.stretches)) {
+      if (top) PG_LOSS_LAUNCH(rows, LOSS_THREADS, 0, (logprob_kernel<BF, WHOLE_GROUPS, true, true>), a, g, o);
+      else PG_LOSS_LAUNCH(rows, LOSS_THREADS, 0, (logprob_kernel<BF, WHOLE_GROUPS, false, true>), a, g, o);
+      return PG_OK;
+    }
+    if (top) PG_LOSS_LAUNCH(g.workgroups, LOSS_THREADS, 0, (logprob_kernel<BF, PASS_GROUPS, true, false>), a, g, o);
+    else PG_LOSS_LAUNCH(g.workgroups, LOSS_THREADS, 0, (logprob_kernel<BF, PASS_GROUPS, false, false>), a, g, o);
     if (top) PG_LOSS_LAUNCH(rows, LOSS_THREADS, 0, (logprob_finish_kernel<BF, true>), a, g, o);
     else if (g.share % g.stretches) PG_LOSS_LAUNCH(rows, WAVE, 0, (logprob_finish_kernel<BF, false>), a, g, o);
     return PG_OK;
@@ -1145,7 +1230,11 @@ extern "C" pg_status pg_distill_loss(const pg_logits* desc, const float* tempera
   const size_t lds = std::min({g.stretches, g.share, LIST_RANGE / LOSS_TOKENS}) * (LOSS_TOKENS / 8);
   return with_kind(a, [&](auto bf) {
     constexpr bool BF = decltype(bf)::value;
-    PG_LOSS_LAUNCH(g.workgroups, LOSS_THREADS, lds, (distill_kernel<BF, PASS_GROUPS>), a, g, o);
+    if (whole_rows(rows, g.stretches)) {
+      PG_LOSS_LAUNCH(rows, LOSS_THREADS, std::max(lds, sizeof(ListLds)), (distill_kernel<BF, WHOLE_GROUPS, true>), a, g, o);
+      return PG_OK;
+    }
+    PG_LOSS_LAUNCH(g.workgroups, LOSS_THREADS, lds, (distill_kernel<BF, PASS_GROUPS, false>), a, g, o);
     PG_LOSS_LAUNCH(rows, WAVE, 0, distill_finish_kernel<BF>, a, g, o);
     return PG_OK;
   });
@@ -1170,7 +1259,7 @@ extern "C" pg_status pg_distill_backward(const pg_logits* desc, const float* tem
 }
 
 // A sequence of up to 4096 tokens is one workgroup's; longer ones are cut into pieces of 1024 tokens or more, some 4096 in all.
-constexpr int64_t SURROGATE_WHOLE = 4096, SURROGATE_PIECE = 1024, SURROGATE_WORKGROUPS = 4096;
+constexpr int64_t SURROGATE_WHOLE = 8192, SURROGATE_PIECE = 1024, SURROGATE_WORKGROUPS = 4096;
 static int64_t surrogate_pieces(int64_t n_seq, int64_t max_len) {
   if (max_len <= SURROGATE_WHOLE) return 1;
   return std::min((max_len + SURROGATE_PIECE - 1) / SURROGATE_PIECE, std::max<int64_t>(1, SURROGATE_WORKGROUPS / n_seq));
@@ -1196,7 +1285,8 @@ extern "C" pg_status pg_token_surrogate(const float* logp, const float* logp_old
   if (pieces > 1 && (uintptr_t)scratch & 15) return fail(PG_ESHAPE, "pg_token_surrogate: scratch is not 16-byte aligned");
   const SurrogateArgs a{logp, logp_old, logp_ref, adv, weight, cu, n_tokens, std::log1p(-clip_low), std::log1p(clip_high), (float)(1.0 - clip_low),
                         (float)(1.0 + clip_high), (float)kl_coef, objective, kl, g_logp, clipped, pieces, (int)(((int64_t)max_len + pieces - 1) / pieces), scratch};
-  PG_LOSS_LAUNCH((int64_t)n_seq * pieces, LOSS_THREADS, 0, surrogate_tokens_kernel, a);
+  if (pieces == 1 && max_len > 1024) PG_LOSS_LAUNCH(n_seq, 1024, 0, surrogate_tokens_kernel<1024>, a);
+  else PG_LOSS_LAUNCH((int64_t)n_seq * pieces, LOSS_THREADS, 0, surrogate_tokens_kernel<LOSS_THREADS>, a);
   if (pieces > 1) PG_LOSS_LAUNCH(n_seq, WAVE, 0, surrogate_finish_kernel, a);
   return PG_OK;
 }
