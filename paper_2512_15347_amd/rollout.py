@@ -2,7 +2,8 @@
 
 Each prompt is expanded to a group of members that share its pages, members draw their tokens from the policy's softmax, and at the
 checkpoints Optimal Variance Filtering keeps the subset of each group whose proxy rewards vary most; the others' pages go back
-to the pool.  Log-probs by original id and group-relative advantages come out, as from the denoising loop.
+to the pool.  Log-probs by original id and group-relative advantages come out, as from the denoising loop.  What the policy learns from them
+follows: log-probs of the drawn tokens under other weights, the clipped objective with its gradient, or a teacher's distribution.
 
     python -m paper_2512_15347_amd.rollout
 
@@ -55,8 +56,13 @@ class Decoder:
         self.cache = pg.Cache.create(cfg["blocks"], 2 * rows * self.width, cfg["kv_heads"], cfg["page"], self.hd, self.width, device=device)
         self.workspace = None
 
-    def forward(self, tokens, positions, table, lens, kv_len, row_of=None, cu=None):
-        """Logits of `tokens` (the last cu[r] .. cu[r+1]-1 of row r, or one a row); token i attends to kv_len[i] tokens of its row."""
+    def forward(self, *tokens, **more):
+        """Logits that follow `tokens`; arguments as of hidden()."""
+        return _linear(self.hidden(*tokens, **more), self.w["head"])
+
+    def hidden(self, tokens, positions, table, lens, kv_len, row_of=None, cu=None):
+        """What the logits are made of, for `tokens` (the last cu[r] .. cu[r+1]-1 of row r, or one a row); token i attends to kv_len[i] tokens of
+        its row."""
         c, hd, n = self.cfg, self.hd, tokens.shape[0]
         need = pg.pg_paged_attention_workspace(self.cache, n, c["heads"], c["max_len"])
         if self.workspace is None or self.workspace.numel() < need:
@@ -70,7 +76,7 @@ class Decoder:
             pg.pg_paged_attention(self.cache, layer, q, table, kv_len, out, c["max_len"], self.workspace, row_of=row_of)
             x = x + _linear(out.view(n, -1), w["o"])
             x = x + _linear(torch.nn.functional.gelu(_linear(_norm(x), w["fc1"]), approximate="tanh").to(torch.bfloat16), w["fc2"])
-        return _linear(_norm(x), self.w["head"])
+        return _norm(x)
 
 
 def sample_groups(decoder, prompts, members, steps, schedule, seed, token_reward, temperature=1.0, penalties=None, allow=None, adv_eps=1e-6):
@@ -162,6 +168,82 @@ def sample_groups(decoder, prompts, members, steps, schedule, seed, token_reward
     return dict(ids=ids, tokens=history, lens=n_prompt + steps, rewards=score, advantages=adv, logp=logp, offsets=offsets)
 
 
+def _drawn(decoder, out):
+    """Hidden states [survivors * steps, D] before every drawn token of sample_groups' survivors, and these tokens; clears the cache."""
+    dev, cache, steps = out["tokens"].device, decoder.cache, out["logp"].shape[0]
+    rows, sizes = out["tokens"].cpu().numpy(), out["lens"].cpu().numpy() - 1          # the last token is followed by none
+    ints = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).to(dev)  # noqa: E731
+    pg.pg_cache_clear(cache)
+    table = torch.full((len(rows), decoder.width), -1, dtype=torch.int32, device=dev)
+    lens = torch.zeros(len(rows), dtype=torch.int32, device=dev)
+    pg.pg_cache_reserve(cache, table, lens, ints(sizes), lens)
+    at = np.concatenate([np.arange(n) for n in sizes])
+    hidden = decoder.hidden(ints(np.concatenate([r[:n] for r, n in zip(rows, sizes)])), ints(at), table, lens, ints(at + 1),
+                            row_of=ints(np.repeat(np.arange(len(rows)), sizes)), cu=ints(np.cumsum([0] + sizes.tolist())))
+    pg.pg_cache_check(cache)
+    places = np.concatenate([end - steps + np.arange(steps) for end in np.cumsum(sizes)])
+    drawn = np.concatenate([r[n + 1 - steps:n + 1] for r, n in zip(rows, sizes)])
+    return hidden[torch.from_numpy(places).to(dev)].contiguous(), ints(drawn)
+
+
+def _rows_of(logits, temperature, allow):
+    """(logits with their mask, a temperature for each row)."""
+    n, dev = logits.shape[0], logits.device
+    more = {} if allow is None else dict(allow=allow, allow_row=torch.zeros(n, dtype=torch.int32, device=dev))
+    return pg.Logits(logits, **more), torch.full((n,), float(temperature), device=dev)
+
+
+def token_logprobs(decoder, out, temperature=1.0, allow=None):
+    """Log-probs of the drawn tokens of sample_groups' survivors under `decoder`'s weights, and entropies: [survivors, steps] each.  Clears the
+    decoder's cache.  Temperature and mask as in sample_groups, which must not have had penalties."""
+    hidden, drawn = _drawn(decoder, out)
+    desc, t = _rows_of(_linear(hidden, decoder.w["head"]), temperature, allow)
+    logp, entropy = torch.empty(desc.rows, device=hidden.device), torch.empty(desc.rows, device=hidden.device)
+    scratch = torch.empty(pg.pg_logprob_scratch_floats(desc.rows, desc.vocab), device=hidden.device)
+    pg.pg_token_logprobs(desc, drawn, logp, scratch, temperature=t, entropy=entropy)
+    return logp.view(out["ids"].shape[0], -1), entropy.view(out["ids"].shape[0], -1)
+
+
+def policy_gradient(decoder, out, clip_low=0.2, clip_high=0.2, kl_coef=0.0, logp_ref=None, entropy_coef=0.0, temperature=1.0, allow=None):
+    """The clipped objective of sample_groups' survivors under `decoder`'s weights, and its gradient, as far as the decoder's output matrix.
+
+    Per sequence the mean over its drawn tokens, as pg_token_surrogate defines it, plus entropy_coef times the mean entropy; the gradient is that
+    of the sequences' mean.  logp_ref: [survivors, steps] of a reference policy (token_logprobs).  Returns objective, kl, clipped [survivors],
+    logp [survivors, steps], and with respect to what is maximised: d_logits [survivors * steps, vocab], hidden (what the logits were made of)
+    and d_head = d_logits^T hidden.  Temperature and mask as in sample_groups, which must not have had penalties."""
+    hidden, drawn = _drawn(decoder, out)
+    dev, n, steps = hidden.device, out["ids"].shape[0], out["logp"].shape[0]
+    desc, t = _rows_of(_linear(hidden, decoder.w["head"]), temperature, allow)
+    logits, empty = desc.keep[0], lambda *shape: torch.empty(*shape, device=dev)
+    logp, stats, g = empty(n * steps), empty(n * steps, pg.PG_LOGPROB_STATS), empty(n * steps)
+    pg.pg_token_logprobs(desc, drawn, logp, empty(pg.pg_logprob_scratch_floats(n * steps, desc.vocab)), temperature=t, stats=stats)
+    old = out["logp"][:, out["ids"].long()].t().contiguous().view(-1)
+    cu = torch.arange(0, n * steps + 1, steps, dtype=torch.int32, device=dev)
+    objective, kl, clipped = empty(n), empty(n), torch.empty(n, dtype=torch.int32, device=dev)
+    pg.pg_token_surrogate(logp, old, out["advantages"], cu, objective, g, clip_low, clip_high, steps, empty(pg.pg_surrogate_scratch_floats(n, steps)),
+                          logp_ref=None if logp_ref is None else logp_ref.contiguous().view(-1), kl_coef=kl_coef, kl=kl, clipped=clipped)
+    objective += entropy_coef * stats[:, 2].view(n, steps).mean(1)
+    more = dict(g_entropy=torch.full_like(g, entropy_coef / (n * steps))) if entropy_coef else {}
+    pg.pg_token_logprobs_backward(desc, drawn, stats, logits, g_logp=g / n, temperature=t, **more)           # in the logits' place
+    return dict(objective=objective, kl=kl, clipped=clipped, logp=logp.view(n, steps), d_logits=logits, hidden=hidden, d_head=logits.t() @ hidden.float())
+
+
+def distill_gradient(decoder, teacher, out, k=20, temperature=1.0, tail=True, allow=None):
+    """The divergence of `decoder` from another decoder's k most likely tokens at every drawn token of sample_groups' survivors, and the gradient of
+    its mean with respect to the decoder's output matrix.  Returns loss [survivors, steps], d_logits, hidden and d_head."""
+    hidden, drawn = _drawn(teacher, out)
+    desc, t = _rows_of(_linear(hidden, teacher.w["head"]), temperature, allow)
+    dev, n, vocab = hidden.device, desc.rows, desc.vocab
+    ids, values = torch.empty(n, k, dtype=torch.int32, device=dev), torch.empty(n, k, device=dev)
+    pg.pg_token_logprobs(desc, drawn, None, torch.empty(pg.pg_logprob_scratch_floats(n, vocab, k), device=dev), temperature=t, top_ids=ids, top_logp=values)
+    hidden, _ = _drawn(decoder, out)
+    desc, _ = _rows_of(_linear(hidden, decoder.w["head"]), temperature, allow)
+    loss, stats, logits = torch.empty(n, device=dev), torch.empty(n, pg.PG_DISTILL_STATS, device=dev), desc.keep[0]
+    pg.pg_distill_loss(desc, ids, values, loss, torch.empty(pg.pg_distill_scratch_floats(n, vocab), device=dev), tail=tail, temperature=t, stats=stats)
+    pg.pg_distill_backward(desc, ids, values, stats, torch.full((n,), 1.0 / n, device=dev), logits, temperature=t)
+    return dict(loss=loss.view(out["ids"].shape[0], -1), d_logits=logits, hidden=hidden, d_head=logits.t() @ hidden.float())
+
+
 def main():
     cfg = SMALL
     rng = np.random.default_rng(MASTER_SEED)
@@ -173,6 +255,10 @@ def main():
         a, b = int(out["offsets"][g]), int(out["offsets"][g + 1])
         print(f"group {g}: {b - a} of 48 members, rewards' spread {float(out['rewards'][a:b].std(unbiased=False)):.3f}, "
               f"best member {int(out['ids'][a + int(out['advantages'][a:b].argmax())])} with advantage {float(out['advantages'][a:b].max()):.2f}")
+    out = sample_groups(decoder, prompts, 48, 40, [(8, 32), (16, 16)], seed=1234, token_reward=reward)
+    step = policy_gradient(decoder, out, entropy_coef=0.01)
+    print(f"without penalties: objective {float(step['objective'].mean()):.4f}, {int(step['clipped'].sum())} of {step['logp'].numel()} tokens cut, "
+          f"gradient of the output matrix {float(step['d_head'].norm()):.4f}")
 
 
 if __name__ == "__main__":
