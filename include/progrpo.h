@@ -492,8 +492,8 @@ pg_status pg_sample_tokens(const pg_logits *desc, const float *temperature, uint
  * (equal logits: the lowest token first) and their log-probs, -1 and -inf past the last token whose logit is above -inf.  Every output may be NULL.
  * target[r] == -1: a row that is left out and not read (logp and entropy 0, no alternatives, gradient 0); any other index that no token has:
  * logp NaN.  target NULL: no row is left out, and logp has to be NULL.  A row with nothing left: logp -inf, entropy 0.  A bad row: NaN, and
- * -1 and NaN for its alternatives.  stats: [rows, PG_LOGPROB_STATS], for the backward pass; stats[r][0] + stats[r][1] is the natural logarithm of
- * the softmax's denominator of y (the largest y, and what the others add).
+ * -1 and NaN for its alternatives.  stats: [rows, PG_LOGPROB_STATS], 16-byte aligned, for the backward pass; stats[r][0] + stats[r][1] is the
+ * natural logarithm of the softmax's denominator (a y near the largest, and the rest).
  * scratch: pg_logprob_scratch_floats() floats, 8-byte aligned, which are enough for every call of no more rows, tokens and alternatives, too. */
 int64_t pg_logprob_scratch_floats(int32_t rows, int32_t vocab, int32_t n_top);
 pg_status pg_token_logprobs(const pg_logits *desc, const float *temperature, const int32_t *target, float *logp, float *entropy,
@@ -510,8 +510,8 @@ pg_status pg_token_logprobs_backward(const pg_logits *desc, const float *tempera
  *   PG_DISTILL_TAIL:  q = exp(teacher_logp), and what is missing to 1 is one more outcome, that of all other allowed tokens together:
  *                     loss = the sum above + q_rest (ln q_rest - ln p_rest); without other tokens (or q_rest <= 0) q_rest = 0
  * A row without a listed token, with nothing left, or (PG_DISTILL_TOP) with a list of -inf alone: loss 0, gradient 0.  q > 0 for a token with
- * p = 0: loss +inf.  A value of a listed token that is NaN or +inf: NaN.  stats: [rows, PG_DISTILL_STATS], for the backward pass (may be NULL).
- * scratch: pg_distill_scratch_floats() floats, enough for every call of no more rows and tokens, too. */
+ * p = 0: loss +inf.  A value of a listed token that is NaN or +inf: NaN.  stats: [rows, PG_DISTILL_STATS], 16-byte aligned, for the backward pass (may be
+ * NULL).  scratch: pg_distill_scratch_floats() floats, 8-byte aligned, enough for every call of no more rows and tokens, too. */
 enum { PG_DISTILL_TOP = 0, PG_DISTILL_TAIL = 1 };
 int64_t pg_distill_scratch_floats(int32_t rows, int32_t vocab);
 pg_status pg_distill_loss(const pg_logits *desc, const float *temperature, int32_t mode, const int32_t *teacher_ids,
@@ -531,7 +531,7 @@ pg_status pg_distill_backward(const pg_logits *desc, const float *temperature, c
  * logp_ref NULL: k = 0.  Every output may be NULL.  A sequence of no tokens gives zeros; tokens past cu[n_seq] are left as they are.
  * g_logp may be one of the inputs of that length.  clip_low in [0, 1], clip_high >= 0 (infinite: no bound); cuts are decided in fp64.
  * max_len >= every length: sizes the split (longer sequences are right too, but slower).  scratch: pg_surrogate_scratch_floats() floats,
- * enough for every call of no more sequences and no larger max_len, too (may be NULL where that is 0). */
+ * 16-byte aligned, enough for every call of no more sequences and no larger max_len, too (may be NULL where that is 0). */
 int64_t pg_surrogate_scratch_floats(int32_t n_seq, int32_t max_len);
 pg_status pg_token_surrogate(const float *logp, const float *logp_old, const float *logp_ref, const float *adv, const float *weight,
                              const int32_t *cu, int32_t n_seq, int32_t n_tokens, int32_t max_len, double clip_low, double clip_high,

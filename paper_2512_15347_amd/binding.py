@@ -647,6 +647,7 @@ class Logits:
         d.allow_row = _i32s(allow_row, rows)
         self.c, self.ref, self.rows, self.vocab = d, C.byref(d), rows, vocab
         self.scratch = pg_sample_scratch_floats(rows, vocab)
+        self.loss_scratch = {}                               # floats, by what they are for
 
 
 def pg_logits_adjust(desc, out, stream=None):
@@ -685,9 +686,19 @@ def _gradient(desc, d_logits):
 
 
 def _scratch(scratch, floats):
-    assert scratch is not None and scratch.is_contiguous() and scratch.numel() * scratch.element_size() >= 4 * floats if floats else True, \
-        f"scratch of {floats} floats wanted"
+    """Address of a scratch tensor of at least so many floats (may be None for 0)."""
+    if floats and (scratch is None or not scratch.is_contiguous() or scratch.numel() * scratch.element_size() < 4 * floats):
+        raise AssertionError(f"scratch of {floats} floats wanted")
     return None if scratch is None else scratch.data_ptr()
+
+
+def _loss_scratch(desc, scratch, top=None):
+    """The same for a call on these logits, of `top` alternatives (None: of a distillation)."""
+    floats = desc.loss_scratch.get(top)
+    if floats is None:
+        floats = pg_distill_scratch_floats(desc.rows, desc.vocab) if top is None else pg_logprob_scratch_floats(desc.rows, desc.vocab, top)
+        desc.loss_scratch[top] = floats
+    return _scratch(scratch, floats)
 
 
 def pg_logprob_scratch_floats(rows, vocab, n_top=0):
@@ -699,7 +710,7 @@ def pg_token_logprobs(desc, target, logp, scratch, temperature=None, entropy=Non
     top = 0 if top_ids is None and top_logp is None else (top_logp if top_ids is None else top_ids).shape[1]
     _check(_lib.pg_token_logprobs(desc.ref, _f32s(temperature, n), _i32s(target, n), _f32s(logp, n), _f32s(entropy, n),
                                   _f32s(stats, n, PG_LOGPROB_STATS), top, _i32s(top_ids, n, top), _f32s(top_logp, n, top),
-                                  _scratch(scratch, pg_logprob_scratch_floats(n, desc.vocab, top)), _stream(stream)))
+                                  _loss_scratch(desc, scratch, top), _stream(stream)))
 
 
 def pg_token_logprobs_backward(desc, target, stats, d_logits, g_logp=None, g_entropy=None, temperature=None, stream=None):
@@ -717,7 +728,7 @@ def pg_distill_loss(desc, teacher_ids, teacher_logp, loss, scratch, tail=False, 
     n, k = desc.rows, teacher_ids.shape[1]
     _check(_lib.pg_distill_loss(desc.ref, _f32s(temperature, n), PG_DISTILL_TAIL if tail else PG_DISTILL_TOP, _i32s(teacher_ids, n, k),
                                 _f32s(teacher_logp, n, k), k, _f32s(loss, n), _f32s(stats, n, PG_DISTILL_STATS),
-                                _scratch(scratch, pg_distill_scratch_floats(n, desc.vocab)), _stream(stream)))
+                                _loss_scratch(desc, scratch), _stream(stream)))
 
 
 def pg_distill_backward(desc, teacher_ids, teacher_logp, stats, g_loss, d_logits, temperature=None, stream=None):

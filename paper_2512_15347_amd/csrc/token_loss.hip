@@ -280,16 +280,21 @@ __device__ __forceinline__ void add_near(const P& x, float r, const LossRow& q, 
 template <bool ENTROPY, bool BF16, int G>
 __device__ __forceinline__ void take(WaveSums& a, Pass<BF16, G>& x, bool holes, const LossRow& q) {
   using P = Pass<BF16, G>;
-  if (a.sums.m == -FLT_MAX) a.sums.m = fmaxf(a.sums.m, x.largest(holes));        // nothing but zeros has been summed
+  if (a.sums.m == -FLT_MAX) {                        // nothing has been summed, or the lowest number alone
+    const float top = x.largest(holes);
+    if (top > a.sums.m) move_to(a.sums, top, q);
+  }
   const float m = a.sums.m, r = m * q.c;
   if (fabsf(r) < 16777216.0f) {                      // d is at most 1/2
     float s = 0.0f, u = 0.0f;
     if (ENTROPY && a.clamp) {
       if (!holes) x.all_count();
       add_near<true, true, ENTROPY, P, G>(x, r, q, s, u);
+    } else if (holes) {
+      add_near<true, false, ENTROPY, P, G>(x, r, q, s, u);
+    } else {
+      add_near<false, false, ENTROPY, P, G>(x, r, q, s, u);
     }
-    else if (holes) add_near<true, false, ENTROPY, P, G>(x, r, q, s, u);
-    else add_near<false, false, ENTROPY, P, G>(x, r, q, s, u);
     if (!__ballot(!(s <= 64.0f && u == u))) {
       const float d = __builtin_fmaf(m, q.c, -r), f = exp2_of(-d);
       s *= f;
@@ -856,8 +861,9 @@ __global__ __launch_bounds__(LOSS_THREADS, WHOLE ? 2 : 8) void distill_kernel(Lo
       const int first = from * LOSS_TOKENS, end = min(to * LOSS_TOKENS, a.l.d.vocab + q.shift);
       for (int i = threadIdx.x; i < (to - from) * (LOSS_TOKENS / 32); i += LOSS_THREADS) listed[i] = 0;
       __syncthreads();
-      const int place = (id < a.l.d.vocab ? id : -1) + q.shift - first;
-      if (id >= 0 && place >= 0 && place < end - first) atomicOr(&listed[place >> 5], 1u << (place & 31));
+      const bool exists = id >= 0 && id < a.l.d.vocab;
+      const int place = exists ? id + q.shift - first : -1;
+      if (place >= 0 && place < end - first) atomicOr(&listed[place >> 5], 1u << (place & 31));
       __syncthreads();
       auto strike = [&](int t) { return t < end ? (uint32_t)((const uint8_t*)listed)[(t - first) >> 3] : 0u; };
       through<BF16, G, true>(a, q, first, end, strike, [&](Pass<BF16, G>& x, int, bool holes) { take<false>(mine, x, holes, q); }, [](int) {});
@@ -903,8 +909,8 @@ __global__ __launch_bounds__(LOSS_THREADS) void distill_backward_kernel(LossArgs
   const bool entry = (int)threadIdx.x < o.k;
   const int id = entry ? o.ids[(int64_t)r * o.k + threadIdx.x] : -1;
   const float t = entry ? o.logp[(int64_t)r * o.k + threadIdx.x] : 0.0f;
-  const int place = (id < vocab ? id : -1) + q.shift - first;
-  const bool mine = id >= 0 && id < vocab && place >= 0 && place < end - first;
+  const int place = id >= 0 && id < vocab ? id + q.shift - first : -1;
+  const bool mine = place >= 0 && place < end - first;
   const float scale = g * q.inv;
   if (threadIdx.x < RANGE / 32) listed[threadIdx.x] = 0;
   if (threadIdx.x == 0) twice = 0;
@@ -1258,7 +1264,8 @@ extern "C" pg_status pg_distill_backward(const pg_logits* desc, const float* tem
   });
 }
 
-// A sequence of up to 4096 tokens is one workgroup's; longer ones are cut into pieces of 1024 tokens or more, some 4096 in all.
+// Sequences of up to 8192 tokens are a workgroup's each; longer ones are cut into pieces of 1024 tokens or more, at most 4096 in all, and joined by a
+// second launch.
 constexpr int64_t SURROGATE_WHOLE = 8192, SURROGATE_PIECE = 1024, SURROGATE_WORKGROUPS = 4096;
 static int64_t surrogate_pieces(int64_t n_seq, int64_t max_len) {
   if (max_len <= SURROGATE_WHOLE) return 1;

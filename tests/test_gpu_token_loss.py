@@ -236,6 +236,49 @@ def test_infinities_nan_and_lowest_values(lib, vocab, bf):
         check_logprobs(got, z, bf, target, None, n_top=n_top, g=g, ge=ge)
 
 
+@pytest.mark.parametrize("bf", [False, True], ids=["f32", "bf16"])
+@pytest.mark.parametrize("value", ["lowest", "-inf"])
+def test_long_runs_that_an_added_mask_has_left(lib, value, bf):
+    """Whole passes, waves and pieces of the type's lowest value, or of -inf, before, between and behind the other logits."""
+    rng = np.random.default_rng(21)
+    vocab, low = 40003, float(torch.finfo(torch.bfloat16 if bf else torch.float32).min) if value == "lowest" else -np.inf
+    z = make_logits(rng, 6, vocab, bf)
+    z[0, :20000] = low
+    z[1, 300:] = low
+    z[2, :39000] = z[2, 39900:] = low
+    z[3, 2000:30000] = low
+    z[4, ::3] = low
+    z[5, np.arange(vocab) // 8 % 64 < 40] = low            # some lanes of every wave
+    target = np.array([30000, 5, 39500, 1, 7, 40 * 8])
+    g, ge = rng.standard_normal(6), rng.standard_normal(6)
+    check_logprobs(run_logprobs(lib, z, bf, target, None, n_top=64, g=g, ge=ge), z, bf, target, None, n_top=64, g=g, ge=ge)
+    # and of rows that are a workgroup's each, several of them one after another
+    rows = np.tile(z[:, :9000], (500, 1))
+    got = run_logprobs(lib, rows, bf, np.tile(target % 9000, 500), None, n_top=3, g=np.tile(g, 500), ge=np.tile(ge, 500))
+    for k in ("logp", "entropy", "top_ids", "d"):          # a row's parts depend on its place: some roundings
+        a, b = np.where(np.isfinite(got[k]), got[k], -1e4).astype(np.float64), got[k].reshape((500, 6) + got[k].shape[1:])
+        first = np.tile(a[:6], (500,) + (1,) * (a.ndim - 1))
+        assert np.allclose(a, first, rtol=2 ** -6 if k == "d" else 1e-5, atol=1e-6 if k != "d" else 1e-7), k
+    check_logprobs({k: v[-6:] for k, v in got.items()}, rows[-6:], bf, (target % 9000), None, n_top=3, g=g, ge=ge)
+    ids, values = teacher_lists(rng, np.where(z == low, -30.0, z), 30)
+    t = np.array([1.0, 0.7, 1.3, 1.0, 1.0, 1.0])
+    check_distill(run_distill(lib, z, bf, ids, values, True, g, t), z, bf, ids, values, True, g, t)
+
+
+@pytest.mark.parametrize("bf", [False, True], ids=["f32", "bf16"])
+def test_rows_that_are_left_out_are_not_read(lib, bf):
+    z = np.full((4, 5001), np.nan)
+    z[2] = rounded(np.random.default_rng(1).standard_normal(5001), bf)
+    target = np.array([-1, 3, 4, -1])
+    got = run_logprobs(lib, z, bf, target, None, n_top=2, g=np.array([1.0, 0.0, 1.0, 2.0]), ge=np.array([1.0, 0.0, 0.0, 1.0]))
+    assert not got["d"][[0, 1, 3]].any() and np.isfinite(got["d"][2]).all() and got["logp"][[0, 3]].tolist() == [0, 0] and np.isnan(got["logp"][1])
+    assert got["entropy"][[0, 3]].tolist() == [0, 0] and (got["top_ids"][[0, 1, 3]] == -1).all() and np.isnan(got["top_logp"][1]).all()
+    ids, values = np.full((4, 3), -1), np.zeros((4, 3))
+    ids[1:3], values[1:3] = [1, 2, 3], -2.0
+    loss, d = run_distill(lib, z, bf, ids, values, True, np.array([1.0, 0.0, 1.0, 1.0]))
+    assert not d[[0, 1, 3]].any() and loss[[0, 3]].tolist() == [0, 0] and np.isnan(loss[1]) and np.isfinite(loss[2])
+
+
 def test_temperatures_that_are_none(lib):
     rng = np.random.default_rng(8)
     z = make_logits(rng, 6, 3001, False)
@@ -527,6 +570,24 @@ def test_distillations_lists(lib, vocab, k, bf, tail):
     got = run_distill(lib, z, bf, ids, values, tail, g, None, open_, allow_row)
     check_distill(got, z, bf, ids, values, tail, g, None, open_, allow_row)
     assert got[0][2] == 0 and got[0][6] == 0 and np.isinf(got[0][4]) and np.isinf(got[0][13]) and np.isnan(got[0][[10, 11, 15]]).all()
+
+
+def test_a_workgroups_part_of_a_row_that_has_more_bits_than_lds(lib):
+    """1400 rows of 200001 tokens: a workgroup's share is 67 stretches, and 64 of them have their bits at a time."""
+    rows, vocab, k = 1400, 200001, 256
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    z = torch.randn(rows, vocab, device=DEV, generator=gen).mul_(3).to(torch.bfloat16)
+    ids = torch.randint(0, vocab, (rows, k), device=DEV, generator=gen).to(torch.int32)
+    values = torch.log_softmax(torch.randn(rows, k + 1, device=DEV, generator=gen), 1)[:, :k].contiguous()
+    desc = lib.Logits(z)
+    loss, stats = torch.empty(rows, device=DEV), torch.empty(rows, lib.PG_DISTILL_STATS, device=DEV)
+    lib.pg_distill_loss(desc, ids, values, loss, torch.empty(lib.pg_distill_scratch_floats(rows, vocab), device=DEV), tail=True, stats=stats)
+    g = torch.randn(rows, device=DEV, generator=gen)
+    some = [0, 1, 2, 699, 700, 1398, 1399]
+    before = z[some].double().cpu().numpy()
+    lib.pg_distill_backward(desc, ids, values, stats, g, z)
+    pick = lambda t: t[some].cpu().numpy()  # noqa: E731
+    check_distill((pick(loss), z[some].double().cpu().numpy()), before, True, pick(ids), pick(values), True, pick(g))
 
 
 @pytest.mark.parametrize("vocab", [50, 5000])
