@@ -5,6 +5,9 @@
 // a teacher's list is compared, S over the tokens that are not on it.  Then ln p = (z - m) / T - ln S and the entropy is ln S - U / S, a
 // sum of terms of one sign.  Differences to m are exact where it matters, so that a row may be shifted by any amount; m and ln S are kept apart
 // for the backward pass for the same reason.
+//
+// Logits are read once for the sums and once more for their gradient, and that is what bounds all but the smallest calls: 6.0 TB/s read, 5.6 TB/s where as much
+// is written.  Times here are of kernels on an MI355X.
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
@@ -99,12 +102,13 @@ __device__ __forceinline__ Sums block_sums(Sums a, const LossRow& q, Sums* waves
   return a;
 }
 
-// Keeps the compiler from unpacking all groups of a pass before it works on the first: eight waves a SIMD instead of five.
+// Keeps the compiler from unpacking all groups of a pass before it works on the first: two groups fit eight waves a SIMD then.
 __device__ __forceinline__ void one_group_at_a_time() { __builtin_amdgcn_sched_barrier(0); }
 
 // A lane's part of one pass over a range: G groups of eight slots and which of their tokens count: those that are in the row and in the range,
 // allowed and not struck out.  16-byte loads may be unaligned, but in bf16, where a row may begin between two 4-byte words, they are a third
-// slower then (4096 x 131073, the forward pass: 311 us, 222 with slots); in fp32 it makes no difference.
+// slower then (4096 x 131073, the forward pass: 311 us, 222 with slots); in fp32 it makes no difference.  Every logit is read once a
+// pass and marked so: 2048 x 131073 in 103 us, 124 without.
 typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(4)));
 
 template <bool BF16, int G>
@@ -274,9 +278,9 @@ __device__ __forceinline__ void add_near(const P& x, float r, const LossRow& q, 
   }
 }
 
-// Adds a pass to the sums.  As a rule m stays, and x = z c - r is one operation, with r = m c as rounded; what r is off, d, is known and goes into
-// the sums afterwards.  Where a lane's sum shows that m is too small (or that there is a NaN), or where r is so large that d is, too, the pass is gone through
-// again: m becomes the largest logit of the wave's, and x = (z - m) c.
+// Adds a pass to the sums; a logit costs an FMA, an exponential, an addition and (entropy) an FMA.  As a rule m stays, and x = z c - r is one operation,
+// with r = m c as rounded; what r is off, d, is known and goes into the sums afterwards.  Where a lane's sum shows that m is too small (or that there is
+// a NaN), or where r is so large that d is, too, the pass is gone through again: m becomes the largest logit of the wave's, and x = (z - m) c.
 template <bool ENTROPY, bool BF16, int G>
 __device__ __forceinline__ void take(WaveSums& a, Pass<BF16, G>& x, bool holes, const LossRow& q) {
   using P = Pass<BF16, G>;
@@ -327,7 +331,9 @@ __device__ __forceinline__ void take(WaveSums& a, Pass<BF16, G>& x, bool holes, 
 }
 
 // How a pass over the logits is laid out.  Rows are stretches of LOSS_TOKENS slots each, and a workgroup takes the next `share` of all rows'
-// stretches: so that all workgroups are resident at once and end together.  What it sums of row r goes to part r + its own number.
+// stretches: so that all workgroups are resident at once and end together.  What it sums of row r goes to part r + its own number.  Against shares of
+// at most 16 stretches, of which there are more than fit at once: 2048 x 131073 in 101 us for 115, 1178 masked rows of 65537 in 41 for 45, but 4096 x 131072
+// in 180 for 174.
 struct LossGrid {
   int stretches, share, workgroups;
 };
@@ -347,7 +353,8 @@ __device__ __forceinline__ bool parts_of(const LossGrid& g, int r, const Sums* p
 // ---------------------------------------------------------------- alternatives
 // The n best tokens lie in the n stretches of CHUNK slots whose largest logits come first (equal ones in the order of their tokens): each of
 // these has a token that comes before all others of the stretches that come after.  So the pass over the logits leaves the largest logit of each
-// stretch, the stretches are chosen from these, and their tokens are looked at again.
+// stretch, the stretches are chosen from these, and their tokens are looked at again.  Lists that the lanes keep while they sum, and join, took 118 us for
+// 1178 rows of 64 alternatives where this takes 20.  Stretches of 32 slots: 73 us for the pass over 1178 x 131073, 71 with 64.
 constexpr int CHUNK_LANES = 8, CHUNK = CHUNK_LANES * LANE_TOKENS;
 
 // Its bits in the order of the numbers; -0 and 0 are equal.
@@ -576,7 +583,10 @@ __device__ __forceinline__ void finish_logprob(const LossArgs& a, const LogprobO
   }
 }
 
-// WHOLE: every workgroup has one row, and no launch comes after this one.
+// Bound by reading: 1178 rows of 131073 in bf16 (309 MB) take 68 us, 74 with the largest of each stretch; 4096 x 65537 (537 MB)
+// 96 us, 5.6 TB/s, and 4096 x 131072 (1074 MB) 171 us, 6.3 TB/s; without any arithmetic a copy of the pass was 3 to 5 % shorter.  Loads of the next pass
+// asked for before this one is summed cost registers and gave nothing (44 us for 41, 188 for 182).
+// WHOLE: every workgroup has one row, and no launch comes after this one: 48 masked rows of 16384 with five alternatives in 13 us.
 template <bool BF16, int G, bool TOP, bool WHOLE>
 __global__ __launch_bounds__(LOSS_THREADS, WHOLE ? 2 : TOP ? 6 : 8) void logprob_kernel(LossArgs a, LossGrid grid, LogprobOut o) {
   __shared__ Sums waves[LOSS_WAVES];
@@ -675,7 +685,8 @@ __device__ __forceinline__ void put_zeros(char* row, int v, int vocab) {
   for (int i = 0; i < G; ++i) put<BF16, PAST>(row, v + i * LOSS_TOKENS, vocab, nothing);
 }
 
-// The gradient is p (c0 + c1 (z - m)) with two numbers of the row, and g / T more at the target.
+// The gradient is p (c0 + c1 (z - m)) with two numbers of the row, and g / T more at the target.  Bound by reading the logits again and writing as much:
+// 4096 x 131072 in bf16 in 350 us, 6.1 TB/s both ways.
 template <bool BF16, int G, bool PAST>
 __global__ __launch_bounds__(LOSS_THREADS) void logprob_backward_kernel(LossArgs a, int pieces, const int32_t* target, const float* stats,
                                                                         const float* g_logp, const float* g_entropy, void* out, int64_t out_stride) {
@@ -781,7 +792,7 @@ struct DistillArgs {
 };
 
 // From the sums over what is not listed to the loss: the lanes of one wave.  In fp64: it is a few hundred values, and what
-// is left over (1 - sum q, Q p_rest - q_rest) is a difference.
+// is left over (1 - sum q, Q p_rest - q_rest) is a difference.  2048 lists take 12 us, bound by the way from one step to the next.
 template <bool BF16>
 __device__ __forceinline__ void finish_distill(const LossArgs& a, const DistillArgs& o, const LossRow& q, int r, const Sums& rest, ListLds& s) {
   const int lane = threadIdx.x & 63, vocab = a.l.d.vocab;
@@ -845,6 +856,7 @@ __device__ __forceinline__ void finish_distill(const LossArgs& a, const DistillA
   }
 }
 
+// The sums over what is not listed, with a bit in LDS for each slot; bound by reading: 2048 x 131073 in bf16 (537 MB) in 103 us, 5.2 TB/s.
 template <bool BF16, int G, bool WHOLE>
 __global__ __launch_bounds__(LOSS_THREADS, WHOLE ? 2 : 8) void distill_kernel(LossArgs a, LossGrid grid, DistillArgs o) {
   __shared__ Sums waves[LOSS_WAVES];
@@ -891,7 +903,8 @@ __global__ __launch_bounds__(WAVE) void distill_finish_kernel(LossArgs a, LossGr
 }
 
 // What is not listed has the gradient g / T (Q p_rest - q_rest) of its share of p_rest; a listed token is written by the lane that holds its
-// entry, and by no other.
+// entry, and by no other.  Bound by reading and writing: 2048 x 131073 in bf16 in 188 us, 5.7 TB/s both ways; 193 with the first rows
+// first, of which less is still near from the pass before (log-probs': no difference).
 template <bool BF16, int G, bool PAST>
 __global__ __launch_bounds__(LOSS_THREADS) void distill_backward_kernel(LossArgs a, int pieces, DistillArgs o, const float* g_loss, void* out,
                                                                         int64_t out_stride) {
@@ -1011,6 +1024,8 @@ struct Token {
   }
 };
 
+// Up to four numbers of a token, read or written once, bound it: 384 sequences of 16384 tokens at most, 3.2 million tokens in all (50 MB), in 16 us and
+// 4 for the second launch; 48 short sequences in 4.5 us.
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void surrogate_tokens_kernel(SurrogateArgs a) {
   constexpr int AT_ONCE = 4;                         // tokens of a lane whose loads are under way together
@@ -1111,10 +1126,12 @@ static int64_t most_slots(int64_t vocab) { return vocab + LANE_TOKENS - 1; }
 static int64_t stretches_of(int64_t slots) { return (slots + LOSS_TOKENS - 1) / LOSS_TOKENS; }
 
 // As many workgroups as are resident at once, if there is a stretch for each; short rows are no more than 8 to a workgroup, which goes
-// through them one after another.
+// through them one after another.  Two groups a lane at a time with eight waves a SIMD: 68 us for 1178 x 131073, four with five waves 83; one: 119 us for
+// 4096 x 65537, two 113.  With the largest of each stretch six waves fit: 73 us, 79 with as many workgroups as eight would take.
 constexpr int64_t LOSS_WORKGROUPS = 2048, TOP_WORKGROUPS = 1536, ROWS_OF_ONE = 8;
 constexpr int PASS_GROUPS = 2, WHOLE_GROUPS = 4, WHOLE_STRETCHES = 8;
-// Few short rows are a workgroup's each, with four groups a lane at a time, in one launch.
+// Few short rows are a workgroup's each, with four groups a lane at a time, in one launch: 48 x 16384 (8 stretches) in 6.3 us for 4.9 + 3.5 in two,
+// with alternatives 14.5 for 5.3 + 9.8, against a list 10.4 for 5.4 + 6.3 (of 16000); at 16 stretches, 32001, 16.4 for 4.6 + 9.7 and 15.4 for 6.6 + 6.4.
 static bool whole_rows(int64_t rows, int64_t stretches) { return stretches <= WHOLE_STRETCHES && rows * stretches <= LOSS_WORKGROUPS; }
 static LossGrid loss_grid(const LossArgs& a, bool top) {
   const int64_t rows = a.l.d.rows, stretches = stretches_of(slots_of(a)), all = rows * stretches, most = top ? TOP_WORKGROUPS : LOSS_WORKGROUPS;
@@ -1179,9 +1196,12 @@ extern "C" pg_status pg_token_logprobs(const pg_logits* desc, const float* tempe
   });
 }
 
+// A bf16 gradient of more than 256 MiB, what the last cache holds: a pass and its gradient, 4096 x 131072, in 549 us, 575 without, as the next pass need
+// not wait for what the caches write back; in fp32 427 for 370.
 static bool past_the_caches(const LossArgs& a) { return a.l.d.dtype == PG_LOGITS_BF16 && (int64_t)a.l.d.rows * a.l.d.vocab * 2 > 256ll << 20; }
 
-// A gradient's workgroup goes through one pass, of four groups a lane in bf16 and of one in fp32 or where there are few rows.
+// A gradient's workgroup goes through one pass, of four groups a lane in bf16 (4096 x 131072 in 350 us; two 357, one 380) and of one in fp32
+// (4096 x 65536 in 360 us; four 391) or where there are few rows, to be spread.
 static bool large_passes(const LossArgs& a) { return a.l.d.dtype == PG_LOGITS_BF16 && a.l.d.rows * ((stretches_of(slots_of(a)) + 3) / 4) >= 1024; }
 // f(whether the logits are bf16, groups a lane takes, whether the gradient goes past the caches), as types
 template <class F>
@@ -1264,8 +1284,8 @@ extern "C" pg_status pg_distill_backward(const pg_logits* desc, const float* tem
   });
 }
 
-// Sequences of up to 8192 tokens are a workgroup's each; longer ones are cut into pieces of 1024 tokens or more, at most 4096 in all, and joined by a
-// second launch.
+// Sequences of up to 8192 tokens are a workgroup's each (48 x 8192: 8.3 us, as long as in two launches); longer ones are cut into pieces of 1024 tokens
+// or more, at most 4096 in all, and joined by a second launch (48 x 16384: 5.9 + 2.8 us, whole 13.2).
 constexpr int64_t SURROGATE_WHOLE = 8192, SURROGATE_PIECE = 1024, SURROGATE_WORKGROUPS = 4096;
 static int64_t surrogate_pieces(int64_t n_seq, int64_t max_len) {
   if (max_len <= SURROGATE_WHOLE) return 1;
