@@ -1006,12 +1006,18 @@ struct Token {
     value = cut ? (A > 0.0f ? a.at_hi : a.at_lo) * A : ra;
     k = 0.0f;
     if (a.ref) {
-      // e^x - x - 1: near 0 x^2 / 2 (1 + x / 3 (1 + x / 4 (...))), whose terms past the eighth are 2^-26 of it at x = 1/2
+      // e^x - x - 1: near 0 x^2 (1/2! + x (1/3! + x (...))), whose terms past the ninth are 2^-26 of it at x = 1/2
       const float x = ref - l;
-      k = 1.0f;
-#pragma unroll
-      for (int j = 10; j > 2; --j) k = __builtin_fmaf(k, x * (1.0f / j), 1.0f);
-      k *= 0.5f * x * x;
+      k = 1.0f / 3628800;
+      k = __builtin_fmaf(k, x, 1.0f / 362880);
+      k = __builtin_fmaf(k, x, 1.0f / 40320);
+      k = __builtin_fmaf(k, x, 1.0f / 5040);
+      k = __builtin_fmaf(k, x, 1.0f / 720);
+      k = __builtin_fmaf(k, x, 1.0f / 120);
+      k = __builtin_fmaf(k, x, 1.0f / 24);
+      k = __builtin_fmaf(k, x, 1.0f / 6);
+      k = __builtin_fmaf(k, x, 0.5f);
+      k *= x * x;
       float slope = k + x;
       if (!(fabsf(x) < 0.5f)) {
         const float e = expf(x);
@@ -1024,8 +1030,8 @@ struct Token {
   }
 };
 
-// Up to four numbers of a token, read or written once, bound it: 384 sequences of 16384 tokens at most, 3.2 million tokens in all (50 MB), in 16 us and
-// 4 for the second launch; 48 short sequences in 4.5 us.
+// Four numbers of a token, read or written once, and some 110 instructions bound it: 384 sequences of 16384 tokens at most, 3.1 million in all (50 MB), in
+// 15 us (9 us of issue) and 4 for the second launch; 48 short sequences in 4.5 us.
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void surrogate_tokens_kernel(SurrogateArgs a) {
   constexpr int AT_ONCE = 4;                         // tokens of a lane whose loads are under way together
@@ -1036,6 +1042,7 @@ __global__ __launch_bounds__(THREADS) void surrogate_tokens_kernel(SurrogateArgs
   const int from = min(max(a.cu[r], 0), a.n_tokens), to = min(max(a.cu[r + 1], from), a.n_tokens), n = to - from;
   const float w = a.weight ? weight : 1.0f / (float)max(n, 1);
   const int64_t first = from + (int64_t)piece * a.piece, end = piece + 1 < a.pieces ? min(first + a.piece, (int64_t)to) : to;
+  if (a.pieces > 1 && first >= end) return;           // its part is not looked at
   float sum = 0.0f, kl = 0.0f;
   int cuts = 0;
   for (int64_t i = first + threadIdx.x; i < end; i += AT_ONCE * THREADS) {
@@ -1084,7 +1091,8 @@ __global__ __launch_bounds__(WAVE) void surrogate_finish_kernel(SurrogateArgs a)
   const int from = min(max(a.cu[r], 0), a.n_tokens), n = min(max(a.cu[r + 1], from), a.n_tokens) - from;
   double sum = 0.0, kl = 0.0;
   int cuts = 0;
-  for (int i = threadIdx.x; i < a.pieces; i += WAVE) {
+  const int some = (int)min((int64_t)a.pieces, ((int64_t)n + a.piece - 1) / a.piece);
+  for (int i = threadIdx.x; i < some; i += WAVE) {
     const float4 p = *(const float4*)(a.parts + 4 * ((int64_t)r * a.pieces + i));
     sum += p.x;
     kl += p.y;
@@ -1285,7 +1293,8 @@ extern "C" pg_status pg_distill_backward(const pg_logits* desc, const float* tem
 }
 
 // Sequences of up to 8192 tokens are a workgroup's each (48 x 8192: 8.3 us, as long as in two launches); longer ones are cut into pieces of 1024 tokens
-// or more, at most 4096 in all, and joined by a second launch (48 x 16384: 5.9 + 2.8 us, whole 13.2).
+// or more, at most 4096 in all, and joined by a second launch (48 x 16384: 5.9 + 2.8 us, whole 13.2; 384 sequences: 15.0 us,
+// 15.7 with 2048, 18.2 with 8192).
 constexpr int64_t SURROGATE_WHOLE = 8192, SURROGATE_PIECE = 1024, SURROGATE_WORKGROUPS = 4096;
 static int64_t surrogate_pieces(int64_t n_seq, int64_t max_len) {
   if (max_len <= SURROGATE_WHOLE) return 1;
