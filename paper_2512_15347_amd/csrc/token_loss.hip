@@ -1030,8 +1030,8 @@ struct Token {
   }
 };
 
-// Four numbers of a token, read or written once, and some 110 instructions bound it: 384 sequences of 16384 tokens at most, 3.1 million in all (50 MB), in
-// 15 us (9 us of issue) and 4 for the second launch; 48 short sequences in 4.5 us.
+// Four numbers of a token, read or written once, and some 90 instructions bound it: 384 sequences of 16384 tokens at most, 3.1 million in all (50 MB), in
+// 15 us (8 us of issue) and 4 for the second launch; 48 short sequences in 4.5 us.
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void surrogate_tokens_kernel(SurrogateArgs a) {
   constexpr int AT_ONCE = 4;                         // tokens of a lane whose loads are under way together
