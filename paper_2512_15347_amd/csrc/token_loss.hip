@@ -107,8 +107,8 @@ __device__ __forceinline__ void one_group_at_a_time() { __builtin_amdgcn_sched_b
 
 // A lane's part of one pass over a range: G groups of eight slots and which of their tokens count: those that are in the row and in the range,
 // allowed and not struck out.  16-byte loads may be unaligned, but in bf16, where a row may begin between two 4-byte words, they are a third
-// slower then (4096 x 131073, the forward pass: 311 us, 222 with slots); in fp32 it makes no difference.  Every logit is read once a
-// pass and marked so: 2048 x 131073 in 103 us, 124 without.
+// slower then (4096 x 131073, the forward pass: 311 us, 222 with slots); in fp32 slots would cost (4096 x 65537 against a list: 215 us, 269 with them).
+// Every logit is read once a pass and marked so: 2048 x 131073 against a list in 103 us, 124 without.
 typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(4)));
 
 template <bool BF16, int G>
@@ -284,12 +284,14 @@ __device__ __forceinline__ void add_near(const P& x, float r, const LossRow& q, 
 template <bool ENTROPY, bool BF16, int G>
 __device__ __forceinline__ void take(WaveSums& a, Pass<BF16, G>& x, bool holes, const LossRow& q) {
   using P = Pass<BF16, G>;
-  if (a.sums.m == -FLT_MAX) {                        // nothing has been summed, or the lowest number alone
+  Sums sum = a.sums;                                 // written back once: stores to it in several branches keep it out of registers
+  if (sum.m == -FLT_MAX) {                           // nothing has been summed, or the lowest number alone
     const float top = x.largest(holes);
-    if (top > a.sums.m) move_to(a.sums, top, q);
+    if (top > sum.m) move_to(sum, top, q);
   }
-  const float m = a.sums.m, r = m * q.c;
-  if (fabsf(r) < 16777216.0f) {                      // d is at most 1/2
+  const float r = sum.m * q.c;
+  bool near = fabsf(r) < 16777216.0f;                // d is at most 1/2
+  if (near) {
     float s = 0.0f, u = 0.0f;
     if (ENTROPY && a.clamp) {
       if (!holes) x.all_count();
@@ -299,35 +301,38 @@ __device__ __forceinline__ void take(WaveSums& a, Pass<BF16, G>& x, bool holes, 
     } else {
       add_near<false, false, ENTROPY, P, G>(x, r, q, s, u);
     }
-    if (!__ballot(!(s <= 64.0f && u == u))) {
-      const float d = __builtin_fmaf(m, q.c, -r), f = exp2_of(-d);
+    near = !__ballot(!(s <= 64.0f && u == u));
+    if (near) {
+      const float d = __builtin_fmaf(sum.m, q.c, -r), f = exp2_of(-d);
       s *= f;
-      a.sums.s += s;
-      if (ENTROPY) a.sums.u += u * f - d * s;
-      return;
+      sum.s += s;
+      if (ENTROPY) sum.u += u * f - d * s;
     }
   }
-  if (!holes) x.all_count();
-  float low = INFINITY;
+  if (!near) {
+    if (!holes) x.all_count();
+    float low = INFINITY;
 #pragma unroll
-  for (int g = 0; g < G; ++g)
+    for (int g = 0; g < G; ++g)
 #pragma unroll
-    for (int e = 0; e < LANE_TOKENS; ++e) low = fminf(low, x.raw_logit(g, e));
-  a.clamp |= __ballot(low == -INFINITY) != 0;
-  const float top = x.largest(holes);
-  if (top > m) move_to(a.sums, top, q);
-  float s = 0.0f, u = 0.0f;
+      for (int e = 0; e < LANE_TOKENS; ++e) low = fminf(low, x.raw_logit(g, e));
+    a.clamp |= __ballot(low == -INFINITY) != 0;
+    const float top = x.largest(holes);
+    if (top > sum.m) move_to(sum, top, q);
+    float s = 0.0f, u = 0.0f;
 #pragma unroll
-  for (int g = 0; g < G; ++g)
+    for (int g = 0; g < G; ++g)
 #pragma unroll
-    for (int e = 0; e < LANE_TOKENS; ++e) {
-      const float y = (x.template logit<true>(g, e) - a.sums.m) * q.c, p = exp2_of(y);
-      s += p;
-      if (ENTROPY) u = __builtin_fmaf(p, fmaxf(y, -FAR), u);
-      if (e + 1 == LANE_TOKENS) one_group_at_a_time();
-    }
-  a.sums.s += s;
-  a.sums.u += u;
+      for (int e = 0; e < LANE_TOKENS; ++e) {
+        const float y = (x.template logit<true>(g, e) - sum.m) * q.c, p = exp2_of(y);
+        s += p;
+        if (ENTROPY) u = __builtin_fmaf(p, fmaxf(y, -FAR), u);
+        if (e + 1 == LANE_TOKENS) one_group_at_a_time();
+      }
+    sum.s += s;
+    if (ENTROPY) sum.u += u;
+  }
+  a.sums = sum;
 }
 
 // How a pass over the logits is laid out.  Rows are stretches of LOSS_TOKENS slots each, and a workgroup takes the next `share` of all rows'
@@ -583,7 +588,7 @@ __device__ __forceinline__ void finish_logprob(const LossArgs& a, const LogprobO
   }
 }
 
-// Bound by reading: 1178 rows of 131073 in bf16 (309 MB) take 68 us, 74 with the largest of each stretch; 4096 x 65537 (537 MB)
+// Bound by reading: 1178 rows of 131073 in bf16 (309 MB) take 68 us, 70 with the largest of each stretch; 4096 x 65537 (537 MB)
 // 96 us, 5.6 TB/s, and 4096 x 131072 (1074 MB) 171 us, 6.3 TB/s; without any arithmetic a copy of the pass was 3 to 5 % shorter.  Loads of the next pass
 // asked for before this one is summed cost registers and gave nothing (44 us for 41, 188 for 182).
 // WHOLE: every workgroup has one row, and no launch comes after this one: 48 masked rows of 16384 with five alternatives in 13 us.
@@ -856,9 +861,10 @@ __device__ __forceinline__ void finish_distill(const LossArgs& a, const DistillA
   }
 }
 
-// The sums over what is not listed, with a bit in LDS for each slot; bound by reading: 2048 x 131073 in bf16 (537 MB) in 103 us, 5.2 TB/s.
+// The sums over what is not listed, with a bit in LDS for each slot; bound by reading: 2048 x 131073 in bf16 (537 MB) in 93 us,
+// 5.8 TB/s.  In fp32 seven waves a SIMD, for which registers suffice: 4096 x 65537 in 214 us, 243 with eight.
 template <bool BF16, int G, bool WHOLE>
-__global__ __launch_bounds__(LOSS_THREADS, WHOLE ? 2 : 8) void distill_kernel(LossArgs a, LossGrid grid, DistillArgs o) {
+__global__ __launch_bounds__(LOSS_THREADS, WHOLE ? 2 : BF16 ? 8 : 7) void distill_kernel(LossArgs a, LossGrid grid, DistillArgs o) {
   __shared__ Sums waves[LOSS_WAVES];
   extern __shared__ uint32_t listed[];               // a bit for each slot of the row's part; WHOLE: then the table of the list
   const int stop = min((int)(blockIdx.x + 1) * grid.share, a.l.d.rows * grid.stretches);
@@ -1141,8 +1147,8 @@ constexpr int PASS_GROUPS = 2, WHOLE_GROUPS = 4, WHOLE_STRETCHES = 8;
 // Few short rows are a workgroup's each, with four groups a lane at a time, in one launch: 48 x 16384 (8 stretches) in 6.3 us for 4.9 + 3.5 in two,
 // with alternatives 14.5 for 5.3 + 9.8, against a list 10.4 for 5.4 + 6.3 (of 16000); at 16 stretches, 32001, 16.4 for 4.6 + 9.7 and 15.4 for 6.6 + 6.4.
 static bool whole_rows(int64_t rows, int64_t stretches) { return stretches <= WHOLE_STRETCHES && rows * stretches <= LOSS_WORKGROUPS; }
-static LossGrid loss_grid(const LossArgs& a, bool top) {
-  const int64_t rows = a.l.d.rows, stretches = stretches_of(slots_of(a)), all = rows * stretches, most = top ? TOP_WORKGROUPS : LOSS_WORKGROUPS;
+static LossGrid loss_grid(const LossArgs& a, int64_t most) {
+  const int64_t rows = a.l.d.rows, stretches = stretches_of(slots_of(a)), all = rows * stretches;
   const int64_t share = whole_rows(rows, stretches) ? stretches : std::min((all + most - 1) / most, ROWS_OF_ONE * stretches);
   return LossGrid{(int)stretches, (int)share, (int)((all + share - 1) / share)};
 }
@@ -1187,7 +1193,7 @@ extern "C" pg_status pg_token_logprobs(const pg_logits* desc, const float* tempe
   if (!scratch) return fail(PG_EINVAL, "pg_token_logprobs: scratch is NULL");
   if ((uintptr_t)scratch & 7) return fail(PG_ESHAPE, "pg_token_logprobs: scratch is not 8-byte aligned");
   const bool top = n_top && (top_ids || top_logp);
-  const LossGrid g = loss_grid(a, top);
+  const LossGrid g = loss_grid(a, top ? TOP_WORKGROUPS : LOSS_WORKGROUPS);
   const LogprobOut o{target, logp, entropy, stats, n_top, top_ids, top_logp, (Sums*)scratch, scratch + part_floats(rows, a.l.d.vocab), n_chunks(a.l.d.vocab)};
   return with_kind(a, [&](auto bf) {
     constexpr bool BF = decltype(bf)::value;
@@ -1259,7 +1265,7 @@ extern "C" pg_status pg_distill_loss(const pg_logits* desc, const float* tempera
   if (rows == 0) return PG_OK;
   if (!loss || !scratch) return fail(PG_EINVAL, "pg_distill_loss: null pointer");
   if ((uintptr_t)scratch & 7) return fail(PG_ESHAPE, "pg_distill_loss: scratch is not 8-byte aligned");
-  const LossGrid g = loss_grid(a, false);
+  const LossGrid g = loss_grid(a, LOSS_WORKGROUPS);
   const DistillArgs o{mode, k, teacher_ids, teacher_logp, loss, stats, (Sums*)scratch};
   const size_t lds = std::min({g.stretches, g.share, LIST_RANGE / LOSS_TOKENS}) * (LOSS_TOKENS / 8);
   return with_kind(a, [&](auto bf) {
