@@ -1,4 +1,4 @@
-"""Plain fp64 checkers of what a token policy learns from (test infrastructure only): log-probs with entropy and alternatives,
+"""Plain fp64 oracle of what a token policy learns from (test infrastructure only): log-probs with entropy and alternatives,
 divergence from a teacher's list, the clipped objective, and their gradients.  Written from the definitions in the C header, one row and
 one sequence at a time, on values in fp64 (what lies there in fp32 or bf16, without rounding)."""
 import numpy as np

@@ -1,4 +1,4 @@
-"""GPU parity of what a token policy learns from against plain fp64 checkers, through the C ABI.
+"""GPU parity of what a token policy learns from against the plain fp64 oracle, through the C ABI.
 
 Tolerances.  u = 2^-24.  1 / T, the product with z - m and the exponential round y - top at most four times, so a weight of the softmax is
 off by u (4 |y - top| + 4) of itself; a lane adds at most vocab / 256 terms one after another and some 64 steps join the lanes and pieces, so a sum

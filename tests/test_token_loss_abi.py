@@ -1,4 +1,4 @@
-"""CPU-only checks of what a token policy learns from: refusals on the host before any launch, sizes, and pins of the fp64 checkers."""
+"""CPU-only checks of what a token policy learns from: refusals on the host before any launch, sizes, and pins of the fp64 oracle."""
 import ctypes as C
 import math
 
@@ -168,14 +168,14 @@ def test_the_binding_refuses_tensors_of_another_kind():
             pg.pg_token_surrogate(f(10), args.pop("old"), args.pop("adv"), args.pop("cu"), args.pop("objective"), args.pop("g"), 0.2, 0.2, 5, **args)
 
 
-# ---------------------------------------------------------------- the checkers
+# ---------------------------------------------------------------- the oracle
 
 def rows(seed, n=6, vocab=23):
     rng = np.random.default_rng(seed)
     return rng, rng.standard_normal((n, vocab)) * 2, rng.integers(0, vocab, size=n)
 
 
-def test_checkers_log_probs_are_the_log_softmax():
+def test_oracles_log_probs_are_the_log_softmax():
     rng, z, target = rows(0)
     allow = rng.random(z.shape) < 0.7
     allow[np.arange(6), target] = True
@@ -195,7 +195,7 @@ def slope(f, z, way, h=1e-6):
     return (f(z + h * way) - f(z - h * way)) / (2 * h)
 
 
-def test_checkers_gradients_are_the_slopes():
+def test_oracles_gradients_are_the_slopes():
     rng, z, target = rows(1)
     allow = rng.random(z.shape) < 0.7
     allow[np.arange(6), target] = True
@@ -213,7 +213,7 @@ def test_checkers_gradients_are_the_slopes():
                 assert abs(slope(lambda x: ref.distill(x, ids, values, tail, 1.4, mask)[0], z[r], way) - d @ way) < 1e-8
 
 
-def test_checkers_distillation_is_the_divergence():
+def test_oracles_distillation_is_the_divergence():
     rng, z, _ = rows(2)
     q = torch.log_softmax(torch.from_numpy(rng.standard_normal((6, 23))), 1)
     ids = np.arange(23)
@@ -229,7 +229,7 @@ def test_checkers_distillation_is_the_divergence():
         assert abs(ref.distill(z[r], few, q[r].numpy()[few], True)[0] - float((a * (a / b).log()).sum())) < 1e-12
 
 
-def test_checkers_objective_is_the_clipped_one():
+def test_oracles_objective_is_the_clipped_one():
     rng = np.random.default_rng(3)
     logp, old, x = (-rng.random(200) * 3 for _ in range(3))
     for adv in (1.3, -0.7, 0.0):
