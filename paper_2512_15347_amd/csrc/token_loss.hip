@@ -397,18 +397,15 @@ __device__ __forceinline__ void no_candidates(TopLds& s) {
     s.bound = ~0u;
   }
 }
-// Of a lane's N keys those that are not 0, with one request for their places.
-template <int N>
-__device__ __forceinline__ void candidates(const uint64_t* key, TopLds& s) {
-  int n = 0;
-#pragma unroll
-  for (int i = 0; i < N; ++i) n += key[i] != 0;
-  if (!n) return;
-  int at = atomicAdd(&s.count, n);
+// Of a lane's keys key(0) .. key(N - 1) those whose bits are set, with one request for their places.
+template <int N, class Key>
+__device__ __forceinline__ void candidates(uint32_t some, TopLds& s, Key key) {
+  if (!some) return;
+  int at = atomicAdd(&s.count, __popc(some));
 #pragma unroll
   for (int i = 0; i < N; ++i)
-    if (key[i]) {
-      if (at < TopLds::CANDIDATES) s.candidate[at] = key[i];
+    if (some >> i & 1) {
+      if (at < TopLds::CANDIDATES) s.candidate[at] = key(i);
       ++at;
     }
 }
@@ -469,8 +466,8 @@ __device__ __forceinline__ void select_by_key(int N, int n, TopLds& s, Item item
   __syncthreads();
   const uint64_t least = s.least;
   for (int i = me; i < N; i += LOSS_THREADS) {
-    const uint64_t key = item(i), mine = key >= least ? key : 0;
-    candidates<1>(&mine, s);
+    const uint64_t key = item(i);
+    candidates<1>(key >= least, s, [&](int) { return key; });
   }
   if (rank_candidates(n, s)) return;
   uint64_t last = ~0ull;
@@ -513,19 +510,17 @@ __device__ __forceinline__ void alternatives(const LossArgs& a, const LossRow& q
   for (int k = 0; k < KEPT; ++k) top = fmaxf(top, kept.z[k]);
   for (int i = me + KEPT * LOSS_THREADS; i < N; i += LOSS_THREADS) top = fmaxf(top, largest[i]);
   const float bound = nth_of_lanes(top, n, s);
-  uint64_t mine[KEPT];
+  uint32_t some = 0;
 #pragma unroll
-  for (int k = 0; k < KEPT; ++k) mine[k] = kept.z[k] >= bound ? key_of(kept.z[k], me + k * LOSS_THREADS) : 0;
-  candidates<KEPT>(mine, s);
-  for (int i = me + KEPT * LOSS_THREADS; i < N; i += LOSS_THREADS) {
-    const uint64_t one = largest[i] >= bound ? key_of(largest[i], i) : 0;
-    candidates<1>(&one, s);
-  }
+  for (int k = 0; k < KEPT; ++k) some |= (uint32_t)(kept.z[k] >= bound && kept.z[k] > -INFINITY) << k;
+  candidates<KEPT>(some, s, [&](int k) { return key_of(kept.z[k], me + k * LOSS_THREADS); });
+  for (int i = me + KEPT * LOSS_THREADS; i < N; i += LOSS_THREADS)
+    candidates<1>(largest[i] >= bound && largest[i] > -INFINITY, s, [&](int) { return key_of(largest[i], i); });
   if (!rank_candidates(n, s)) select_by_key(N, n, s, [&](int i) { return key_of(largest[i], i); });
   // the lanes look at these stretches again, eight tokens each
   const float least = logit_of(s.best[n - 1]);       // NaN for 0: nothing is below it
   const int end = vocab + q.shift;
-  uint64_t key[AGAIN * LANE_TOKENS];
+  int first[AGAIN];                                  // their first tokens
   Pass<BF16, 1> x[AGAIN];
 #pragma unroll
   for (int k = 0; k < AGAIN; ++k) {
@@ -533,18 +528,21 @@ __device__ __forceinline__ void alternatives(const LossArgs& a, const LossRow& q
     const uint64_t chunk = i < n ? s.best[i] : 0;
     const int slot = chunk ? place_of(chunk) * CHUNK + me % CHUNK_LANES * LANE_TOKENS : end;
     x[k].load_part(a, q, slot - me * LANE_TOKENS, end);
-#pragma unroll
-    for (int e = 0; e < LANE_TOKENS; ++e) key[k * LANE_TOKENS + e] = slot - q.shift + e;
+    first[k] = slot - q.shift;
   }
+  auto logit = [&](int e) { return x[e / LANE_TOKENS].template logit<true>(0, e % LANE_TOKENS); };
+  auto key = [&](int e) { return key_of(logit(e), first[e / LANE_TOKENS] + e % LANE_TOKENS); };
   no_candidates(s);
   __syncthreads();
+  some = 0;
 #pragma unroll
-  for (int e = 0; e < AGAIN * LANE_TOKENS; ++e) {
-    const float y = x[e / LANE_TOKENS].template logit<true>(0, e % LANE_TOKENS);
-    key[e] = y < least ? 0 : key_of(y, (int)key[e]);
-  }
-  candidates<AGAIN * LANE_TOKENS>(key, s);
-  if (!rank_candidates(n, s)) select_by_key(LOSS_THREADS * LANE_TOKENS * AGAIN, n, s, [&](int i) { return key[i / LOSS_THREADS]; });
+  for (int e = 0; e < AGAIN * LANE_TOKENS; ++e) some |= (uint32_t)(!(logit(e) < least) && logit(e) > -INFINITY) << e;
+  candidates<AGAIN * LANE_TOKENS>(some, s, key);
+  if (rank_candidates(n, s)) return;
+  uint64_t all[AGAIN * LANE_TOKENS];
+#pragma unroll
+  for (int e = 0; e < AGAIN * LANE_TOKENS; ++e) all[e] = some >> e & 1 ? key(e) : 0;
+  select_by_key(LOSS_THREADS * LANE_TOKENS * AGAIN, n, s, [&](int i) { return all[i / LOSS_THREADS]; });
 }
 
 struct LogprobOut {
@@ -588,10 +586,10 @@ __device__ __forceinline__ void finish_logprob(const LossArgs& a, const LogprobO
   }
 }
 
-// Bound by reading: 1178 rows of 131073 in bf16 (309 MB) take 68 us, 70 with the largest of each stretch; 4096 x 65537 (537 MB)
+// Bound by reading: 1178 rows of 131073 in bf16 (309 MB) take 54 us, 5.8 TB/s, and 70 with the largest of each stretch (6 of the 16 for its stores, past the caches 3 more); 4096 x 65537 (537 MB)
 // 96 us, 5.6 TB/s, and 4096 x 131072 (1074 MB) 171 us, 6.3 TB/s; without any arithmetic a copy of the pass was 3 to 5 % shorter.  Loads of the next pass
 // asked for before this one is summed cost registers and gave nothing (44 us for 41, 188 for 182).
-// WHOLE: every workgroup has one row, and no launch comes after this one: 48 masked rows of 16384 with five alternatives in 13 us.
+// WHOLE: every workgroup has one row, and no launch comes after this one: 48 masked rows of 16384 with five alternatives in 12.7 us.
 template <bool BF16, int G, bool TOP, bool WHOLE>
 __global__ __launch_bounds__(LOSS_THREADS, WHOLE ? 2 : TOP ? 6 : 8) void logprob_kernel(LossArgs a, LossGrid grid, LogprobOut o) {
   __shared__ Sums waves[LOSS_WAVES];
@@ -1140,12 +1138,12 @@ static int64_t most_slots(int64_t vocab) { return vocab + LANE_TOKENS - 1; }
 static int64_t stretches_of(int64_t slots) { return (slots + LOSS_TOKENS - 1) / LOSS_TOKENS; }
 
 // As many workgroups as are resident at once, if there is a stretch for each; short rows are no more than 8 to a workgroup, which goes
-// through them one after another.  Two groups a lane at a time with eight waves a SIMD: 68 us for 1178 x 131073, four with five waves 83; one: 119 us for
+// through them one after another.  Two groups a lane at a time with eight waves a SIMD: 68 us for 1178 x 131073 (with loads that the caches keep), four with five waves 83; one: 119 us for
 // 4096 x 65537, two 113.  With the largest of each stretch six waves fit: 73 us, 79 with as many workgroups as eight would take.
 constexpr int64_t LOSS_WORKGROUPS = 2048, TOP_WORKGROUPS = 1536, ROWS_OF_ONE = 8;
 constexpr int PASS_GROUPS = 2, WHOLE_GROUPS = 4, WHOLE_STRETCHES = 8;
 // Few short rows are a workgroup's each, with four groups a lane at a time, in one launch: 48 x 16384 (8 stretches) in 6.3 us for 4.9 + 3.5 in two,
-// with alternatives 14.5 for 5.3 + 9.8, against a list 10.4 for 5.4 + 6.3 (of 16000); at 16 stretches, 32001, 16.4 for 4.6 + 9.7 and 15.4 for 6.6 + 6.4.
+// with alternatives 12.7 for 5.3 + 9.8, against a list 10.4 for 5.4 + 6.3 (of 16000); at 16 stretches, 32001, 16.4 for 4.6 + 9.7 and 15.4 for 6.6 + 6.4.
 static bool whole_rows(int64_t rows, int64_t stretches) { return stretches <= WHOLE_STRETCHES && rows * stretches <= LOSS_WORKGROUPS; }
 static LossGrid loss_grid(const LossArgs& a, int64_t most) {
   const int64_t rows = a.l.d.rows, stretches = stretches_of(slots_of(a)), all = rows * stretches;
