@@ -586,9 +586,9 @@ __device__ __forceinline__ void finish_logprob(const LossArgs& a, const LogprobO
   }
 }
 
-// Bound by reading: 1178 rows of 131073 in bf16 (309 MB) take 54 us, 5.8 TB/s, and 70 with the largest of each stretch (6 of the 16 for its stores, past the caches 3 more); 4096 x 65537 (537 MB)
-// 96 us, 5.6 TB/s, and 4096 x 131072 (1074 MB) 171 us, 6.3 TB/s; without any arithmetic a copy of the pass was 3 to 5 % shorter.  Loads of the next pass
-// asked for before this one is summed cost registers and gave nothing (44 us for 41, 188 for 182).
+// Bound by reading: 1178 rows of 131073 in bf16 (309 MB) take 54 us, 5.8 TB/s, and 70 with the largest of each stretch (6 of the 16 for its stores, past
+// the caches 3 more); 4096 x 65537 (537 MB) 96 us, 5.6 TB/s, and 4096 x 131072 (1074 MB) 171 us, 6.3 TB/s; without any arithmetic a copy of the pass was
+// 3 to 5 % shorter.  Loads of the next pass asked for before this one is summed cost registers and gave nothing (44 us for 41, 188 for 182).
 // WHOLE: every workgroup has one row, and no launch comes after this one: 48 masked rows of 16384 with five alternatives in 12.7 us.
 template <bool BF16, int G, bool TOP, bool WHOLE>
 __global__ __launch_bounds__(LOSS_THREADS, WHOLE ? 2 : TOP ? 6 : 8) void logprob_kernel(LossArgs a, LossGrid grid, LogprobOut o) {
@@ -1138,12 +1138,13 @@ static int64_t most_slots(int64_t vocab) { return vocab + LANE_TOKENS - 1; }
 static int64_t stretches_of(int64_t slots) { return (slots + LOSS_TOKENS - 1) / LOSS_TOKENS; }
 
 // As many workgroups as are resident at once, if there is a stretch for each; short rows are no more than 8 to a workgroup, which goes
-// through them one after another.  Two groups a lane at a time with eight waves a SIMD: 68 us for 1178 x 131073 (with loads that the caches keep), four with five waves 83; one: 119 us for
-// 4096 x 65537, two 113.  With the largest of each stretch six waves fit: 73 us, 79 with as many workgroups as eight would take.
+// through them one after another.  Two groups a lane at a time with eight waves a SIMD: 68 us for 1178 x 131073 (with loads that the caches keep), four
+// with five waves 83; one: 119 us for 4096 x 65537, two 113.  With the largest of each stretch six waves fit: 73 us, 79 with as many workgroups as eight
+// would take.
 constexpr int64_t LOSS_WORKGROUPS = 2048, TOP_WORKGROUPS = 1536, ROWS_OF_ONE = 8;
 constexpr int PASS_GROUPS = 2, WHOLE_GROUPS = 4, WHOLE_STRETCHES = 8;
 // Few short rows are a workgroup's each, with four groups a lane at a time, in one launch: 48 x 16384 (8 stretches) in 6.3 us for 4.9 + 3.5 in two,
-// with alternatives 12.7 for 5.3 + 9.8, against a list 10.4 for 5.4 + 6.3 (of 16000); at 16 stretches, 32001, 16.4 for 4.6 + 9.7 and 15.4 for 6.6 + 6.4.
+// with alternatives 14.5 for 5.3 + 9.8, against a list 10.4 for 5.4 + 6.3 (of 16000); at 16 stretches, 32001, 16.4 for 4.6 + 9.7 and 15.4 for 6.6 + 6.4.
 static bool whole_rows(int64_t rows, int64_t stretches) { return stretches <= WHOLE_STRETCHES && rows * stretches <= LOSS_WORKGROUPS; }
 static LossGrid loss_grid(const LossArgs& a, int64_t most) {
   const int64_t rows = a.l.d.rows, stretches = stretches_of(slots_of(a)), all = rows * stretches;
