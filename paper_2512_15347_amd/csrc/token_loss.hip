@@ -560,7 +560,7 @@ struct LogprobOut {
 template <bool BF16>
 __device__ __forceinline__ void finish_logprob(const LossArgs& a, const LogprobOut& o, const LossRow& q, int r, int target, float at_target, const Sums& sum,
                                                const Kept& kept, TopLds* s) {
-  const bool gone = target == -1, bad = sum.s != sum.s, none = sum.s == 0.0f;
+  const bool gone = target == -1, bad = !gone && sum.s != sum.s, none = gone || sum.s == 0.0f;     // a temperature that is none makes even empty sums NaN
   const float ln_s = none ? 0.0f : logf(sum.s);
   if (threadIdx.x == 0) {
     const float h = none ? 0.0f : ln_s - LN2 * (sum.u / sum.s);

@@ -1,0 +1,31 @@
+"""What a token policy learns from, at the edges of what its calls allow: against the plain fp64 oracle, through the C ABI."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import token_loss as ref
+from test_gpu_token_loss import DEV, TINY, U, Softmax, check_distill, check_logprobs, check_surrogate, dev, make_logits, mask_words, near, rounded, \
+    run_distill, run_logprobs, run_surrogate, store_tol, teacher_lists
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("n_top", [0, 5])
+@pytest.mark.parametrize("rows,vocab", [(7, 3001), (7, 40001), (2500, 300)], ids=["one launch", "rows in pieces", "rows one after another"])
+def test_rows_left_out_whose_temperature_is_none(lib, rows, vocab, n_top):
+    """Padding: neither its logits nor its temperature reach an output."""
+    rng = np.random.default_rng(rows + vocab)
+    z = make_logits(rng, rows, vocab, False)
+    target, t = rng.integers(0, vocab, size=rows), rng.uniform(0.6, 1.4, size=rows)
+    t[:6] = [math.nan, -1.0, math.inf, math.nan, 1.0, -math.inf]
+    target[[0, 1, 2, 4, 5]] = -1                           # of the rows without a temperature the fourth alone is not left out
+    z[2] = math.nan
+    g, ge = rng.standard_normal(rows), rng.standard_normal(rows)
+    got = run_logprobs(lib, z, False, target, t, n_top=n_top, g=g, ge=ge)
+    gone = target == -1
+    assert not got["logp"][gone].any() and not got["entropy"][gone].any() and not got["d"][gone].any() and np.isnan(got["logp"][3])
+    if n_top:
+        assert (got["top_ids"][gone] == -1).all() and (got["top_logp"][gone] == -math.inf).all()
+    check_logprobs(got, z, False, target, t, n_top=n_top, g=g, ge=ge)
