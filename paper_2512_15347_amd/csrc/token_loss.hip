@@ -855,7 +855,8 @@ __device__ __forceinline__ void finish_distill(const LossArgs& a, const DistillA
   if (o.stats) {
     float4* x = (float4*)(o.stats + (int64_t)r * PG_DISTILL_STATS);
     x[0] = float4{m, (float)log(s_all), rest.m, others ? logf(rest.s) : 0.0f};
-    x[1] = float4{(float)(all * p_rest - q_rest), (float)t0, (float)all, active ? 1.0f : 0.0f};
+    // the teacher's largest value and the logarithm of their sum, apart: values shifted by 10^4 would lose 2^-11 of q to t0 as one number
+    x[1] = float4{(float)(all * p_rest - q_rest), top ? most : 0.0f, active ? (float)all : -1.0f, top ? (float)log(sum_q) : 0.0f};
   }
 }
 
@@ -920,7 +921,7 @@ __global__ __launch_bounds__(LOSS_THREADS) void distill_backward_kernel(LossArgs
   const LossRow q = loss_row<BF16>(a, r);
   const int vocab = a.l.d.vocab, first = piece * RANGE, end = min(first + RANGE, vocab + q.shift);
   const float4 s0 = ((const float4*)(o.stats + (int64_t)r * PG_DISTILL_STATS))[0], s1 = ((const float4*)(o.stats + (int64_t)r * PG_DISTILL_STATS))[1];
-  const float g = s1.w == 0.0f ? 0.0f : g_loss[r];
+  const float g = s1.z < 0.0f ? 0.0f : g_loss[r];     // -1 for a row that nothing is learnt from
   char* to = (char*)out + (int64_t)r * out_stride * ELT;
   if (g == 0.0f) return put_zeros<BF16, PAST, G>(to, first + (int)threadIdx.x * LANE_TOKENS - q.shift, vocab);
   const bool entry = (int)threadIdx.x < o.k;
@@ -944,7 +945,7 @@ __global__ __launch_bounds__(LOSS_THREADS) void distill_backward_kernel(LossArgs
   if (writes) {
     const float z = open_logit<BF16>(a, q, id);
     const float p = exp2_of(__builtin_fmaf(fmaxf(z - s0.x, q.lim), q.c, -s0.y * LOG2E));
-    const float d = z == -INFINITY ? 0.0f : scale * (s1.z * p - expf(t - s1.y));
+    const float d = z == -INFINITY ? 0.0f : scale * (s1.z * p - expf((t - s1.y) - s1.w));
     if (BF16) ((uint16_t*)to)[id] = (uint16_t)pack_bf16x2(d, 0.0f);
     else ((float*)to)[id] = d;
   }

@@ -29,3 +29,24 @@ def test_rows_left_out_whose_temperature_is_none(lib, rows, vocab, n_top):
     if n_top:
         assert (got["top_ids"][gone] == -1).all() and (got["top_logp"][gone] == -math.inf).all()
     check_logprobs(got, z, False, target, t, n_top=n_top, g=g, ge=ge)
+
+
+@pytest.mark.parametrize("shift", [0.0, 1e3, -1e4, 1e5])
+def test_a_shifted_list_has_the_same_gradient(lib, shift):
+    """PG_DISTILL_TOP takes values up to a constant: rounded to fp32 they are the list, and nothing more is lost of them."""
+    rng = np.random.default_rng(31)
+    rows, vocab, k = 4, 3001, 64
+    z = make_logits(rng, rows, vocab, False)
+    ids, values = teacher_lists(rng, z, k)
+    values = (values.astype(np.float64) + shift).astype(np.float32)
+    g = np.ones(rows)
+    got = run_distill(lib, z, False, ids, values, False, g)
+    check_distill(got, z, False, ids, values, False, g)
+    for r in range(rows):
+        v = values[r].astype(np.float64)
+        w = np.exp(v - v.max()) / np.exp(v - v.max()).sum()
+        s = Softmax(z[r], 1.0, None)
+        want = ref.distill(z[r], ids[r], v, False)[1][ids[r]]
+        # q: differences to the largest and to the logarithm of the sum (at most ln k), rounded once each, and the exponential
+        tol = s.p[ids[r]] * (s.p_rel[ids[r]] + 8 * U) + w * U * (2 * (v.max() - v) + 4 * math.log(k) + 8)
+        near(got[1][r][ids[r]], want, tol + store_tol(want, False) + TINY, f"gradient of row {r}'s listed tokens")
