@@ -113,5 +113,6 @@ def surrogate(logp, old, adv, clip_low, clip_high, ref=None, kl_coef=0.0, weight
         if ref is not None:
             x = np.asarray(ref, dtype=np.float64) - logp
             kl = np.where(np.expm1(x) == np.inf, np.inf, np.expm1(x) - x)
-            term, g = term - kl_coef * kl, g + kl_coef * np.expm1(x)
+            if kl_coef != 0:                               # 0 e^1000 is 0, which fp64 would make no number
+                term, g = term - kl_coef * kl, g + kl_coef * np.expm1(x)
     return dict(objective=w * term.sum(), kl=kl.mean(), clipped=int(cut.sum()), g_logp=w * g)

@@ -991,12 +991,39 @@ struct SurrogateArgs {
   float* parts;                                      // [sequences, pieces, 4]
 };
 
-// What a sequence's sums give.
-__device__ __forceinline__ void finish_surrogate(const SurrogateArgs& a, int r, int n, double sum, double kl, int cuts) {
-  const float w = a.weight ? a.weight[r] : 1.0f / (float)max(n, 1);
-  if (a.objective) a.objective[r] = n ? (float)(w * sum) : 0.0f;
-  if (a.kl) a.kl[r] = (float)(kl / max(n, 1));
+// What a sequence's sums give: the objective is weighted, the divergence a mean already.
+__device__ __forceinline__ void finish_surrogate(const SurrogateArgs& a, int r, float objective, float kl, int cuts) {
+  if (a.objective) a.objective[r] = objective;
+  if (a.kl) a.kl[r] = kl;
   if (a.clipped) a.clipped[r] = cuts;
+}
+
+// Tokens for which fp32 is enough: exponentials and what they are multiplied with are of at most e^NEAR and LARGE, so that no product and no sum of a
+// lane's passes 10^38.  All others, and all where a factor is larger or no number, go through fp64 until they are scaled.  Decided for all tokens that a lane
+// has at once; with it 384 sequences of 16384 tokens at most take 16.3 us a call, 16.0 without.
+constexpr float NEAR = 40.0f, LARGE = 1e12f;
+__device__ __forceinline__ bool is_near(float l, float old, float ref, bool has_ref) {
+  return fabsf(l - old) < NEAR && (!has_ref || fabsf(ref - l) < NEAR);
+}
+
+// e^x - x - 1 near 0: x^2 (1/2! + x (1/3! + x (...))), whose terms past the ninth are 2^-26 of it at x = 1/2
+__device__ __forceinline__ float near_exp(float x) {
+  float k = 1.0f / 3628800;
+  k = __builtin_fmaf(k, x, 1.0f / 362880);
+  k = __builtin_fmaf(k, x, 1.0f / 40320);
+  k = __builtin_fmaf(k, x, 1.0f / 5040);
+  k = __builtin_fmaf(k, x, 1.0f / 720);
+  k = __builtin_fmaf(k, x, 1.0f / 120);
+  k = __builtin_fmaf(k, x, 1.0f / 24);
+  k = __builtin_fmaf(k, x, 1.0f / 6);
+  k = __builtin_fmaf(k, x, 0.5f);
+  return k * (x * x);
+}
+// e^x with fp32's digits and fp64's range: 2^n e^(x - n ln 2).  (The library's exp and expm1 take 96 registers: five waves a SIMD for eight.)
+__device__ __forceinline__ double wide_exp(double x) {
+  if (!(fabs(x) < 2000.0)) return x > 0.0 ? (double)INFINITY : x < 0.0 ? 0.0 : x;
+  const double n = rint(x * 1.4426950408889634);
+  return ldexp((double)expf((float)fma(n, -0.6931471805599453, x)), (int)n);
 }
 
 // One token's part of the objective, of the divergence and of the gradient; whether it was cut.
@@ -1006,31 +1033,47 @@ struct Token {
   __device__ __forceinline__ Token(const SurrogateArgs& a, float A, float l, float old, float ref) {
     const double d = (double)l - (double)old;
     cut = A > 0.0f ? d > a.hi : A < 0.0f && d < a.lo;
-    const float ra = A == 0.0f ? 0.0f : expf((float)d) * A;
+    const float ra = expf((float)d) * A;
     g = cut ? 0.0f : ra;
     value = cut ? (A > 0.0f ? a.at_hi : a.at_lo) * A : ra;
     k = 0.0f;
     if (a.ref) {
-      // e^x - x - 1: near 0 x^2 (1/2! + x (1/3! + x (...))), whose terms past the ninth are 2^-26 of it at x = 1/2
       const float x = ref - l;
-      k = 1.0f / 3628800;
-      k = __builtin_fmaf(k, x, 1.0f / 362880);
-      k = __builtin_fmaf(k, x, 1.0f / 40320);
-      k = __builtin_fmaf(k, x, 1.0f / 5040);
-      k = __builtin_fmaf(k, x, 1.0f / 720);
-      k = __builtin_fmaf(k, x, 1.0f / 120);
-      k = __builtin_fmaf(k, x, 1.0f / 24);
-      k = __builtin_fmaf(k, x, 1.0f / 6);
-      k = __builtin_fmaf(k, x, 0.5f);
-      k *= x * x;
+      k = near_exp(x);
       float slope = k + x;
       if (!(fabsf(x) < 0.5f)) {
         const float e = expf(x);
-        k = e == INFINITY ? e : e - x - 1.0f;
+        k = e - x - 1.0f;
         slope = e - 1.0f;
       }
       value -= a.kl_coef * k;
       g += a.kl_coef * slope;
+    }
+  }
+};
+struct FarToken {
+  double value, k, g;
+  bool cut;
+  __device__ FarToken(const SurrogateArgs& a, float A, float l, float old, float ref) {
+    const double d = (double)l - (double)old, ra = A == 0.0f ? 0.0 : wide_exp(d) * A;
+    cut = A > 0.0f ? d > a.hi : A < 0.0f && d < a.lo;
+    g = cut ? 0.0 : ra;
+    value = cut ? (double)(A > 0.0f ? a.at_hi : a.at_lo) * A : ra;
+    k = 0.0;
+    if (a.ref) {
+      const double x = (double)ref - (double)l;
+      double e;
+      if (fabs(x) < 0.5) {
+        k = near_exp((float)x);
+        e = k + x;
+      } else {
+        e = wide_exp(x) - 1.0;
+        k = e == INFINITY ? e : e - x;
+      }
+      if (a.kl_coef != 0.0f) {                       // else the reference reaches the divergence alone
+        value -= a.kl_coef * k;
+        g += a.kl_coef * e;
+      }
     }
   }
 };
@@ -1040,7 +1083,7 @@ struct Token {
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void surrogate_tokens_kernel(SurrogateArgs a) {
   constexpr int AT_ONCE = 4;                         // tokens of a lane whose loads are under way together
-  __shared__ float sums[THREADS / WAVE][2];
+  __shared__ double sums[THREADS / WAVE][2];
   __shared__ int counts[THREADS / WAVE];
   const int r = blockIdx.x / a.pieces, piece = blockIdx.x - r * a.pieces;
   const float A = a.adv[r], weight = a.weight ? a.weight[r] : 0.0f;
@@ -1048,7 +1091,9 @@ __global__ __launch_bounds__(THREADS) void surrogate_tokens_kernel(SurrogateArgs
   const float w = a.weight ? weight : 1.0f / (float)max(n, 1);
   const int64_t first = from + (int64_t)piece * a.piece, end = piece + 1 < a.pieces ? min(first + a.piece, (int64_t)to) : to;
   if (a.pieces > 1 && first >= end) return;           // its part is not looked at
+  const bool ordinary = fabsf(A) < LARGE && fabsf(a.kl_coef) < LARGE;
   float sum = 0.0f, kl = 0.0f;
+  double far_sum = 0.0, far_kl = 0.0;
   int cuts = 0;
   for (int64_t i = first + threadIdx.x; i < end; i += AT_ONCE * THREADS) {
     float l[AT_ONCE], old[AT_ONCE], ref[AT_ONCE];
@@ -1059,22 +1104,41 @@ __global__ __launch_bounds__(THREADS) void surrogate_tokens_kernel(SurrogateArgs
       old[j] = a.old[at];
       ref[j] = a.ref ? a.ref[at] : 0.0f;
     }
+    bool near = ordinary;
 #pragma unroll
-    for (int j = 0; j < AT_ONCE; ++j)
-      if (i + j * THREADS < end) {
-        const Token t(a, A, l[j], old[j], ref[j]);
-        sum += t.value;
-        kl += t.k;
+    for (int j = 0; j < AT_ONCE; ++j) near &= is_near(l[j], old[j], ref[j], a.ref);
+    if (near) {
+#pragma unroll
+      for (int j = 0; j < AT_ONCE; ++j)
+        if (i + j * THREADS < end) {
+          const Token t(a, A, l[j], old[j], ref[j]);
+          sum += t.value;
+          kl += t.k;
+          cuts += t.cut;
+          if (a.g_logp) a.g_logp[i + j * THREADS] = w * t.g;
+        }
+    } else {                                         // read again: nothing has been written there, also where g_logp is one of the inputs
+#pragma unroll 1
+      for (int64_t at = i; at < min(i + AT_ONCE * THREADS, end); at += THREADS) {
+        const FarToken t(a, A, a.logp[at], a.old[at], a.ref ? a.ref[at] : 0.0f);
+        far_sum += t.value;
+        far_kl += t.k;
         cuts += t.cut;
-        if (a.g_logp) a.g_logp[i + j * THREADS] = w * t.g;
+        if (a.g_logp) a.g_logp[at] = (float)(w * t.g);
       }
+    }
   }
   sum = wave_allsum(sum);
   kl = wave_allsum(kl);
   for (int o = 32; o; o >>= 1) cuts += __shfl_xor(cuts, o);
+  const bool some = __ballot(far_sum != 0.0 || far_kl != 0.0);
+  if (some) {
+    far_sum = lanes_sum(far_sum);
+    far_kl = lanes_sum(far_kl);
+  }
   if ((threadIdx.x & 63) == 0) {
-    sums[threadIdx.x >> 6][0] = sum;
-    sums[threadIdx.x >> 6][1] = kl;
+    sums[threadIdx.x >> 6][0] = sum + far_sum;
+    sums[threadIdx.x >> 6][1] = kl + far_kl;
     counts[threadIdx.x >> 6] = cuts;
   }
   __syncthreads();
@@ -1087,8 +1151,9 @@ __global__ __launch_bounds__(THREADS) void surrogate_tokens_kernel(SurrogateArgs
     all_kl += sums[i][1];
     cuts += counts[i];
   }
-  if (a.pieces == 1) finish_surrogate(a, r, n, all, all_kl, cuts);
-  else *(float4*)(a.parts + 4ll * blockIdx.x) = float4{(float)all, (float)all_kl, __builtin_bit_cast(float, cuts), 0.0f};
+  const float objective = n ? (float)(w * all) : 0.0f, mean = (float)(all_kl / max(n, 1));
+  if (a.pieces == 1) finish_surrogate(a, r, objective, mean, cuts);
+  else *(float4*)(a.parts + 4ll * blockIdx.x) = float4{objective, mean, __builtin_bit_cast(float, cuts), 0.0f};
 }
 
 __global__ __launch_bounds__(WAVE) void surrogate_finish_kernel(SurrogateArgs a) {
@@ -1106,7 +1171,7 @@ __global__ __launch_bounds__(WAVE) void surrogate_finish_kernel(SurrogateArgs a)
   sum = lanes_sum(sum);
   kl = lanes_sum(kl);
   for (int o = 32; o; o >>= 1) cuts += __shfl_xor(cuts, o);
-  if (threadIdx.x == 0) finish_surrogate(a, r, n, sum, kl, cuts);
+  if (threadIdx.x == 0) finish_surrogate(a, r, (float)sum, (float)kl, cuts);
 }
 
 // ---------------------------------------------------------------- host side

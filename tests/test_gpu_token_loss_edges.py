@@ -50,3 +50,44 @@ def test_a_shifted_list_has_the_same_gradient(lib, shift):
         # q: differences to the largest and to the logarithm of the sum (at most ln k), rounded once each, and the exponential
         tol = s.p[ids[r]] * (s.p_rel[ids[r]] + 8 * U) + w * U * (2 * (v.max() - v) + 4 * math.log(k) + 8)
         near(got[1][r][ids[r]], want, tol + store_tol(want, False) + TINY, f"gradient of row {r}'s listed tokens")
+
+
+def far_sequences(rng, lens, adv, distances):
+    """Sequences near the old policy, some tokens of which are `distances` away from the old and from the reference policy."""
+    seqs, refs = [], []
+    for n, a in zip(lens, adv):
+        logp = -np.abs(rng.standard_normal(n)) * 2
+        old, x = logp + rng.standard_normal(n) * 0.1, logp + rng.standard_normal(n) * 0.2
+        at = rng.integers(0, n, size=len(distances))
+        x[at] = logp[at] + distances
+        old[at[::2]] = logp[at[::2]] - np.asarray(distances)[::2]
+        seqs.append((logp, old, a))
+        refs.append(x)
+    return seqs, refs
+
+
+@pytest.mark.parametrize("lens", [[1, 5, 300], [5000, 70, 8192], [9000, 20000, 3]])
+@pytest.mark.parametrize("kl_coef,adv,weight,distances", [
+    (0.0, 0.7, None, [89.0, 120.0, 300.0]), (0.0, -1e-3, 2.0, [700.0, 1000.0, 41.0]), (1e-6, 1e-5, None, [89.0, 95.0, 60.0]),
+    (1e-25, -1e-30, None, [130.0, 90.0, 89.0]), (0.05, -2.0, 1e-20, [100.0, 110.0, 95.0]), (0.1, 1e20, 1e-9, [39.0, 45.0, -60.0])])
+def test_tokens_far_from_the_other_policies(lib, lens, kl_coef, adv, weight, distances):
+    """Ratios and divergences that are no numbers of fp32 before they are scaled by what makes them some."""
+    rng = np.random.default_rng(sum(lens))
+    seqs, refs = far_sequences(rng, lens, [adv, -adv, adv], distances)
+    w = None if weight is None else [weight] * 3
+    for hi in (0.28, math.inf):
+        got = run_surrogate(lib, seqs, 0.2, hi, refs=refs, kl_coef=kl_coef, weight=w)
+        check_surrogate(got, seqs, 0.2, hi, refs, kl_coef, w)
+        if kl_coef == 0.0 and adv > 0 and hi < 1:          # ratios above the bound are cut
+            assert np.isfinite(got["objective"][[0, 2]]).all()
+
+
+def test_the_divergence_can_be_watched_alone(lib):
+    """kl_coef 0: a reference that is no number, or infinitely far away, reaches kl alone."""
+    seqs = [([-1.0, -2.0], [-1.1, -2.0], 1.5), ([-1.0, -math.inf], [-1.0, -2.0], 1.0), ([-1.0], [-1.2], -1.0)]
+    without = run_surrogate(lib, seqs, 0.2, 0.2)
+    got = run_surrogate(lib, seqs, 0.2, 0.2, refs=[[-1.0, math.nan], [-1.0, -1.0], [-math.inf]], kl_coef=0.0)
+    assert np.array_equal(got["clipped"], without["clipped"]) and np.isfinite(got["objective"]).all()
+    for k in ("objective", "g_logp"):                      # a few roundings of one or two terms
+        near(got[k], without[k], 16 * U * np.abs(without[k]), k)
+    assert np.isnan(got["kl"][0]) and (got["kl"][1:] == math.inf).all()
