@@ -1224,9 +1224,10 @@ static int64_t most_parts(int64_t rows, int64_t vocab) {
 static int n_chunks(int64_t vocab) { return (int)((most_slots(vocab) + CHUNK - 1) / CHUNK); }
 static int64_t part_floats(int64_t rows, int64_t vocab) { return (most_parts(rows, vocab) * (int64_t)(sizeof(Sums) / sizeof(float)) + 3) / 4 * 4; }
 
-// launches F<bf16, ...> with `lds` bytes
+// launches F<bf16, ...> with `lds` bytes; a grid has fewer than 2^32 lanes
 #define PG_LOSS_LAUNCH(blocks, threads, lds, F, ...)                                                         \
   do {                                                                                                       \
+    if ((int64_t)(blocks) * (threads) >> 32) return fail(PG_ESHAPE, "%lld workgroups", (long long)(blocks)); \
     F<<<dim3((unsigned)(blocks)), dim3(threads), lds, (hipStream_t)stream>>>(__VA_ARGS__);                   \
     PG_LAUNCH_CHECK(#F);                                                                                     \
   } while (0)
@@ -1392,7 +1393,8 @@ extern "C" pg_status pg_token_surrogate(const float* logp, const float* logp_old
   if (pieces > 1 && (uintptr_t)scratch & 15) return fail(PG_ESHAPE, "pg_token_surrogate: scratch is not 16-byte aligned");
   const SurrogateArgs a{logp, logp_old, logp_ref, adv, weight, cu, n_tokens, std::log1p(-clip_low), std::log1p(clip_high), (float)(1.0 - clip_low),
                         (float)(1.0 + clip_high), (float)kl_coef, objective, kl, g_logp, clipped, pieces, (int)(((int64_t)max_len + pieces - 1) / pieces), scratch};
-  if (pieces == 1 && max_len > 1024) PG_LOSS_LAUNCH(n_seq, 1024, 0, surrogate_tokens_kernel<1024>, a);
+  // of 2^22 sequences or more 1024 lanes each are more than a grid has
+  if (pieces == 1 && max_len > 1024 && n_seq < 1 << 22) PG_LOSS_LAUNCH(n_seq, 1024, 0, surrogate_tokens_kernel<1024>, a);
   else PG_LOSS_LAUNCH((int64_t)n_seq * pieces, LOSS_THREADS, 0, surrogate_tokens_kernel<LOSS_THREADS>, a);
   if (pieces > 1) PG_LOSS_LAUNCH(n_seq, WAVE, 0, surrogate_finish_kernel, a);
   return PG_OK;

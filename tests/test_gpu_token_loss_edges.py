@@ -91,3 +91,25 @@ def test_the_divergence_can_be_watched_alone(lib):
     for k in ("objective", "g_logp"):                      # a few roundings of one or two terms
         near(got[k], without[k], 16 * U * np.abs(without[k]), k)
     assert np.isnan(got["kl"][0]) and (got["kl"][1:] == math.inf).all()
+
+
+def test_more_sequences_than_wide_workgroups_fit_a_grid(lib):
+    """2^22 sequences, of which 1024 lanes each would be 2^32 in all: sequences of no tokens, of one and of many."""
+    n = 1 << 22
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    lens = (torch.rand(n, device=DEV, generator=gen) < 0.01).long()
+    lens[0], lens[n // 2], lens[n - 1] = 2000, 300, 1500
+    cu = torch.cat([torch.zeros(1, dtype=torch.long, device=DEV), lens.cumsum(0)])
+    tokens = int(cu[-1])
+    logp = -torch.rand(tokens, device=DEV, generator=gen)
+    old, adv = logp + 0.1 * torch.randn(tokens, device=DEV, generator=gen), torch.randn(n, device=DEV, generator=gen)
+    objective, g = torch.full((n,), 99.0, device=DEV), torch.full((tokens,), 99.0, device=DEV)
+    assert lib.pg_surrogate_scratch_floats(n, 2000) == 0
+    lib.pg_token_surrogate(logp, old, adv, cu.int(), objective, g, 1.0, math.inf, 2000)
+    seq = torch.repeat_interleave(torch.arange(n, device=DEV), lens)
+    ra = torch.exp(logp.double() - old.double()) * adv.double()[seq]
+    want = torch.zeros(n, dtype=torch.float64, device=DEV).index_add_(0, seq, ra / lens[seq])
+    # a lane adds at most 8 terms, 14 steps join the lanes, each term is off by some 12 roundings
+    tol = torch.zeros(n, dtype=torch.float64, device=DEV).index_add_(0, seq, ra.abs() / lens[seq]) * 40 * U
+    assert ((objective.double() - want).abs() <= tol).all()
+    assert ((g.double() - ra / lens[seq]).abs() <= 16 * U * (ra / lens[seq]).abs()).all()
