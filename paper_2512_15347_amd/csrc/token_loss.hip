@@ -35,7 +35,8 @@ struct LossRow {
   int shift;                                         // slot t, of which eight are 16 aligned bytes, has token t - shift
   const uint8_t* allow;                              // bit v % 8 of byte v / 8; NULL: `unmasked` for all of them
   uint32_t unmasked;
-  float inv;                                         // 1 / temperature, NaN for one that is no temperature
+  float t;                                           // the temperature, 1 for 0, NaN for one that is none
+  float inv;                                         // its inverse, of 2^-126 where it is smaller: a number
   float c;                                           // the same in base 2
   float lim;                                         // z - m below which p is 0: (z - m) c < -FAR
 };
@@ -49,11 +50,19 @@ __device__ __forceinline__ LossRow loss_row(const LossArgs& a, int r) {
   q.allow = d.allow && mask >= 0 && mask < d.n_masks ? (const uint8_t*)(d.allow + (int64_t)mask * a.l.words) : nullptr;
   q.unmasked = d.allow && mask != -1 ? 0u : 0xFFu;   // an index that no mask has allows nothing
   const float t = a.temperature ? a.temperature[r] : 1.0f;
-  q.inv = !(t >= 0.0f && t < INFINITY) ? __builtin_nanf("") : t == 0.0f ? 1.0f : 1.0f / t;
-  q.c = q.inv * LOG2E;
-  q.lim = -FAR * LN2 * (t > 0.0f && t < INFINITY ? t : 1.0f);
+  q.t = !(t >= 0.0f && t < INFINITY) ? __builtin_nanf("") : t == 0.0f ? 1.0f : t;
+  const float above = q.t < FLT_MIN ? FLT_MIN : q.t;
+  q.inv = 1.0f / above;
+  q.c = LOG2E / above;
+  q.lim = -FAR * LN2 * (above == above ? above : 1.0f);
   return q;
 }
+// (z - m) / T, and the same in base 2; halves, as a difference of two logits may pass fp32's range where a large temperature brings it back.
+__device__ __forceinline__ float over_t(float z, float m, const LossRow& q) {
+  const float h = q.t > 1.0f ? 0.5f : 1.0f;
+  return (h * z - h * m) / (h * q.t);
+}
+__device__ __forceinline__ float in_base_2(float z, float m, const LossRow& q) { return __builtin_fmaf(z, 0.5f, -0.5f * m) * (2.0f * q.c); }
 __device__ __forceinline__ bool allowed(const LossRow& q, int64_t v) { return (q.allow ? (uint32_t)q.allow[v >> 3] : q.unmasked) >> (v & 7) & 1; }
 template <bool BF16>
 __device__ __forceinline__ float logit_at(const LossArgs& a, const LossRow& q, int64_t v) {
@@ -72,7 +81,7 @@ struct Sums {
 __device__ __forceinline__ Sums no_sums() { return Sums{-FLT_MAX, 0.0f, 0.0f}; }
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ void move_to(Sums& a, float m, const LossRow& q) {
-  const float x = (a.m - m) * q.c, f = exp2_of(x);
+  const float x = in_base_2(a.m, m, q), f = exp2_of(x);
   a.u = f * (a.u + fmaxf(x, -FAR) * a.s);
   a.s = f * a.s;
   a.m = m;
@@ -324,7 +333,7 @@ __device__ __forceinline__ void take(WaveSums& a, Pass<BF16, G>& x, bool holes, 
     for (int g = 0; g < G; ++g)
 #pragma unroll
       for (int e = 0; e < LANE_TOKENS; ++e) {
-        const float y = (x.template logit<true>(g, e) - sum.m) * q.c, p = exp2_of(y);
+        const float y = in_base_2(x.template logit<true>(g, e), sum.m, q), p = exp2_of(y);
         s += p;
         if (ENTROPY) u = __builtin_fmaf(p, fmaxf(y, -FAR), u);
         if (e + 1 == LANE_TOKENS) one_group_at_a_time();
@@ -568,10 +577,10 @@ __device__ __forceinline__ void finish_logprob(const LossArgs& a, const LogprobO
     if (o.logp) {
       float l = __builtin_nanf("");
       if (gone) l = 0.0f;
-      else if (target >= 0 && target < a.l.d.vocab && !bad) l = none ? -INFINITY : (at_target - sum.m) * q.inv - ln_s;
+      else if (target >= 0 && target < a.l.d.vocab && !bad) l = none ? -INFINITY : over_t(at_target, sum.m, q) - ln_s;
       o.logp[r] = l;
     }
-    if (o.stats) *(float4*)(o.stats + 4ll * r) = float4{none ? -INFINITY : sum.m * q.inv, ln_s, h, sum.m};
+    if (o.stats) *(float4*)(o.stats + 4ll * r) = float4{none ? -INFINITY : sum.m / q.t, ln_s, h, sum.m};
   }
   if (!s) return;
   const int n = o.n_top;
@@ -582,7 +591,7 @@ __device__ __forceinline__ void finish_logprob(const LossArgs& a, const LogprobO
   }
   if ((int)threadIdx.x < n) {
     if (o.top_ids) o.top_ids[(int64_t)r * n + threadIdx.x] = key ? place_of(key) : -1;
-    if (o.top_logp) o.top_logp[(int64_t)r * n + threadIdx.x] = bad ? __builtin_nanf("") : key ? (logit_of(key) - sum.m) * q.inv - ln_s : -INFINITY;
+    if (o.top_logp) o.top_logp[(int64_t)r * n + threadIdx.x] = bad ? __builtin_nanf("") : key ? over_t(logit_of(key), sum.m, q) - ln_s : -INFINITY;
   }
 }
 

@@ -113,3 +113,50 @@ def test_more_sequences_than_wide_workgroups_fit_a_grid(lib):
     tol = torch.zeros(n, dtype=torch.float64, device=DEV).index_add_(0, seq, ra.abs() / lens[seq]) * 40 * U
     assert ((objective.double() - want).abs() <= tol).all()
     assert ((g.double() - ra / lens[seq]).abs() <= 16 * U * (ra / lens[seq]).abs()).all()
+
+
+TEMPERATURES = [1e-3, 1e-12, 1e-20, 3e-25, 1e-30, 2e-38, 1e-39, 1e-44, 1e6, 1e12, 1e20, 1e30, 1e36, 1e37, 3e38]
+
+
+def logits_for(rng, t, vocab, bf):
+    """Of a few temperatures, above 1; or ordinary ones, of which one or few equal ones remain."""
+    if t > 1:
+        return np.clip(rng.standard_normal(vocab) * 2.0 * t, -3.3e38, 3.3e38)
+    z = rng.standard_normal(vocab) * 3
+    z[rng.integers(0, vocab, size=3)] = z.max()
+    return z
+
+
+def extreme_rows(rng, bf, vocab):
+    t = np.array(TEMPERATURES, dtype=np.float32)
+    z = rounded(np.stack([logits_for(rng, float(v), vocab, bf) for v in t]), bf)
+    return t, z
+
+
+def with_holes(rng, z, target):
+    """Masks that leave the targets, and logits of -inf."""
+    open_ = rng.random(z.shape) < 0.8
+    open_[np.arange(len(z)), target] = True
+    z[:, 3::7] = -math.inf
+    return open_
+
+
+def targets(rng, z):
+    target = rng.integers(0, z.shape[1], size=len(z))
+    target[::2] = z[::2].argmax(1)
+    return target
+
+
+@pytest.mark.parametrize("holes", [False, True], ids=["whole", "holes"])
+@pytest.mark.parametrize("bf", [False, True], ids=["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [70, 3001, 33000])
+def test_every_temperature_gives_numbers(lib, vocab, bf, holes):
+    """From the smallest number to nearly the largest, with logits of -inf and masks or without."""
+    rng = np.random.default_rng(vocab)
+    t, z = extreme_rows(rng, bf, vocab)
+    target = targets(rng, z)
+    open_ = with_holes(rng, z, target) if holes else None
+    for n_top in (0, 5):
+        got = run_logprobs(lib, z, bf, target, t, open_, None, n_top)
+        check_logprobs(got, z, bf, target, t, open_, None, n_top)
+        assert not np.isnan(got["logp"]).any() and not np.isnan(got["entropy"]).any()
