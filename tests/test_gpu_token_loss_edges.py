@@ -160,3 +160,19 @@ def test_every_temperature_gives_numbers(lib, vocab, bf, holes):
         got = run_logprobs(lib, z, bf, target, t, open_, None, n_top)
         check_logprobs(got, z, bf, target, t, open_, None, n_top)
         assert not np.isnan(got["logp"]).any() and not np.isnan(got["entropy"]).any()
+
+
+@pytest.mark.parametrize("holes", [False, True], ids=["whole", "holes"])
+@pytest.mark.parametrize("bf", [False, True], ids=["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [70, 3001, 33000])
+def test_every_temperature_has_gradients(lib, vocab, bf, holes):
+    """Of log-probs and entropies together, and of each alone."""
+    rng = np.random.default_rng(vocab)
+    t, z = extreme_rows(rng, bf, vocab)
+    rows, target = len(t), targets(rng, z)
+    open_ = with_holes(rng, z, target) if holes else None
+    g, ge = rng.standard_normal(rows), rng.standard_normal(rows) * 0.3
+    for a, b in ((g, ge), (g, None), (np.zeros(rows), ge)):
+        got = run_logprobs(lib, z, bf, target, t, open_, None, 0, a, b)
+        check_logprobs(got, z, bf, target, t, open_, None, 0, a, b)
+        assert not np.isnan(got["d"]).any()
