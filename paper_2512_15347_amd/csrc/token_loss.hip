@@ -854,19 +854,20 @@ __device__ __forceinline__ void finish_distill(const LossArgs& a, const DistillA
   const double bad = __ballot(wrong) ? __builtin_nan("") : 0.0;
   const bool top = o.mode == PG_DISTILL_TOP;
   double s_all = 0.0, sum_q = 0.0;
+  const double inv = 1.0 / (double)q.t;
 #pragma unroll
   for (int i = 0; i < LIST_LANES; ++i)
     if (count >> i & 1) {
-      s_all += exp(((double)z[i] - m) * q.inv);
+      s_all += exp(((double)z[i] - m) * inv);
       sum_q += exp(top ? (double)t[i] - most : (double)t[i]);
     }
   const bool others = rest.s != 0.0f;
-  s_all = lanes_sum(s_all) + (others ? rest.s * exp(((double)rest.m - m) * q.inv) : 0.0);
+  s_all = lanes_sum(s_all) + (others ? rest.s * exp(((double)rest.m - m) * inv) : 0.0);
   sum_q = lanes_sum(sum_q);
   const bool active = __ballot(count != 0) && s_all != 0.0 && !(top && most == -INFINITY && bad == 0.0);
   double total = 0.0, q_rest = 0.0, p_rest = 0.0, all = 0.0, t0 = 0.0;
   if (active) {
-    const double ln_s = log(s_all), ln_rest = ((double)rest.m - m) * q.inv + log((double)rest.s) - ln_s;
+    const double ln_s = log(s_all), ln_rest = ((double)rest.m - m) * inv + log((double)rest.s) - ln_s;
     t0 = top ? most + log(sum_q) : 0.0;
     if (others) p_rest = exp(ln_rest);
     if (!top && others) q_rest = fmax(0.0, 1.0 - sum_q);
@@ -874,7 +875,7 @@ __device__ __forceinline__ void finish_distill(const LossArgs& a, const DistillA
     for (int i = 0; i < LIST_LANES; ++i)
       if (count >> i & 1) {
         const double lq = t[i] - t0, w = exp(lq);
-        if (w > 0.0) total += w * (lq - (((double)z[i] - m) * q.inv - ln_s));
+        if (w > 0.0) total += w * (lq - (((double)z[i] - m) * inv - ln_s));
         all += w;
       }
     total = lanes_sum(total) + bad;
@@ -960,7 +961,6 @@ __global__ __launch_bounds__(LOSS_THREADS) void distill_backward_kernel(LossArgs
   const float t = entry ? o.logp[(int64_t)r * o.k + threadIdx.x] : 0.0f;
   const int place = id >= 0 && id < vocab ? id + q.shift - first : -1;
   const bool mine = place >= 0 && place < end - first;
-  const float scale = g * q.inv;
   if (threadIdx.x < RANGE / 32) listed[threadIdx.x] = 0;
   if (threadIdx.x == 0) twice = 0;
   token[threadIdx.x] = id;
@@ -975,16 +975,18 @@ __global__ __launch_bounds__(LOSS_THREADS) void distill_backward_kernel(LossArgs
     for (int i = 0; i < (int)threadIdx.x; ++i) writes &= token[i] != id;       // the first of equal ids counts
   if (writes) {
     const float z = open_logit<BF16>(a, q, id);
-    const float p = exp2_of(__builtin_fmaf(fmaxf(z - s0.x, q.lim), q.c, -s0.y * LOG2E));
-    const float d = z == -INFINITY ? 0.0f : scale * (s1.z * p - expf((t - s1.y) - s1.w));
+    const float p = expf(fmaxf(over_t(z, s0.x, q), -FAR * LN2) - s0.y);
+    const float d = z == -INFINITY ? 0.0f : g * (s1.z * p - expf((t - s1.y) - s1.w)) / q.t;
     if (BF16) ((uint16_t*)to)[id] = (uint16_t)pack_bf16x2(d, 0.0f);
     else ((float*)to)[id] = d;
   }
-  const float c = scale * s1.x, less = s0.w * LOG2E;
+  const float c = g * q.inv * s1.x, less = s0.w * LOG2E;
   auto strike = [&](int t) { return t < end ? (uint32_t)((const uint8_t*)listed)[(t - first) >> 3] : 0u; };
-  const bool odd = !(fabsf(c) < INFINITY && less == less);
-  auto each = [&](const Pass<BF16, G>& x, int base, auto all) {
-    constexpr bool HOLES = !decltype(all)::value;
+  // as in the log-probs' gradient
+  const bool odd = !(fabsf(c) < INFINITY && less == less && q.t >= FLT_MIN && q.lim > -INFINITY);
+  auto plain = [&](float z) { return z == -INFINITY ? 0.0f : g * (s1.x * expf(fmaxf(over_t(z, s0.z, q), -FAR * LN2) - s0.w)) / q.t; };
+  auto each = [&](const Pass<BF16, G>& x, int base, auto all, auto by_hand) {
+    constexpr bool HOLES = !decltype(all)::value, PLAIN = decltype(by_hand)::value;
 #pragma unroll
     for (int i = 0; i < G; ++i) {
       const int v = base + i * LOSS_TOKENS + (int)threadIdx.x * LANE_TOKENS - q.shift;
@@ -992,6 +994,11 @@ __global__ __launch_bounds__(LOSS_THREADS) void distill_backward_kernel(LossArgs
 #pragma unroll
       for (int e = 0; e < LANE_TOKENS; ++e) {
         const float z = x.template logit<HOLES>(i, e);
+        if (PLAIN) {
+          d[e] = plain(z);
+          one_group_at_a_time();
+          continue;
+        }
         d[e] = c * exp2_of(__builtin_fmaf(fmaxf(z - s0.z, q.lim), q.c, -less));
         if (HOLES && z == -INFINITY) d[e] = 0.0f;
       }
@@ -1000,11 +1007,12 @@ __global__ __launch_bounds__(LOSS_THREADS) void distill_backward_kernel(LossArgs
   };
   // a pass without a token that counts may have listed ones among those that are not allowed
   through<BF16, G, true>(a, q, first, end, strike, [&](const Pass<BF16, G>& x, int base, bool holes) {
-    if (holes || odd) each(x, base, std::false_type{});
-    else each(x, base, std::true_type{});
+    if (odd) each(x, base, std::false_type{}, std::true_type{});
+    else if (holes) each(x, base, std::false_type{}, std::false_type{});
+    else each(x, base, std::true_type{}, std::false_type{});
   }, [&](int base) {
     Pass<BF16, G> nothing{};
-    each(nothing, base, std::false_type{});
+    each(nothing, base, std::false_type{}, std::false_type{});
   });
 }
 

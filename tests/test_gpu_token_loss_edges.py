@@ -176,3 +176,24 @@ def test_every_temperature_has_gradients(lib, vocab, bf, holes):
         got = run_logprobs(lib, z, bf, target, t, open_, None, 0, a, b)
         check_logprobs(got, z, bf, target, t, open_, None, 0, a, b)
         assert not np.isnan(got["d"]).any()
+
+
+@pytest.mark.parametrize("holes", [False, True], ids=["whole", "holes"])
+@pytest.mark.parametrize("bf", [False, True], ids=["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [70, 3001, 33000])
+def test_distillation_at_every_temperature(lib, vocab, bf, holes):
+    rng = np.random.default_rng(vocab + 1)
+    t, z = extreme_rows(rng, bf, vocab)
+    rows, k = len(t), 20
+    if holes:
+        z[:, 3::7] = -math.inf
+    ids = np.stack([rng.permutation(np.flatnonzero(row > -math.inf))[:k] for row in z]).astype(np.int32)
+    ids[::2, 0] = z[::2].argmax(1)
+    ids[::2, 1:] = np.where(ids[::2, 1:] == ids[::2, :1], -1, ids[::2, 1:])
+    values = np.log(rng.dirichlet(np.ones(k + 1), size=rows)[:, :k])
+    g = rng.standard_normal(rows) * 100
+    check_distill(run_distill(lib, z, bf, ids, values, False, g, t), z, bf, ids, values, False, g, t)
+    # what is not listed has some of the mass above 1, where the logits are of that size
+    warm = t > 1
+    args = z[warm], bf, ids[warm], values[warm], True, g[warm], t[warm]
+    check_distill(run_distill(lib, *args), *args)
