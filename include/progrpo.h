@@ -489,7 +489,8 @@ pg_status pg_sample_tokens(const pg_logits *desc, const float *temperature, uint
 #define PG_DISTILL_STATS 8
 
 /* logp[r] = ln p of target[r]; entropy[r] = -sum p ln p; top_ids, top_logp [rows, n_top]: the most likely tokens in falling order
- * (equal logits: the lowest token first) and their log-probs, -1 and -inf past the last token whose logit is above -inf.  Every output may be NULL.
+ * (equal logits: the lowest token first) and their log-probs, -1 and -inf past the last token whose logit is above -inf.  No log-prob is above 0 and
+ * no entropy below.  Every output may be NULL.
  * target[r] == -1: a row that is left out and not read (logp and entropy 0, no alternatives, gradient 0, whatever its temperature is); any other index that no token has:
  * logp NaN.  target NULL: no row is left out, and logp has to be NULL.  A row with nothing left: logp -inf, entropy 0.  A bad row: NaN, and
  * -1 and NaN for its alternatives.  stats: [rows, PG_LOGPROB_STATS], 16-byte aligned, for the backward pass; stats[r][0] + stats[r][1] is the

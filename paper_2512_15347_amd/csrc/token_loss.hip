@@ -572,12 +572,13 @@ __device__ __forceinline__ void finish_logprob(const LossArgs& a, const LogprobO
   const bool gone = target == -1, bad = !gone && sum.s != sum.s, none = gone || sum.s == 0.0f;     // a temperature that is none makes even empty sums NaN
   const float ln_s = none ? 0.0f : logf(sum.s);
   if (threadIdx.x == 0) {
-    const float h = none ? 0.0f : ln_s - LN2 * (sum.u / sum.s);
+    // a sum of one token's weight may be rounded to just below 1
+    const float sure = none ? 0.0f : ln_s - LN2 * (sum.u / sum.s), h = sure < 0.0f ? 0.0f : sure;
     if (o.entropy) o.entropy[r] = h;
     if (o.logp) {
       float l = __builtin_nanf("");
       if (gone) l = 0.0f;
-      else if (target >= 0 && target < a.l.d.vocab && !bad) l = none ? -INFINITY : over_t(at_target, sum.m, q) - ln_s;
+      else if (target >= 0 && target < a.l.d.vocab && !bad) l = none ? -INFINITY : fminf(over_t(at_target, sum.m, q) - ln_s, 0.0f);
       o.logp[r] = l;
     }
     if (o.stats) *(float4*)(o.stats + 4ll * r) = float4{none ? -INFINITY : sum.m / q.t, ln_s, h, sum.m};
@@ -591,7 +592,7 @@ __device__ __forceinline__ void finish_logprob(const LossArgs& a, const LogprobO
   }
   if ((int)threadIdx.x < n) {
     if (o.top_ids) o.top_ids[(int64_t)r * n + threadIdx.x] = key ? place_of(key) : -1;
-    if (o.top_logp) o.top_logp[(int64_t)r * n + threadIdx.x] = bad ? __builtin_nanf("") : key ? over_t(logit_of(key), sum.m, q) - ln_s : -INFINITY;
+    if (o.top_logp) o.top_logp[(int64_t)r * n + threadIdx.x] = bad ? __builtin_nanf("") : key ? fminf(over_t(logit_of(key), sum.m, q) - ln_s, 0.0f) : -INFINITY;
   }
 }
 

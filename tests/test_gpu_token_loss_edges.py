@@ -197,3 +197,18 @@ def test_distillation_at_every_temperature(lib, vocab, bf, holes):
     warm = t > 1
     args = z[warm], bf, ids[warm], values[warm], True, g[warm], t[warm]
     check_distill(run_distill(lib, *args), *args)
+
+
+@pytest.mark.parametrize("bf", [False, True], ids=["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [300, 9001, 40001])
+def test_no_log_prob_is_above_0_and_no_entropy_below(lib, vocab, bf):
+    """Rows of which one token has all of the mass, at any logit and temperature."""
+    rng = np.random.default_rng(vocab)
+    rows = 200
+    z = np.full((rows, vocab), -1e4)
+    target = rng.integers(0, vocab, size=rows)
+    z[np.arange(rows), target] = rng.uniform(-30, 30, size=rows)
+    z, t = rounded(z, bf), rng.uniform(0.3, 3.0, size=rows)
+    got = run_logprobs(lib, z, bf, target, t, n_top=2)
+    assert (got["logp"] <= 0).all() and (got["entropy"] >= 0).all() and (got["top_logp"] <= 0).all()
+    check_logprobs(got, z, bf, target, t, n_top=2)
