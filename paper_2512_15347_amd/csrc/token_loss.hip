@@ -852,7 +852,7 @@ __device__ __forceinline__ void finish_distill(const LossArgs& a, const DistillA
     }
   m = wave_max(m);
   most = wave_max(most);
-  const double bad = __ballot(wrong) ? __builtin_nan("") : 0.0;
+  wrong = __ballot(wrong);
   const bool top = o.mode == PG_DISTILL_TOP;
   double s_all = 0.0, sum_q = 0.0;
   const double inv = 1.0 / (double)q.t;
@@ -865,11 +865,13 @@ __device__ __forceinline__ void finish_distill(const LossArgs& a, const DistillA
   const bool others = rest.s != 0.0f;
   s_all = lanes_sum(s_all) + (others ? rest.s * exp(((double)rest.m - m) * inv) : 0.0);
   sum_q = lanes_sum(sum_q);
-  const bool active = __ballot(count != 0) && s_all != 0.0 && !(top && most == -INFINITY && bad == 0.0);
-  double total = 0.0, q_rest = 0.0, p_rest = 0.0, all = 0.0, t0 = 0.0;
+  const bool active = __ballot(count != 0) && s_all != 0.0 && !(top && most == -INFINITY && !wrong);
+  const double bad = wrong || s_all != s_all ? __builtin_nan("") : 0.0;      // also where no entry has a weight
+  const double ln_q = top ? log(sum_q) : 0.0;
+  double total = 0.0, q_rest = 0.0, p_rest = 0.0, all = 0.0;
   if (active) {
     const double ln_s = log(s_all), ln_rest = ((double)rest.m - m) * inv + log((double)rest.s) - ln_s;
-    t0 = top ? most + log(sum_q) : 0.0;
+    const double t0 = top ? most + ln_q : 0.0;
     if (others) p_rest = exp(ln_rest);
     if (!top && others) q_rest = fmax(0.0, 1.0 - sum_q);
 #pragma unroll
@@ -889,7 +891,7 @@ __device__ __forceinline__ void finish_distill(const LossArgs& a, const DistillA
     float4* x = (float4*)(o.stats + (int64_t)r * PG_DISTILL_STATS);
     x[0] = float4{m, (float)log(s_all), rest.m, others ? logf(rest.s) : 0.0f};
     // the teacher's largest value and the logarithm of their sum, apart: values shifted by 10^4 would lose 2^-11 of q to t0 as one number
-    x[1] = float4{(float)(all * p_rest - q_rest), top ? most : 0.0f, active ? (float)all : -1.0f, top ? (float)log(sum_q) : 0.0f};
+    x[1] = float4{(float)(all * p_rest - q_rest), top ? most : 0.0f, active ? (float)all : -1.0f, (float)ln_q};
   }
 }
 

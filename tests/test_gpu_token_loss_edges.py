@@ -212,3 +212,20 @@ def test_no_log_prob_is_above_0_and_no_entropy_below(lib, vocab, bf):
     got = run_logprobs(lib, z, bf, target, t, n_top=2)
     assert (got["logp"] <= 0).all() and (got["entropy"] >= 0).all() and (got["top_logp"] <= 0).all()
     check_logprobs(got, z, bf, target, t, n_top=2)
+
+
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+@pytest.mark.parametrize("vocab", [20, 3000, 20000])
+def test_a_bad_row_is_loud_whatever_its_list_says(lib, vocab, value):
+    """The list has every token that is allowed, and gives none of them any weight."""
+    rng = np.random.default_rng(vocab)
+    z = make_logits(rng, 3, vocab, False)
+    k = 20
+    ids = np.stack([rng.permutation(vocab)[:k] for _ in range(3)]).astype(np.int32)
+    open_ = np.zeros((3, vocab), dtype=bool)
+    open_[np.arange(3)[:, None], ids] = True
+    z[1, ids[1, 7]] = value
+    values, g = np.full((3, k), -math.inf), np.ones(3)
+    got = run_distill(lib, z, False, ids, values, True, g, None, open_, np.arange(3))
+    assert np.isnan(got[0][1]) and got[0][[0, 2]].tolist() == [0, 0]
+    check_distill(got, z, False, ids, values, True, g, None, open_, np.arange(3))
