@@ -11,6 +11,7 @@
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
+#include <cstddef>
 #include <type_traits>
 #include "common.hpp"
 #include "operands.hpp"
@@ -391,10 +392,11 @@ struct TopLds {
   static constexpr int CANDIDATES = 4 * LOSS_THREADS;
   static constexpr int AT_ONCE = 16;                 // the list is compared so many at a time, zeros behind it
   uint64_t lane[LOSS_THREADS], candidate[CANDIDATES + AT_ONCE], best[PG_TOP_MAX], least;
-  float top[LOSS_THREADS / 2];
+  alignas(sizeof(float4)) float top[LOSS_THREADS / 2];
   uint32_t bound;
   int count;
 };
+static_assert(offsetof(TopLds, top) % sizeof(float4) == 0 && alignof(TopLds) % sizeof(float4) == 0, "four of `top` are read at once");
 
 // Before and after the collection of candidates; s.best is the n largest of them in falling order (0: there are no more).
 __device__ __forceinline__ void no_candidates(TopLds& s) {
