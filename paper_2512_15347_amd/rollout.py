@@ -84,8 +84,8 @@ def sample_groups(decoder, prompts, members, steps, schedule, seed, token_reward
     steps, in any order).
 
     token_reward: fp32 [vocab]; a sequence's proxy reward is the mean over its drawn tokens.  penalties: (repetition, frequency, presence).
-    allow: int32 [1, words] mask of tokens that may be drawn.  Returns survivors' ids, tokens, rewards and advantages, and logp [steps,
-    groups * members] by original id (NaN where pruned).  Raises PgError if pages ran out, a member had nothing to draw from or
+    allow: int32 [1, words] mask of tokens that may be drawn.  Returns survivors' ids, tokens, rewards and advantages, logp [steps,
+    groups * members] by original id (NaN where pruned), and the penalties.  Raises PgError if pages ran out, a member had nothing to draw from or
     a reward at a checkpoint was no number."""
     dev, c, P = token_reward.device, decoder.cfg, len(prompts)
     if min(len(p) for p in prompts) < 1 or max(len(p) for p in prompts) + steps > c["max_len"] + 1:
@@ -165,7 +165,7 @@ def sample_groups(decoder, prompts, members, steps, schedule, seed, token_reward
         raise pg.PgError(pg.PG_EINVAL, "a member had no token to draw: a mask that allows none, or logits that are no numbers")
     if int(status[0]):
         raise pg.PgError(pg.PG_ENAN, "a non-finite proxy reward reached the selection")
-    return dict(ids=ids, tokens=history, lens=n_prompt + steps, rewards=score, advantages=adv, logp=logp, offsets=offsets)
+    return dict(ids=ids, tokens=history, lens=n_prompt + steps, rewards=score, advantages=adv, logp=logp, offsets=offsets, penalties=penalties)
 
 
 def _drawn(decoder, out):
@@ -193,9 +193,16 @@ def _rows_of(logits, temperature, allow):
     return pg.Logits(logits, **more), torch.full((n,), float(temperature), device=dev)
 
 
+def _without_penalties(out):
+    """Raises ValueError for rollouts whose tokens were drawn from other logits than the decoder's."""
+    if out.get("penalties") is not None and tuple(float(p) for p in out["penalties"]) != (1.0, 0.0, 0.0):
+        raise ValueError(f"rollouts drawn with penalties {tuple(out['penalties'])}: their log-probs are not those of the decoder's own logits")
+
+
 def token_logprobs(decoder, out, temperature=1.0, allow=None):
     """Log-probs of the drawn tokens of sample_groups' survivors under `decoder`'s weights, and entropies: [survivors, steps] each.  Clears the
-    decoder's cache.  Temperature and mask as in sample_groups, which must not have had penalties."""
+    decoder's cache.  Temperature and mask as in sample_groups, which must not have had penalties (ValueError)."""
+    _without_penalties(out)
     hidden, drawn = _drawn(decoder, out)
     desc, t = _rows_of(_linear(hidden, decoder.w["head"]), temperature, allow)
     logp, entropy = torch.empty(desc.rows, device=hidden.device), torch.empty(desc.rows, device=hidden.device)
@@ -210,7 +217,8 @@ def policy_gradient(decoder, out, clip_low=0.2, clip_high=0.2, kl_coef=0.0, logp
     Per sequence the mean over its drawn tokens, as pg_token_surrogate defines it, plus entropy_coef times the mean entropy; the gradient is that
     of the sequences' mean.  logp_ref: [survivors, steps] of a reference policy (token_logprobs).  Returns objective, kl, clipped [survivors],
     logp [survivors, steps], and with respect to what is maximised: d_logits [survivors * steps, vocab], hidden (what the logits were made of)
-    and d_head = d_logits^T hidden.  Temperature and mask as in sample_groups, which must not have had penalties."""
+    and d_head = d_logits^T hidden.  Temperature and mask as in sample_groups, which must not have had penalties (ValueError)."""
+    _without_penalties(out)
     hidden, drawn = _drawn(decoder, out)
     dev, n, steps = hidden.device, out["ids"].shape[0], out["logp"].shape[0]
     desc, t = _rows_of(_linear(hidden, decoder.w["head"]), temperature, allow)
@@ -230,7 +238,7 @@ def policy_gradient(decoder, out, clip_low=0.2, clip_high=0.2, kl_coef=0.0, logp
 
 def distill_gradient(decoder, teacher, out, k=20, temperature=1.0, tail=True, allow=None):
     """The divergence of `decoder` from another decoder's k most likely tokens at every drawn token of sample_groups' survivors, and the gradient of
-    its mean with respect to the decoder's output matrix.  Returns loss [survivors, steps], d_logits, hidden and d_head."""
+    its mean with respect to the decoder's output matrix, both from their own logits, whatever penalties the tokens were drawn with.  Returns loss [survivors, steps], d_logits, hidden and d_head."""
     hidden, drawn = _drawn(teacher, out)
     desc, t = _rows_of(_linear(hidden, teacher.w["head"]), temperature, allow)
     dev, n, vocab = hidden.device, desc.rows, desc.vocab

@@ -126,3 +126,17 @@ def test_what_does_not_fit_is_refused(rolled):
         rollout.policy_gradient(decoder, out, clip_low=1.5)
     with pytest.raises(pg.PgError):
         rollout.distill_gradient(decoder, other, out, k=65)
+
+
+def test_rollouts_say_what_penalties_they_were_drawn_with(rolled):
+    rollout, decoder, _, out, _ = rolled
+    assert out["penalties"] is None
+    reward = torch.zeros(CFG["vocab"], device=DEV)
+    drawn = [rollout.sample_groups(decoder, [[1, 2, 3]], 4, 3, [], seed=5, token_reward=reward, penalties=p) for p in ((1.3, 0.0, 0.2), (1.0, 0.0, 0.0), None)]
+    for call in (rollout.token_logprobs, rollout.policy_gradient):
+        with pytest.raises(ValueError):
+            call(decoder, drawn[0])
+    # penalties that change nothing: the draws and what is learnt from them are those without
+    steps = [rollout.policy_gradient(decoder, o) for o in drawn[1:]]
+    assert torch.equal(drawn[1]["tokens"], drawn[2]["tokens"]) and torch.equal(steps[0]["d_logits"], steps[1]["d_logits"])
+    assert torch.isfinite(rollout.distill_gradient(decoder, decoder, drawn[0])["loss"]).all()
