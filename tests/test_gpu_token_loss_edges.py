@@ -229,3 +229,24 @@ def test_a_bad_row_is_loud_whatever_its_list_says(lib, vocab, value):
     got = run_distill(lib, z, False, ids, values, True, g, None, open_, np.arange(3))
     assert np.isnan(got[0][1]) and got[0][[0, 2]].tolist() == [0, 0]
     check_distill(got, z, False, ids, values, True, g, None, open_, np.arange(3))
+
+
+@pytest.mark.parametrize("bf", [False, True], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab", [(3, 1000), (48, 16384), (5, 70001)])
+def test_a_drawn_tokens_log_prob_is_the_draws(lib, rows, vocab, bf):
+    """pg_token_logprobs of what pg_sample_tokens drew, from the same logits, temperatures and masks."""
+    rng = np.random.default_rng(rows)
+    z = make_logits(rng, rows, vocab, bf)
+    t = rng.uniform(0.5, 1.5, size=rows)
+    t[0] = 0.0
+    open_ = rng.random((rows, vocab)) < 0.7
+    logits = dev(z, np.float32).to(torch.bfloat16 if bf else torch.float32)
+    desc, temperature = lib.Logits(logits, allow=dev(mask_words(open_), np.int32)), dev(t, np.float32)
+    token, drawn, logp = torch.empty(rows, dtype=torch.int32, device=DEV), torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    lib.pg_sample_tokens(desc, temperature, 5, 0, None, token, drawn, torch.empty(desc.scratch, device=DEV))
+    lib.pg_token_logprobs(desc, token, logp, torch.empty(lib.pg_logprob_scratch_floats(rows, vocab), device=DEV), temperature=temperature)
+    for r in range(rows):
+        s = Softmax(z[r], float(np.float32(t[r])), open_[r])
+        v = int(token[r])
+        # each of the two is off by what the sums' and the logit's roundings allow
+        assert open_[r, v] and abs(float(drawn[r]) - float(logp[r])) <= 2 * s.logp_tol(v) + 8 * U * abs(s.y.max())
