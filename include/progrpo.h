@@ -531,7 +531,8 @@ pg_status pg_distill_backward(const pg_logits *desc, const float *temperature, c
  * kl[r]: mean of k; clipped[r]: tokens whose gradient was cut (rho above 1 + clip_high with A > 0, or below 1 - clip_low with A < 0).
  * logp_ref NULL: k = 0.  kl_coef 0: logp_ref reaches kl alone, whatever it holds.  Products are rounded to fp32 after they are scaled by w, so that
  * exponentials may pass fp32's range.  Every output may be NULL.  A sequence of no tokens gives zeros; tokens past cu[n_seq] are left as they are.
- * g_logp may be one of the inputs of that length.  clip_low in [0, 1], clip_high >= 0 (infinite: no bound); cuts are decided in fp64.
+ * g_logp may be one of the inputs of that length.  clip_low in [0, 1], clip_high >= 0 (infinite: no bound), kl_coef a number of fp32; cuts are
+ * decided in fp64.
  * max_len >= every length: sizes the split (longer sequences are right too, but slower).  scratch: pg_surrogate_scratch_floats() floats,
  * 16-byte aligned, enough for every call of no more sequences and no larger max_len, too (may be NULL where that is 0). */
 int64_t pg_surrogate_scratch_floats(int32_t n_seq, int32_t max_len);

@@ -1428,7 +1428,7 @@ extern "C" pg_status pg_token_surrogate(const float* logp, const float* logp_old
                                         void* stream) {
   if (n_seq < 0 || n_tokens < 0 || max_len < 0) return fail(PG_EINVAL, "pg_token_surrogate: %d sequences, %d tokens, length %d", n_seq, n_tokens, max_len);
   if (n_seq > 1 << 23) return fail(PG_ESHAPE, "pg_token_surrogate: %d sequences (at most %d)", n_seq, 1 << 23);
-  if (!(clip_low >= 0.0 && clip_low <= 1.0) || !(clip_high >= 0.0) || !std::isfinite(kl_coef))
+  if (!(clip_low >= 0.0 && clip_low <= 1.0) || !(clip_high >= 0.0) || !std::isfinite((float)kl_coef))
     return fail(PG_EINVAL, "pg_token_surrogate: clip %g below and %g above, kl_coef %g", clip_low, clip_high, kl_coef);
   if (n_seq == 0) return PG_OK;
   if (!adv || !cu || (n_tokens && (!logp || !logp_old))) return fail(PG_EINVAL, "pg_token_surrogate: null pointer");

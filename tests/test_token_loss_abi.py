@@ -114,6 +114,13 @@ def test_the_objective_refuses_bad_arguments():
         assert surrogate(most=1 << 20, scratch=None) == pg.PG_EINVAL
 
 
+def test_a_coefficient_past_fp32s_range_is_refused():
+    """The kernels take it in fp32, where it would be infinite and 0 times it no number."""
+    for beta in (1e39, -1e300):
+        assert surrogate(beta=beta) == pg.PG_EINVAL, beta
+    assert surrogate(n=0, beta=3e38) == pg.PG_OK
+
+
 # ---------------------------------------------------------------- sizes that are asked for once hold for smaller calls
 
 ROWS = sorted({1, 2, 3, 7, 48, 640, 700, 2049, 65535, 65536, 1 << 20} | set(range(5, 3000, 61)) | {b + i for b in (256, 512, 1280, 2048, 4096) for i in (-1, 0, 1)})
