@@ -1,10 +1,11 @@
 // What a token policy learns from: log-probs of given tokens with entropy and alternatives, the divergence from a teacher's most likely
 // tokens, the clipped objective of sequences, and their gradients.
 //
-// Of a row only three sums are needed, all relative to its largest logit m: S = sum exp((z - m) / T), U = sum exp((z - m) / T) (z - m) / T and, where
-// a teacher's list is compared, S over the tokens that are not on it.  Then ln p = (z - m) / T - ln S and the entropy is ln S - U / S, a
-// sum of terms of one sign.  Differences to m are exact where it matters, so that a row may be shifted by any amount; m and ln S are kept apart
-// for the backward pass for the same reason.
+// Of a row only three sums are needed, all relative to a logit m of its own that is near the largest: S = sum exp((z - m) / T), U = sum exp((z - m) / T) (z - m) / T
+// and, where a teacher's list is compared, S over the tokens that are not on it.  Then ln p = (z - m) / T - ln S and the entropy is ln S - U / S.  The largest
+// logit's weight is at most 2^6: where it is above 1 the two are differences of numbers of up to 4.2, but m's own weight is at least 2^-6 of the
+// largest then, so that -ln p and the entropy are 0.015 or more, and 5e-7 off.  Differences to m are exact where it matters, so that a row may be
+// shifted by any amount; m and ln S are kept apart for the backward pass for the same reason.
 //
 // Logits are read once for the sums and once more for their gradient, and that is what bounds all but the smallest calls: 6.0 TB/s read, 5.6 TB/s where as much
 // is written.  Times here are of kernels on an MI355X.
@@ -117,8 +118,9 @@ __device__ __forceinline__ void one_group_at_a_time() { __builtin_amdgcn_sched_b
 
 // A lane's part of one pass over a range: G groups of eight slots and which of their tokens count: those that are in the row and in the range,
 // allowed and not struck out.  16-byte loads may be unaligned, but in bf16, where a row may begin between two 4-byte words, they are a third
-// slower then (4096 x 131073, the forward pass: 311 us, 222 with slots); in fp32 slots would cost (4096 x 65537 against a list: 215 us, 269 with them).
-// Every logit is read once a pass and marked so: 2048 x 131073 against a list in 103 us, 124 without.
+// slower then; in fp32 slots would cost (4096 x 65537 against a list: 215 us, a quarter more with them).
+// Every logit is read once a pass and marked so, in us with and without: 4096 x 65537 94 and 100, 1178 x 131073 63 and 68, 4096 x 131072
+// 177 and 199, 2048 x 131073 against a list 104 and 115.
 typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(4)));
 
 template <bool BF16, int G>
@@ -346,9 +348,10 @@ __device__ __forceinline__ void take(WaveSums& a, Pass<BF16, G>& x, bool holes, 
 }
 
 // How a pass over the logits is laid out.  Rows are stretches of LOSS_TOKENS slots each, and a workgroup takes the next `share` of all rows'
-// stretches: so that all workgroups are resident at once and end together.  What it sums of row r goes to part r + its own number.  Against shares of
-// at most 16 stretches, of which there are more than fit at once: 2048 x 131073 in 101 us for 115, 1178 masked rows of 65537 in 41 for 45, but 4096 x 131072
-// in 180 for 174.
+// stretches: so that all workgroups are resident at once and end together (but for fp32 lists, where 1792 fit: even shares for as many took 241 us for
+// 4096 x 65537, for 2048 of them 214).  What it sums of row r goes to part r + its own number.  Shares of
+// at most 16 stretches, of which there are more than fit at once, cost 14 % more for 2048 x 131073 against a list and 10 % for 1178 masked rows of 65537, but
+// 3 % less for 4096 x 131072.
 struct LossGrid {
   int stretches, share, workgroups;
 };
@@ -369,7 +372,7 @@ __device__ __forceinline__ bool parts_of(const LossGrid& g, int r, const Sums* p
 // The n best tokens lie in the n stretches of CHUNK slots whose largest logits come first (equal ones in the order of their tokens): each of
 // these has a token that comes before all others of the stretches that come after.  So the pass over the logits leaves the largest logit of each
 // stretch, the stretches are chosen from these, and their tokens are looked at again.  Lists that the lanes keep while they sum, and join, took 118 us for
-// 1178 rows of 64 alternatives where this takes 20.  Stretches of 32 slots: 73 us for the pass over 1178 x 131073, 71 with 64.
+// 1178 rows of 64 alternatives where this takes 19.  Stretches of 32 slots: 3 % more for the pass over 1178 x 131073.
 constexpr int CHUNK_LANES = 8, CHUNK = CHUNK_LANES * LANE_TOKENS;
 
 // Its bits in the order of the numbers; -0 and 0 are equal.
@@ -599,9 +602,9 @@ __device__ __forceinline__ void finish_logprob(const LossArgs& a, const LogprobO
 }
 
 // Bound by reading: 1178 rows of 131073 in bf16 (309 MB) take 54 us, 5.8 TB/s, and 70 with the largest of each stretch (6 of the 16 for its stores, past
-// the caches 3 more); 4096 x 65537 (537 MB) 96 us, 5.6 TB/s, and 4096 x 131072 (1074 MB) 171 us, 6.3 TB/s; without any arithmetic a copy of the pass was
-// 3 to 5 % shorter.  Loads of the next pass asked for before this one is summed cost registers and gave nothing (44 us for 41, 188 for 182).
-// WHOLE: every workgroup has one row, and no launch comes after this one: 48 masked rows of 16384 with five alternatives in 12.7 us.
+// the caches 3 more); 4096 x 65537 (537 MB) 94 us, 5.7 TB/s, and 4096 x 131072 (1074 MB) 169 us, 6.4 TB/s; in fp32 4096 x 65536 (1074 MB) 187 us, 5.7 TB/s.  Without
+// any arithmetic a copy of the pass was 3 to 5 % shorter.  Loads of the next pass asked for before this one is summed cost registers and gave
+// nothing (3 to 7 % more).  WHOLE: every workgroup has one row, and no launch comes after this one: 48 masked rows of 16384 with five alternatives in 12.4 us.
 template <bool BF16, int G, bool TOP, bool WHOLE>
 __global__ __launch_bounds__(LOSS_THREADS, WHOLE ? 2 : TOP ? 6 : 8) void logprob_kernel(LossArgs a, LossGrid grid, LogprobOut o) {
   __shared__ Sums waves[LOSS_WAVES];
@@ -702,7 +705,7 @@ __device__ __forceinline__ void put_zeros(char* row, int v, int vocab) {
 
 // The gradient is p (c0 + c1 log2 p) with two numbers of the row, and g / T more at the target; where such a number, or the bound on z - m, passes fp32's
 // range, at temperatures near an end of it, a token's is worked out before it is divided by T.  Bound by reading the logits again and writing as much:
-// 4096 x 131072 in bf16 in 350 us, 6.1 TB/s both ways.
+// 4096 x 131072 in bf16 in 361 us, 5.9 TB/s both ways.
 template <bool BF16, int G, bool PAST>
 __global__ __launch_bounds__(LOSS_THREADS) void logprob_backward_kernel(LossArgs a, int pieces, const int32_t* target, const float* stats,
                                                                         const float* g_logp, const float* g_entropy, void* out, int64_t out_stride) {
@@ -898,7 +901,7 @@ __device__ __forceinline__ void finish_distill(const LossArgs& a, const DistillA
 }
 
 // The sums over what is not listed, with a bit in LDS for each slot; bound by reading: 2048 x 131073 in bf16 (537 MB) in 93 us,
-// 5.8 TB/s.  In fp32 seven waves a SIMD, for which registers suffice: 4096 x 65537 in 214 us, 243 with eight.
+// 5.8 TB/s.  In fp32 seven waves a SIMD, for which registers suffice: 4096 x 65537 in 214 us, 5.0 TB/s, 243 with eight.
 template <bool BF16, int G, bool WHOLE>
 __global__ __launch_bounds__(LOSS_THREADS, WHOLE ? 2 : BF16 ? 8 : 7) void distill_kernel(LossArgs a, LossGrid grid, DistillArgs o) {
   __shared__ Sums waves[LOSS_WAVES];
@@ -945,7 +948,7 @@ __global__ __launch_bounds__(WAVE) void distill_finish_kernel(LossArgs a, LossGr
 }
 
 // What is not listed has the gradient g / T (Q p_rest - q_rest) of its share of p_rest; a listed token is written by the lane that holds its
-// entry, and by no other.  Bound by reading and writing: 2048 x 131073 in bf16 in 188 us, 5.7 TB/s both ways; 193 with the first rows
+// entry, and by no other.  Bound by reading and writing: 2048 x 131073 in bf16 in 188 us, 5.7 TB/s both ways, in fp32 4096 x 65537 in 456 us, 4.7 TB/s; in bf16 193 with the first rows
 // first, of which less is still near from the pass before (log-probs': no difference).
 template <bool BF16, int G, bool PAST>
 __global__ __launch_bounds__(LOSS_THREADS) void distill_backward_kernel(LossArgs a, int pieces, DistillArgs o, const float* g_loss, void* out,
@@ -1122,8 +1125,8 @@ struct FarToken {
   }
 };
 
-// Four numbers of a token, read or written once, and some 90 instructions bound it: 384 sequences of 16384 tokens at most, 3.1 million in all (50 MB), in
-// 15 us (8 us of issue) and 4 for the second launch; 48 short sequences in 4.5 us.
+// Four numbers of a token, read or written once, and some 110 instructions bound it: 384 sequences of 16384 tokens at most, 3.1 million in all (50 MB), in
+// 15.4 us (9 us of issue) and 4 for the second launch; 48 short sequences in 4.5 us.
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void surrogate_tokens_kernel(SurrogateArgs a) {
   constexpr int AT_ONCE = 4;                         // tokens of a lane whose loads are under way together
@@ -1248,13 +1251,14 @@ static int64_t most_slots(int64_t vocab) { return vocab + LANE_TOKENS - 1; }
 static int64_t stretches_of(int64_t slots) { return (slots + LOSS_TOKENS - 1) / LOSS_TOKENS; }
 
 // As many workgroups as are resident at once, if there is a stretch for each; short rows are no more than 8 to a workgroup, which goes
-// through them one after another.  Two groups a lane at a time with eight waves a SIMD: 68 us for 1178 x 131073 (with loads that the caches keep), four
-// with five waves 83; one: 119 us for 4096 x 65537, two 113.  With the largest of each stretch six waves fit: 73 us, 79 with as many workgroups as eight
-// would take.
+// through them one after another.  Two groups a lane at a time with eight waves a SIMD: four with five waves cost 22 % more for 1178 x 131073, one
+// 5 % more for 4096 x 65537.  With the largest of each stretch six waves fit: 8 % more with as many workgroups as eight would take.
 constexpr int64_t LOSS_WORKGROUPS = 2048, TOP_WORKGROUPS = 1536, ROWS_OF_ONE = 8;
 constexpr int PASS_GROUPS = 2, WHOLE_GROUPS = 4, WHOLE_STRETCHES = 8;
-// Few short rows are a workgroup's each, with four groups a lane at a time, in one launch: 48 x 16384 (8 stretches) in 6.3 us for 4.9 + 3.5 in two,
-// with alternatives 14.5 for 5.3 + 9.8, against a list 10.4 for 5.4 + 6.3 (of 16000); at 16 stretches, 32001, 16.4 for 4.6 + 9.7 and 15.4 for 6.6 + 6.4.
+// Few short rows are a workgroup's each, with four groups a lane at a time, in one launch.  In us, against the two launches (and the way from one to the
+// other, some 2): 48 x 16384 (8 stretches) 6.7 for 5.0 + 3.4, 256 x 16384 8.6 for 10.5 + 3.9; with alternatives 12.1 for 5.3 + 8.2, 14.7 for 8.5 + 7.8, 500 x 8192
+// 13.5 for 8.4 + 8.4, but 1000 x 4096 21.4 for 8.5 + 9.5; against a list 48 x 16000 10.2 for 4.9 + 6.3, 1000 x 4000 12.0 for 9.5 + 7.0.  At 12 stretches, 48 x
+// 24001 with alternatives, 15.8 for 5.9 + 8.1; at 16, 48 x 32001, 11.0 for 5.8 + 3.4, 18.5 for 6.2 + 8.4, and 14.1 for 5.7 + 6.5 against a list.
 static bool whole_rows(int64_t rows, int64_t stretches) { return stretches <= WHOLE_STRETCHES && rows * stretches <= LOSS_WORKGROUPS; }
 static LossGrid loss_grid(const LossArgs& a, int64_t most) {
   const int64_t rows = a.l.d.rows, stretches = stretches_of(slots_of(a)), all = rows * stretches;
@@ -1320,12 +1324,15 @@ extern "C" pg_status pg_token_logprobs(const pg_logits* desc, const float* tempe
   });
 }
 
-// A bf16 gradient of more than 256 MiB, what the last cache holds: a pass and its gradient, 4096 x 131072, in 549 us, 575 without, as the next pass need
-// not wait for what the caches write back; in fp32 427 for 370.
+// A bf16 gradient of more than 256 MiB, what the last cache holds: the next pass need not wait for what the caches write back.  Passes and gradients in turn, in
+// us with and without: 1100 x 131073 (288 MB) 170 and 183, 2048 x 131073 289 and 303, 4096 x 131072 563 and 565; against a list 165 and 184, 297 and 313.
+// Smaller ones are left where their reader finds them, although nothing but these two passes, again and again, is faster without: 900 x 131073 (236 MB)
+// 141 and 154, 1178 x 65537 (154 MB) 102 and 102.  In fp32 the gradient takes 427 for 370.
 static bool past_the_caches(const LossArgs& a) { return a.l.d.dtype == PG_LOGITS_BF16 && (int64_t)a.l.d.rows * a.l.d.vocab * 2 > 256ll << 20; }
 
-// A gradient's workgroup goes through one pass, of four groups a lane in bf16 (4096 x 131072 in 350 us; two 357, one 380) and of one in fp32
-// (4096 x 65536 in 360 us; four 391) or where there are few rows, to be spread.
+// A gradient's workgroup goes through one pass, of four groups a lane in bf16 (4096 x 131072: two groups 2 % more, one 9 %) and of one in fp32, or where there
+// are few rows, to be spread.  One, two and four groups in fp32, us: 4096 x 65537 435, 428 and 451, 4096 x 6000 40, 57 and 43; against a list, which
+// each workgroup looks up anew, 456, 458 and 484, 55, 79 and 64, and 1000 x 32001 61, 62 and 69.
 static bool large_passes(const LossArgs& a) { return a.l.d.dtype == PG_LOGITS_BF16 && a.l.d.rows * ((stretches_of(slots_of(a)) + 3) / 4) >= 1024; }
 // f(whether the logits are bf16, groups a lane takes, whether the gradient goes past the caches), as types
 template <class F>
@@ -1408,9 +1415,9 @@ extern "C" pg_status pg_distill_backward(const pg_logits* desc, const float* tem
   });
 }
 
-// Sequences of up to 8192 tokens are a workgroup's each (48 x 8192: 8.3 us, as long as in two launches); longer ones are cut into pieces of 1024 tokens
-// or more, at most 4096 in all, and joined by a second launch (48 x 16384: 5.9 + 2.8 us, whole 13.2; 384 sequences: 15.0 us,
-// 15.7 with 2048, 18.2 with 8192).
+// Sequences of up to 8192 tokens are a workgroup's each (48 x 8192: 7.7 us, as long as in two launches); longer ones are cut into pieces of some 1024 tokens
+// (from 911 on) or more, at most 4096 in all, and joined by a second launch (48 x 16384: 5.8 + 2.7 us, whole 12.5; 384 sequences of up to 16384: 15.4 us,
+// 16.2 with 2048, 19.4 with 8192).
 constexpr int64_t SURROGATE_WHOLE = 8192, SURROGATE_PIECE = 1024, SURROGATE_WORKGROUPS = 4096;
 static int64_t surrogate_pieces(int64_t n_seq, int64_t max_len) {
   if (max_len <= SURROGATE_WHOLE) return 1;
