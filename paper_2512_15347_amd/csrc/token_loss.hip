@@ -1146,7 +1146,7 @@ __global__ __launch_bounds__(THREADS) void surrogate_tokens_kernel(SurrogateArgs
     float l[AT_ONCE], old[AT_ONCE], ref[AT_ONCE];
 #pragma unroll
     for (int j = 0; j < AT_ONCE; ++j) {
-      const int64_t at = min(i + j * THREADS, end - 1);
+      const int64_t at = i + j * THREADS < end ? i + j * THREADS : i;       // past the end the lane's own, which no other lane writes
       l[j] = a.logp[at];
       old[j] = a.old[at];
       ref[j] = a.ref ? a.ref[at] : 0.0f;

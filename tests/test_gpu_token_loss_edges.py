@@ -93,6 +93,31 @@ def test_the_divergence_can_be_watched_alone(lib):
     assert np.isnan(got["kl"][0]) and (got["kl"][1:] == math.inf).all()
 
 
+def test_gradients_in_the_place_of_an_input(lib):
+    """Of log-probs, old ones or the reference's: the same bits as apart, with gradients that would be far from anything if they were read as inputs."""
+    rng = np.random.default_rng(8)
+    lens = [800, 1, 1025, 300, 5000, 9000, 257] * 20
+    cu = np.cumsum([0] + lens)
+    n, seqs = int(cu[-1]), len(lens)
+    logp = -np.abs(rng.standard_normal(n)) * 2
+    old, x = logp + rng.standard_normal(n) * 0.2, logp + rng.standard_normal(n) * 0.3
+    old[rng.integers(0, n, size=50)] -= 60.0               # and some that are far indeed
+    adv, weight = dev(rng.standard_normal(seqs) * 1e5, np.float32), torch.ones(seqs, device=DEV)
+    scratch = torch.empty(lib.pg_surrogate_scratch_floats(seqs, 9000), device=DEV)
+
+    def run(place):
+        t = dict(logp=dev(logp, np.float32), old=dev(old, np.float32), ref=dev(x, np.float32), apart=torch.empty(n, device=DEV))
+        objective = torch.empty(seqs, device=DEV)
+        lib.pg_token_surrogate(t["logp"], t["old"], adv, dev(cu, np.int32), objective, t[place], 0.2, math.inf, 9000, scratch, logp_ref=t["ref"], kl_coef=0.1,
+                               weight=weight)
+        return objective, t[place]
+
+    want = run("apart")
+    for place in ("logp", "old", "ref"):
+        got = run(place)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), place
+
+
 def test_more_sequences_than_wide_workgroups_fit_a_grid(lib):
     """2^22 sequences, of which 1024 lanes each would be 2^32 in all: sequences of no tokens, of one and of many."""
     n = 1 << 22
