@@ -1047,7 +1047,7 @@ __device__ __forceinline__ void finish_surrogate(const SurrogateArgs& a, int r, 
 
 // Tokens for which fp32 is enough: exponentials and what they are multiplied with are of at most e^NEAR and LARGE, so that no product and no sum of a
 // lane's passes 10^38.  All others, and all where a factor is larger or no number, go through fp64 until they are scaled.  Decided for all tokens that a lane
-// has at once; with it 384 sequences of 16384 tokens at most take 16.3 us a call, 16.0 without.
+// has at once; with it 384 sequences of 16384 tokens at most take 16.1 us a call, 15.9 without.
 constexpr float NEAR = 40.0f, LARGE = 1e12f;
 __device__ __forceinline__ bool is_near(float l, float old, float ref, bool has_ref) {
   return fabsf(l - old) < NEAR && (!has_ref || fabsf(ref - l) < NEAR);
@@ -1126,7 +1126,7 @@ struct FarToken {
 };
 
 // Four numbers of a token, read or written once, and some 110 instructions bound it: 384 sequences of 16384 tokens at most, 3.1 million in all (50 MB), in
-// 15.4 us (9 us of issue) and 4 for the second launch; 48 short sequences in 4.5 us.
+// 15.1 us (9 us of issue) and 4 for the second launch; 48 short sequences in 4.5 us.
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void surrogate_tokens_kernel(SurrogateArgs a) {
   constexpr int AT_ONCE = 4;                         // tokens of a lane whose loads are under way together
