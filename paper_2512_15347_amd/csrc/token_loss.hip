@@ -1416,8 +1416,8 @@ extern "C" pg_status pg_distill_backward(const pg_logits* desc, const float* tem
 }
 
 // Sequences of up to 8192 tokens are a workgroup's each (48 x 8192: 7.7 us, as long as in two launches); longer ones are cut into pieces of some 1024 tokens
-// (from 911 on) or more, at most 4096 in all, and joined by a second launch (48 x 16384: 5.8 + 2.7 us, whole 12.5; 384 sequences of up to 16384: 15.4 us,
-// 16.2 with 2048, 19.4 with 8192).
+// (from 911 on) or more, at most 4096 in all, and joined by a second launch (48 x 16384: 5.8 + 2.7 us, whole 12.5; 384 sequences of up to 16384
+// 15.1 us, 5 % more with 2048 in all, 25 % with 8192).
 constexpr int64_t SURROGATE_WHOLE = 8192, SURROGATE_PIECE = 1024, SURROGATE_WORKGROUPS = 4096;
 static int64_t surrogate_pieces(int64_t n_seq, int64_t max_len) {
   if (max_len <= SURROGATE_WHOLE) return 1;
